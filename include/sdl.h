@@ -17,6 +17,7 @@
  * diagnostics on the same arrays.  sdl_fragment_outer_step_plan_static is the fused step
  * for callers that cannot allocate; sdl_flat_layout says where to put the flat arrays and
  * sdl_memory_probe measures what the memory system gives (neither is part of the method).
+ * sdl_layer_norm*, sdl_rotary* and sdl_attention* are the operators of the decoder between two outer steps.
  * The M replicas ("workers") are M parameter arrays
  * resident in one GPU's memory; no call communicates with another device.
  *
@@ -497,6 +498,103 @@ int sdl_flat_layout(uint64_t total_numel, uint32_t M, int separate_w_now, uint64
 typedef enum { SDL_PROBE_COPY = 0, SDL_PROBE_COPY_NT = 1, SDL_PROBE_READ_NT = 2, SDL_PROBE_FILL_NT = 3 } sdl_probe_t;
 int sdl_memory_probe(sdl_probe_t kind, void* dst, const void* src, uint64_t nbytes, void* stream);
 int sdl_copy_bytes(void* dst, const void* src, uint64_t nbytes, void* stream);
+
+/* ---- Operators of the inner step and of evaluation ------------------------------------
+ *
+ * What the decoder whose replicas are synchronised here is made of besides matrix products (Section 3.2 of the
+ * paper: a decoder with normalised queries and keys, sequences of 1,024 and 2,048 tokens): layer norm, rotary
+ * positions and attention, each with its backward pass.  Activations are [batch][tokens][heads][width]
+ * arrays in bf16 or fp32 at any strides, with neighbouring elements along the width: a part of a fused
+ * projection's output, a cache kept by head or by token.  Sums, norms, softmax and its statistics are fp32
+ * whatever the type; results are rounded once when they are stored.
+ *
+ * The conventions above hold (status codes, streams, no allocation).  An array that is written must not
+ * share memory with another one of the call except where said; that is the caller's to see to, as parts of one
+ * array may well lie in between each other.  Speed wants rows that start on 16 bytes; results do not depend on it. */
+typedef enum { SDL_DTYPE_FP32 = 0, SDL_DTYPE_BF16 = 1 } sdl_dtype_t;
+
+/* An array [batch][tokens][heads][width] in device memory: the address of its first element and the distances, in
+ * elements, between neighbours along batch, tokens and heads.  Any strides for an array that is read (0: one row for
+ * all); none of an array that is written may be 0 where its extent is above 1 (SDL_ERR_INVALID_ARG). */
+typedef struct { void* data; int64_t stride_batch, stride_token, stride_head; } sdl_view_t;
+
+/* Layer norm of every row of `width` elements:
+ *     mean = sum x / width,  rstd = 1 / sqrt(sum (x - mean)^2 / width + eps),  y = (x - mean) * rstd * weight + bias
+ * weight, bias: [width] of param_dtype, NULL for 1 and 0.  mean, rstd: fp32 [batch][tokens][heads], or NULL; the
+ * backward pass needs them.  y may be x itself, with the same strides.  Rows without tokens: nothing is done.
+ * Errors: SDL_ERR_INVALID_ARG (missing array, bad type, width 0, eps negative or not finite), SDL_ERR_UNSUPPORTED
+ * (width above SDL_NORM_MAX_WIDTH, 2^31 rows and more), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+#define SDL_NORM_MAX_WIDTH 16384u
+int sdl_layer_norm(const sdl_view_t* x, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t width, sdl_dtype_t dtype,
+                   const void* weight, const void* bias, sdl_dtype_t param_dtype, float eps, const sdl_view_t* y, float* mean,
+                   float* rstd, void* stream);
+
+/* Its gradients, from dy, x and the forward pass' mean and rstd; with h = (x - mean) * rstd and a = dy * weight:
+ *     dx = rstd * (a - sum a / width - h * sum (a h) / width),  dweight = sum over rows of dy h,  dbias = sum over rows of dy
+ * dx may be dy itself, with the same strides.  dweight, dbias: [width] of param_dtype, or NULL where one is not wanted; they are written, not
+ * added to (0 without rows).  The order of their sums is fixed by the sizes.  workspace: device memory, 4-byte aligned, of at
+ * least sdl_layer_norm_workspace_bytes(width) bytes, contents irrelevant; may be NULL without dweight and dbias. */
+size_t sdl_layer_norm_workspace_bytes(uint32_t width);
+int sdl_layer_norm_backward(const sdl_view_t* dy, const sdl_view_t* x, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t width,
+                            sdl_dtype_t dtype, const void* weight, sdl_dtype_t param_dtype, const float* mean, const float* rstd,
+                            const sdl_view_t* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary positions.  The first `rot` elements of every head are rot / 2 pairs, (i, i + rot / 2) in the half layout and
+ * (2 i, 2 i + 1) in the interleaved one; the elements behind them are copied.  With p the token's position:
+ *     (a, b) -> scale * (a cos(p f[i]) - b sin(p f[i]),  a sin(p f[i]) + b cos(p f[i]))
+ * inverse != 0 turns the other way, with the same scale, which is the gradient's way back.  positions: int32
+ * [batch][tokens] in device memory, or NULL for first_position + token.  frequencies: fp64 [rot / 2] in device memory, radians a
+ * position; the angle is reduced in 64 bits, so that positions far into a long context lose nothing.  out may be x itself, with the same
+ * strides.  Queries and keys that lie side by side in a fused projection's output are one call.
+ * Errors: SDL_ERR_INVALID_ARG (missing array, bad enum, odd rot, rot above width, scale not finite), SDL_ERR_UNSUPPORTED
+ * (width above SDL_ROTARY_MAX_WIDTH; 2^31 groups of eight pairs and more), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+#define SDL_ROTARY_MAX_WIDTH 1024u
+typedef enum { SDL_ROTARY_HALF = 0, SDL_ROTARY_INTERLEAVED = 1 } sdl_rotary_layout_t;
+int sdl_rotary(const sdl_view_t* x, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t width, sdl_dtype_t dtype, uint32_t rot,
+               sdl_rotary_layout_t layout, const int32_t* positions, int32_t first_position, const double* frequencies, float scale,
+               int inverse, const sdl_view_t* out, void* stream);
+
+/* The frequencies f[i] = base^(-2 i / rot), i < rot / 2, into a HOST array; no device is touched.
+ *     SDL_ROTARY_PLAIN    as they are (factor, low, high and trained_length are not looked at)
+ *     SDL_ROTARY_LINEAR   f / factor: positions of a context `factor` times as long as the trained one, pressed together
+ *     SDL_ROTARY_PARTS    by the turns n = trained_length f / (2 pi) that a pair makes over the trained length: f / factor where
+ *                         n <= low, f where n >= high, and in between f (k + (1 - k) / factor), k = (n - low) / (high - low) */
+typedef enum { SDL_ROTARY_PLAIN = 0, SDL_ROTARY_LINEAR = 1, SDL_ROTARY_PARTS = 2 } sdl_rotary_scaling_t;
+int sdl_rotary_frequencies(uint32_t rot, double base, sdl_rotary_scaling_t scaling, double factor, double low, double high,
+                           uint32_t trained_length, double* out);
+
+/* Attention of q [batch][queries][heads][width] over k, v [batch][keys][kv_heads][width]; heads is a multiple of kv_heads, and
+ * query head h reads key head h / (heads / kv_heads):
+ *     S = scale q k^T,  P = softmax of S over the keys that a query sees,  out = P v,  lse = log of the sum of exp(S)
+ * q_len, k_len: int32 [batch] in device memory, the valid queries and keys of every sequence (NULL: all of them; what is out of range is
+ * taken as the nearest valid length).  Nothing behind a length is read into a result.  causal != 0: valid query t sees the keys up to
+ * t + k_len - q_len, so that the last query stands at the last key, as new tokens over a cache do; otherwise it sees all valid ones.  A query that
+ * is not valid or sees no key gets out = 0 and lse = -infinity.  q, k and v are finite within the lengths: what is not may spread to
+ * queries that do not see it.
+ * out: [batch][queries][heads][width].  lse: fp32 [batch][heads][queries] (natural logarithm), or NULL; the backward pass needs it.
+ * Products have the type's inputs and fp32 sums (bf16: probabilities are rounded to bf16 before they meet v).  workspace: device
+ * memory, 4-byte aligned, of at least sdl_attention_workspace_bytes(...) bytes (0 for many shapes), contents irrelevant.  Results
+ * do not depend on anything but the arguments.
+ * Errors: SDL_ERR_INVALID_ARG (missing array, bad type, width 0, heads no multiple of kv_heads, scale not positive and
+ * finite, workspace too small), SDL_ERR_UNSUPPORTED (width above SDL_ATTENTION_MAX_WIDTH; more than 2^30 keys, queries times heads or
+ * batch times heads), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+#define SDL_ATTENTION_MAX_WIDTH 128u
+size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width);
+int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, uint32_t batch, uint32_t queries, uint32_t keys,
+                  uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len,
+                  const int32_t* k_len, const sdl_view_t* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradients, from d_out, the inputs, and the forward pass' out and lse; P is worked out again from lse:
+ *     D = sum over the width of d_out out,  dS = P (d_out v^T - D),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T d_out
+ * dk and dv of a key head are the sums over its query heads.  Rows behind a length, and of queries that see nothing, are 0.  The order of
+ * every sum is fixed by the arguments: two calls give the same bits.  dq, dk, dv are written, not added to; they may lie in one array.
+ * workspace: as above, sdl_attention_backward_workspace_bytes(...) bytes.  Errors as above. */
+size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width);
+int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, const sdl_view_t* out,
+                           const float* lse, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
+                           uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len,
+                           const sdl_view_t* dq, const sdl_view_t* dk, const sdl_view_t* dv, void* workspace, size_t workspace_bytes,
+                           void* stream);
 
 const char* sdl_status_string(int status);
 

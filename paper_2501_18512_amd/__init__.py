@@ -40,6 +40,11 @@ class _Span(ctypes.Structure):
     _fields_ = [("offset", ctypes.c_uint64), ("numel", ctypes.c_uint64), ("unit", ctypes.c_int32)]
 
 
+class _View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_batch", ctypes.c_int64), ("stride_token", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2501_18512_amd/build.py` "
@@ -120,6 +125,18 @@ def _load() -> ctypes.CDLL:
     lib.sdl_outer_grad_cosine.argtypes = [vp, pp, u32, u64, vp, vp, ctypes.c_size_t, vp]
     lib.sdl_outer_grad_cosine_plan.argtypes = [vp, u32, vp, pp, u32, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sdl_cosine_combine.argtypes = [vp, u64, u32, u32, vp, vp]
+    pv, shape4, shape6 = ctypes.POINTER(_View), [u32] * 4, [u32] * 6
+    lib.sdl_layer_norm.argtypes = [pv, *shape4, ctypes.c_int, vp, vp, ctypes.c_int, f32, pv, vp, vp, vp]
+    lib.sdl_layer_norm_workspace_bytes.argtypes = [u32]
+    lib.sdl_layer_norm_workspace_bytes.restype = ctypes.c_size_t
+    lib.sdl_layer_norm_backward.argtypes = [pv, pv, *shape4, ctypes.c_int, vp, ctypes.c_int, vp, vp, pv, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.sdl_rotary.argtypes = [pv, *shape4, ctypes.c_int, u32, ctypes.c_int, vp, ctypes.c_int32, vp, f32, ctypes.c_int, pv, vp]
+    lib.sdl_rotary_frequencies.argtypes = [u32, ctypes.c_double, ctypes.c_int, ctypes.c_double, ctypes.c_double, ctypes.c_double, u32, vp]
+    for name in ("sdl_attention_workspace_bytes", "sdl_attention_backward_workspace_bytes"):
+        getattr(lib, name).argtypes = shape6
+        getattr(lib, name).restype = ctypes.c_size_t
+    lib.sdl_attention.argtypes = [pv, pv, pv, *shape6, ctypes.c_int, f32, ctypes.c_int, vp, vp, pv, vp, vp, ctypes.c_size_t, vp]
+    lib.sdl_attention_backward.argtypes = [pv] * 5 + [vp, *shape6, ctypes.c_int, f32, ctypes.c_int, vp, vp, pv, pv, pv, vp, ctypes.c_size_t, vp]
     lib.sdl_status_string.argtypes = [ctypes.c_int]
     lib.sdl_status_string.restype = ctypes.c_char_p
     return lib
@@ -622,3 +639,169 @@ def alloc_exchange(fmt: int, n: int, M: int, device="cuda"):
     codes = [torch.empty(max(cb, 16), dtype=torch.uint8, device=device) for _ in range(M)]
     scales = [torch.empty(max(sb, 16), dtype=torch.uint8, device=device) for _ in range(M)]
     return codes, scales
+
+
+# ------------------------------------------------------------------ operators of the inner step and of evaluation
+
+DTYPE_FP32, DTYPE_BF16 = 0, 1
+_DTYPES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+NORM_MAX_WIDTH, ROTARY_MAX_WIDTH, ATTENTION_MAX_WIDTH = 16384, 1024, 128
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_PARTS = 0, 1, 2
+
+
+def _dtype(t) -> int:
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise ValueError(f"the operators take float32 and bfloat16, not {t.dtype}") from None
+
+
+def _shape4(t) -> Tuple[int, int, int, int]:
+    """[batch, tokens, heads, width] of a tensor of one to four dimensions: what is missing is in front of the tokens, or is one head."""
+    s = t.shape
+    n = len(s)
+    if n == 4:
+        return tuple(s)
+    if n == 3:
+        return s[0], s[1], 1, s[2]
+    if n == 2:
+        return 1, s[0], 1, s[1]
+    if n == 1:
+        return 1, 1, 1, s[0]
+    raise ValueError("the operators take tensors of one to four dimensions")
+
+
+def _view(t, shape=None, dtype=None) -> _View:
+    if not t.is_cuda:
+        raise ValueError("sdl calls take device tensors; there is no CPU path")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"a tensor of shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"a tensor of {t.dtype} where {dtype} is needed")
+    s = t.stride()
+    n = len(s)
+    if s[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError("neighbouring elements of a row must be neighbours in memory")
+    return _View(t.data_ptr(), s[0] if n > 2 else 0, s[-2] if n in (2, 3) else s[1] if n == 4 else 0, s[2] if n == 4 else 0)
+
+
+def _flat(t, numel: int, dtype, what: str) -> int:
+    """Address of a contiguous array of that many elements; None is the null pointer."""
+    if t is None:
+        return 0
+    _require_device(t)
+    if t.dtype != dtype or t.numel() != numel:
+        raise ValueError(f"{what}: {numel} elements of {dtype} are needed")
+    return t.data_ptr()
+
+
+def _space(workspace) -> Tuple[int, int]:
+    if workspace is None:
+        return 0, 0
+    _require_device(workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _params(weight, others, width: int):
+    """Type and addresses of a norm's parameter arrays."""
+    given = [t for t in (weight, *others) if t is not None]
+    dtype = given[0].dtype if given else torch.float32
+    return _dtype(given[0]) if given else DTYPE_FP32, [_flat(t, width, dtype, "parameters of a norm") for t in (weight, *others)]
+
+
+def alloc_layer_norm(x):
+    """(mean, rstd, workspace) for the norm of x and its backward pass."""
+    _, _, _, width = _shape4(x)
+    rows = x.shape[:-1]
+    return (torch.empty(rows, dtype=torch.float32, device=x.device), torch.empty(rows, dtype=torch.float32, device=x.device),
+            torch.empty(max(_lib.sdl_layer_norm_workspace_bytes(width), 4), dtype=torch.uint8, device=x.device))
+
+
+def sdl_layer_norm_workspace_bytes(width: int) -> int:
+    return _lib.sdl_layer_norm_workspace_bytes(width)
+
+
+def sdl_layer_norm(x, weight, bias, eps: float, y, mean=None, rstd=None, stream=None):
+    shape = _shape4(x)
+    rows = shape[0] * shape[1] * shape[2]
+    param_dtype, (w, b) = _params(weight, (bias,), shape[3])
+    vx, vy = _view(x), _view(y, x.shape, x.dtype)
+    _check(_lib.sdl_layer_norm(vx, *shape, _dtype(x), w, b, param_dtype, eps, vy, _flat(mean, rows, torch.float32, "mean"),
+                               _flat(rstd, rows, torch.float32, "rstd"), _stream(stream)), "sdl_layer_norm")
+
+
+def sdl_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream=None):
+    shape = _shape4(x)
+    rows = shape[0] * shape[1] * shape[2]
+    param_dtype, (w, dw, db) = _params(weight, (dweight, dbias), shape[3])
+    vd, vx, vo = _view(dy, x.shape, x.dtype), _view(x), _view(dx, x.shape, x.dtype)
+    _check(_lib.sdl_layer_norm_backward(vd, vx, *shape, _dtype(x), w, param_dtype, _flat(mean, rows, torch.float32, "mean"),
+                                        _flat(rstd, rows, torch.float32, "rstd"), vo, dw, db, *_space(workspace), _stream(stream)),
+           "sdl_layer_norm_backward")
+
+
+def sdl_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, low: float = 1.0,
+                           high: float = 4.0, trained_length: int = 0) -> torch.Tensor:
+    """The rot / 2 frequencies as an fp64 tensor in host memory."""
+    out = torch.empty(rot // 2, dtype=torch.float64)
+    _check(_lib.sdl_rotary_frequencies(rot, base, scaling, factor, low, high, trained_length, out.data_ptr() or None),
+           "sdl_rotary_frequencies")
+    return out
+
+
+def sdl_rotary(x, positions, frequencies, out, layout: int = ROTARY_HALF, scale: float = 1.0, inverse: bool = False,
+               first_position: int = 0, stream=None):
+    """positions: int32 [batch, tokens], or None for first_position, first_position + 1, ...; frequencies: fp64 [rot / 2] on the device."""
+    shape = _shape4(x)
+    vx, vo = _view(x), _view(out, x.shape, x.dtype)
+    half = frequencies.numel()
+    _check(_lib.sdl_rotary(vx, *shape, _dtype(x), 2 * half, layout, _flat(positions, shape[0] * shape[1], torch.int32, "positions"),
+                           first_position, _flat(frequencies, half, torch.float64, "frequencies"), scale, bool(inverse), vo,
+                           _stream(stream)), "sdl_rotary")
+
+
+def _attention_shape(q, k) -> Tuple[int, int, int, int, int, int]:
+    if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        raise ValueError("attention takes q [batch, queries, heads, width] and k, v [batch, keys, kv_heads, width]")
+    return q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
+
+
+def sdl_attention_workspace_bytes(batch: int, queries: int, keys: int, heads: int, kv_heads: int, width: int) -> int:
+    return _lib.sdl_attention_workspace_bytes(batch, queries, keys, heads, kv_heads, width)
+
+
+def sdl_attention_backward_workspace_bytes(batch: int, queries: int, keys: int, heads: int, kv_heads: int, width: int) -> int:
+    return _lib.sdl_attention_backward_workspace_bytes(batch, queries, keys, heads, kv_heads, width)
+
+
+def alloc_attention(q, k, backward: bool = False):
+    """Workspace for sdl_attention on tensors like these, and for sdl_attention_backward if asked."""
+    shape = _attention_shape(q, k)
+    n = _lib.sdl_attention_workspace_bytes(*shape)
+    if backward:
+        n = max(n, _lib.sdl_attention_backward_workspace_bytes(*shape))
+    return torch.empty(max(n, 4), dtype=torch.uint8, device=q.device)
+
+
+def sdl_attention(q, k, v, out, lse=None, workspace=None, scale: Optional[float] = None, causal: bool = False, q_len=None, k_len=None,
+                  stream=None):
+    """scale: 1 / sqrt(width) if not given."""
+    shape = B, Lq, _, H, _, D = _attention_shape(q, k)
+    dt = q.dtype
+    vq, vk, vv, vo = _view(q), _view(k, None, dt), _view(v, k.shape, dt), _view(out, q.shape, dt)
+    _check(_lib.sdl_attention(vq, vk, vv, *shape, _dtype(q), D ** -0.5 if scale is None else scale, bool(causal),
+                              _flat(q_len, B, torch.int32, "q_len"), _flat(k_len, B, torch.int32, "k_len"), vo,
+                              _flat(lse, B * H * Lq, torch.float32, "lse"), *_space(workspace), _stream(stream)), "sdl_attention")
+
+
+def sdl_attention_backward(d_out, q, k, v, out, lse, dq, dk, dv, workspace, scale: Optional[float] = None, causal: bool = False, q_len=None,
+                           k_len=None, stream=None):
+    shape = B, Lq, _, H, _, D = _attention_shape(q, k)
+    dt = q.dtype
+    views = [_view(d_out, q.shape, dt), _view(q), _view(k, None, dt), _view(v, k.shape, dt), _view(out, q.shape, dt)]
+    grads = [_view(dq, q.shape, dt), _view(dk, k.shape, dt), _view(dv, k.shape, dt)]
+    _check(_lib.sdl_attention_backward(*views, _flat(lse, B * H * Lq, torch.float32, "lse"), *shape, _dtype(q),
+                                       D ** -0.5 if scale is None else scale, bool(causal), _flat(q_len, B, torch.int32, "q_len"),
+                                       _flat(k_len, B, torch.int32, "k_len"), *grads, *_space(workspace), _stream(stream)),
+           "sdl_attention_backward")

@@ -1,0 +1,228 @@
+// Device code that attention's forward and backward kernels share (gfx950).  Internal to csrc/.
+//
+// Layouts of the 32x32 matrix instructions, for lane l, half = l / 32, c = l % 32:
+//   A (32 x 16)  row c,    k = 8 half + j        B (16 x 32)  column c, k = 8 half + j        j = 0..7
+//   D (32 x 32)  column c, row 8 (i / 4) + 4 half + i % 4                                     i = 0..15
+// The sum over k may run in any order as long as A and B agree on it.  Eight registers i = 8 u .. 8 u + 7 of a D tile hold the rows
+// 16 u + order(half, j) of their column, order(half, j) = 8 (j / 4) + 4 half + j % 4: they are a B operand of a second product, as
+// they stand, whose A operand takes its k in that order.  So the scores are formed with the queries (or keys) that a
+// lane keeps as columns, and probabilities never move between lanes.
+#pragma once
+
+#include "sdl_operand.h"
+
+namespace sdl_device {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// One operand of a product over 16 values of k: eight elements a lane.
+template <typename T> struct Frag;
+template <> struct Frag<__bf16> { bf16x8_t v; };
+template <> struct Frag<float> { float v[8]; };
+
+__device__ __forceinline__ void mma(f32x16_t& d, const Frag<__bf16>& a, const Frag<__bf16>& b)
+{
+    d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, d, 0, 0, 0);
+}
+// fp32: one instruction has k = 0, 1 in the two halves; the j-th takes k = j and 8 + j
+__device__ __forceinline__ void mma(f32x16_t& d, const Frag<float>& a, const Frag<float>& b)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], d, 0, 0, 0);
+}
+
+__device__ __forceinline__ void set_frag(Frag<__bf16>& f, const Eight<__bf16>& x) { f.v = __builtin_bit_cast(bf16x8_t, x.w); }
+__device__ __forceinline__ void set_frag(Frag<float>& f, const Eight<float>& x)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j] = x.get(j);
+}
+
+// Registers 8 u .. 8 u + 7 of a D tile as an operand.  bf16: probabilities and their gradients are rounded to nearest here; the sums over them
+// stay in fp32.
+__device__ __forceinline__ Frag<__bf16> frag_of(const f32x16_t& d, int u, __bf16)
+{
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack_bf16(d[8 * u + 2 * j], d[8 * u + 2 * j + 1]);
+    return Frag<__bf16>{__builtin_bit_cast(bf16x8_t, w)};
+}
+__device__ __forceinline__ Frag<float> frag_of(const f32x16_t& d, int u, float)
+{
+    Frag<float> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j] = d[8 * u + j];
+    return f;
+}
+
+// A tile of rows of HD elements in shared memory.  The 16-byte pieces of a row are swapped around by an xor with spread(row), so that
+// neither the reads along rows (eight lanes, eight rows, one piece) nor the ones across them (four rows, four pieces) meet in a bank.
+template <typename T, int HD>
+struct Tile {
+    static constexpr int kPieces = HD * (int)sizeof(T) / 16;
+    static constexpr int kPer = 16 / (int)sizeof(T);            // elements of a piece
+
+    static __device__ __forceinline__ int spread(int r)
+    {
+        return kPieces >= 16 ? (((r & 3) << 2) | ((r >> 2) & 3)) : ((((r >> 1) & 1) << 2) | ((r >> 2) & 3));
+    }
+    static __device__ __forceinline__ int piece(int r, int p) { return r * kPieces + (p ^ spread(r)); }      // in 16-byte units
+
+    static __device__ __forceinline__ void put(T* tile, int r, int c8, const Eight<T>& x)
+    {
+        u32x4* p = reinterpret_cast<u32x4*>(tile);
+        if constexpr (sizeof(T) == 2) {
+            p[piece(r, c8)] = x.w;
+        } else {
+            p[piece(r, 2 * c8)] = x.lo;
+            p[piece(r, 2 * c8 + 1)] = x.hi;
+        }
+    }
+    // elements [8 c8, 8 c8 + 8) of row r
+    static __device__ __forceinline__ Frag<T> along(const T* tile, int r, int c8)
+    {
+        const u32x4* p = reinterpret_cast<const u32x4*>(tile);
+        Frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            f.v = __builtin_bit_cast(bf16x8_t, p[piece(r, c8)]);
+        } else {
+            const u32x4 a = p[piece(r, 2 * c8)], b = p[piece(r, 2 * c8 + 1)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f.v[j] = u2f(a[j]), f.v[4 + j] = u2f(b[j]);
+        }
+        return f;
+    }
+    // column d0 + lane % 32 of the rows r0 + order(half, j).  bf16: the transposing read gives lane i of 16 the i-th column of a
+    // block of 4 rows and 16 columns, of which lane 4 r + q names the q-th quarter of row r.
+    static __device__ __forceinline__ Frag<T> across(const T* tile, int r0, int d0)
+    {
+        const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
+        Frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+            const int r = r0 + 4 * half + ((lane & 15) >> 2), d = d0 + (lane & 16) + 4 * (lane & 3);
+            const char* base = reinterpret_cast<const char*>(tile);
+            const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + piece(r, d >> 3) * 16 + (d & 4) * 2));
+            const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + piece(r + 8, d >> 3) * 16 + (d & 4) * 2));
+            const bf16x4_t x = __builtin_bit_cast(bf16x4_t, a), y = __builtin_bit_cast(bf16x4_t, b);
+            f.v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            const int d = d0 + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = r0 + 8 * (j / 4) + 4 * half + j % 4;
+                f.v[j] = u2f(reinterpret_cast<const uint32_t*>(tile)[piece(r, d >> 2) * 4 + (d & 3)]);
+            }
+        }
+        return f;
+    }
+};
+
+// x of lane l and of lane l ^ 32
+__device__ __forceinline__ float half_max(float x)
+{
+    const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false));
+    return fmaxf(u2f(p[0]), u2f(p[1]));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false));
+    return u2f(p[0]) + u2f(p[1]);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Four neighbouring elements of a row of n from element `at` on.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, uint32_t at, uint32_t n, float a, float b, float c, float d)
+{
+    if (at + 4 <= n) {
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<u32x2_elem*>(row + at) = u32x2_elem{pack_bf16(a, b), pack_bf16(c, d)};
+        else
+            *reinterpret_cast<u32x4_f32elem*>(row + at) = u32x4_f32elem{f2u(a), f2u(b), f2u(c), f2u(d)};
+        return;
+    }
+    const float v[4] = {a, b, c, d};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (at + j < n) row[at + j] = (T)v[j];
+}
+
+// The problem, as every kernel takes it.  The query heads of a key head are taken together: row r of a (batch, key head)
+// is query token r / group, head r % group of the group, so that keys and values are read once for all of them and the
+// gradients of a shared head are one sum.
+struct Attention {
+    View q, k, v, out, d_out, dq, dk, dv;
+    float* lse;                 // [batch][heads][queries]
+    float* delta;               // the same shape, in the workspace
+    const int32_t* q_len;
+    const int32_t* k_len;
+    Div group;                  // query heads of a key head
+    uint32_t queries, keys, kv_heads, width, batch;
+    float scale, scale_log2;    // and times log2(e)
+    uint32_t causal;
+};
+
+// One (batch, key head) of it: valid lengths, and which keys a row sees.  The last valid query stands at the last valid key.
+struct Sequence {
+    uint32_t b, g;
+    int32_t nq, nk;             // valid queries, keys
+    int32_t shift;              // query t sees keys up to t + shift (causal)
+
+    __device__ __forceinline__ Sequence(const Attention& a, uint32_t b_, uint32_t g_) : b(b_), g(g_)
+    {
+        nq = (int32_t)a.queries;
+        nk = (int32_t)a.keys;
+        if (a.q_len) nq = min(nq, max(a.q_len[b], 0));
+        if (a.k_len) nk = min(nk, max(a.k_len[b], 0));
+        shift = nk - nq;
+    }
+    // keys that valid query t sees: [0, seen(t))
+    __device__ __forceinline__ int32_t seen(const Attention& a, int32_t t) const
+    {
+        return a.causal ? max(0, min(nk, t + shift + 1)) : nk;
+    }
+};
+
+// Consecutive workgroups go to different compute dies (eight, each with its own cache): the work is handed out in runs of neighbours
+// per die, so that the workgroups that read the same keys and values share a cache.
+__device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n)
+{
+    const uint32_t die = id & 7u, each = n >> 3, more = n & 7u;
+    return die * each + min(die, more) + (id >> 3);
+}
+
+template <typename T>
+__device__ __forceinline__ T* at_row(const View& v, uint32_t b, uint32_t token, uint32_t head)
+{
+    return reinterpret_cast<T*>(v.data) + ((int64_t)b * v.batch + (int64_t)token * v.token + (int64_t)head * v.head);
+}
+
+// Host: the checks that do not look at the arrays, and the arguments that do not depend on the pass.
+inline int sdl_attention_problem(Attention& p, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
+                                 uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len)
+{
+    if (!known(dtype) || width == 0 || !(scale > 0.0f) || scale > 3.4028235e38f) return SDL_ERR_INVALID_ARG;
+    if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return SDL_ERR_INVALID_ARG;
+    if (width > SDL_ATTENTION_MAX_WIDTH || keys > 0x40000000u) return SDL_ERR_UNSUPPORTED;
+    if ((uint64_t)queries * heads > 0x40000000u || (uint64_t)batch * heads > 0x40000000u) return SDL_ERR_UNSUPPORTED;
+    if (!aligned_to(q_len, 4) || !aligned_to(k_len, 4)) return SDL_ERR_ALIGNMENT;
+    p.q_len = q_len;
+    p.k_len = k_len;
+    p.group = make_div(heads ? heads / kv_heads : 1);
+    p.queries = queries;
+    p.keys = keys;
+    p.kv_heads = kv_heads;
+    p.width = width;
+    p.batch = batch;
+    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    p.causal = causal != 0;
+    return SDL_OK;
+}
+
+}  // namespace sdl_device

@@ -1,0 +1,247 @@
+// Attention, forward (gfx950):  S = scale q k^T, masked;  P = softmax(S);  out = P v;  lse = log sum exp S.
+//
+// One pass over the keys with the running maximum m and sum l of every row.  A workgroup has 4 wavefronts of 32 rows; a tile of
+// keys and values goes through shared memory.  S^T = k q^T has a row's scores in the registers of two lanes, and P^T as it stands is the
+// operand of out^T = v^T P^T (sdl_attention.h), so that m, l and the rescaling of the result are a lane's own.
+// Where there are too few rows to fill the chip, the keys are split over workgroups, which leave normalised results and their
+// log sums in the workspace, and a second kernel joins them.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "sdl_attention.h"
+
+namespace {
+
+using namespace sdl_device;
+
+constexpr int kRowsPerWave = 32, kWaves = 4, kRows = kRowsPerWave * kWaves;
+constexpr uint32_t kMaxSplits = 64;
+
+struct ForwardArgs {
+    Attention p;
+    float* part_out;        // [split][batch][key head][row][width], with more than one split
+    float* part_lse;        // [split][batch][key head][row]
+    uint32_t row_blocks, splits, workgroups;
+};
+
+template <typename T, int HD, int BN>
+__global__ void __launch_bounds__(kWaves * kWave) sdl_attention_kernel(const ForwardArgs a)
+{
+    constexpr int kTiles = BN / 32, kSteps = HD / 16, kOut = HD / 32;
+    typedef Tile<T, HD> Smem;
+    __shared__ __attribute__((aligned(16))) T ks[BN * HD];
+    __shared__ __attribute__((aligned(16))) T vs[BN * HD];
+    const Attention& p = a.p;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
+
+    uint32_t id = die_order(blockIdx.x, a.workgroups);
+    const uint32_t split = id % a.splits;
+    id /= a.splits;
+    const uint32_t block = a.row_blocks - 1 - id % a.row_blocks;      // the longest first
+    id /= a.row_blocks;
+    const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
+
+    const uint32_t n_rows = p.queries * p.group.d;
+    const uint32_t row = block * kRows + wave * kRowsPerWave + c;
+    const uint32_t row_in = min(row, n_rows - 1);
+    const int32_t t = (int32_t)div(row_in, p.group);
+    const uint32_t head = s.g * p.group.d + (row_in - (uint32_t)t * p.group.d);
+    const bool valid = row < n_rows && t < s.nq;
+
+    Frag<T> q[kSteps];
+    {
+        const T* src = at_row<T>(p.q, s.b, (uint32_t)t, head);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) set_frag(q[k], load8(src, k * 16 + half * 8, valid ? p.width : 0));
+    }
+    const int32_t sees = valid ? s.seen(p, t) : 0;
+    // the workgroup's keys: [first tile, last tile) of this split
+    const int32_t t_first = (int32_t)div(min(block * kRows, n_rows - 1), p.group);
+    const int32_t t_last = min((int32_t)div(min(block * kRows + kRows, n_rows) - 1, p.group), s.nq - 1);
+    const int32_t keys = t_last < t_first ? 0 : s.seen(p, t_last);      // no valid row: nothing to see
+    const int32_t every = t_last < t_first ? 0 : s.seen(p, t_first);    // keys that all valid rows see
+    const int32_t tiles = (keys + BN - 1) / BN;
+    const int32_t tile0 = (int32_t)((uint64_t)tiles * split / a.splits), tile1 = (int32_t)((uint64_t)tiles * (split + 1) / a.splits);
+
+    f32x16_t o[kOut] = {};
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int32_t tile = tile0; tile < tile1; ++tile) {
+        const int32_t key0 = tile * BN;
+        __syncthreads();
+#pragma unroll 4
+        for (int i = threadIdx.x; i < BN * (HD / 8); i += kWaves * kWave) {
+            const int r = i / (HD / 8), c8 = i % (HD / 8);
+            const uint32_t key = (uint32_t)min(key0 + r, s.nk - 1);       // behind the last key: that key again, with probability 0
+            Smem::put(ks, r, c8, load8(at_row<T>(p.k, s.b, key, s.g), c8 * 8, p.width));
+            Smem::put(vs, r, c8, load8(at_row<T>(p.v, s.b, key, s.g), c8 * 8, p.width));
+        }
+        __syncthreads();
+        f32x16_t sc[kTiles] = {};
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma(sc[n], Smem::along(ks, n * 32 + c, 2 * k + half), q[k]);
+        if (key0 + BN > every) {
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key0 + n * 32 + 8 * (i / 4) + 4 * half + i % 4 >= sees) sc[n][i] = -__builtin_inff();
+        }
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[n][i]);
+        top = half_max(top) * p.scale_log2;
+        if (__any(top > m)) {
+            const float now = fmaxf(m, top), by = exp2_fast(m - (now == -__builtin_inff() ? 0.0f : now));
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) o[n] *= by;
+        }
+        const float off = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                sc[n][i] = exp2_fast(__builtin_fmaf(sc[n][i], p.scale_log2, -off));
+                l += sc[n][i];
+            }
+#pragma unroll
+        for (int u = 0; u < BN / 16; ++u) {
+            const Frag<T> pr = frag_of(sc[u / 2], u % 2, T());
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) mma(o[n], Smem::across(vs, u * 16, n * 32), pr);
+        }
+    }
+    l = half_sum(l);
+    if (row >= n_rows) return;
+    if (sees == 0) {                      // rows that see nothing, in a workgroup whose tiles need no mask for those that do
+        l = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kOut; ++n) o[n] = f32x16_t{};
+    }
+    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    const float lse = l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (a.splits == 1) {
+        T* dst = at_row<T>(p.out, s.b, (uint32_t)t, head);
+#pragma unroll
+        for (int n = 0; n < kOut; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                store4(dst, n * 32 + 2 * i + 4 * half, p.width, o[n][i] * by, o[n][i + 1] * by, o[n][i + 2] * by, o[n][i + 3] * by);
+        if (p.lse && half == 0) p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = lse;
+    } else {
+        const uint64_t line = (((uint64_t)split * p.batch + s.b) * p.kv_heads + s.g) * n_rows + row;
+        float* dst = a.part_out + line * p.width;
+#pragma unroll
+        for (int n = 0; n < kOut; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                store4(dst, n * 32 + 2 * i + 4 * half, p.width, o[n][i] * by, o[n][i + 1] * by, o[n][i + 2] * by, o[n][i + 3] * by);
+        if (half == 0) a.part_lse[line] = lse;
+    }
+}
+
+// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s: one wavefront a row, two elements a lane.
+template <typename T>
+__global__ void __launch_bounds__(256) sdl_attention_join_kernel(const ForwardArgs a)
+{
+    const Attention& p = a.p;
+    const uint32_t n_rows = p.queries * p.group.d, lane = threadIdx.x & (kWave - 1);
+    const uint64_t line = (uint64_t)blockIdx.x * 4 + threadIdx.x / kWave, lines = (uint64_t)p.batch * p.kv_heads * n_rows;
+    if (line >= lines) return;
+    float top = -__builtin_inff();
+    for (uint32_t s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_lse[s * lines + line]);
+    const float off = top == -__builtin_inff() ? 0.0f : top;
+    float sum = 0.0f, x = 0.0f, y = 0.0f;
+    const uint32_t d = 2 * lane;
+    for (uint32_t s = 0; s < a.splits; ++s) {
+        const float by = exp2_fast((a.part_lse[s * lines + line] - off) * kLog2e);
+        const float* src = a.part_out + (s * lines + line) * p.width;
+        sum += by;
+        if (d < p.width) x = __builtin_fmaf(by, src[d], x);
+        if (d + 1 < p.width) y = __builtin_fmaf(by, src[d + 1], y);
+    }
+    const uint32_t row = (uint32_t)(line % n_rows), t = div(row, p.group), bg = (uint32_t)(line / n_rows);
+    const uint32_t b = bg / p.kv_heads, head = (bg % p.kv_heads) * p.group.d + (row - t * p.group.d);
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T* dst = at_row<T>(p.out, b, t, head);
+    if (d < p.width) dst[d] = (T)(x * by);
+    if (d + 1 < p.width) dst[d + 1] = (T)(y * by);
+    if (p.lse && lane == 0)
+        p.lse[((uint64_t)b * p.kv_heads * p.group.d + head) * p.queries + t] = sum == 0.0f ? -__builtin_inff() : off + __builtin_amdgcn_logf(sum) * kLn2;
+}
+
+// Splits of the keys: as many as give 512 workgroups (two for every compute unit), of at least 256 keys.
+uint32_t splits_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads)
+{
+    const uint64_t rows = (uint64_t)queries * (heads / kv_heads);
+    const uint64_t groups = (rows + kRows - 1) / kRows * batch * kv_heads;
+    uint64_t n = groups ? 512 / groups : 1;
+    if (n > keys / 256) n = keys / 256;
+    if (n > kMaxSplits) n = kMaxSplits;
+    return n < 1 ? 1u : (uint32_t)n;
+}
+
+template <typename T>
+int forward(const ForwardArgs& a, hipStream_t st)
+{
+    const dim3 grid(a.workgroups), block(kWaves * kWave);
+    constexpr int kNarrow = sizeof(T) == 2 ? 64 : 32;       // keys of a tile: 32 KB of shared memory at width 128
+    if (a.p.width <= 64)
+        hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow>), grid, block, 0, st, a);
+    int rc = launched();
+    if (rc != SDL_OK || a.splits == 1) return rc;
+    const uint64_t lines = (uint64_t)a.p.batch * a.p.kv_heads * a.p.queries * a.p.group.d;
+    hipLaunchKernelGGL((sdl_attention_join_kernel<T>), dim3((uint32_t)((lines + 3) / 4)), dim3(256), 0, st, a);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width)
+{
+    if (kv_heads == 0 || heads % kv_heads != 0 || width == 0 || width > SDL_ATTENTION_MAX_WIDTH) return 0;
+    const uint32_t n = splits_of(batch, queries, keys, heads, kv_heads);
+    return n == 1 ? 0 : (size_t)n * batch * heads * queries * (width + 1) * sizeof(float);
+}
+
+int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, uint32_t batch, uint32_t queries, uint32_t keys,
+                  uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len,
+                  const int32_t* k_len, const sdl_view_t* out, float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    ForwardArgs a{};
+    int rc = sdl_attention_problem(a.p, batch, queries, keys, heads, kv_heads, width, dtype, scale, causal, q_len, k_len);
+    if (rc != SDL_OK) return rc;
+    if (batch == 0 || queries == 0 || heads == 0) return SDL_OK;
+    if ((rc = check_view(q, dtype)) != SDL_OK || (rc = check_output(out, dtype, batch, queries, heads)) != SDL_OK) return rc;
+    if (keys && ((rc = check_view(k, dtype)) != SDL_OK || (rc = check_view(v, dtype)) != SDL_OK)) return rc;
+    if (!aligned_to(lse, 4) || !aligned_to(workspace, 4)) return SDL_ERR_ALIGNMENT;
+    const size_t need = sdl_attention_workspace_bytes(batch, queries, keys, heads, kv_heads, width);
+    if (need && (!workspace || workspace_bytes < need)) return SDL_ERR_INVALID_ARG;
+    a.p.q = kernel_view(q);
+    if (keys) a.p.k = kernel_view(k), a.p.v = kernel_view(v);
+    a.p.out = kernel_view(out);
+    a.p.lse = lse;
+    a.splits = splits_of(batch, queries, keys, heads, kv_heads);
+    a.part_out = static_cast<float*>(workspace);
+    a.part_lse = a.part_out + (size_t)a.splits * batch * heads * queries * width;
+    const uint64_t rows = (uint64_t)queries * a.p.group.d;
+    a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
+    const uint64_t groups = (uint64_t)a.row_blocks * a.splits * batch * kv_heads;
+    if (groups > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
+    a.workgroups = (uint32_t)groups;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == SDL_DTYPE_BF16 ? forward<__bf16>(a, st) : forward<float>(a, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,285 @@
+// Attention, backward (gfx950):  P = exp(S - lse);  D = rowsum(d_out out);  dS = P (d_out v^T - D);
+//                                dq = scale dS k;  dk = scale dS^T q;  dv = P^T d_out.
+//
+// Two kernels, which both form S and d_out v^T again: 7 products of the size of S instead of the 5 that one kernel for all three would
+// take.  That one would have to add every key tile's share of dq up in memory, by fp32 atomics in an order of their own or through a buffer
+// per key tile: at 256 keys a workgroup and width 128 the two products more cost 131 kFLOP a row and tile, about 0.1 ns at the
+// rate of a large product, the sums 1 KB or more of traffic, about 0.2 ns.
+//   dq       rows are a wavefront's own, as in the forward pass: S^T = k q^T and dP^T = v d_out^T leave dS^T where dq^T = k^T dS^T wants it
+//   dk, dv   keys are a wavefront's own: S = q k^T and dP = d_out v^T leave P and dS where dv^T = d_out^T P and dk^T = q^T dS want them
+// D is worked out by the first and read by the second.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "sdl_attention.h"
+
+namespace {
+
+using namespace sdl_device;
+
+constexpr int kWaves = 4, kRows = 32 * kWaves, kKeys = 32 * kWaves, kTile = 32;
+
+struct BackwardArgs {
+    Attention p;
+    uint32_t blocks;        // of rows or keys, per (batch, key head)
+    uint32_t workgroups;
+};
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dq_kernel(const BackwardArgs a)
+{
+    constexpr int kSteps = HD / 16, kOut = HD / 32;
+    typedef Tile<T, HD> Smem;
+    __shared__ __attribute__((aligned(16))) T ks[kTile * HD];
+    __shared__ __attribute__((aligned(16))) T vs[kTile * HD];
+    const Attention& p = a.p;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
+
+    uint32_t id = die_order(blockIdx.x, a.workgroups);
+    const uint32_t block = a.blocks - 1 - id % a.blocks;       // the longest first
+    id /= a.blocks;
+    const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
+
+    const uint32_t n_rows = p.queries * p.group.d;
+    const uint32_t row = block * kRows + wave * 32 + c;
+    const uint32_t row_in = min(row, n_rows - 1);
+    const int32_t t = (int32_t)div(row_in, p.group);
+    const uint32_t head = s.g * p.group.d + (row_in - (uint32_t)t * p.group.d);
+    const bool valid = row < n_rows && t < s.nq;
+    const int32_t sees = valid ? s.seen(p, t) : 0;
+    const int32_t t_first = (int32_t)div(min(block * kRows, n_rows - 1), p.group);
+    const int32_t t_last = min((int32_t)div(min(block * kRows + kRows, n_rows) - 1, p.group), s.nq - 1);
+    const int32_t keys = t_last < t_first ? 0 : s.seen(p, t_last);
+    const int32_t every = t_last < t_first ? 0 : s.seen(p, t_first);
+
+    Frag<T> q[kSteps], g[kSteps];
+    float delta = 0.0f;
+    {
+        const uint32_t n = valid ? p.width : 0;
+        const T* src = at_row<T>(p.q, s.b, (uint32_t)t, head);
+        const T* src_g = at_row<T>(p.d_out, s.b, (uint32_t)t, head);
+        const T* src_o = at_row<T>(p.out, s.b, (uint32_t)t, head);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const Eight<T> x = load8(src_g, k * 16 + half * 8, n), y = load8(src_o, k * 16 + half * 8, n);
+            set_frag(q[k], load8(src, k * 16 + half * 8, n));
+            set_frag(g[k], x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta = __builtin_fmaf(x.get(j), y.get(j), delta);
+        }
+        delta = half_sum(delta);
+    }
+    const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + (uint32_t)t;
+    if (row < n_rows && half == 0) p.delta[stat] = delta;
+    const float lse2 = sees > 0 ? p.lse[stat] * kLog2e : 0.0f;
+
+    f32x16_t acc[kOut] = {};
+    for (int32_t key0 = 0; key0 < keys; key0 += kTile) {
+        __syncthreads();
+#pragma unroll 2
+        for (int i = threadIdx.x; i < kTile * (HD / 8); i += kWaves * kWave) {
+            const int r = i / (HD / 8), c8 = i % (HD / 8);
+            const uint32_t key = (uint32_t)min(key0 + r, s.nk - 1);
+            Smem::put(ks, r, c8, load8(at_row<T>(p.k, s.b, key, s.g), c8 * 8, p.width));
+            Smem::put(vs, r, c8, load8(at_row<T>(p.v, s.b, key, s.g), c8 * 8, p.width));
+        }
+        __syncthreads();
+        f32x16_t sc = {}, dp = {};
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            mma(sc, Smem::along(ks, c, 2 * k + half), q[k]);
+            mma(dp, Smem::along(vs, c, 2 * k + half), g[k]);
+        }
+        const bool cut = key0 + kTile > every;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float pr = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2));
+            sc[i] = pr * (dp[i] - delta);
+            if (cut && key0 + 8 * (i / 4) + 4 * half + i % 4 >= sees) sc[i] = 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const Frag<T> ds = frag_of(sc, u, T());
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(ks, u * 16, n * 32), ds);
+        }
+    }
+    if (row >= n_rows) return;
+    T* dst = at_row<T>(p.dq, s.b, (uint32_t)t, head);
+    const float by = p.scale;
+#pragma unroll
+    for (int n = 0; n < kOut; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const bool some = sees > 0;
+            store4(dst, n * 32 + 2 * i + 4 * half, p.width, some ? acc[n][i] * by : 0.0f, some ? acc[n][i + 1] * by : 0.0f,
+                   some ? acc[n][i + 2] * by : 0.0f, some ? acc[n][i + 3] * by : 0.0f);
+        }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dkv_kernel(const BackwardArgs a)
+{
+    constexpr int kSteps = HD / 16, kOut = HD / 32;
+    typedef Tile<T, HD> Smem;
+    __shared__ __attribute__((aligned(16))) T qs[kTile * HD];
+    __shared__ __attribute__((aligned(16))) T gs[kTile * HD];
+    __shared__ __attribute__((aligned(16))) float lse2s[kTile];
+    __shared__ __attribute__((aligned(16))) float deltas[kTile];
+    __shared__ __attribute__((aligned(16))) int32_t seens[kTile];
+    const Attention& p = a.p;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
+
+    uint32_t id = die_order(blockIdx.x, a.workgroups);
+    const uint32_t block = id % a.blocks;                      // the longest first
+    id /= a.blocks;
+    const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
+
+    const int32_t key0 = (int32_t)(block * kKeys), wave_key0 = key0 + wave * 32, key = wave_key0 + c;
+    Frag<T> k[kSteps], v[kSteps];
+    {
+        const uint32_t n = key < s.nk ? p.width : 0, at = (uint32_t)max(0, min(key, s.nk - 1));
+        const T* src_k = at_row<T>(p.k, s.b, at, s.g);
+        const T* src_v = at_row<T>(p.v, s.b, at, s.g);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            set_frag(k[i], load8(src_k, i * 16 + half * 8, n));
+            set_frag(v[i], load8(src_v, i * 16 + half * 8, n));
+        }
+    }
+    // rows that see a key of the block: those of the tokens from key0 - shift on
+    const uint32_t row_end = key0 < s.nk ? (uint32_t)s.nq * p.group.d : 0;
+    const uint32_t row_begin = p.causal ? (uint32_t)min(max(0, key0 - s.shift), s.nq) * p.group.d / kTile * kTile : 0;
+
+    f32x16_t dk[kOut] = {}, dv[kOut] = {};
+    for (uint32_t row0 = row_begin; row0 < row_end; row0 += kTile) {
+        __syncthreads();
+#pragma unroll 2
+        for (int i = threadIdx.x; i < kTile * (HD / 8); i += kWaves * kWave) {
+            const int r = i / (HD / 8), c8 = i % (HD / 8);
+            const uint32_t row = min(row0 + r, row_end - 1);
+            const uint32_t t = div(row, p.group), head = s.g * p.group.d + (row - t * p.group.d);
+            Smem::put(qs, r, c8, load8(at_row<T>(p.q, s.b, t, head), c8 * 8, p.width));
+            Smem::put(gs, r, c8, load8(at_row<T>(p.d_out, s.b, t, head), c8 * 8, p.width));
+        }
+        if (threadIdx.x < kTile) {
+            const uint32_t row = row0 + threadIdx.x, at = min(row, row_end - 1);
+            const uint32_t t = div(at, p.group), head = s.g * p.group.d + (at - t * p.group.d);
+            const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t;
+            const int32_t sees = row < row_end ? s.seen(p, (int32_t)t) : 0;
+            seens[threadIdx.x] = sees;
+            lse2s[threadIdx.x] = sees > 0 ? p.lse[stat] * kLog2e : 0.0f;
+            deltas[threadIdx.x] = p.delta[stat];
+        }
+        __syncthreads();
+        f32x16_t sc = {}, dp = {};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            mma(sc, Smem::along(qs, c, 2 * i + half), k[i]);
+            mma(dp, Smem::along(gs, c, 2 * i + half), v[i]);
+        }
+        // every row of the tile sees every key of the wavefront
+        const bool cut = row0 + kTile > row_end || s.seen(p, (int32_t)div(row0, p.group)) < wave_key0 + 32;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 8 * (i / 4) + 4 * half + i % 4;
+            const float pr = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2s[r]));
+            sc[i] = pr;
+            dp[i] = pr * (dp[i] - deltas[r]);
+            if (cut && key >= seens[r]) sc[i] = 0.0f, dp[i] = 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) {
+                mma(dv[n], Smem::across(gs, u * 16, n * 32), pr);
+                mma(dk[n], Smem::across(qs, u * 16, n * 32), ds);
+            }
+        }
+    }
+    if (key >= (int32_t)p.keys) return;
+    T* dst_k = at_row<T>(p.dk, s.b, (uint32_t)key, s.g);
+    T* dst_v = at_row<T>(p.dv, s.b, (uint32_t)key, s.g);
+    const bool some = key < s.nk;
+#pragma unroll
+    for (int n = 0; n < kOut; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const uint32_t at = n * 32 + 2 * i + 4 * half;
+            store4(dst_k, at, p.width, some ? dk[n][i] * p.scale : 0.0f, some ? dk[n][i + 1] * p.scale : 0.0f,
+                   some ? dk[n][i + 2] * p.scale : 0.0f, some ? dk[n][i + 3] * p.scale : 0.0f);
+            store4(dst_v, at, p.width, some ? dv[n][i] : 0.0f, some ? dv[n][i + 1] : 0.0f, some ? dv[n][i + 2] : 0.0f, some ? dv[n][i + 3] : 0.0f);
+        }
+}
+
+template <typename T, int HD>
+int backward(BackwardArgs& a, hipStream_t st)
+{
+    const Attention& p = a.p;
+    const uint64_t rows = (uint64_t)p.queries * p.group.d, heads = (uint64_t)p.batch * p.kv_heads;
+    const uint64_t row_blocks = (rows + kRows - 1) / kRows, key_blocks = ((uint64_t)p.keys + kKeys - 1) / kKeys;
+    if (row_blocks * heads > 0x7fffffffu || key_blocks * heads > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
+    if (rows) {
+        a.blocks = (uint32_t)row_blocks;
+        a.workgroups = (uint32_t)(row_blocks * heads);
+        hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD>), dim3(a.workgroups), dim3(kWaves * kWave), 0, st, a);
+        const int rc = launched();
+        if (rc != SDL_OK) return rc;
+    }
+    if (!key_blocks) return SDL_OK;
+    a.blocks = (uint32_t)key_blocks;
+    a.workgroups = (uint32_t)(key_blocks * heads);
+    hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD>), dim3(a.workgroups), dim3(kWaves * kWave), 0, st, a);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width)
+{
+    (void)keys;
+    if (kv_heads == 0 || heads % kv_heads != 0 || width == 0 || width > SDL_ATTENTION_MAX_WIDTH) return 0;
+    return (size_t)batch * heads * queries * sizeof(float);
+}
+
+int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, const sdl_view_t* out,
+                           const float* lse, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
+                           uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len,
+                           const sdl_view_t* dq, const sdl_view_t* dk, const sdl_view_t* dv, void* workspace, size_t workspace_bytes,
+                           void* stream)
+{
+    BackwardArgs a{};
+    int rc = sdl_attention_problem(a.p, batch, queries, keys, heads, kv_heads, width, dtype, scale, causal, q_len, k_len);
+    if (rc != SDL_OK) return rc;
+    if (batch == 0 || heads == 0 || (queries == 0 && keys == 0)) return SDL_OK;
+    if (queries) {
+        if ((rc = check_view(d_out, dtype)) != SDL_OK || (rc = check_view(q, dtype)) != SDL_OK || (rc = check_view(out, dtype)) != SDL_OK) return rc;
+        if ((rc = check_output(dq, dtype, batch, queries, heads)) != SDL_OK) return rc;
+        if (!lse || !workspace) return SDL_ERR_INVALID_ARG;
+        if (!aligned_to(lse, 4) || !aligned_to(workspace, 4)) return SDL_ERR_ALIGNMENT;
+        if (workspace_bytes < sdl_attention_backward_workspace_bytes(batch, queries, keys, heads, kv_heads, width)) return SDL_ERR_INVALID_ARG;
+        a.p.d_out = kernel_view(d_out);
+        a.p.q = kernel_view(q);
+        a.p.out = kernel_view(out);
+        a.p.dq = kernel_view(dq);
+        a.p.lse = const_cast<float*>(lse);
+        a.p.delta = static_cast<float*>(workspace);
+    }
+    if (keys) {
+        if ((rc = check_view(k, dtype)) != SDL_OK || (rc = check_view(v, dtype)) != SDL_OK) return rc;
+        if ((rc = check_output(dk, dtype, batch, keys, kv_heads)) != SDL_OK || (rc = check_output(dv, dtype, batch, keys, kv_heads)) != SDL_OK) return rc;
+        a.p.k = kernel_view(k);
+        a.p.v = kernel_view(v);
+        a.p.dk = kernel_view(dk);
+        a.p.dv = kernel_view(dv);
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == SDL_DTYPE_BF16) return width <= 64 ? backward<__bf16, 64>(a, st) : backward<__bf16, 128>(a, st);
+    return width <= 64 ? backward<float, 64>(a, st) : backward<float, 128>(a, st);
+}
+
+}  // extern "C"
