@@ -121,6 +121,100 @@ struct Tile {
     }
 };
 
+template <typename T>
+__device__ __forceinline__ T* at_row(const View& v, uint32_t b, uint32_t token, uint32_t head)
+{
+    return reinterpret_cast<T*>(v.data) + ((int64_t)b * v.batch + (int64_t)token * v.token + (int64_t)head * v.head);
+}
+
+// Copies of tiles into shared memory that bypass the registers: a wavefront's instruction brings 64 pieces of 16 bytes, which land
+// one behind the other, so that the rearrangement of a row's pieces is made in the addresses they come from.  The compiler does not see these
+// copies: loads_done() is to come before the barrier after which a tile is read.
+__device__ __forceinline__ uint32_t lds_offset(const void* p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+__device__ __forceinline__ void copy_piece(const char* base, uint32_t offset, uint32_t to)
+{
+    // a write of m0 needs one wait state before the instruction that reads it; nothing else in these kernels uses m0
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");
+}
+// Waits for this wavefront's copies and reads of shared memory, then for the workgroup.
+__device__ __forceinline__ void loads_done()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
+
+// A workgroup of WAVES wavefronts brings tiles of ROWS consecutive tokens of one head.  The offset of a lane's piece from the first row of
+// its share is the same in every tile; ASYNC is for rows that start on 16 bytes and lie at most 2^31 bytes apart in a tile, the other way
+// takes any element alignment and goes through registers.
+template <typename T, int HD, int ROWS, int WAVES, bool ASYNC>
+struct TileCopy {
+    typedef Tile<T, HD> Smem;
+    static constexpr int kPieces = Smem::kPieces;
+    static constexpr int kRowsPerCopy = kWave / kPieces;                    // rows of one instruction
+    static constexpr int kStep = kRowsPerCopy * WAVES;                      // rows of all wavefronts' instructions
+    static constexpr int kCopies = ROWS / kStep;
+    static_assert(ROWS % kStep == 0, "whole copies");
+
+    const char* base;       // first row of the head
+    int64_t stride;         // bytes between tokens
+    uint32_t width;         // elements of a row
+
+    __device__ __forceinline__ TileCopy(const View& v, uint32_t b, uint32_t head, uint32_t width_)
+    {
+        base = reinterpret_cast<const char*>(at_row<T>(v, b, 0, head));
+        stride = v.token * (int64_t)sizeof(T);
+        width = width_;
+    }
+    // Once: pieces behind the width are never brought, and have to be zero.
+    __device__ __forceinline__ void clear(T* tile) const
+    {
+        if (!ASYNC || width == HD) return;
+        for (uint32_t i = threadIdx.x; i < ROWS * kPieces; i += WAVES * kWave)
+            if (((i % kPieces) ^ (uint32_t)Smem::spread(i / kPieces)) * 16 >= width * sizeof(T)) reinterpret_cast<u32x4*>(tile)[i] = u32x4{0, 0, 0, 0};
+    }
+    // Rows [row0, row0 + ROWS) of `rows`; what lies behind the last row is that row again.
+    __device__ __forceinline__ void bring(T* tile, int32_t row0, int32_t rows) const
+    {
+        if constexpr (ASYNC) {
+            const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+            const uint32_t row = wave * kRowsPerCopy + lane / kPieces, to = lds_offset(tile) + wave * (kWave * 16);
+            const char* from = base + row0 * stride;
+            // the rearrangement has a period of 16 rows
+            uint32_t piece[kCopies];
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) piece[i] = (lane % kPieces) ^ (uint32_t)Smem::spread(row + (i * kStep) % 16);
+            if (row0 + ROWS <= rows && width == HD) {
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) copy_piece(from + i * kStep * stride, row * (uint32_t)stride + piece[i] * 16, to + i * (kStep * kPieces * 16));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i)
+                    if (piece[i] * 16 < width * sizeof(T))
+                        copy_piece(from, min(row + i * kStep, (uint32_t)(rows - 1 - row0)) * (uint32_t)stride + piece[i] * 16, to + i * (kStep * kPieces * 16));
+            }
+        } else {
+#pragma unroll 4
+            for (int i = threadIdx.x; i < ROWS * (HD / 8); i += WAVES * kWave) {
+                const int r = i / (HD / 8), c8 = i % (HD / 8);
+                const T* from = reinterpret_cast<const T*>(base + (int64_t)min(row0 + r, rows - 1) * stride);
+                Smem::put(tile, r, c8, load8(from, c8 * 8, width));
+            }
+        }
+    }
+};
+
+// Host: whether the tiles of a view may be brought by the asynchronous copies.
+inline bool async_rows(const View& v, uint32_t width, size_t size)
+{
+    const int64_t bytes = v.token * (int64_t)size;
+    return aligned_to(v.data, 16) && width * size % 16 == 0 && v.batch * (int64_t)size % 16 == 0 && v.head * (int64_t)size % 16 == 0 &&
+           bytes % 16 == 0 && bytes >= 0 && bytes < (1 << 24);
+}
+
 // x of lane l and of lane l ^ 32
 __device__ __forceinline__ float half_max(float x)
 {
@@ -194,12 +288,6 @@ __device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n)
 {
     const uint32_t die = id & 7u, each = n >> 3, more = n & 7u;
     return die * each + min(die, more) + (id >> 3);
-}
-
-template <typename T>
-__device__ __forceinline__ T* at_row(const View& v, uint32_t b, uint32_t token, uint32_t head)
-{
-    return reinterpret_cast<T*>(v.data) + ((int64_t)b * v.batch + (int64_t)token * v.token + (int64_t)head * v.head);
 }
 
 // Host: the checks that do not look at the arrays, and the arguments that do not depend on the pass.

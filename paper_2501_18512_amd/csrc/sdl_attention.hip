@@ -26,13 +26,13 @@ struct ForwardArgs {
     uint32_t row_blocks, splits, workgroups;
 };
 
-template <typename T, int HD, int BN>
-__global__ void __launch_bounds__(kWaves * kWave) sdl_attention_kernel(const ForwardArgs a)
+template <typename T, int HD, int BN, bool ASYNC>
+__global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_kernel(const ForwardArgs a)
 {
     constexpr int kTiles = BN / 32, kSteps = HD / 16, kOut = HD / 32;
     typedef Tile<T, HD> Smem;
-    __shared__ __attribute__((aligned(16))) T ks[BN * HD];
-    __shared__ __attribute__((aligned(16))) T vs[BN * HD];
+    __shared__ __attribute__((aligned(16))) T ks[2][BN * HD];
+    __shared__ __attribute__((aligned(16))) T vs[2][BN * HD];
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
 
@@ -65,24 +65,28 @@ __global__ void __launch_bounds__(kWaves * kWave) sdl_attention_kernel(const For
     const int32_t tiles = (keys + BN - 1) / BN;
     const int32_t tile0 = (int32_t)((uint64_t)tiles * split / a.splits), tile1 = (int32_t)((uint64_t)tiles * (split + 1) / a.splits);
 
+    const TileCopy<T, HD, BN, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
+
     f32x16_t o[kOut] = {};
     float m = -__builtin_inff(), l = 0.0f;
-    for (int32_t tile = tile0; tile < tile1; ++tile) {
+    if (tile0 < tile1) {
+        copy_k.bring(ks[0], tile0 * BN, s.nk);
+        copy_v.bring(vs[0], tile0 * BN, s.nk);
+    }
+    auto step = [&](int32_t tile, T* k_now, T* v_now, T* k_next, T* v_next) __attribute__((always_inline)) {
         const int32_t key0 = tile * BN;
-        __syncthreads();
-#pragma unroll 4
-        for (int i = threadIdx.x; i < BN * (HD / 8); i += kWaves * kWave) {
-            const int r = i / (HD / 8), c8 = i % (HD / 8);
-            const uint32_t key = (uint32_t)min(key0 + r, s.nk - 1);       // behind the last key: that key again, with probability 0
-            Smem::put(ks, r, c8, load8(at_row<T>(p.k, s.b, key, s.g), c8 * 8, p.width));
-            Smem::put(vs, r, c8, load8(at_row<T>(p.v, s.b, key, s.g), c8 * 8, p.width));
+        loads_done();               // this tile is there, and all are done with the one before it
+        if (tile + 1 < tile1) {
+            copy_k.bring(k_next, key0 + BN, s.nk);
+            copy_v.bring(v_next, key0 + BN, s.nk);
         }
-        __syncthreads();
         f32x16_t sc[kTiles] = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) mma(sc[n], Smem::along(ks, n * 32 + c, 2 * k + half), q[k]);
+            for (int n = 0; n < kTiles; ++n) mma(sc[n], Smem::along(k_now, n * 32 + c, 2 * k + half), q[k]);
         if (key0 + BN > every) {
 #pragma unroll
             for (int n = 0; n < kTiles; ++n)
@@ -115,8 +119,12 @@ __global__ void __launch_bounds__(kWaves * kWave) sdl_attention_kernel(const For
         for (int u = 0; u < BN / 16; ++u) {
             const Frag<T> pr = frag_of(sc[u / 2], u % 2, T());
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) mma(o[n], Smem::across(vs, u * 16, n * 32), pr);
+            for (int n = 0; n < kOut; ++n) mma(o[n], Smem::across(v_now, u * 16, n * 32), pr);
         }
+    };
+    for (int32_t tile = tile0; tile < tile1; tile += 2) {
+        step(tile, ks[0], vs[0], ks[1], vs[1]);
+        if (tile + 1 < tile1) step(tile + 1, ks[1], vs[1], ks[0], vs[0]);
     }
     l = half_sum(l);
     if (row >= n_rows) return;
@@ -192,11 +200,15 @@ template <typename T>
 int forward(const ForwardArgs& a, hipStream_t st)
 {
     const dim3 grid(a.workgroups), block(kWaves * kWave);
-    constexpr int kNarrow = sizeof(T) == 2 ? 64 : 32;       // keys of a tile: 32 KB of shared memory at width 128
-    if (a.p.width <= 64)
-        hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64>), grid, block, 0, st, a);
-    else
-        hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow>), grid, block, 0, st, a);
+    constexpr int kNarrow = sizeof(T) == 2 ? 64 : 32;       // keys of a tile: 64 KB of shared memory at width 128
+    const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
+    if (a.p.width <= 64) {
+        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64, false>), grid, block, 0, st, a);
+    } else {
+        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow, false>), grid, block, 0, st, a);
+    }
     int rc = launched();
     if (rc != SDL_OK || a.splits == 1) return rc;
     const uint64_t lines = (uint64_t)a.p.batch * a.p.kv_heads * a.p.queries * a.p.group.d;
