@@ -26,13 +26,13 @@ struct BackwardArgs {
     uint32_t workgroups;
 };
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dq_kernel(const BackwardArgs a)
+template <typename T, int HD, bool ASYNC>
+__global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dq_kernel(const BackwardArgs a)
 {
     constexpr int kSteps = HD / 16, kOut = HD / 32;
     typedef Tile<T, HD> Smem;
-    __shared__ __attribute__((aligned(16))) T ks[kTile * HD];
-    __shared__ __attribute__((aligned(16))) T vs[kTile * HD];
+    __shared__ __attribute__((aligned(16))) T ks[2][kTile * HD];
+    __shared__ __attribute__((aligned(16))) T vs[2][kTile * HD];
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
 
@@ -74,36 +74,44 @@ __global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dq_kernel(const 
     if (row < n_rows && half == 0) p.delta[stat] = delta;
     const float lse2 = sees > 0 ? p.lse[stat] * kLog2e : 0.0f;
 
+    const TileCopy<T, HD, kTile, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
+
     f32x16_t acc[kOut] = {};
-    for (int32_t key0 = 0; key0 < keys; key0 += kTile) {
-        __syncthreads();
-#pragma unroll 2
-        for (int i = threadIdx.x; i < kTile * (HD / 8); i += kWaves * kWave) {
-            const int r = i / (HD / 8), c8 = i % (HD / 8);
-            const uint32_t key = (uint32_t)min(key0 + r, s.nk - 1);
-            Smem::put(ks, r, c8, load8(at_row<T>(p.k, s.b, key, s.g), c8 * 8, p.width));
-            Smem::put(vs, r, c8, load8(at_row<T>(p.v, s.b, key, s.g), c8 * 8, p.width));
+    if (keys > 0) {
+        copy_k.bring(ks[0], 0, s.nk);
+        copy_v.bring(vs[0], 0, s.nk);
+    }
+    auto step = [&](int32_t key0, T* k_now, T* v_now, T* k_next, T* v_next) __attribute__((always_inline)) {
+        loads_done();               // this tile is there, and all are done with the one before it
+        if (key0 + kTile < keys) {
+            copy_k.bring(k_next, key0 + kTile, s.nk);
+            copy_v.bring(v_next, key0 + kTile, s.nk);
         }
-        __syncthreads();
         f32x16_t sc = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            mma(sc, Smem::along(ks, c, 2 * k + half), q[k]);
-            mma(dp, Smem::along(vs, c, 2 * k + half), g[k]);
+            mma(sc, Smem::along(k_now, c, 2 * k + half), q[k]);
+            mma(dp, Smem::along(v_now, c, 2 * k + half), g[k]);
         }
-        const bool cut = key0 + kTile > every;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float pr = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2));
-            sc[i] = pr * (dp[i] - delta);
-            if (cut && key0 + 8 * (i / 4) + 4 * half + i % 4 >= sees) sc[i] = 0.0f;
+        for (int i = 0; i < 16; ++i) sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2)) * (dp[i] - delta);
+        if (key0 + kTile > every) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (key0 + 8 * (i / 4) + 4 * half + i % 4 >= sees) sc[i] = 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const Frag<T> ds = frag_of(sc, u, T());
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(ks, u * 16, n * 32), ds);
+            for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(k_now, u * 16, n * 32), ds);
         }
+    };
+    for (int32_t key0 = 0; key0 < keys; key0 += 2 * kTile) {
+        step(key0, ks[0], vs[0], ks[1], vs[1]);
+        if (key0 + kTile < keys) step(key0 + kTile, ks[1], vs[1], ks[0], vs[0]);
     }
     if (row >= n_rows) return;
     T* dst = at_row<T>(p.dq, s.b, (uint32_t)t, head);
@@ -118,16 +126,18 @@ __global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dq_kernel(const 
         }
 }
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dkv_kernel(const BackwardArgs a)
+template <typename T, int HD, bool ASYNC>
+__global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dkv_kernel(const BackwardArgs a)
 {
     constexpr int kSteps = HD / 16, kOut = HD / 32;
     typedef Tile<T, HD> Smem;
-    __shared__ __attribute__((aligned(16))) T qs[kTile * HD];
-    __shared__ __attribute__((aligned(16))) T gs[kTile * HD];
-    __shared__ __attribute__((aligned(16))) float lse2s[kTile];
-    __shared__ __attribute__((aligned(16))) float deltas[kTile];
-    __shared__ __attribute__((aligned(16))) int32_t seens[kTile];
+    __shared__ __attribute__((aligned(16))) T qs[2][kTile * HD];
+    __shared__ __attribute__((aligned(16))) T gs[2][kTile * HD];
+    // At width 128 k and v together would not leave the sums their registers (256 a lane, two wavefronts on a SIMD).
+    constexpr bool kShareV = HD > 64;
+    __shared__ __attribute__((aligned(16))) T vs[kShareV ? kKeys * HD : 8];
+    __shared__ __attribute__((aligned(16))) float lse2s[2][kTile];
+    __shared__ __attribute__((aligned(16))) float deltas[2][kTile];
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
 
@@ -137,7 +147,7 @@ __global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dkv_kernel(const
     const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
 
     const int32_t key0 = (int32_t)(block * kKeys), wave_key0 = key0 + wave * 32, key = wave_key0 + c;
-    Frag<T> k[kSteps], v[kSteps];
+    Frag<T> k[kSteps], v[kShareV ? 1 : kSteps];
     {
         const uint32_t n = key < s.nk ? p.width : 0, at = (uint32_t)max(0, min(key, s.nk - 1));
         const T* src_k = at_row<T>(p.k, s.b, at, s.g);
@@ -145,59 +155,85 @@ __global__ void __launch_bounds__(kWaves * kWave) sdl_attention_dkv_kernel(const
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             set_frag(k[i], load8(src_k, i * 16 + half * 8, n));
-            set_frag(v[i], load8(src_v, i * 16 + half * 8, n));
+            if constexpr (!kShareV) set_frag(v[i], load8(src_v, i * 16 + half * 8, n));
         }
     }
-    // rows that see a key of the block: those of the tokens from key0 - shift on
-    const uint32_t row_end = key0 < s.nk ? (uint32_t)s.nq * p.group.d : 0;
-    const uint32_t row_begin = p.causal ? (uint32_t)min(max(0, key0 - s.shift), s.nq) * p.group.d / kTile * kTile : 0;
+    // Query tokens that see a key of the block, head by head of the group: [t_begin, t_end) in tiles.
+    const int32_t t_end = key0 < s.nk ? s.nq : 0;
+    const int32_t t_begin = p.causal ? min(max(0, key0 - s.shift), s.nq) / kTile * kTile : 0;
+    const int32_t per_head = t_end > t_begin ? (t_end - t_begin + kTile - 1) / kTile : 0, tiles = per_head * (int32_t)p.group.d;
 
     f32x16_t dk[kOut] = {}, dv[kOut] = {};
-    for (uint32_t row0 = row_begin; row0 < row_end; row0 += kTile) {
-        __syncthreads();
-#pragma unroll 2
-        for (int i = threadIdx.x; i < kTile * (HD / 8); i += kWaves * kWave) {
-            const int r = i / (HD / 8), c8 = i % (HD / 8);
-            const uint32_t row = min(row0 + r, row_end - 1);
-            const uint32_t t = div(row, p.group), head = s.g * p.group.d + (row - t * p.group.d);
-            Smem::put(qs, r, c8, load8(at_row<T>(p.q, s.b, t, head), c8 * 8, p.width));
-            Smem::put(gs, r, c8, load8(at_row<T>(p.d_out, s.b, t, head), c8 * 8, p.width));
-        }
+    uint32_t next_head = s.g * p.group.d;          // what is brought next
+    int32_t next_t = t_begin;
+    auto bring = [&](T* q_to, T* g_to, float* lse2_to, float* delta_to) __attribute__((always_inline)) {
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).bring(q_to, next_t, t_end);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).bring(g_to, next_t, t_end);
         if (threadIdx.x < kTile) {
-            const uint32_t row = row0 + threadIdx.x, at = min(row, row_end - 1);
-            const uint32_t t = div(at, p.group), head = s.g * p.group.d + (at - t * p.group.d);
-            const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t;
-            const int32_t sees = row < row_end ? s.seen(p, (int32_t)t) : 0;
-            seens[threadIdx.x] = sees;
-            lse2s[threadIdx.x] = sees > 0 ? p.lse[stat] * kLog2e : 0.0f;
-            deltas[threadIdx.x] = p.delta[stat];
+            const int32_t t = min(next_t + (int32_t)threadIdx.x, t_end - 1);
+            const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + next_head) * p.queries + (uint32_t)t;
+            const float lse = p.lse[stat];
+            lse2_to[threadIdx.x] = lse == -__builtin_inff() ? 0.0f : lse * kLog2e;      // a row that sees nothing is masked below
+            delta_to[threadIdx.x] = p.delta[stat];
         }
-        __syncthreads();
+        next_t += kTile;
+        if (next_t >= t_end) next_t = t_begin, ++next_head;
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).clear(qs[i]);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).clear(gs[i]);
+    }
+    if (tiles > 0) {
+        if constexpr (kShareV) {
+            const TileCopy<T, HD, kKeys, kWaves, ASYNC> copy_v(p.v, s.b, s.g, p.width);
+            copy_v.clear(vs);
+            copy_v.bring(vs, key0, s.nk);
+        }
+        bring(qs[0], gs[0], lse2s[0], deltas[0]);
+    }
+    int32_t t0 = t_begin;
+    auto step = [&](bool more, int now) __attribute__((always_inline)) {
+        loads_done();               // this tile is there, and all are done with the one before it
+        if (more) bring(qs[now ^ 1], gs[now ^ 1], lse2s[now ^ 1], deltas[now ^ 1]);
         f32x16_t sc = {}, dp = {};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            mma(sc, Smem::along(qs, c, 2 * i + half), k[i]);
-            mma(dp, Smem::along(gs, c, 2 * i + half), v[i]);
+            mma(sc, Smem::along(qs[now], c, 2 * i + half), k[i]);
+            if constexpr (kShareV)
+                mma(dp, Smem::along(gs[now], c, 2 * i + half), Smem::along(vs, wave * 32 + c, 2 * i + half));
+            else
+                mma(dp, Smem::along(gs[now], c, 2 * i + half), v[i]);
         }
-        // every row of the tile sees every key of the wavefront
-        const bool cut = row0 + kTile > row_end || s.seen(p, (int32_t)div(row0, p.group)) < wave_key0 + 32;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = 8 * (i / 4) + 4 * half + i % 4;
-            const float pr = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2s[r]));
-            sc[i] = pr;
-            dp[i] = pr * (dp[i] - deltas[r]);
-            if (cut && key >= seens[r]) sc[i] = 0.0f, dp[i] = 0.0f;
+            sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2s[now][r]));
+            dp[i] = sc[i] * (dp[i] - deltas[now][r]);
+        }
+        // unless every row of the tile sees every key of the wavefront
+        if (t0 + kTile > t_end || s.seen(p, t0) < wave_key0 + 32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int32_t t = t0 + 8 * (i / 4) + 4 * half + i % 4;
+                if (t >= t_end || key >= s.seen(p, t)) sc[i] = 0.0f, dp[i] = 0.0f;
+            }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
 #pragma unroll
             for (int n = 0; n < kOut; ++n) {
-                mma(dv[n], Smem::across(gs, u * 16, n * 32), pr);
-                mma(dk[n], Smem::across(qs, u * 16, n * 32), ds);
+                mma(dv[n], Smem::across(gs[now], u * 16, n * 32), pr);
+                mma(dk[n], Smem::across(qs[now], u * 16, n * 32), ds);
             }
         }
+        t0 += kTile;
+        if (t0 >= t_end) t0 = t_begin;
+    };
+    for (int32_t tile = 0; tile < tiles; tile += 2) {
+        step(tile + 1 < tiles, 0);
+        if (tile + 1 < tiles) step(tile + 2 < tiles, 1);
     }
     if (key >= (int32_t)p.keys) return;
     T* dst_k = at_row<T>(p.dk, s.b, (uint32_t)key, s.g);
@@ -224,14 +260,22 @@ int backward(BackwardArgs& a, hipStream_t st)
     if (rows) {
         a.blocks = (uint32_t)row_blocks;
         a.workgroups = (uint32_t)(row_blocks * heads);
-        hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD>), dim3(a.workgroups), dim3(kWaves * kWave), 0, st, a);
+        const dim3 grid(a.workgroups), block(kWaves * kWave);
+        if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), grid, block, 0, st, a);
+        else
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), grid, block, 0, st, a);
         const int rc = launched();
         if (rc != SDL_OK) return rc;
     }
     if (!key_blocks) return SDL_OK;
     a.blocks = (uint32_t)key_blocks;
     a.workgroups = (uint32_t)(key_blocks * heads);
-    hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD>), dim3(a.workgroups), dim3(kWaves * kWave), 0, st, a);
+    const dim3 grid(a.workgroups), block(kWaves * kWave);
+    if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), grid, block, 0, st, a);
     return launched();
 }
 
