@@ -58,55 +58,63 @@ __device__ __forceinline__ Frag<float> frag_of(const f32x16_t& d, int u, float)
     return f;
 }
 
-// A tile of rows of HD elements in shared memory.  The 16-byte pieces of a row are swapped around by an xor with spread(row), so that
-// neither the reads along rows (eight lanes, eight rows, one piece) nor the ones across them (four rows, four pieces) meet in a bank.
+// A tile of rows of HD elements in shared memory, as the copies below can lay it down: groups of 1024 bytes, 16 bytes apart, and within a
+// group the 16-byte pieces of row x swapped around by an xor of some of their number's bits with a value of x.  Neither the reads along rows (eight lanes,
+// eight rows, one piece) nor the ones across them (four rows, four pieces) meet in a bank, and the offsets of a lane's reads differ by
+// constants but for a few.
 template <typename T, int HD>
 struct Tile {
-    static constexpr int kPieces = HD * (int)sizeof(T) / 16;
-    static constexpr int kPer = 16 / (int)sizeof(T);            // elements of a piece
+    static constexpr int kPieces = HD * (int)sizeof(T) / 16;     // of a row
+    static constexpr int kGroup = kWave / kPieces;                // rows of a group
+    static constexpr int kGroupBytes = kWave * 16 + 16;
+    static constexpr int kMask = kPieces == 8 ? 6 : kPieces == 16 ? 12 : 4;
+    static_assert(kPieces == 8 || kPieces == 16 || kPieces == 32, "widths of 64 and 128");
 
-    static __device__ __forceinline__ int spread(int r)
+    static constexpr int bytes(int rows) { return rows / kGroup * kGroupBytes; }
+    static __device__ __forceinline__ int swap(int x)
     {
-        return kPieces >= 16 ? (((r & 3) << 2) | ((r >> 2) & 3)) : ((((r >> 1) & 1) << 2) | ((r >> 2) & 3));
+        return kPieces == 8 ? ((x & 2) << 1) | ((x & 4) >> 1) : x << 2;
     }
-    static __device__ __forceinline__ int piece(int r, int p) { return r * kPieces + (p ^ spread(r)); }      // in 16-byte units
-
-    static __device__ __forceinline__ void put(T* tile, int r, int c8, const Eight<T>& x)
+    static __device__ __forceinline__ int place(int x, int p) { return ((p & kMask) ^ swap(x)) + (p & ~kMask); }    // its own inverse
+    static __device__ __forceinline__ int at(int r, int p)
     {
-        u32x4* p = reinterpret_cast<u32x4*>(tile);
+        const int x = r % kGroup;
+        return r / kGroup * kGroupBytes + x * (kPieces * 16) + place(x, p) * 16;
+    }
+
+    static __device__ __forceinline__ void put(char* tile, int r, int c8, const Eight<T>& v)
+    {
         if constexpr (sizeof(T) == 2) {
-            p[piece(r, c8)] = x.w;
+            *reinterpret_cast<u32x4*>(tile + at(r, c8)) = v.w;
         } else {
-            p[piece(r, 2 * c8)] = x.lo;
-            p[piece(r, 2 * c8 + 1)] = x.hi;
+            *reinterpret_cast<u32x4*>(tile + at(r, 2 * c8)) = v.lo;
+            *reinterpret_cast<u32x4*>(tile + at(r, 2 * c8 + 1)) = v.hi;
         }
     }
     // elements [8 c8, 8 c8 + 8) of row r
-    static __device__ __forceinline__ Frag<T> along(const T* tile, int r, int c8)
+    static __device__ __forceinline__ Frag<T> along(const char* tile, int r, int c8)
     {
-        const u32x4* p = reinterpret_cast<const u32x4*>(tile);
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
-            f.v = __builtin_bit_cast(bf16x8_t, p[piece(r, c8)]);
+            f.v = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(tile + at(r, c8)));
         } else {
-            const u32x4 a = p[piece(r, 2 * c8)], b = p[piece(r, 2 * c8 + 1)];
+            const u32x4 a = *reinterpret_cast<const u32x4*>(tile + at(r, 2 * c8)), b = *reinterpret_cast<const u32x4*>(tile + at(r, 2 * c8 + 1));
 #pragma unroll
             for (int j = 0; j < 4; ++j) f.v[j] = u2f(a[j]), f.v[4 + j] = u2f(b[j]);
         }
         return f;
     }
-    // column d0 + lane % 32 of the rows r0 + order(half, j).  bf16: the transposing read gives lane i of 16 the i-th column of a
-    // block of 4 rows and 16 columns, of which lane 4 r + q names the q-th quarter of row r.
-    static __device__ __forceinline__ Frag<T> across(const T* tile, int r0, int d0)
+    // column d0 + lane % 32 of the rows r0 + order(half, j), r0 a multiple of 16.  bf16: the transposing read gives lane i of 16 the i-th
+    // column of a block of 4 rows and 16 columns, of which lane 4 r + q names the q-th quarter of row r.
+    static __device__ __forceinline__ Frag<T> across(const char* tile, int r0, int d0)
     {
         const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
-            const int r = r0 + 4 * half + ((lane & 15) >> 2), d = d0 + (lane & 16) + 4 * (lane & 3);
-            const char* base = reinterpret_cast<const char*>(tile);
-            const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + piece(r, d >> 3) * 16 + (d & 4) * 2));
-            const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + piece(r + 8, d >> 3) * 16 + (d & 4) * 2));
+            const int r = 4 * half + ((lane & 15) >> 2), p = (d0 >> 3) + ((lane & 16) >> 3) + ((lane & 2) >> 1), q = (lane & 1) * 8;
+            const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + at(r0 + r, p) + q));
+            const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + at(r0 + r + 8, p) + q));
             const bf16x4_t x = __builtin_bit_cast(bf16x4_t, a), y = __builtin_bit_cast(bf16x4_t, b);
             f.v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
@@ -114,7 +122,7 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int r = r0 + 8 * (j / 4) + 4 * half + j % 4;
-                f.v[j] = u2f(reinterpret_cast<const uint32_t*>(tile)[piece(r, d >> 2) * 4 + (d & 3)]);
+                f.v[j] = u2f(*reinterpret_cast<const uint32_t*>(tile + at(r, d >> 2) + (d & 3) * 4));
             }
         }
         return f;
@@ -154,8 +162,7 @@ template <typename T, int HD, int ROWS, int WAVES, bool ASYNC>
 struct TileCopy {
     typedef Tile<T, HD> Smem;
     static constexpr int kPieces = Smem::kPieces;
-    static constexpr int kRowsPerCopy = kWave / kPieces;                    // rows of one instruction
-    static constexpr int kStep = kRowsPerCopy * WAVES;                      // rows of all wavefronts' instructions
+    static constexpr int kStep = Smem::kGroup * WAVES;                      // rows of all wavefronts' instructions
     static constexpr int kCopies = ROWS / kStep;
     static_assert(ROWS % kStep == 0, "whole copies");
 
@@ -170,31 +177,27 @@ struct TileCopy {
         width = width_;
     }
     // Once: pieces behind the width are never brought, and have to be zero.
-    __device__ __forceinline__ void clear(T* tile) const
+    __device__ __forceinline__ void clear(char* tile) const
     {
         if (!ASYNC || width == HD) return;
-        for (uint32_t i = threadIdx.x; i < ROWS * kPieces; i += WAVES * kWave)
-            if (((i % kPieces) ^ (uint32_t)Smem::spread(i / kPieces)) * 16 >= width * sizeof(T)) reinterpret_cast<u32x4*>(tile)[i] = u32x4{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < ROWS * kPieces; i += WAVES * kWave)
+            if ((i % kPieces) * 16 >= (int)(width * sizeof(T))) *reinterpret_cast<u32x4*>(tile + Smem::at(i / kPieces, i % kPieces)) = u32x4{0, 0, 0, 0};
     }
     // Rows [row0, row0 + ROWS) of `rows`; what lies behind the last row is that row again.
-    __device__ __forceinline__ void bring(T* tile, int32_t row0, int32_t rows) const
+    __device__ __forceinline__ void bring(char* tile, int32_t row0, int32_t rows) const
     {
         if constexpr (ASYNC) {
             const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-            const uint32_t row = wave * kRowsPerCopy + lane / kPieces, to = lds_offset(tile) + wave * (kWave * 16);
+            const uint32_t row = wave * Smem::kGroup + lane / kPieces, to = lds_offset(tile) + wave * Smem::kGroupBytes;
+            const uint32_t piece = (uint32_t)Smem::place(lane / kPieces, lane % kPieces);       // that comes to lie where the lane's 16 bytes land
             const char* from = base + row0 * stride;
-            // the rearrangement has a period of 16 rows
-            uint32_t piece[kCopies];
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i) piece[i] = (lane % kPieces) ^ (uint32_t)Smem::spread(row + (i * kStep) % 16);
             if (row0 + ROWS <= rows && width == HD) {
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) copy_piece(from + i * kStep * stride, row * (uint32_t)stride + piece[i] * 16, to + i * (kStep * kPieces * 16));
-            } else {
+                for (int i = 0; i < kCopies; ++i) copy_piece(from + i * kStep * stride, row * (uint32_t)stride + piece * 16, to + i * (WAVES * Smem::kGroupBytes));
+            } else if (piece * 16 < width * sizeof(T)) {
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i)
-                    if (piece[i] * 16 < width * sizeof(T))
-                        copy_piece(from, min(row + i * kStep, (uint32_t)(rows - 1 - row0)) * (uint32_t)stride + piece[i] * 16, to + i * (kStep * kPieces * 16));
+                    copy_piece(from, min(row + i * kStep, (uint32_t)(rows - 1 - row0)) * (uint32_t)stride + piece * 16, to + i * (WAVES * Smem::kGroupBytes));
             }
         } else {
 #pragma unroll 4

@@ -31,10 +31,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 {
     constexpr int kTiles = BN / 32, kSteps = HD / 16, kOut = HD / 32;
     typedef Tile<T, HD> Smem;
-    __shared__ __attribute__((aligned(16))) T ks[2][BN * HD];
-    __shared__ __attribute__((aligned(16))) T vs[2][BN * HD];
+    __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(BN)];
+    __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(BN)];
     const Attention& p = a.p;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
     uint32_t id = die_order(blockIdx.x, a.workgroups);
     const uint32_t split = id % a.splits;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         copy_k.bring(ks[0], tile0 * BN, s.nk);
         copy_v.bring(vs[0], tile0 * BN, s.nk);
     }
-    auto step = [&](int32_t tile, T* k_now, T* v_now, T* k_next, T* v_next) __attribute__((always_inline)) {
+    auto step = [&](int32_t tile, char* k_now, char* v_now, char* k_next, char* v_next) __attribute__((always_inline)) {
         const int32_t key0 = tile * BN;
         loads_done();               // this tile is there, and all are done with the one before it
         if (tile + 1 < tile1) {

@@ -31,10 +31,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 {
     constexpr int kSteps = HD / 16, kOut = HD / 32;
     typedef Tile<T, HD> Smem;
-    __shared__ __attribute__((aligned(16))) T ks[2][kTile * HD];
-    __shared__ __attribute__((aligned(16))) T vs[2][kTile * HD];
+    __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(kTile)];
+    __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(kTile)];
     const Attention& p = a.p;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
     uint32_t id = die_order(blockIdx.x, a.workgroups);
     const uint32_t block = a.blocks - 1 - id % a.blocks;       // the longest first
@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         copy_k.bring(ks[0], 0, s.nk);
         copy_v.bring(vs[0], 0, s.nk);
     }
-    auto step = [&](int32_t key0, T* k_now, T* v_now, T* k_next, T* v_next) __attribute__((always_inline)) {
+    auto step = [&](int32_t key0, char* k_now, char* v_now, char* k_next, char* v_next) __attribute__((always_inline)) {
         loads_done();               // this tile is there, and all are done with the one before it
         if (key0 + kTile < keys) {
             copy_k.bring(k_next, key0 + kTile, s.nk);
@@ -131,15 +131,16 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 {
     constexpr int kSteps = HD / 16, kOut = HD / 32;
     typedef Tile<T, HD> Smem;
-    __shared__ __attribute__((aligned(16))) T qs[2][kTile * HD];
-    __shared__ __attribute__((aligned(16))) T gs[2][kTile * HD];
     // At width 128 k and v together would not leave the sums their registers (256 a lane, two wavefronts on a SIMD).
     constexpr bool kShareV = HD > 64;
-    __shared__ __attribute__((aligned(16))) T vs[kShareV ? kKeys * HD : 8];
-    __shared__ __attribute__((aligned(16))) float lse2s[2][kTile];
-    __shared__ __attribute__((aligned(16))) float deltas[2][kTile];
+    // v comes last: a constant offset of a read reaches 64 KB
+    __shared__ __attribute__((aligned(16))) struct {
+        char q[2][Smem::bytes(kTile)], g[2][Smem::bytes(kTile)];
+        float lse2[2][kTile], delta[2][kTile];
+        char v[kShareV ? Smem::bytes(kKeys) : 16];
+    } mem;
     const Attention& p = a.p;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
     uint32_t id = die_order(blockIdx.x, a.workgroups);
     const uint32_t block = id % a.blocks;                      // the longest first
@@ -163,10 +164,15 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t t_begin = p.causal ? min(max(0, key0 - s.shift), s.nq) / kTile * kTile : 0;
     const int32_t per_head = t_end > t_begin ? (t_end - t_begin + kTile - 1) / kTile : 0, tiles = per_head * (int32_t)p.group.d;
 
+    // from which token on the lane's key is seen, and every key of the wavefront
+    const int32_t never = 0x7fffff00;
+    const int32_t t_key = key < s.nk ? (p.causal ? key - s.shift : 0) : never;
+    const int32_t t_full = wave_key0 + 32 <= s.nk ? (p.causal ? wave_key0 + 31 - s.shift : 0) : never;
+
     f32x16_t dk[kOut] = {}, dv[kOut] = {};
     uint32_t next_head = s.g * p.group.d;          // what is brought next
     int32_t next_t = t_begin;
-    auto bring = [&](T* q_to, T* g_to, float* lse2_to, float* delta_to) __attribute__((always_inline)) {
+    auto bring = [&](char* q_to, char* g_to, float* lse2_to, float* delta_to) __attribute__((always_inline)) {
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).bring(q_to, next_t, t_end);
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).bring(g_to, next_t, t_end);
         if (threadIdx.x < kTile) {
@@ -181,51 +187,49 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).clear(qs[i]);
-        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).clear(gs[i]);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).clear(mem.q[i]);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).clear(mem.g[i]);
     }
     if (tiles > 0) {
         if constexpr (kShareV) {
             const TileCopy<T, HD, kKeys, kWaves, ASYNC> copy_v(p.v, s.b, s.g, p.width);
-            copy_v.clear(vs);
-            copy_v.bring(vs, key0, s.nk);
+            copy_v.clear(mem.v);
+            copy_v.bring(mem.v, key0, s.nk);
         }
-        bring(qs[0], gs[0], lse2s[0], deltas[0]);
+        bring(mem.q[0], mem.g[0], mem.lse2[0], mem.delta[0]);
     }
     int32_t t0 = t_begin;
     auto step = [&](bool more, int now) __attribute__((always_inline)) {
         loads_done();               // this tile is there, and all are done with the one before it
-        if (more) bring(qs[now ^ 1], gs[now ^ 1], lse2s[now ^ 1], deltas[now ^ 1]);
+        if (more) bring(mem.q[now ^ 1], mem.g[now ^ 1], mem.lse2[now ^ 1], mem.delta[now ^ 1]);
         f32x16_t sc = {}, dp = {};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            mma(sc, Smem::along(qs[now], c, 2 * i + half), k[i]);
+            mma(sc, Smem::along(mem.q[now], c, 2 * i + half), k[i]);
             if constexpr (kShareV)
-                mma(dp, Smem::along(gs[now], c, 2 * i + half), Smem::along(vs, wave * 32 + c, 2 * i + half));
+                mma(dp, Smem::along(mem.g[now], c, 2 * i + half), Smem::along(mem.v, wave * 32 + c, 2 * i + half));
             else
-                mma(dp, Smem::along(gs[now], c, 2 * i + half), v[i]);
+                mma(dp, Smem::along(mem.g[now], c, 2 * i + half), v[i]);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = 8 * (i / 4) + 4 * half + i % 4;
-            sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2s[now][r]));
-            dp[i] = sc[i] * (dp[i] - deltas[now][r]);
+            sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -mem.lse2[now][r]));
+            dp[i] = sc[i] * (dp[i] - mem.delta[now][r]);
         }
-        // unless every row of the tile sees every key of the wavefront
-        if (t0 + kTile > t_end || s.seen(p, t0) < wave_key0 + 32) {
+        if (t0 < t_full || t0 + kTile > t_end) {
+            const int32_t t = t0 + 4 * half;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int32_t t = t0 + 8 * (i / 4) + 4 * half + i % 4;
-                if (t >= t_end || key >= s.seen(p, t)) sc[i] = 0.0f, dp[i] = 0.0f;
-            }
+            for (int i = 0; i < 16; ++i)
+                if (t < t_key - (8 * (i / 4) + i % 4) || t >= t_end - (8 * (i / 4) + i % 4)) sc[i] = 0.0f, dp[i] = 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
 #pragma unroll
             for (int n = 0; n < kOut; ++n) {
-                mma(dv[n], Smem::across(gs[now], u * 16, n * 32), pr);
-                mma(dk[n], Smem::across(qs[now], u * 16, n * 32), ds);
+                mma(dv[n], Smem::across(mem.g[now], u * 16, n * 32), pr);
+                mma(dk[n], Smem::across(mem.q[now], u * 16, n * 32), ds);
             }
         }
         t0 += kTile;
