@@ -579,7 +579,8 @@ int sdl_rotary_frequencies(uint32_t rot, double base, sdl_rotary_scaling_t scali
  * finite, workspace too small), SDL_ERR_UNSUPPORTED (width above SDL_ATTENTION_MAX_WIDTH; more than 2^30 keys, queries times heads or
  * batch times heads), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
 #define SDL_ATTENTION_MAX_WIDTH 128u
-size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width);
+size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width,
+                                     sdl_dtype_t dtype);
 int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, uint32_t batch, uint32_t queries, uint32_t keys,
                   uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len,
                   const int32_t* k_len, const sdl_view_t* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
@@ -589,7 +590,8 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
  * dk and dv of a key head are the sums over its query heads.  Rows behind a length, and of queries that see nothing, are 0.  The order of
  * every sum is fixed by the arguments: two calls give the same bits.  dq, dk, dv are written, not added to; they may lie in one array.
  * workspace: as above, sdl_attention_backward_workspace_bytes(...) bytes.  Errors as above. */
-size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width);
+size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width,
+                                              sdl_dtype_t dtype);
 int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, const sdl_view_t* out,
                            const float* lse, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
                            uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len,

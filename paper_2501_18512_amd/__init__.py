@@ -133,7 +133,7 @@ def _load() -> ctypes.CDLL:
     lib.sdl_rotary.argtypes = [pv, *shape4, ctypes.c_int, u32, ctypes.c_int, vp, ctypes.c_int32, vp, f32, ctypes.c_int, pv, vp]
     lib.sdl_rotary_frequencies.argtypes = [u32, ctypes.c_double, ctypes.c_int, ctypes.c_double, ctypes.c_double, ctypes.c_double, u32, vp]
     for name in ("sdl_attention_workspace_bytes", "sdl_attention_backward_workspace_bytes"):
-        getattr(lib, name).argtypes = shape6
+        getattr(lib, name).argtypes = [*shape6, ctypes.c_int]
         getattr(lib, name).restype = ctypes.c_size_t
     lib.sdl_attention.argtypes = [pv, pv, pv, *shape6, ctypes.c_int, f32, ctypes.c_int, vp, vp, pv, vp, vp, ctypes.c_size_t, vp]
     lib.sdl_attention_backward.argtypes = [pv] * 5 + [vp, *shape6, ctypes.c_int, f32, ctypes.c_int, vp, vp, pv, pv, pv, vp, ctypes.c_size_t, vp]
@@ -767,20 +767,20 @@ def _attention_shape(q, k) -> Tuple[int, int, int, int, int, int]:
     return q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
 
 
-def sdl_attention_workspace_bytes(batch: int, queries: int, keys: int, heads: int, kv_heads: int, width: int) -> int:
-    return _lib.sdl_attention_workspace_bytes(batch, queries, keys, heads, kv_heads, width)
+def sdl_attention_workspace_bytes(batch: int, queries: int, keys: int, heads: int, kv_heads: int, width: int, dtype: int) -> int:
+    return _lib.sdl_attention_workspace_bytes(batch, queries, keys, heads, kv_heads, width, dtype)
 
 
-def sdl_attention_backward_workspace_bytes(batch: int, queries: int, keys: int, heads: int, kv_heads: int, width: int) -> int:
-    return _lib.sdl_attention_backward_workspace_bytes(batch, queries, keys, heads, kv_heads, width)
+def sdl_attention_backward_workspace_bytes(batch: int, queries: int, keys: int, heads: int, kv_heads: int, width: int, dtype: int) -> int:
+    return _lib.sdl_attention_backward_workspace_bytes(batch, queries, keys, heads, kv_heads, width, dtype)
 
 
 def alloc_attention(q, k, backward: bool = False):
     """Workspace for sdl_attention on tensors like these, and for sdl_attention_backward if asked."""
     shape = _attention_shape(q, k)
-    n = _lib.sdl_attention_workspace_bytes(*shape)
+    n = _lib.sdl_attention_workspace_bytes(*shape, _dtype(q))
     if backward:
-        n = max(n, _lib.sdl_attention_backward_workspace_bytes(*shape))
+        n = max(n, _lib.sdl_attention_backward_workspace_bytes(*shape, _dtype(q)))
     return torch.empty(max(n, 4), dtype=torch.uint8, device=q.device)
 
 

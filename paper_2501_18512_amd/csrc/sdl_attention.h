@@ -293,14 +293,21 @@ __device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n)
     return die * each + min(die, more) + (id >> 3);
 }
 
+// Host: whether the kernels take such a problem.
+inline bool sdl_attention_shape(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype)
+{
+    constexpr uint64_t kMost = 0x40000000u;
+    return known(dtype) && kv_heads != 0 && heads % kv_heads == 0 && width != 0 && width <= SDL_ATTENTION_MAX_WIDTH && keys <= kMost &&
+           (uint64_t)queries * heads <= kMost && (uint64_t)batch * heads <= kMost;
+}
+
 // Host: the checks that do not look at the arrays, and the arguments that do not depend on the pass.
 inline int sdl_attention_problem(Attention& p, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
                                  uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len)
 {
-    if (!known(dtype) || width == 0 || !(scale > 0.0f) || scale > 3.4028235e38f) return SDL_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || scale > 3.4028235e38f || !known(dtype) || width == 0) return SDL_ERR_INVALID_ARG;
     if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return SDL_ERR_INVALID_ARG;
-    if (width > SDL_ATTENTION_MAX_WIDTH || keys > 0x40000000u) return SDL_ERR_UNSUPPORTED;
-    if ((uint64_t)queries * heads > 0x40000000u || (uint64_t)batch * heads > 0x40000000u) return SDL_ERR_UNSUPPORTED;
+    if (heads && !sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return SDL_ERR_UNSUPPORTED;
     if (!aligned_to(q_len, 4) || !aligned_to(k_len, 4)) return SDL_ERR_ALIGNMENT;
     p.q_len = q_len;
     p.k_len = k_len;

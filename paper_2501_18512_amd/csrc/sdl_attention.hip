@@ -3,8 +3,9 @@
 // One pass over the keys with the running maximum m and sum l of every row.  A workgroup has 4 wavefronts of 32 rows; a tile of
 // keys and values goes through shared memory.  S^T = k q^T has a row's scores in the registers of two lanes, and P^T as it stands is the
 // operand of out^T = v^T P^T (sdl_attention.h), so that m, l and the rescaling of the result are a lane's own.
-// Where there are too few rows to fill the chip, the keys are split over workgroups, which leave normalised results and their
-// log sums in the workspace, and a second kernel joins them.
+// Where there are too few rows to fill the chip, the keys are cut into chunks for a workgroup each, which leave normalised results and their
+// log sums in the workspace, and a second kernel joins them.  Chunks have one size whatever a sequence's length, so that short sequences beside
+// long ones leave no one waiting.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -17,13 +18,13 @@ namespace {
 using namespace sdl_device;
 
 constexpr int kRowsPerWave = 32, kWaves = 4, kRows = kRowsPerWave * kWaves;
-constexpr uint32_t kMaxSplits = 64;
+constexpr uint32_t kMaxSplits = kWave;         // the join has one a lane
 
 struct ForwardArgs {
     Attention p;
     float* part_out;        // [split][batch][key head][row][width], with more than one split
     float* part_lse;        // [split][batch][key head][row]
-    uint32_t row_blocks, splits, workgroups;
+    uint32_t row_blocks, splits, chunk, workgroups;         // chunk: keys of a split
 };
 
 template <typename T, int HD, int BN, bool ASYNC>
@@ -63,7 +64,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t keys = t_last < t_first ? 0 : s.seen(p, t_last);      // no valid row: nothing to see
     const int32_t every = t_last < t_first ? 0 : s.seen(p, t_first);    // keys that all valid rows see
     const int32_t tiles = (keys + BN - 1) / BN;
-    const int32_t tile0 = (int32_t)((uint64_t)tiles * split / a.splits), tile1 = (int32_t)((uint64_t)tiles * (split + 1) / a.splits);
+    const int32_t tile0 = (int32_t)(split * (a.chunk / BN)), tile1 = min(tiles, tile0 + (int32_t)(a.chunk / BN));
+    if (split > 0 && tile0 >= tile1) return;         // a chunk that no row sees is not looked at by the join
+    // whether the wavefront has a row that sees a key of the chunk: the others help with the copies only
+    const bool busy = __any(sees > tile0 * BN);
 
     const TileCopy<T, HD, BN, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
 #pragma unroll
@@ -82,6 +86,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             copy_k.bring(k_next, key0 + BN, s.nk);
             copy_v.bring(v_next, key0 + BN, s.nk);
         }
+        if (!busy) return;
         f32x16_t sc[kTiles] = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
@@ -155,46 +160,64 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     }
 }
 
-// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s: one wavefront a row, two elements a lane.
+// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s: one wavefront a row, two elements a lane, and the weight
+// of split s in lane s.
 template <typename T>
 __global__ void __launch_bounds__(256) sdl_attention_join_kernel(const ForwardArgs a)
 {
     const Attention& p = a.p;
     const uint32_t n_rows = p.queries * p.group.d, lane = threadIdx.x & (kWave - 1);
-    const uint64_t line = (uint64_t)blockIdx.x * 4 + threadIdx.x / kWave, lines = (uint64_t)p.batch * p.kv_heads * n_rows;
+    const uint32_t lines = p.batch * p.kv_heads * n_rows;
+    const uint32_t line = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
     if (line >= lines) return;
-    float top = -__builtin_inff();
-    for (uint32_t s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_lse[s * lines + line]);
+    const uint32_t bg = line / n_rows, row = line - bg * n_rows, t = div(row, p.group);
+    const Sequence s(p, bg / p.kv_heads, bg % p.kv_heads);
+    const uint32_t head = s.g * p.group.d + (row - t * p.group.d);
+    const uint32_t sees = (int32_t)t < s.nq ? (uint32_t)s.seen(p, (int32_t)t) : 0;
+    const uint32_t n = (sees + a.chunk - 1) / a.chunk;
+    const float mine = lane < n ? a.part_lse[(uint64_t)lane * lines + line] : -__builtin_inff();
+    float top = mine;
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
     const float off = top == -__builtin_inff() ? 0.0f : top;
-    float sum = 0.0f, x = 0.0f, y = 0.0f;
+    const float weight = exp2_fast((mine - off) * kLog2e), sum = lane_sum<kWave>(weight);
+    const float scaled = sum == 0.0f ? 0.0f : weight / sum;
+    float x = 0.0f, y = 0.0f;
     const uint32_t d = 2 * lane;
-    for (uint32_t s = 0; s < a.splits; ++s) {
-        const float by = exp2_fast((a.part_lse[s * lines + line] - off) * kLog2e);
-        const float* src = a.part_out + (s * lines + line) * p.width;
-        sum += by;
-        if (d < p.width) x = __builtin_fmaf(by, src[d], x);
-        if (d + 1 < p.width) y = __builtin_fmaf(by, src[d + 1], y);
+    const float* src = a.part_out + (uint64_t)line * p.width;
+#pragma unroll 8
+    for (uint32_t i = 0; i < n; ++i) {
+        const float by = u2f(__builtin_amdgcn_readlane(f2u(scaled), i));
+        const float* from = src + (uint64_t)i * lines * p.width;
+        if (d < p.width) x = __builtin_fmaf(by, from[d], x);
+        if (d + 1 < p.width) y = __builtin_fmaf(by, from[d + 1], y);
     }
-    const uint32_t row = (uint32_t)(line % n_rows), t = div(row, p.group), bg = (uint32_t)(line / n_rows);
-    const uint32_t b = bg / p.kv_heads, head = (bg % p.kv_heads) * p.group.d + (row - t * p.group.d);
-    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T* dst = at_row<T>(p.out, b, t, head);
-    if (d < p.width) dst[d] = (T)(x * by);
-    if (d + 1 < p.width) dst[d + 1] = (T)(y * by);
+    T* dst = at_row<T>(p.out, s.b, t, head);
+    if (d < p.width) dst[d] = (T)x;
+    if (d + 1 < p.width) dst[d + 1] = (T)y;
     if (p.lse && lane == 0)
-        p.lse[((uint64_t)b * p.kv_heads * p.group.d + head) * p.queries + t] = sum == 0.0f ? -__builtin_inff() : off + __builtin_amdgcn_logf(sum) * kLn2;
+        p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = sum == 0.0f ? -__builtin_inff() : off + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
-// Splits of the keys: as many as give 512 workgroups (two for every compute unit), of at least 256 keys.
-uint32_t splits_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads)
+// Keys of a chunk: as few as make about `kFill` workgroups of a problem that has fewer, and no fewer than pay for a workgroup's start and its
+// share of the join (256; an fp32 tile takes the matrix units 16 times as long: 64).
+constexpr uint32_t kFill = 1024;
+
+uint32_t chunk_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, sdl_dtype_t dtype)
 {
     const uint64_t rows = (uint64_t)queries * (heads / kv_heads);
-    const uint64_t groups = (rows + kRows - 1) / kRows * batch * kv_heads;
-    uint64_t n = groups ? 512 / groups : 1;
-    if (n > keys / 256) n = keys / 256;
-    if (n > kMaxSplits) n = kMaxSplits;
-    return n < 1 ? 1u : (uint32_t)n;
+    const uint64_t groups = (rows + kRows - 1) / kRows * batch * kv_heads, least = dtype == SDL_DTYPE_BF16 ? 256 : 64;
+    uint64_t n = keys;
+    if (groups < kFill / 2) {
+        n = keys * groups / kFill;
+        if (n < least) n = least;
+        if (n < (keys + kMaxSplits - 1) / kMaxSplits) n = (keys + kMaxSplits - 1) / kMaxSplits;
+    }
+    n = (n + 63) / 64 * 64;           // whole tiles
+    return n < 64 ? 64u : (uint32_t)n;
 }
+
+uint32_t splits_of(uint32_t chunk, uint32_t keys) { return keys <= chunk ? 1u : (keys + chunk - 1) / chunk; }
 
 template <typename T>
 int forward(const ForwardArgs& a, hipStream_t st)
@@ -220,10 +243,10 @@ int forward(const ForwardArgs& a, hipStream_t st)
 
 extern "C" {
 
-size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width)
+size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype)
 {
-    if (kv_heads == 0 || heads % kv_heads != 0 || width == 0 || width > SDL_ATTENTION_MAX_WIDTH) return 0;
-    const uint32_t n = splits_of(batch, queries, keys, heads, kv_heads);
+    if (!sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return 0;
+    const uint32_t n = splits_of(chunk_of(batch, queries, keys, heads, kv_heads, dtype), keys);
     return n == 1 ? 0 : (size_t)n * batch * heads * queries * (width + 1) * sizeof(float);
 }
 
@@ -238,19 +261,20 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
     if ((rc = check_view(q, dtype)) != SDL_OK || (rc = check_output(out, dtype, batch, queries, heads)) != SDL_OK) return rc;
     if (keys && ((rc = check_view(k, dtype)) != SDL_OK || (rc = check_view(v, dtype)) != SDL_OK)) return rc;
     if (!aligned_to(lse, 4) || !aligned_to(workspace, 4)) return SDL_ERR_ALIGNMENT;
-    const size_t need = sdl_attention_workspace_bytes(batch, queries, keys, heads, kv_heads, width);
+    const size_t need = sdl_attention_workspace_bytes(batch, queries, keys, heads, kv_heads, width, dtype);
     if (need && (!workspace || workspace_bytes < need)) return SDL_ERR_INVALID_ARG;
     a.p.q = kernel_view(q);
     if (keys) a.p.k = kernel_view(k), a.p.v = kernel_view(v);
     a.p.out = kernel_view(out);
     a.p.lse = lse;
-    a.splits = splits_of(batch, queries, keys, heads, kv_heads);
+    a.chunk = chunk_of(batch, queries, keys, heads, kv_heads, dtype);
+    a.splits = splits_of(a.chunk, keys);
     a.part_out = static_cast<float*>(workspace);
     a.part_lse = a.part_out + (size_t)a.splits * batch * heads * queries * width;
     const uint64_t rows = (uint64_t)queries * a.p.group.d;
     a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
     const uint64_t groups = (uint64_t)a.row_blocks * a.splits * batch * kv_heads;
-    if (groups > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
+    if (groups > 0x7fffffffu || (a.splits > 1 && (uint64_t)batch * queries * heads > 0x7fffffffu)) return SDL_ERR_UNSUPPORTED;
     a.workgroups = (uint32_t)groups;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == SDL_DTYPE_BF16 ? forward<__bf16>(a, st) : forward<float>(a, st);

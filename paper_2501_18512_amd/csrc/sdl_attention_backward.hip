@@ -7,7 +7,8 @@
 // rate of a large product, the sums 1 KB or more of traffic, about 0.2 ns.
 //   dq       rows are a wavefront's own, as in the forward pass: S^T = k q^T and dP^T = v d_out^T leave dS^T where dq^T = k^T dS^T wants it
 //   dk, dv   keys are a wavefront's own: S = q k^T and dP = d_out v^T leave P and dS where dv^T = d_out^T P and dk^T = q^T dS want them
-// D is worked out by the first and read by the second.
+// D is worked out by the first and read by the second.  Where the workgroups are too few to fill the chip, a chunk of the keys (or of the
+// rows) goes to a workgroup each, which leaves its sums in the workspace, and a third kernel adds them up in order.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -22,8 +23,23 @@ constexpr int kWaves = 4, kRows = 32 * kWaves, kKeys = 32 * kWaves, kTile = 32;
 
 struct BackwardArgs {
     Attention p;
+    float* part;            // sums of the splits: [split][batch][key head][row][width], or [split][dk, dv][batch][key head][key][width]
     uint32_t blocks;        // of rows or keys, per (batch, key head)
+    uint32_t splits, chunk; // chunk: keys of a split, or tiles of query tokens
     uint32_t workgroups;
+};
+
+// The query tokens that see a key of a block, in tiles, head by head of the group.
+struct Seers {
+    int32_t begin, end, per_head, tiles;
+
+    __device__ __forceinline__ Seers(const Attention& p, const Sequence& s, int32_t key0)
+    {
+        end = key0 < s.nk ? s.nq : 0;
+        begin = p.causal ? min(max(0, key0 - s.shift), s.nq) / kTile * kTile : 0;
+        per_head = end > begin ? (end - begin + kTile - 1) / kTile : 0;
+        tiles = per_head * (int32_t)p.group.d;
+    }
 };
 
 template <typename T, int HD, bool ASYNC>
@@ -37,6 +53,8 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
     uint32_t id = die_order(blockIdx.x, a.workgroups);
+    const uint32_t split = id % a.splits;
+    id /= a.splits;
     const uint32_t block = a.blocks - 1 - id % a.blocks;       // the longest first
     id /= a.blocks;
     const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
@@ -50,8 +68,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t sees = valid ? s.seen(p, t) : 0;
     const int32_t t_first = (int32_t)div(min(block * kRows, n_rows - 1), p.group);
     const int32_t t_last = min((int32_t)div(min(block * kRows + kRows, n_rows) - 1, p.group), s.nq - 1);
-    const int32_t keys = t_last < t_first ? 0 : s.seen(p, t_last);
+    const int32_t key_begin = (int32_t)(split * a.chunk);
+    const int32_t keys = min(t_last < t_first ? 0 : s.seen(p, t_last), key_begin + (int32_t)a.chunk);     // of this split: [key_begin, keys)
     const int32_t every = t_last < t_first ? 0 : s.seen(p, t_first);
+    if (split > 0 && key_begin >= keys) return;          // a chunk that no row sees is not looked at when the sums are added
 
     Frag<T> q[kSteps], g[kSteps];
     float delta = 0.0f;
@@ -71,7 +91,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         delta = half_sum(delta);
     }
     const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + (uint32_t)t;
-    if (row < n_rows && half == 0) p.delta[stat] = delta;
+    if (row < n_rows && half == 0 && split == 0) p.delta[stat] = delta;
     const float lse2 = sees > 0 ? p.lse[stat] * kLog2e : 0.0f;
 
     const TileCopy<T, HD, kTile, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
@@ -79,16 +99,18 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
 
     f32x16_t acc[kOut] = {};
-    if (keys > 0) {
-        copy_k.bring(ks[0], 0, s.nk);
-        copy_v.bring(vs[0], 0, s.nk);
+    if (key_begin < keys) {
+        copy_k.bring(ks[0], key_begin, s.nk);
+        copy_v.bring(vs[0], key_begin, s.nk);
     }
+    const bool busy = __any(sees > key_begin);          // whether the wavefront has a row that sees something
     auto step = [&](int32_t key0, char* k_now, char* v_now, char* k_next, char* v_next) __attribute__((always_inline)) {
         loads_done();               // this tile is there, and all are done with the one before it
         if (key0 + kTile < keys) {
             copy_k.bring(k_next, key0 + kTile, s.nk);
             copy_v.bring(v_next, key0 + kTile, s.nk);
         }
+        if (!busy) return;
         f32x16_t sc = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -109,11 +131,19 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(k_now, u * 16, n * 32), ds);
         }
     };
-    for (int32_t key0 = 0; key0 < keys; key0 += 2 * kTile) {
+    for (int32_t key0 = key_begin; key0 < keys; key0 += 2 * kTile) {
         step(key0, ks[0], vs[0], ks[1], vs[1]);
         if (key0 + kTile < keys) step(key0 + kTile, ks[1], vs[1], ks[0], vs[0]);
     }
     if (row >= n_rows) return;
+    if (a.splits > 1) {
+        float* dst = a.part + ((((uint64_t)split * p.batch + s.b) * p.kv_heads + s.g) * n_rows + row) * p.width;
+#pragma unroll
+        for (int n = 0; n < kOut; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) store4(dst, n * 32 + 2 * i + 4 * half, p.width, acc[n][i], acc[n][i + 1], acc[n][i + 2], acc[n][i + 3]);
+        return;
+    }
     T* dst = at_row<T>(p.dq, s.b, (uint32_t)t, head);
     const float by = p.scale;
 #pragma unroll
@@ -143,6 +173,8 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
     uint32_t id = die_order(blockIdx.x, a.workgroups);
+    const uint32_t split = id % a.splits;
+    id /= a.splits;
     const uint32_t block = id % a.blocks;                      // the longest first
     id /= a.blocks;
     const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
@@ -159,10 +191,9 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             if constexpr (!kShareV) set_frag(v[i], load8(src_v, i * 16 + half * 8, n));
         }
     }
-    // Query tokens that see a key of the block, head by head of the group: [t_begin, t_end) in tiles.
-    const int32_t t_end = key0 < s.nk ? s.nq : 0;
-    const int32_t t_begin = p.causal ? min(max(0, key0 - s.shift), s.nq) / kTile * kTile : 0;
-    const int32_t per_head = t_end > t_begin ? (t_end - t_begin + kTile - 1) / kTile : 0, tiles = per_head * (int32_t)p.group.d;
+    const Seers seers(p, s, key0);
+    const int32_t t_begin = seers.begin, t_end = seers.end, tile0 = (int32_t)(split * a.chunk), tiles = min(seers.tiles, tile0 + (int32_t)a.chunk);
+    if (split > 0 && tile0 >= tiles) return;         // nothing there for this split, and nothing is looked at when the sums are added
 
     // from which token on the lane's key is seen, and every key of the wavefront
     const int32_t never = 0x7fffff00;
@@ -170,8 +201,9 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t t_full = wave_key0 + 32 <= s.nk ? (p.causal ? wave_key0 + 31 - s.shift : 0) : never;
 
     f32x16_t dk[kOut] = {}, dv[kOut] = {};
-    uint32_t next_head = s.g * p.group.d;          // what is brought next
-    int32_t next_t = t_begin;
+    const int32_t skip = seers.per_head > 0 ? tile0 / seers.per_head : 0;
+    uint32_t next_head = s.g * p.group.d + skip;          // what is brought next
+    int32_t next_t = t_begin + (tile0 - skip * seers.per_head) * kTile;
     auto bring = [&](char* q_to, char* g_to, float* lse2_to, float* delta_to) __attribute__((always_inline)) {
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).bring(q_to, next_t, t_end);
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).bring(g_to, next_t, t_end);
@@ -190,7 +222,8 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).clear(mem.q[i]);
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).clear(mem.g[i]);
     }
-    if (tiles > 0) {
+    int32_t t0 = next_t;
+    if (tile0 < tiles) {
         if constexpr (kShareV) {
             const TileCopy<T, HD, kKeys, kWaves, ASYNC> copy_v(p.v, s.b, s.g, p.width);
             copy_v.clear(mem.v);
@@ -198,7 +231,6 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         }
         bring(mem.q[0], mem.g[0], mem.lse2[0], mem.delta[0]);
     }
-    int32_t t0 = t_begin;
     auto step = [&](bool more, int now) __attribute__((always_inline)) {
         loads_done();               // this tile is there, and all are done with the one before it
         if (more) bring(mem.q[now ^ 1], mem.g[now ^ 1], mem.lse2[now ^ 1], mem.delta[now ^ 1]);
@@ -235,11 +267,24 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         t0 += kTile;
         if (t0 >= t_end) t0 = t_begin;
     };
-    for (int32_t tile = 0; tile < tiles; tile += 2) {
+    for (int32_t tile = tile0; tile < tiles; tile += 2) {
         step(tile + 1 < tiles, 0);
         if (tile + 1 < tiles) step(tile + 2 < tiles, 1);
     }
     if (key >= (int32_t)p.keys) return;
+    if (a.splits > 1) {
+        const uint64_t each = (uint64_t)p.batch * p.kv_heads * p.keys;
+        float* dst = a.part + (2 * split * each + ((uint64_t)s.b * p.kv_heads + s.g) * p.keys + (uint32_t)key) * p.width;
+#pragma unroll
+        for (int n = 0; n < kOut; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const uint32_t at = n * 32 + 2 * i + 4 * half;
+                store4(dst, at, p.width, dk[n][i], dk[n][i + 1], dk[n][i + 2], dk[n][i + 3]);
+                store4(dst + each * p.width, at, p.width, dv[n][i], dv[n][i + 1], dv[n][i + 2], dv[n][i + 3]);
+            }
+        return;
+    }
     T* dst_k = at_row<T>(p.dk, s.b, (uint32_t)key, s.g);
     T* dst_v = at_row<T>(p.dv, s.b, (uint32_t)key, s.g);
     const bool some = key < s.nk;
@@ -254,44 +299,137 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         }
 }
 
-template <typename T, int HD>
-int backward(BackwardArgs& a, hipStream_t st)
+// The sums of the splits added up, in order: four elements a thread.  DQ: rows; otherwise keys, of dk and dv.
+template <typename T, bool DQ>
+__global__ void __launch_bounds__(256) sdl_attention_add_kernel(const BackwardArgs a, const Div quarters, const uint64_t n)
 {
     const Attention& p = a.p;
-    const uint64_t rows = (uint64_t)p.queries * p.group.d, heads = (uint64_t)p.batch * p.kv_heads;
-    const uint64_t row_blocks = (rows + kRows - 1) / kRows, key_blocks = ((uint64_t)p.keys + kKeys - 1) / kKeys;
-    if (row_blocks * heads > 0x7fffffffu || key_blocks * heads > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
-    if (rows) {
-        a.blocks = (uint32_t)row_blocks;
-        a.workgroups = (uint32_t)(row_blocks * heads);
-        const dim3 grid(a.workgroups), block(kWaves * kWave);
+    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= n) return;
+    const uint32_t line = div((uint32_t)id, quarters), at = ((uint32_t)id - line * quarters.d) * 4;       // line: [dk, dv][batch][key head][row or key]
+    const uint32_t per = DQ ? p.queries * p.group.d : p.keys, bg = line / per, i = line - bg * per;
+    const uint32_t heads = p.batch * p.kv_heads, which = DQ ? 0 : bg / heads, within = bg - which * heads;
+    const Sequence s(p, within / p.kv_heads, within % p.kv_heads);
+    uint32_t used, token, head;
+    if constexpr (DQ) {
+        token = div(i, p.group);
+        head = s.g * p.group.d + (i - token * p.group.d);
+        const uint32_t sees = (int32_t)token < s.nq ? (uint32_t)s.seen(p, (int32_t)token) : 0;
+        used = (sees + a.chunk - 1) / a.chunk;
+    } else {
+        token = i;
+        head = s.g;
+        const Seers seers(p, s, (int32_t)(i / kKeys * kKeys));
+        used = (int32_t)i < s.nk ? ((uint32_t)seers.tiles + a.chunk - 1) / a.chunk : 0;
+    }
+    const float* src = a.part + (uint64_t)line * p.width + at;
+    const uint64_t step = (DQ ? 1 : 2) * (uint64_t)heads * per * p.width;
+    f32x4_t sum = {};
+    if (at + 4 <= p.width) {
+#pragma unroll 4
+        for (uint32_t k = 0; k < used; ++k) sum += *reinterpret_cast<const f32x4_elem*>(src + k * step);
+    } else {
+        for (uint32_t k = 0; k < used; ++k)
+            for (uint32_t j = 0; j < 4; ++j) sum[j] += at + j < p.width ? src[k * step + j] : 0.0f;
+    }
+    if (DQ || which == 0) sum *= p.scale;
+    T* dst = at_row<T>(DQ ? p.dq : which ? p.dv : p.dk, s.b, token, head);
+    store4(dst, at, p.width, sum[0], sum[1], sum[2], sum[3]);
+}
+
+// How the work is cut.  A problem with fewer than kFill / 2 workgroups is cut into chunks of the long axis, down to those that pay for a
+// workgroup's start and for the sums that it leaves (256 keys or rows; an fp32 tile takes the matrix units 16 times as long: 64).
+constexpr uint64_t kFill = 512;
+
+struct Cut {
+    uint32_t chunk, splits;
+};
+
+Cut cut(uint64_t groups, uint64_t tiles, sdl_dtype_t dtype)          // in tiles
+{
+    uint64_t n = tiles;
+    if (groups < kFill / 2) {
+        const uint64_t least = dtype == SDL_DTYPE_BF16 ? 256 / kTile : 64 / kTile;
+        n = (tiles * groups + kFill - 1) / kFill;
+        if (n < least) n = least;
+    }
+    if (n < 1) n = 1;
+    return Cut{(uint32_t)n, tiles <= n ? 1u : (uint32_t)((tiles + n - 1) / n)};
+}
+
+struct Plan {
+    uint64_t row_blocks, key_blocks, heads;
+    Cut keys, rows;         // of the kernel of dq, of the one of dk and dv
+    size_t delta, part;     // floats of the workspace
+};
+
+Plan plan_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype)
+{
+    Plan w{};
+    const uint64_t group = heads / kv_heads, rows = queries * group;
+    w.heads = (uint64_t)batch * kv_heads;
+    w.row_blocks = (rows + kRows - 1) / kRows;
+    w.key_blocks = ((uint64_t)keys + kKeys - 1) / kKeys;
+    w.keys = cut(w.row_blocks * w.heads, ((uint64_t)keys + kTile - 1) / kTile, dtype);
+    w.rows = cut(w.key_blocks * w.heads, ((uint64_t)queries + kTile - 1) / kTile * group, dtype);
+    w.delta = ((size_t)batch * heads * queries + 3) / 4 * 4;
+    const size_t of_keys = w.keys.splits > 1 ? (size_t)w.keys.splits * w.heads * rows * width : 0;
+    const size_t of_rows = w.rows.splits > 1 ? (size_t)w.rows.splits * 2 * w.heads * keys * width : 0;
+    w.part = of_keys > of_rows ? of_keys : of_rows;
+    return w;
+}
+
+template <typename T, bool DQ>
+int add(const BackwardArgs& a, uint64_t lines, hipStream_t st)
+{
+    const uint32_t quarters = (a.p.width + 3) / 4;
+    const uint64_t n = lines * quarters;
+    hipLaunchKernelGGL((sdl_attention_add_kernel<T, DQ>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, st, a, make_div(quarters), n);
+    return launched();
+}
+
+template <typename T, int HD>
+int backward(BackwardArgs& a, const Plan& w, hipStream_t st)
+{
+    const Attention& p = a.p;
+    const dim3 block(kWaves * kWave);
+    if (w.row_blocks) {
+        a.blocks = (uint32_t)w.row_blocks;
+        a.splits = w.keys.splits;
+        a.chunk = w.keys.chunk * kTile;
+        a.workgroups = (uint32_t)(w.row_blocks * w.heads * w.keys.splits);
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), dim3(a.workgroups), block, 0, st, a);
         else
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), grid, block, 0, st, a);
-        const int rc = launched();
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), dim3(a.workgroups), block, 0, st, a);
+        int rc = launched();
+        if (rc == SDL_OK && a.splits > 1) rc = add<T, true>(a, (uint64_t)p.queries * p.group.d * w.heads, st);
         if (rc != SDL_OK) return rc;
     }
-    if (!key_blocks) return SDL_OK;
-    a.blocks = (uint32_t)key_blocks;
-    a.workgroups = (uint32_t)(key_blocks * heads);
-    const dim3 grid(a.workgroups), block(kWaves * kWave);
+    if (!w.key_blocks) return SDL_OK;
+    a.blocks = (uint32_t)w.key_blocks;
+    a.splits = w.rows.splits;
+    a.chunk = w.rows.chunk;
+    a.workgroups = (uint32_t)(w.key_blocks * w.heads * w.rows.splits);
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), dim3(a.workgroups), block, 0, st, a);
     else
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), grid, block, 0, st, a);
-    return launched();
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), dim3(a.workgroups), block, 0, st, a);
+    int rc = launched();
+    if (rc == SDL_OK && a.splits > 1) rc = add<T, false>(a, 2 * (uint64_t)p.keys * w.heads, st);
+    return rc;
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width)
+size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width,
+                                              sdl_dtype_t dtype)
 {
-    (void)keys;
-    if (kv_heads == 0 || heads % kv_heads != 0 || width == 0 || width > SDL_ATTENTION_MAX_WIDTH) return 0;
-    return (size_t)batch * heads * queries * sizeof(float);
+    if (heads == 0 || !sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return 0;
+    const Plan w = plan_of(batch, queries, keys, heads, kv_heads, width, dtype);
+    return (w.delta + w.part) * sizeof(float);
 }
 
 int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, const sdl_view_t* out,
@@ -304,18 +442,25 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
     int rc = sdl_attention_problem(a.p, batch, queries, keys, heads, kv_heads, width, dtype, scale, causal, q_len, k_len);
     if (rc != SDL_OK) return rc;
     if (batch == 0 || heads == 0 || (queries == 0 && keys == 0)) return SDL_OK;
+    const Plan w = plan_of(batch, queries, keys, heads, kv_heads, width, dtype);
+    // numbers of workgroups, and of threads that add sums up, that a launch can have
+    constexpr uint64_t kMost = 0x7fffffffu;
+    if (w.row_blocks * w.heads > kMost / w.keys.splits || w.key_blocks * w.heads > kMost / w.rows.splits) return SDL_ERR_UNSUPPORTED;
+    if (w.keys.splits > 1 && (uint64_t)batch * queries * heads * ((width + 3) / 4) > kMost) return SDL_ERR_UNSUPPORTED;
+    if (w.rows.splits > 1 && 2 * (uint64_t)batch * kv_heads * keys * ((width + 3) / 4) > kMost) return SDL_ERR_UNSUPPORTED;
     if (queries) {
         if ((rc = check_view(d_out, dtype)) != SDL_OK || (rc = check_view(q, dtype)) != SDL_OK || (rc = check_view(out, dtype)) != SDL_OK) return rc;
         if ((rc = check_output(dq, dtype, batch, queries, heads)) != SDL_OK) return rc;
         if (!lse || !workspace) return SDL_ERR_INVALID_ARG;
         if (!aligned_to(lse, 4) || !aligned_to(workspace, 4)) return SDL_ERR_ALIGNMENT;
-        if (workspace_bytes < sdl_attention_backward_workspace_bytes(batch, queries, keys, heads, kv_heads, width)) return SDL_ERR_INVALID_ARG;
+        if (workspace_bytes < (w.delta + w.part) * sizeof(float)) return SDL_ERR_INVALID_ARG;
         a.p.d_out = kernel_view(d_out);
         a.p.q = kernel_view(q);
         a.p.out = kernel_view(out);
         a.p.dq = kernel_view(dq);
         a.p.lse = const_cast<float*>(lse);
         a.p.delta = static_cast<float*>(workspace);
+        a.part = a.p.delta + w.delta;
     }
     if (keys) {
         if ((rc = check_view(k, dtype)) != SDL_OK || (rc = check_view(v, dtype)) != SDL_OK) return rc;
@@ -326,8 +471,8 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
         a.p.dv = kernel_view(dv);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == SDL_DTYPE_BF16) return width <= 64 ? backward<__bf16, 64>(a, st) : backward<__bf16, 128>(a, st);
-    return width <= 64 ? backward<float, 64>(a, st) : backward<float, 128>(a, st);
+    if (dtype == SDL_DTYPE_BF16) return width <= 64 ? backward<__bf16, 64>(a, w, st) : backward<__bf16, 128>(a, w, st);
+    return width <= 64 ? backward<float, 64>(a, w, st) : backward<float, 128>(a, w, st);
 }
 
 }  // extern "C"

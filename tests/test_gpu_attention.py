@@ -147,7 +147,7 @@ def test_split_keys_give_what_one_pass_gives(dtype):
     """Few rows over many keys go through several workgroups; the same rows among many others do not."""
     B, Lk, H, G, D = 2, 3000, 4, 2, 64
     case = (B, 3, Lk, H, G, D, True, None, [3000, 1203])
-    assert sdl.sdl_attention_workspace_bytes(B, 3, Lk, H, G, D) > 0
+    assert sdl.sdl_attention_workspace_bytes(B, 3, Lk, H, G, D, sdl.DTYPE_BF16 if dtype == BF16 else sdl.DTYPE_FP32) > 0
     _check(case, dtype, seed=9)
 
 

@@ -86,7 +86,7 @@ def test_attention(status, change):
 
 def test_attention_that_splits_its_keys_needs_its_workspace():
     few = dict(batch=1, queries=1, keys=4096, heads=1, kv_heads=1)
-    need = sdl.sdl_attention_workspace_bytes(1, 1, 4096, 1, 1, 64)
+    need = sdl.sdl_attention_workspace_bytes(1, 1, 4096, 1, 1, 64, sdl.DTYPE_BF16)
     assert need > 0
     assert call("sdl_attention", **few, workspace=None) == INVALID
     assert call("sdl_attention", **few, workspace_bytes=need - 1) == INVALID
@@ -104,8 +104,9 @@ def test_attention_backward(status, change):
 def test_workspace_sizes_of_what_is_refused_are_nothing():
     assert sdl.sdl_layer_norm_workspace_bytes(16385) == 0
     for f in (sdl.sdl_attention_workspace_bytes, sdl.sdl_attention_backward_workspace_bytes):
-        assert f(1, 1, 1 << 20, 3, 2, 64) == 0 and f(1, 1, 1 << 20, 2, 0, 64) == 0 and f(1, 1, 1 << 20, 2, 2, 0) == 0
-        assert f(1, 1, 1 << 20, 2, 2, 129) == 0 and f(0, 0, 0, 0, 1, 64) == 0
+        assert f(1, 1, 1 << 20, 2, 2, 64, 1) > 0
+        assert f(1, 1, 1 << 20, 3, 2, 64, 1) == 0 and f(1, 1, 1 << 20, 2, 0, 64, 1) == 0 and f(1, 1, 1 << 20, 2, 2, 0, 1) == 0
+        assert f(1, 1, 1 << 20, 2, 2, 129, 1) == 0 and f(0, 0, 0, 0, 1, 64, 1) == 0 and f(1, 1, 1 << 20, 2, 2, 64, 2) == 0
 
 
 def test_the_binding_refuses_what_is_no_such_tensor():
