@@ -285,13 +285,26 @@ struct Sequence {
     }
 };
 
-// Consecutive workgroups go to different compute dies (eight, each with its own cache): the work is handed out in runs of neighbours
-// per die, so that the workgroups that read the same keys and values share a cache.
-__device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t n)
-{
-    const uint32_t die = id & 7u, each = n >> 3, more = n & 7u;
-    return die * each + min(die, more) + (id >> 3);
-}
+// Consecutive workgroups go to different compute dies (eight, each with its own cache).  The `each` workgroups of a unit, a (batch, key head), read the
+// same keys and values: they stay on one die, and neighbouring units, whose lengths may differ, on different ones; where there are
+// fewer than eight units (left), every die has its share of the long and the short workgroups of one or more.
+struct Place {
+    uint32_t unit, within;
+
+    __device__ __forceinline__ Place(uint32_t id, uint32_t units, uint32_t each)
+    {
+        const uint32_t whole = units & ~7u, left = units & 7u;
+        if (id < whole * each) {
+            const uint32_t slot = id >> 3, row = slot / each;
+            unit = row * 8 + (id & 7u);
+            within = slot - row * each;
+        } else {
+            const uint32_t rest = id - whole * each, col = rest / left;
+            unit = whole + (rest - col * left);
+            within = col;
+        }
+    }
+};
 
 // Host: whether the kernels take such a problem.
 inline bool sdl_attention_shape(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype)

@@ -24,7 +24,7 @@ struct ForwardArgs {
     Attention p;
     float* part_out;        // [split][batch][key head][row][width], with more than one split
     float* part_lse;        // [split][batch][key head][row]
-    uint32_t row_blocks, splits, chunk, workgroups;         // chunk: keys of a split
+    uint32_t row_blocks, splits, chunk;         // chunk: keys of a split
 };
 
 template <typename T, int HD, int BN, bool ASYNC>
@@ -37,12 +37,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    uint32_t id = die_order(blockIdx.x, a.workgroups);
-    const uint32_t split = id % a.splits;
-    id /= a.splits;
-    const uint32_t block = a.row_blocks - 1 - id % a.row_blocks;      // the longest first
-    id /= a.row_blocks;
-    const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.row_blocks * a.splits);
+    const uint32_t split = place.within % a.splits;
+    const uint32_t block = a.row_blocks - 1 - place.within / a.splits;      // the longest first
+    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
 
     const uint32_t n_rows = p.queries * p.group.d;
     const uint32_t row = block * kRows + wave * kRowsPerWave + c;
@@ -222,7 +220,7 @@ uint32_t splits_of(uint32_t chunk, uint32_t keys) { return keys <= chunk ? 1u : 
 template <typename T>
 int forward(const ForwardArgs& a, hipStream_t st)
 {
-    const dim3 grid(a.workgroups), block(kWaves * kWave);
+    const dim3 grid(a.row_blocks * a.splits * a.p.batch * a.p.kv_heads), block(kWaves * kWave);
     constexpr int kNarrow = sizeof(T) == 2 ? 64 : 32;       // keys of a tile: 64 KB of shared memory at width 128
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
     if (a.p.width <= 64) {
@@ -275,7 +273,6 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
     a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
     const uint64_t groups = (uint64_t)a.row_blocks * a.splits * batch * kv_heads;
     if (groups > 0x7fffffffu || (a.splits > 1 && (uint64_t)batch * queries * heads > 0x7fffffffu)) return SDL_ERR_UNSUPPORTED;
-    a.workgroups = (uint32_t)groups;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == SDL_DTYPE_BF16 ? forward<__bf16>(a, st) : forward<float>(a, st);
 }

@@ -26,7 +26,6 @@ struct BackwardArgs {
     float* part;            // sums of the splits: [split][batch][key head][row][width], or [split][dk, dv][batch][key head][key][width]
     uint32_t blocks;        // of rows or keys, per (batch, key head)
     uint32_t splits, chunk; // chunk: keys of a split, or tiles of query tokens
-    uint32_t workgroups;
 };
 
 // The query tokens that see a key of a block, in tiles, head by head of the group.
@@ -52,12 +51,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    uint32_t id = die_order(blockIdx.x, a.workgroups);
-    const uint32_t split = id % a.splits;
-    id /= a.splits;
-    const uint32_t block = a.blocks - 1 - id % a.blocks;       // the longest first
-    id /= a.blocks;
-    const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits);
+    const uint32_t split = place.within % a.splits;
+    const uint32_t block = a.blocks - 1 - place.within / a.splits;       // the longest first
+    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
 
     const uint32_t n_rows = p.queries * p.group.d;
     const uint32_t row = block * kRows + wave * 32 + c;
@@ -172,12 +169,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    uint32_t id = die_order(blockIdx.x, a.workgroups);
-    const uint32_t split = id % a.splits;
-    id /= a.splits;
-    const uint32_t block = id % a.blocks;                      // the longest first
-    id /= a.blocks;
-    const Sequence s(p, id / p.kv_heads, id % p.kv_heads);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits);
+    const uint32_t split = place.within % a.splits;
+    const uint32_t block = place.within / a.splits;                      // the longest first
+    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
 
     const int32_t key0 = (int32_t)(block * kKeys), wave_key0 = key0 + wave * 32, key = wave_key0 + c;
     Frag<T> k[kSteps], v[kShareV ? 1 : kSteps];
@@ -397,11 +392,11 @@ int backward(BackwardArgs& a, const Plan& w, hipStream_t st)
         a.blocks = (uint32_t)w.row_blocks;
         a.splits = w.keys.splits;
         a.chunk = w.keys.chunk * kTile;
-        a.workgroups = (uint32_t)(w.row_blocks * w.heads * w.keys.splits);
+        const dim3 grid((uint32_t)(w.row_blocks * w.heads * w.keys.splits));
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), dim3(a.workgroups), block, 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), grid, block, 0, st, a);
         else
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), dim3(a.workgroups), block, 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), grid, block, 0, st, a);
         int rc = launched();
         if (rc == SDL_OK && a.splits > 1) rc = add<T, true>(a, (uint64_t)p.queries * p.group.d * w.heads, st);
         if (rc != SDL_OK) return rc;
@@ -410,11 +405,11 @@ int backward(BackwardArgs& a, const Plan& w, hipStream_t st)
     a.blocks = (uint32_t)w.key_blocks;
     a.splits = w.rows.splits;
     a.chunk = w.rows.chunk;
-    a.workgroups = (uint32_t)(w.key_blocks * w.heads * w.rows.splits);
+    const dim3 grid((uint32_t)(w.key_blocks * w.heads * w.rows.splits));
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), dim3(a.workgroups), block, 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), grid, block, 0, st, a);
     else
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), dim3(a.workgroups), block, 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), grid, block, 0, st, a);
     int rc = launched();
     if (rc == SDL_OK && a.splits > 1) rc = add<T, false>(a, 2 * (uint64_t)p.keys * w.heads, st);
     return rc;
