@@ -147,6 +147,11 @@ __device__ __forceinline__ void copy_piece(const char* base, uint32_t offset, ui
     // a write of m0 needs one wait state before the instruction that reads it; nothing else in these kernels uses m0
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");
 }
+// Four bytes a lane, from any addresses.
+__device__ __forceinline__ void copy_word(const float* from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(to) : "memory");
+}
 // Waits for this wavefront's copies and reads of shared memory, then for the workgroup.
 __device__ __forceinline__ void loads_done()
 {
@@ -255,7 +260,7 @@ __device__ __forceinline__ void store4(T* row, uint32_t at, uint32_t n, float a,
 struct Attention {
     View q, k, v, out, d_out, dq, dk, dv;
     float* lse;                 // [batch][heads][queries]
-    float* delta;               // the same shape, in the workspace
+    float* row_stats;           // backward: lse in base 2 and D, of that shape each, in the workspace
     const int32_t* q_len;
     const int32_t* k_len;
     Div group;                  // query heads of a key head
@@ -285,23 +290,25 @@ struct Sequence {
     }
 };
 
-// Consecutive workgroups go to different compute dies (eight, each with its own cache).  The `each` workgroups of a unit, a (batch, key head), read the
-// same keys and values: they stay on one die, and neighbouring units, whose lengths may differ, on different ones; where there are
-// fewer than eight units (left), every die has its share of the long and the short workgroups of one or more.
+// Consecutive workgroups go to different compute dies (eight, each with its own cache of 16 channels, which take turns every 256 bytes).  The `each`
+// workgroups of a unit, a (batch, key head), read the same keys and values and stay on one die.  Where the rows of a head lie 4 KB apart, as 16
+// heads of 128 do, all of them are in one channel: so a die has eight units at work at a time, and, as a die's units move on by one head
+// from row to row of eight, of different heads (and of all sequences, whose lengths may differ).  Units that are left over are spread over all dies.
 struct Place {
     uint32_t unit, within;
 
     __device__ __forceinline__ Place(uint32_t id, uint32_t units, uint32_t each)
     {
-        const uint32_t whole = units & ~7u, left = units & 7u;
-        if (id < whole * each) {
-            const uint32_t slot = id >> 3, row = slot / each;
-            unit = row * 8 + (id & 7u);
-            within = slot - row * each;
+        const uint32_t rows = units >> 3, left = units & 7u;
+        if (id < rows * 8 * each) {
+            const uint32_t die = id & 7u, slot = id >> 3, set = slot / (8 * each), in_set = slot - set * 8 * each, n = min(8u, rows - 8 * set);
+            within = in_set / n;
+            const uint32_t row = set * 8 + (in_set - within * n);
+            unit = row * 8 + ((die - row) & 7u);
         } else {
-            const uint32_t rest = id - whole * each, col = rest / left;
-            unit = whole + (rest - col * left);
-            within = col;
+            const uint32_t rest = id - rows * 8 * each;
+            within = rest / left;
+            unit = rows * 8 + (rest - within * left);
         }
     }
 };

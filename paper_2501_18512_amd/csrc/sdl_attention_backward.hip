@@ -19,24 +19,32 @@ namespace {
 
 using namespace sdl_device;
 
-constexpr int kWaves = 4, kRows = 32 * kWaves, kKeys = 32 * kWaves, kTile = 32;
+constexpr int kWaves = 4, kRows = 32 * kWaves;          // of the kernel of dq
+
+// Keys or query tokens that go through shared memory at a time, and the keys of a workgroup of the other kernel (32 a wavefront).  A tile
+// has to last as long as the next one takes to come.  bf16 at width 128: eight wavefronts, as two workgroups of four would have room for tiles of 32
+// only (v of their keys lies in shared memory as well): 241 us with 4 and 32, see the figures above for 8 and 64.
+__host__ __device__ constexpr int tile_of(bool bf16) { return bf16 ? 64 : 32; }
+__host__ __device__ constexpr int key_waves(bool bf16, bool wide) { return bf16 && wide ? 8 : 4; }
 
 struct BackwardArgs {
     Attention p;
     float* part;            // sums of the splits: [split][batch][key head][row][width], or [split][dk, dv][batch][key head][key][width]
     uint32_t blocks;        // of rows or keys, per (batch, key head)
     uint32_t splits, chunk; // chunk: keys of a split, or tiles of query tokens
+    uint32_t tile, keys;    // tokens of a tile, keys of a block
+    uint64_t stats;         // rows of all sequences: the workspace has their lse in base 2, then their D
 };
 
 // The query tokens that see a key of a block, in tiles, head by head of the group.
 struct Seers {
     int32_t begin, end, per_head, tiles;
 
-    __device__ __forceinline__ Seers(const Attention& p, const Sequence& s, int32_t key0)
+    __device__ __forceinline__ Seers(const Attention& p, const Sequence& s, int32_t key0, int32_t tile)
     {
         end = key0 < s.nk ? s.nq : 0;
-        begin = p.causal ? min(max(0, key0 - s.shift), s.nq) / kTile * kTile : 0;
-        per_head = end > begin ? (end - begin + kTile - 1) / kTile : 0;
+        begin = p.causal ? min(max(0, key0 - s.shift), s.nq) / tile * tile : 0;
+        per_head = end > begin ? (end - begin + tile - 1) / tile : 0;
         tiles = per_head * (int32_t)p.group.d;
     }
 };
@@ -44,7 +52,7 @@ struct Seers {
 template <typename T, int HD, bool ASYNC>
 __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dq_kernel(const BackwardArgs a)
 {
-    constexpr int kSteps = HD / 16, kOut = HD / 32;
+    constexpr int kSteps = HD / 16, kOut = HD / 32, kTile = tile_of(sizeof(T) == 2), kParts = kTile / 32;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(kTile)];
     __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(kTile)];
@@ -88,8 +96,11 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         delta = half_sum(delta);
     }
     const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + (uint32_t)t;
-    if (row < n_rows && half == 0 && split == 0) p.delta[stat] = delta;
     const float lse2 = sees > 0 ? p.lse[stat] * kLog2e : 0.0f;
+    if (row < n_rows && half == 0 && split == 0) {
+        p.row_stats[stat] = lse2;
+        p.row_stats[a.stats + stat] = delta;
+    }
 
     const TileCopy<T, HD, kTile, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
 #pragma unroll
@@ -108,22 +119,28 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             copy_v.bring(v_next, key0 + kTile, s.nk);
         }
         if (!busy) return;
-        f32x16_t sc = {}, dp = {};
+        f32x16_t sc[kParts] = {}, dp[kParts] = {};
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            mma(sc, Smem::along(k_now, c, 2 * k + half), q[k]);
-            mma(dp, Smem::along(v_now, c, 2 * k + half), g[k]);
-        }
+        for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -lse2)) * (dp[i] - delta);
+            for (int n = 0; n < kParts; ++n) {
+                mma(sc[n], Smem::along(k_now, n * 32 + c, 2 * k + half), q[k]);
+                mma(dp[n], Smem::along(v_now, n * 32 + c, 2 * k + half), g[k]);
+            }
+#pragma unroll
+        for (int n = 0; n < kParts; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[n][i] = exp2_fast(__builtin_fmaf(sc[n][i], p.scale_log2, -lse2)) * (dp[n][i] - delta);
         if (key0 + kTile > every) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (key0 + 8 * (i / 4) + 4 * half + i % 4 >= sees) sc[i] = 0.0f;
+            for (int n = 0; n < kParts; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key0 + n * 32 + 8 * (i / 4) + 4 * half + i % 4 >= sees) sc[n][i] = 0.0f;
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const Frag<T> ds = frag_of(sc, u, T());
+        for (int u = 0; u < kTile / 16; ++u) {
+            const Frag<T> ds = frag_of(sc[u / 2], u % 2, T());
 #pragma unroll
             for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(k_now, u * 16, n * 32), ds);
         }
@@ -154,16 +171,18 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 }
 
 template <typename T, int HD, bool ASYNC>
-__global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dkv_kernel(const BackwardArgs a)
+__global__ void __launch_bounds__(key_waves(sizeof(T) == 2, HD > 64) * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dkv_kernel(const BackwardArgs a)
 {
-    constexpr int kSteps = HD / 16, kOut = HD / 32;
+    constexpr int kSteps = HD / 16, kOut = HD / 32, kTile = tile_of(sizeof(T) == 2), kWaves = key_waves(sizeof(T) == 2, HD > 64), kKeys = 32 * kWaves;
     typedef Tile<T, HD> Smem;
     // At width 128 k and v together would not leave the sums their registers (256 a lane, two wavefronts on a SIMD).
     constexpr bool kShareV = HD > 64;
-    // v comes last: a constant offset of a read reaches 64 KB
+    struct Stage {
+        char q[Smem::bytes(kTile)], g[Smem::bytes(kTile)];
+        float stats[2][kTile];          // lse in base 2, D
+    };
     __shared__ __attribute__((aligned(16))) struct {
-        char q[2][Smem::bytes(kTile)], g[2][Smem::bytes(kTile)];
-        float lse2[2][kTile], delta[2][kTile];
+        Stage stage[2];
         char v[kShareV ? Smem::bytes(kKeys) : 16];
     } mem;
     const Attention& p = a.p;
@@ -186,7 +205,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             if constexpr (!kShareV) set_frag(v[i], load8(src_v, i * 16 + half * 8, n));
         }
     }
-    const Seers seers(p, s, key0);
+    const Seers seers(p, s, key0, kTile);
     const int32_t t_begin = seers.begin, t_end = seers.end, tile0 = (int32_t)(split * a.chunk), tiles = min(seers.tiles, tile0 + (int32_t)a.chunk);
     if (split > 0 && tile0 >= tiles) return;         // nothing there for this split, and nothing is looked at when the sums are added
 
@@ -199,23 +218,21 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t skip = seers.per_head > 0 ? tile0 / seers.per_head : 0;
     uint32_t next_head = s.g * p.group.d + skip;          // what is brought next
     int32_t next_t = t_begin + (tile0 - skip * seers.per_head) * kTile;
-    auto bring = [&](char* q_to, char* g_to, float* lse2_to, float* delta_to) __attribute__((always_inline)) {
-        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).bring(q_to, next_t, t_end);
-        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).bring(g_to, next_t, t_end);
-        if (threadIdx.x < kTile) {
-            const int32_t t = min(next_t + (int32_t)threadIdx.x, t_end - 1);
-            const uint64_t stat = ((uint64_t)s.b * p.kv_heads * p.group.d + next_head) * p.queries + (uint32_t)t;
-            const float lse = p.lse[stat];
-            lse2_to[threadIdx.x] = lse == -__builtin_inff() ? 0.0f : lse * kLog2e;      // a row that sees nothing is masked below
-            delta_to[threadIdx.x] = p.delta[stat];
+    auto bring = [&](Stage& to) __attribute__((always_inline)) {
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).bring(to.q, next_t, t_end);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).bring(to.g, next_t, t_end);
+        if (wave == 0) {
+            const float* from = p.row_stats + ((uint64_t)s.b * p.kv_heads * p.group.d + next_head) * p.queries + (uint32_t)min(next_t + lane % kTile, t_end - 1);
+#pragma unroll
+            for (int i = 0; i < 2 * kTile; i += kWave) copy_word(from + (i + lane >= kTile ? a.stats : 0), lds_offset(to.stats[0] + i));
         }
         next_t += kTile;
         if (next_t >= t_end) next_t = t_begin, ++next_head;
     };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).clear(mem.q[i]);
-        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).clear(mem.g[i]);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).clear(mem.stage[i].q);
+        TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).clear(mem.stage[i].g);
     }
     int32_t t0 = next_t;
     if (tile0 < tiles) {
@@ -224,47 +241,49 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             copy_v.clear(mem.v);
             copy_v.bring(mem.v, key0, s.nk);
         }
-        bring(mem.q[0], mem.g[0], mem.lse2[0], mem.delta[0]);
+        bring(mem.stage[0]);
     }
-    auto step = [&](bool more, int now) __attribute__((always_inline)) {
+    for (int32_t tile = tile0, now = 0; tile < tiles; ++tile, now ^= 1) {
         loads_done();               // this tile is there, and all are done with the one before it
-        if (more) bring(mem.q[now ^ 1], mem.g[now ^ 1], mem.lse2[now ^ 1], mem.delta[now ^ 1]);
-        f32x16_t sc = {}, dp = {};
+        if (tile + 1 < tiles) bring(mem.stage[now ^ 1]);
+        const Stage& in = mem.stage[now];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            mma(sc, Smem::along(mem.q[now], c, 2 * i + half), k[i]);
-            if constexpr (kShareV)
-                mma(dp, Smem::along(mem.g[now], c, 2 * i + half), Smem::along(mem.v, wave * 32 + c, 2 * i + half));
-            else
-                mma(dp, Smem::along(mem.g[now], c, 2 * i + half), v[i]);
-        }
+        for (int part = 0; part < kTile; part += 32) {
+            __builtin_amdgcn_sched_barrier(0);          // reads of the next part this early would not leave enough registers
+            f32x16_t sc = {}, dp = {};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = 8 * (i / 4) + 4 * half + i % 4;
-            sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -mem.lse2[now][r]));
-            dp[i] = sc[i] * (dp[i] - mem.delta[now][r]);
-        }
-        if (t0 < t_full || t0 + kTile > t_end) {
-            const int32_t t = t0 + 4 * half;
+            for (int i = 0; i < kSteps; ++i) {
+                mma(sc, Smem::along(in.q, part + c, 2 * i + half), k[i]);
+                if constexpr (kShareV)
+                    mma(dp, Smem::along(in.g, part + c, 2 * i + half), Smem::along(mem.v, wave * 32 + c, 2 * i + half));
+                else
+                    mma(dp, Smem::along(in.g, part + c, 2 * i + half), v[i]);
+            }
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (t < t_key - (8 * (i / 4) + i % 4) || t >= t_end - (8 * (i / 4) + i % 4)) sc[i] = 0.0f, dp[i] = 0.0f;
-        }
+            for (int i = 0; i < 16; ++i) {
+                const int r = part + 8 * (i / 4) + 4 * half + i % 4;
+                sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -in.stats[0][r]));
+                dp[i] = sc[i] * (dp[i] - in.stats[1][r]);
+            }
+            // unless every row of the tile sees every key of the wavefront
+            if (t0 < t_full || t0 + kTile > t_end) {
+                const int32_t t = t0 + part + 4 * half;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
+                for (int i = 0; i < 16; ++i)
+                    if (t < t_key - (8 * (i / 4) + i % 4) || t >= t_end - (8 * (i / 4) + i % 4)) sc[i] = 0.0f, dp[i] = 0.0f;
+            }
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) {
-                mma(dv[n], Smem::across(mem.g[now], u * 16, n * 32), pr);
-                mma(dk[n], Smem::across(mem.q[now], u * 16, n * 32), ds);
+            for (int u = 0; u < 2; ++u) {
+                const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
+#pragma unroll
+                for (int n = 0; n < kOut; ++n) {
+                    mma(dv[n], Smem::across(in.g, part + u * 16, n * 32), pr);
+                    mma(dk[n], Smem::across(in.q, part + u * 16, n * 32), ds);
+                }
             }
         }
         t0 += kTile;
         if (t0 >= t_end) t0 = t_begin;
-    };
-    for (int32_t tile = tile0; tile < tiles; tile += 2) {
-        step(tile + 1 < tiles, 0);
-        if (tile + 1 < tiles) step(tile + 2 < tiles, 1);
     }
     if (key >= (int32_t)p.keys) return;
     if (a.splits > 1) {
@@ -314,7 +333,7 @@ __global__ void __launch_bounds__(256) sdl_attention_add_kernel(const BackwardAr
     } else {
         token = i;
         head = s.g;
-        const Seers seers(p, s, (int32_t)(i / kKeys * kKeys));
+        const Seers seers(p, s, (int32_t)(i / a.keys * a.keys), (int32_t)a.tile);
         used = (int32_t)i < s.nk ? ((uint32_t)seers.tiles + a.chunk - 1) / a.chunk : 0;
     }
     const float* src = a.part + (uint64_t)line * p.width + at;
@@ -344,7 +363,7 @@ Cut cut(uint64_t groups, uint64_t tiles, sdl_dtype_t dtype)          // in tiles
 {
     uint64_t n = tiles;
     if (groups < kFill / 2) {
-        const uint64_t least = dtype == SDL_DTYPE_BF16 ? 256 / kTile : 64 / kTile;
+        const uint64_t least = dtype == SDL_DTYPE_BF16 ? 4 : 2;
         n = (tiles * groups + kFill - 1) / kFill;
         if (n < least) n = least;
     }
@@ -355,19 +374,21 @@ Cut cut(uint64_t groups, uint64_t tiles, sdl_dtype_t dtype)          // in tiles
 struct Plan {
     uint64_t row_blocks, key_blocks, heads;
     Cut keys, rows;         // of the kernel of dq, of the one of dk and dv
-    size_t delta, part;     // floats of the workspace
+    size_t stats, part;     // rows of statistics, of two floats each, and the floats of the sums
+    size_t floats() const { return (2 * stats + 3) / 4 * 4 + part; }
 };
 
 Plan plan_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype)
 {
     Plan w{};
-    const uint64_t group = heads / kv_heads, rows = queries * group;
+    const bool bf16 = dtype == SDL_DTYPE_BF16;
+    const uint64_t group = heads / kv_heads, rows = queries * group, tile = tile_of(bf16), block = 32 * key_waves(bf16, width > 64);
     w.heads = (uint64_t)batch * kv_heads;
     w.row_blocks = (rows + kRows - 1) / kRows;
-    w.key_blocks = ((uint64_t)keys + kKeys - 1) / kKeys;
-    w.keys = cut(w.row_blocks * w.heads, ((uint64_t)keys + kTile - 1) / kTile, dtype);
-    w.rows = cut(w.key_blocks * w.heads, ((uint64_t)queries + kTile - 1) / kTile * group, dtype);
-    w.delta = ((size_t)batch * heads * queries + 3) / 4 * 4;
+    w.key_blocks = (keys + block - 1) / block;
+    w.keys = cut(w.row_blocks * w.heads, (keys + tile - 1) / tile, dtype);
+    w.rows = cut(w.key_blocks * w.heads, (queries + tile - 1) / tile * group, dtype);
+    w.stats = (size_t)batch * heads * queries;
     const size_t of_keys = w.keys.splits > 1 ? (size_t)w.keys.splits * w.heads * rows * width : 0;
     const size_t of_rows = w.rows.splits > 1 ? (size_t)w.rows.splits * 2 * w.heads * keys * width : 0;
     w.part = of_keys > of_rows ? of_keys : of_rows;
@@ -387,16 +408,20 @@ template <typename T, int HD>
 int backward(BackwardArgs& a, const Plan& w, hipStream_t st)
 {
     const Attention& p = a.p;
-    const dim3 block(kWaves * kWave);
+    constexpr bool bf16 = sizeof(T) == 2;
+    constexpr int key_threads = key_waves(bf16, HD > 64) * kWave;
+    a.tile = tile_of(bf16);
+    a.keys = 32 * key_waves(bf16, HD > 64);
+    a.stats = w.stats;
     if (w.row_blocks) {
         a.blocks = (uint32_t)w.row_blocks;
         a.splits = w.keys.splits;
-        a.chunk = w.keys.chunk * kTile;
+        a.chunk = w.keys.chunk * a.tile;
         const dim3 grid((uint32_t)(w.row_blocks * w.heads * w.keys.splits));
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), grid, dim3(kWaves * kWave), 0, st, a);
         else
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), grid, dim3(kWaves * kWave), 0, st, a);
         int rc = launched();
         if (rc == SDL_OK && a.splits > 1) rc = add<T, true>(a, (uint64_t)p.queries * p.group.d * w.heads, st);
         if (rc != SDL_OK) return rc;
@@ -407,9 +432,9 @@ int backward(BackwardArgs& a, const Plan& w, hipStream_t st)
     a.chunk = w.rows.chunk;
     const dim3 grid((uint32_t)(w.key_blocks * w.heads * w.rows.splits));
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), grid, dim3(key_threads), 0, st, a);
     else
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), grid, dim3(key_threads), 0, st, a);
     int rc = launched();
     if (rc == SDL_OK && a.splits > 1) rc = add<T, false>(a, 2 * (uint64_t)p.keys * w.heads, st);
     return rc;
@@ -424,7 +449,7 @@ size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, 
 {
     if (heads == 0 || !sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return 0;
     const Plan w = plan_of(batch, queries, keys, heads, kv_heads, width, dtype);
-    return (w.delta + w.part) * sizeof(float);
+    return w.floats() * sizeof(float);
 }
 
 int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, const sdl_view_t* out,
@@ -448,14 +473,14 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
         if ((rc = check_output(dq, dtype, batch, queries, heads)) != SDL_OK) return rc;
         if (!lse || !workspace) return SDL_ERR_INVALID_ARG;
         if (!aligned_to(lse, 4) || !aligned_to(workspace, 4)) return SDL_ERR_ALIGNMENT;
-        if (workspace_bytes < (w.delta + w.part) * sizeof(float)) return SDL_ERR_INVALID_ARG;
+        if (workspace_bytes < w.floats() * sizeof(float)) return SDL_ERR_INVALID_ARG;
         a.p.d_out = kernel_view(d_out);
         a.p.q = kernel_view(q);
         a.p.out = kernel_view(out);
         a.p.dq = kernel_view(dq);
         a.p.lse = const_cast<float*>(lse);
-        a.p.delta = static_cast<float*>(workspace);
-        a.part = a.p.delta + w.delta;
+        a.p.row_stats = static_cast<float*>(workspace);
+        a.part = a.p.row_stats + (w.floats() - w.part);
     }
     if (keys) {
         if ((rc = check_view(k, dtype)) != SDL_OK || (rc = check_view(v, dtype)) != SDL_OK) return rc;
