@@ -34,6 +34,17 @@ __device__ __forceinline__ void mma(f32x16_t& d, const Frag<float>& a, const Fra
     for (int j = 0; j < 8; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], d, 0, 0, 0);
 }
 
+// The 16x16 instructions, 32 values of k: lane l has row or column l % 16 and k = 8 (l / 16) + j; D is column l % 16, rows 4 (l / 16) + i.
+__device__ __forceinline__ void mma16(f32x4_t& d, const Frag<__bf16>& a, const Frag<__bf16>& b)
+{
+    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, d, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(f32x4_t& d, const Frag<float>& a, const Frag<float>& b, int n = 8)
+{
+#pragma unroll
+    for (int j = 0; j < n; ++j) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], d, 0, 0, 0);
+}
+
 __device__ __forceinline__ void set_frag(Frag<__bf16>& f, const Eight<__bf16>& x) { f.v = __builtin_bit_cast(bf16x8_t, x.w); }
 __device__ __forceinline__ void set_frag(Frag<float>& f, const Eight<float>& x)
 {
@@ -104,6 +115,25 @@ struct Tile {
         }
         return f;
     }
+    // For the 16x16 instructions: column d0 + lane % 16 of the rows 4 (lane / 16) + i and, bf16, 16 more, i = 0..3.
+    static __device__ __forceinline__ Frag<T> across16(const char* tile, int d0)
+    {
+        const int lane = threadIdx.x & (kWave - 1), quarter = lane >> 4;
+        Frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+            const int r = 4 * quarter + ((lane & 15) >> 2), p = (d0 >> 3) + ((lane & 2) >> 1), q = (lane & 1) * 8;
+            const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + at(r, p) + q));
+            const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + at(r + 16, p) + q));
+            const bf16x4_t x = __builtin_bit_cast(bf16x4_t, a), y = __builtin_bit_cast(bf16x4_t, b);
+            f.v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            const int d = d0 + (lane & 15);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.v[i] = u2f(*reinterpret_cast<const uint32_t*>(tile + at(4 * quarter + i, d >> 2) + (d & 3) * 4));
+        }
+        return f;
+    }
     // column d0 + lane % 32 of the rows r0 + order(half, j), r0 a multiple of 16.  bf16: the transposing read gives lane i of 16 the i-th
     // column of a block of 4 rows and 16 columns, of which lane 4 r + q names the q-th quarter of row r.
     static __device__ __forceinline__ Frag<T> across(const char* tile, int r0, int d0)
@@ -142,20 +172,26 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
 {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
+// (ONCE: data that no one reads again goes past the caches.)
+template <bool ONCE>
 __device__ __forceinline__ void copy_piece(const char* base, uint32_t offset, uint32_t to)
 {
     // a write of m0 needs one wait state before the instruction that reads it; nothing else in these kernels uses m0
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(to) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");
 }
 // Four bytes a lane, from any addresses.
 __device__ __forceinline__ void copy_word(const float* from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(to) : "memory");
 }
+__device__ __forceinline__ void own_loads_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory"); }
 // Waits for this wavefront's copies and reads of shared memory, then for the workgroup.
 __device__ __forceinline__ void loads_done()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+    own_loads_done();
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
 }
@@ -163,7 +199,7 @@ __device__ __forceinline__ void loads_done()
 // A workgroup of WAVES wavefronts brings tiles of ROWS consecutive tokens of one head.  The offset of a lane's piece from the first row of
 // its share is the same in every tile; ASYNC is for rows that start on 16 bytes and lie at most 2^31 bytes apart in a tile, the other way
 // takes any element alignment and goes through registers.
-template <typename T, int HD, int ROWS, int WAVES, bool ASYNC>
+template <typename T, int HD, int ROWS, int WAVES, bool ASYNC, bool ONCE = false>
 struct TileCopy {
     typedef Tile<T, HD> Smem;
     static constexpr int kPieces = Smem::kPieces;
@@ -192,17 +228,17 @@ struct TileCopy {
     __device__ __forceinline__ void bring(char* tile, int32_t row0, int32_t rows) const
     {
         if constexpr (ASYNC) {
-            const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+            const uint32_t lane = threadIdx.x & (kWave - 1), wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
             const uint32_t row = wave * Smem::kGroup + lane / kPieces, to = lds_offset(tile) + wave * Smem::kGroupBytes;
             const uint32_t piece = (uint32_t)Smem::place(lane / kPieces, lane % kPieces);       // that comes to lie where the lane's 16 bytes land
             const char* from = base + row0 * stride;
             if (row0 + ROWS <= rows && width == HD) {
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) copy_piece(from + i * kStep * stride, row * (uint32_t)stride + piece * 16, to + i * (WAVES * Smem::kGroupBytes));
+                for (int i = 0; i < kCopies; ++i) copy_piece<ONCE>(from + i * kStep * stride, row * (uint32_t)stride + piece * 16, to + i * (WAVES * Smem::kGroupBytes));
             } else if (piece * 16 < width * sizeof(T)) {
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i)
-                    copy_piece(from, min(row + i * kStep, (uint32_t)(rows - 1 - row0)) * (uint32_t)stride + piece * 16, to + i * (WAVES * Smem::kGroupBytes));
+                    copy_piece<ONCE>(from, min(row + i * kStep, (uint32_t)(rows - 1 - row0)) * (uint32_t)stride + piece * 16, to + i * (WAVES * Smem::kGroupBytes));
             }
         } else {
 #pragma unroll 4
@@ -233,6 +269,18 @@ __device__ __forceinline__ float half_sum(float x)
 {
     const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false));
     return u2f(p[0]) + u2f(p[1]);
+}
+
+// the same over the four lanes l % 16, + 16, + 32, + 48
+__device__ __forceinline__ float quarter_max(float x)
+{
+    const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(f2u(x), f2u(x), false, false));
+    return half_max(fmaxf(u2f(p[0]), u2f(p[1])));
+}
+__device__ __forceinline__ float quarter_sum(float x)
+{
+    const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(f2u(x), f2u(x), false, false));
+    return half_sum(u2f(p[0]) + u2f(p[1]));
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -18,14 +18,21 @@ namespace {
 using namespace sdl_device;
 
 constexpr int kRowsPerWave = 32, kWaves = 4, kRows = kRowsPerWave * kWaves;
-constexpr uint32_t kMaxSplits = kWave;         // the join has one a lane
+constexpr uint32_t kMaxSplits = 256;           // the join has one a thread
 
 struct ForwardArgs {
     Attention p;
     float* part_out;        // [split][batch][key head][row][width], with more than one split
     float* part_lse;        // [split][batch][key head][row]
     uint32_t row_blocks, splits, chunk;         // chunk: keys of a split
+    uint32_t few;                               // few rows: the splits take turns
 };
+
+// Splits that keys make: one at least, which says that there are none.
+__device__ __forceinline__ int32_t splits_in_use(const ForwardArgs& a, int32_t keys)
+{
+    return max(1, (int32_t)(((uint32_t)keys + a.chunk - 1) / a.chunk));
+}
 
 template <typename T, int HD, int BN, bool ASYNC>
 __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_kernel(const ForwardArgs a)
@@ -158,56 +165,175 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     }
 }
 
-// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s: one wavefront a row, two elements a lane, and the weight
-// of split s in lane s.
+// The same for up to 16 rows, tokens that are generated one by one, where reading the keys and values is all there is to it.  A workgroup is one wavefront
+// with tiles of its own, so that nothing waits for anything but its own copies, and the compute unit's other wavefronts (four at width 128) fill in. The rows
+// are the columns of the 16x16 instructions.  The splits of a (batch, key head) take turns with the tiles, so that what they read at a time lies side by side.
+template <typename T, int HD, bool ASYNC, bool ONCE>
+__global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardArgs a)
+{
+    constexpr int BN = sizeof(T) == 2 ? 32 : 16, kTiles = BN / 16, kSteps = HD / 32, kOut = HD / 16;
+    typedef Tile<T, HD> Smem;
+    __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(BN)];
+    __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(BN)];
+    const Attention& p = a.p;
+    const int lane = threadIdx.x, c = lane & 15, quarter = lane >> 4;
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits);
+    const uint32_t split = place.within;
+    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
+    const int32_t keys = s.nq > 0 ? s.seen(p, s.nq - 1) : 0, splits = splits_in_use(a, keys);
+    if ((int32_t)split >= splits) return;               // not looked at by the join
+    const TileCopy<T, HD, BN, 1, ASYNC, ONCE> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
+    const int32_t key_begin = (int32_t)split * BN, step = splits * BN;
+    if (key_begin < keys) {
+        copy_k.bring(ks[0], key_begin, s.nk);
+        copy_v.bring(vs[0], key_begin, s.nk);
+    }
+
+    const uint32_t n_rows = p.queries * p.group.d, row = min((uint32_t)c, n_rows - 1), t = div(row, p.group);
+    const uint32_t head = s.g * p.group.d + (row - t * p.group.d);
+    const bool valid = (uint32_t)c < n_rows && (int32_t)t < s.nq;
+    const int32_t sees = valid ? s.seen(p, (int32_t)t) : 0;
+    Frag<T> q[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) set_frag(q[k], load8(at_row<T>(p.q, s.b, t, head), k * 32 + quarter * 8, valid ? p.width : 0));
+
+    f32x4_t o[kOut] = {};
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int32_t key0 = key_begin, now = 0; key0 < keys; key0 += step, now ^= 1) {
+        own_loads_done();
+        if (key0 + step < keys) {
+            copy_k.bring(ks[now ^ 1], key0 + step, s.nk);
+            copy_v.bring(vs[now ^ 1], key0 + step, s.nk);
+        }
+        f32x4_t sc[kTiles] = {};
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma16(sc[n], Smem::along(ks[now], n * 16 + c, 4 * k + quarter), q[k]);
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (key0 + n * 16 + 4 * quarter + i >= sees) sc[n][i] = -__builtin_inff();
+                top = fmaxf(top, sc[n][i]);
+            }
+        top = quarter_max(top) * p.scale_log2;
+        if (__any(top > m)) {
+            const float up = fmaxf(m, top), by = exp2_fast(m - (up == -__builtin_inff() ? 0.0f : up));
+            m = up;
+            l *= by;
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) o[n] *= by;
+        }
+        const float off = m == -__builtin_inff() ? 0.0f : m;
+        Frag<T> pr;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sc[n][i] = exp2_fast(__builtin_fmaf(sc[n][i], p.scale_log2, -off));
+                l += sc[n][i];
+            }
+        if constexpr (sizeof(T) == 2) {
+            pr.v = __builtin_bit_cast(bf16x8_t, u32x4{pack_bf16(sc[0][0], sc[0][1]), pack_bf16(sc[0][2], sc[0][3]),
+                                                      pack_bf16(sc[kTiles - 1][0], sc[kTiles - 1][1]), pack_bf16(sc[kTiles - 1][2], sc[kTiles - 1][3])});
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) mma16(o[n], Smem::across16(vs[now], n * 16), pr);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pr.v[i] = sc[0][i];
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) mma16(o[n], Smem::across16(vs[now], n * 16), pr, 4);
+        }
+    }
+    l = quarter_sum(l);
+    if ((uint32_t)c >= n_rows) return;
+    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    const float lse = l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (a.splits == 1) {
+        T* dst = at_row<T>(p.out, s.b, t, head);
+#pragma unroll
+        for (int n = 0; n < kOut; ++n) store4(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
+        if (p.lse && quarter == 0) p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = lse;
+    } else {
+        const uint64_t line = (((uint64_t)split * p.batch + s.b) * p.kv_heads + s.g) * n_rows + row;
+        float* dst = a.part_out + line * p.width;
+#pragma unroll
+        for (int n = 0; n < kOut; ++n) store4(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
+        if (quarter == 0) a.part_lse[line] = lse;
+    }
+}
+
+// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s.  A workgroup has one row: its threads hold a split's
+// weight each, then eight groups of 32 take turns with the splits, four elements a thread.
 template <typename T>
 __global__ void __launch_bounds__(256) sdl_attention_join_kernel(const ForwardArgs a)
 {
+    __shared__ float weights[kMaxSplits], parts[2][4];
+    __shared__ f32x4_t sums[8][32];
     const Attention& p = a.p;
-    const uint32_t n_rows = p.queries * p.group.d, lane = threadIdx.x & (kWave - 1);
-    const uint32_t lines = p.batch * p.kv_heads * n_rows;
-    const uint32_t line = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
-    if (line >= lines) return;
+    const uint32_t n_rows = p.queries * p.group.d, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const uint32_t lines = p.batch * p.kv_heads * n_rows, line = blockIdx.x;
     const uint32_t bg = line / n_rows, row = line - bg * n_rows, t = div(row, p.group);
     const Sequence s(p, bg / p.kv_heads, bg % p.kv_heads);
-    const uint32_t head = s.g * p.group.d + (row - t * p.group.d);
-    const uint32_t sees = (int32_t)t < s.nq ? (uint32_t)s.seen(p, (int32_t)t) : 0;
-    const uint32_t n = (sees + a.chunk - 1) / a.chunk;
-    const float mine = lane < n ? a.part_lse[(uint64_t)lane * lines + line] : -__builtin_inff();
+    const uint32_t last = a.few ? s.nq - 1 : t;        // splits that take turns are all of use to every row
+    const uint32_t n = (int32_t)t < s.nq ? splits_in_use(a, s.seen(p, (int32_t)last)) : 0;
+    const uint32_t group = threadIdx.x / 32, d = threadIdx.x % 32 * 4;
+    const float* src = a.part_out + (uint64_t)line * p.width + d;
+    const uint64_t step = (uint64_t)lines * p.width;
+    const float mine = threadIdx.x < n ? a.part_lse[(uint64_t)threadIdx.x * lines + line] : -__builtin_inff();
     float top = mine;
 #pragma unroll
     for (int m = 1; m < kWave; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-    const float off = top == -__builtin_inff() ? 0.0f : top;
-    const float weight = exp2_fast((mine - off) * kLog2e), sum = lane_sum<kWave>(weight);
-    const float scaled = sum == 0.0f ? 0.0f : weight / sum;
-    float x = 0.0f, y = 0.0f;
-    const uint32_t d = 2 * lane;
-    const float* src = a.part_out + (uint64_t)line * p.width;
-#pragma unroll 8
-    for (uint32_t i = 0; i < n; ++i) {
-        const float by = u2f(__builtin_amdgcn_readlane(f2u(scaled), i));
-        const float* from = src + (uint64_t)i * lines * p.width;
-        if (d < p.width) x = __builtin_fmaf(by, from[d], x);
-        if (d + 1 < p.width) y = __builtin_fmaf(by, from[d + 1], y);
+    if (lane == 0) parts[0][wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(parts[0][0], parts[0][1]), fmaxf(parts[0][2], parts[0][3]));
+    const float off = top == -__builtin_inff() ? 0.0f : top, weight = exp2_fast((mine - off) * kLog2e);
+    float sum = lane_sum<kWave>(weight);
+    if (lane == 0) parts[1][wave] = sum;
+    weights[threadIdx.x] = weight;
+    __syncthreads();
+    sum = (parts[1][0] + parts[1][1]) + (parts[1][2] + parts[1][3]);
+    f32x4_t x = {};
+    if (d + 4 <= p.width) {
+#pragma unroll 4
+        for (uint32_t i = group; i < n; i += 8) x += weights[i] * *reinterpret_cast<const f32x4_elem*>(src + i * step);
+    } else {
+        for (uint32_t i = group; i < n; i += 8)
+            for (uint32_t j = 0; j < 4; ++j) x[j] += d + j < p.width ? weights[i] * src[i * step + j] : 0.0f;
     }
-    T* dst = at_row<T>(p.out, s.b, t, head);
-    if (d < p.width) dst[d] = (T)x;
-    if (d + 1 < p.width) dst[d + 1] = (T)y;
-    if (p.lse && lane == 0)
+    sums[group][threadIdx.x % 32] = x;
+    __syncthreads();
+    const uint32_t head = s.g * p.group.d + (row - t * p.group.d);
+    if (threadIdx.x < 32 && d < p.width) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) x += sums[i][threadIdx.x];
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        store4(at_row<T>(p.out, s.b, t, head), d, p.width, x[0] * by, x[1] * by, x[2] * by, x[3] * by);
+    }
+    if (p.lse && threadIdx.x == 0)
         p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = sum == 0.0f ? -__builtin_inff() : off + __builtin_amdgcn_logf(sum) * kLn2;
 }
 
-// Keys of a chunk: as few as make about `kFill` workgroups of a problem that has fewer, and no fewer than pay for a workgroup's start and its
-// share of the join (256; an fp32 tile takes the matrix units 16 times as long: 64).
-constexpr uint32_t kFill = 1024;
+// Keys of a split.  A problem that has fewer workgroups than fill the chip is cut, down to what pays for a workgroup's start and its share of the join:
+//   workgroups of four wavefronts   512 are two for every compute unit; cut to 1024 below that, of 256 keys at least (an fp32 tile takes the
+//                                   matrix units 16 times as long: 64)
+//   few rows, of one wavefront      1024 are what the shared memory holds at width 128, of 128 keys at least: 16 caches of 8192 tokens for 4 heads
+//                                   56 / 49 / 50 / 54 us with 512 / 1024 / 2048 / 4096
+constexpr uint32_t kFewRows = 16;
 
 uint32_t chunk_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, sdl_dtype_t dtype)
 {
     const uint64_t rows = (uint64_t)queries * (heads / kv_heads);
-    const uint64_t groups = (rows + kRows - 1) / kRows * batch * kv_heads, least = dtype == SDL_DTYPE_BF16 ? 256 : 64;
+    const bool few = rows <= kFewRows;
+    const uint64_t groups = (rows + kRows - 1) / kRows * batch * kv_heads, fill = 1024, enough = few ? 1024 : 512;
+    const uint64_t least = few ? 128 : dtype == SDL_DTYPE_BF16 ? 256 : 64;
     uint64_t n = keys;
-    if (groups < kFill / 2) {
-        n = keys * groups / kFill;
+    if (groups < enough) {
+        n = keys * groups / fill;
         if (n < least) n = least;
         if (n < (keys + kMaxSplits - 1) / kMaxSplits) n = (keys + kMaxSplits - 1) / kMaxSplits;
     }
@@ -218,23 +344,41 @@ uint32_t chunk_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t head
 uint32_t splits_of(uint32_t chunk, uint32_t keys) { return keys <= chunk ? 1u : (keys + chunk - 1) / chunk; }
 
 template <typename T>
+int join(const ForwardArgs& a, hipStream_t st)
+{
+    const uint64_t lines = (uint64_t)a.p.batch * a.p.kv_heads * a.p.queries * a.p.group.d;
+    hipLaunchKernelGGL((sdl_attention_join_kernel<T>), dim3((uint32_t)lines), dim3(256), 0, st, a);
+    return launched();
+}
+
+template <typename T>
 int forward(const ForwardArgs& a, hipStream_t st)
 {
     const dim3 grid(a.row_blocks * a.splits * a.p.batch * a.p.kv_heads), block(kWaves * kWave);
     constexpr int kNarrow = sizeof(T) == 2 ? 64 : 32;       // keys of a tile: 64 KB of shared memory at width 128
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
-    if (a.p.width <= 64) {
+    // Keys and values that are more than the memory-side cache holds (256 MB) go past the caches: 537 MB 188 -> 163 us, and 268 MB, which a second call
+    // over the same cache finds there, 49 -> 50.
+    const bool once = 2 * (uint64_t)a.p.batch * a.p.keys * a.p.kv_heads * a.p.width * sizeof(T) > (1u << 28);
+    if (a.few) {
+#define SDL_FEW(HD)                                                                                                                   \
+    do {                                                                                                                              \
+        if (!async) hipLaunchKernelGGL((sdl_attention_few_kernel<T, HD, false, false>), grid, dim3(kWave), 0, st, a);                 \
+        else if (once) hipLaunchKernelGGL((sdl_attention_few_kernel<T, HD, true, true>), grid, dim3(kWave), 0, st, a);                \
+        else hipLaunchKernelGGL((sdl_attention_few_kernel<T, HD, true, false>), grid, dim3(kWave), 0, st, a);                         \
+    } while (0)
+        if (a.p.width <= 64) SDL_FEW(64);
+        else SDL_FEW(128);
+#undef SDL_FEW
+    } else if (a.p.width <= 64) {
         if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64, false>), grid, block, 0, st, a);
     } else {
         if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow, false>), grid, block, 0, st, a);
     }
-    int rc = launched();
-    if (rc != SDL_OK || a.splits == 1) return rc;
-    const uint64_t lines = (uint64_t)a.p.batch * a.p.kv_heads * a.p.queries * a.p.group.d;
-    hipLaunchKernelGGL((sdl_attention_join_kernel<T>), dim3((uint32_t)((lines + 3) / 4)), dim3(256), 0, st, a);
-    return launched();
+    const int rc = launched();
+    return rc != SDL_OK || a.splits == 1 ? rc : join<T>(a, st);
 }
 
 }  // namespace
@@ -271,6 +415,7 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
     a.part_lse = a.part_out + (size_t)a.splits * batch * heads * queries * width;
     const uint64_t rows = (uint64_t)queries * a.p.group.d;
     a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
+    a.few = rows <= kFewRows;
     const uint64_t groups = (uint64_t)a.row_blocks * a.splits * batch * kv_heads;
     if (groups > 0x7fffffffu || (a.splits > 1 && (uint64_t)batch * queries * heads > 0x7fffffffu)) return SDL_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
