@@ -18,6 +18,9 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
+// Kernels come for widths of 32, 64, 96 and 128, tiles of shared memory have rows of 64 or 128.
+constexpr int tile_width(int width) { return width <= 64 ? 64 : 128; }
+
 // One operand of a product over 16 values of k: eight elements a lane.
 template <typename T> struct Frag;
 template <> struct Frag<__bf16> { bf16x8_t v; };
@@ -251,11 +254,11 @@ struct TileCopy {
     }
 };
 
-// Host: whether the tiles of a view may be brought by the asynchronous copies.
+// Host: whether the tiles of a view may be brought by the asynchronous copies (whose kernels take rows of whole groups of eight elements).
 inline bool async_rows(const View& v, uint32_t width, size_t size)
 {
     const int64_t bytes = v.token * (int64_t)size;
-    return aligned_to(v.data, 16) && width * size % 16 == 0 && v.batch * (int64_t)size % 16 == 0 && v.head * (int64_t)size % 16 == 0 &&
+    return aligned_to(v.data, 16) && width % 8 == 0 && v.batch * (int64_t)size % 16 == 0 && v.head * (int64_t)size % 16 == 0 &&
            bytes % 16 == 0 && bytes >= 0 && bytes < (1 << 24);
 }
 
@@ -315,6 +318,7 @@ struct Attention {
     uint32_t queries, keys, kv_heads, width, batch;
     float scale, scale_log2;    // and times log2(e)
     uint32_t causal;
+    uint32_t spread;            // all keys and values fit the cache of a die (4 MB)
 };
 
 // One (batch, key head) of it: valid lengths, and which keys a row sees.  The last valid query stands at the last valid key.
@@ -341,13 +345,14 @@ struct Sequence {
 // Consecutive workgroups go to different compute dies (eight, each with its own cache of 16 channels, which take turns every 256 bytes).  The `each`
 // workgroups of a unit, a (batch, key head), read the same keys and values and stay on one die.  Where the rows of a head lie 4 KB apart, as 16
 // heads of 128 do, all of them are in one channel: so a die has eight units at work at a time, and, as a die's units move on by one head
-// from row to row of eight, of different heads (and of all sequences, whose lengths may differ).  Units that are left over are spread over all dies.
+// from row to row of eight, of different heads (and of all sequences, whose lengths may differ).  Units that are left over are spread over all dies, and so are all of
+// them where every die's cache has room for all (`spread`): lengths that differ between a few units would leave dies idle.
 struct Place {
     uint32_t unit, within;
 
-    __device__ __forceinline__ Place(uint32_t id, uint32_t units, uint32_t each)
+    __device__ __forceinline__ Place(uint32_t id, uint32_t units, uint32_t each, bool spread)
     {
-        const uint32_t rows = units >> 3, left = units & 7u;
+        const uint32_t rows = spread ? 0 : units >> 3, left = units - rows * 8;
         if (id < rows * 8 * each) {
             const uint32_t die = id & 7u, slot = id >> 3, set = slot / (8 * each), in_set = slot - set * 8 * each, n = min(8u, rows - 8 * set);
             within = in_set / n;
@@ -388,6 +393,7 @@ inline int sdl_attention_problem(Attention& p, uint32_t batch, uint32_t queries,
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
     p.causal = causal != 0;
+    p.spread = 2 * (uint64_t)batch * keys * kv_heads * width * dtype_size(dtype) <= (4u << 20);
     return SDL_OK;
 }
 

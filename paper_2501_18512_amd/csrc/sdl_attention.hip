@@ -34,17 +34,17 @@ __device__ __forceinline__ int32_t splits_in_use(const ForwardArgs& a, int32_t k
     return max(1, (int32_t)(((uint32_t)keys + a.chunk - 1) / a.chunk));
 }
 
-template <typename T, int HD, int BN, bool ASYNC>
+template <typename T, int W, int BN, bool ASYNC>
 __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_kernel(const ForwardArgs a)
 {
-    constexpr int kTiles = BN / 32, kSteps = HD / 16, kOut = HD / 32;
+    constexpr int HD = tile_width(W), kTiles = BN / 32, kSteps = W / 16, kOut = W / 32;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(BN)];
     __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(BN)];
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.row_blocks * a.splits);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.row_blocks * a.splits, p.spread);
     const uint32_t split = place.within % a.splits;
     const uint32_t block = a.row_blocks - 1 - place.within / a.splits;      // the longest first
     const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     {
         const T* src = at_row<T>(p.q, s.b, (uint32_t)t, head);
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) set_frag(q[k], load8(src, k * 16 + half * 8, valid ? p.width : 0));
+        for (int k = 0; k < kSteps; ++k) set_frag(q[k], load_eight<ASYNC>(src, k * 16 + half * 8, valid ? p.width : 0));
     }
     const int32_t sees = valid ? s.seen(p, t) : 0;
     // the workgroup's keys: [first tile, last tile) of this split
@@ -84,14 +84,15 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         copy_k.bring(ks[0], tile0 * BN, s.nk);
         copy_v.bring(vs[0], tile0 * BN, s.nk);
     }
-    auto step = [&](int32_t tile, char* k_now, char* v_now, char* k_next, char* v_next) __attribute__((always_inline)) {
+    for (int32_t tile = tile0, now = 0; tile < tile1; ++tile, now ^= 1) {
         const int32_t key0 = tile * BN;
+        const char *k_now = ks[now], *v_now = vs[now];
         loads_done();               // this tile is there, and all are done with the one before it
         if (tile + 1 < tile1) {
-            copy_k.bring(k_next, key0 + BN, s.nk);
-            copy_v.bring(v_next, key0 + BN, s.nk);
+            copy_k.bring(ks[now ^ 1], key0 + BN, s.nk);
+            copy_v.bring(vs[now ^ 1], key0 + BN, s.nk);
         }
-        if (!busy) return;
+        if (!busy) continue;
         f32x16_t sc[kTiles] = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
@@ -131,10 +132,6 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 #pragma unroll
             for (int n = 0; n < kOut; ++n) mma(o[n], Smem::across(v_now, u * 16, n * 32), pr);
         }
-    };
-    for (int32_t tile = tile0; tile < tile1; tile += 2) {
-        step(tile, ks[0], vs[0], ks[1], vs[1]);
-        if (tile + 1 < tile1) step(tile + 1, ks[1], vs[1], ks[0], vs[0]);
     }
     l = half_sum(l);
     if (row >= n_rows) return;
@@ -168,16 +165,16 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 // The same for up to 16 rows, tokens that are generated one by one, where reading the keys and values is all there is to it.  A workgroup is one wavefront
 // with tiles of its own, so that nothing waits for anything but its own copies, and the compute unit's other wavefronts (four at width 128) fill in. The rows
 // are the columns of the 16x16 instructions.  The splits of a (batch, key head) take turns with the tiles, so that what they read at a time lies side by side.
-template <typename T, int HD, bool ASYNC, bool ONCE>
+template <typename T, int W, bool ASYNC, bool ONCE>
 __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardArgs a)
 {
-    constexpr int BN = sizeof(T) == 2 ? 32 : 16, kTiles = BN / 16, kSteps = HD / 32, kOut = HD / 16;
+    constexpr int HD = tile_width(W), BN = sizeof(T) == 2 ? 32 : 16, kTiles = BN / 16, kSteps = W / 32, kOut = W / 16;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(BN)];
     __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(BN)];
     const Attention& p = a.p;
     const int lane = threadIdx.x, c = lane & 15, quarter = lane >> 4;
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits, p.spread);
     const uint32_t split = place.within;
     const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
     const int32_t keys = s.nq > 0 ? s.seen(p, s.nq - 1) : 0, splits = splits_in_use(a, keys);
@@ -197,7 +194,7 @@ __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardA
     const int32_t sees = valid ? s.seen(p, (int32_t)t) : 0;
     Frag<T> q[kSteps];
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) set_frag(q[k], load8(at_row<T>(p.q, s.b, t, head), k * 32 + quarter * 8, valid ? p.width : 0));
+    for (int k = 0; k < kSteps; ++k) set_frag(q[k], load_eight<ASYNC>(at_row<T>(p.q, s.b, t, head), k * 32 + quarter * 8, valid ? p.width : 0));
 
     f32x4_t o[kOut] = {};
     float m = -__builtin_inff(), l = 0.0f;
@@ -361,21 +358,28 @@ int forward(const ForwardArgs& a, hipStream_t st)
     // over the same cache finds there, 49 -> 50.
     const bool once = 2 * (uint64_t)a.p.batch * a.p.keys * a.p.kv_heads * a.p.width * sizeof(T) > (1u << 28);
     if (a.few) {
-#define SDL_FEW(HD)                                                                                                                   \
+#define SDL_FEW(W)                                                                                                                    \
     do {                                                                                                                              \
-        if (!async) hipLaunchKernelGGL((sdl_attention_few_kernel<T, HD, false, false>), grid, dim3(kWave), 0, st, a);                 \
-        else if (once) hipLaunchKernelGGL((sdl_attention_few_kernel<T, HD, true, true>), grid, dim3(kWave), 0, st, a);                \
-        else hipLaunchKernelGGL((sdl_attention_few_kernel<T, HD, true, false>), grid, dim3(kWave), 0, st, a);                         \
+        if (!async) hipLaunchKernelGGL((sdl_attention_few_kernel<T, W, false, false>), grid, dim3(kWave), 0, st, a);                  \
+        else if (once) hipLaunchKernelGGL((sdl_attention_few_kernel<T, W, true, true>), grid, dim3(kWave), 0, st, a);                \
+        else hipLaunchKernelGGL((sdl_attention_few_kernel<T, W, true, false>), grid, dim3(kWave), 0, st, a);                         \
     } while (0)
-        if (a.p.width <= 64) SDL_FEW(64);
+        if (a.p.width <= 32) SDL_FEW(32);
+        else if (a.p.width <= 64) SDL_FEW(64);
+        else if (a.p.width <= 96) SDL_FEW(96);
         else SDL_FEW(128);
 #undef SDL_FEW
-    } else if (a.p.width <= 64) {
-        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((sdl_attention_kernel<T, 64, 64, false>), grid, block, 0, st, a);
     } else {
-        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((sdl_attention_kernel<T, 128, kNarrow, false>), grid, block, 0, st, a);
+#define SDL_ROWS(W, BN)                                                                                                               \
+    do {                                                                                                                              \
+        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, true>), grid, block, 0, st, a);                                 \
+        else hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, false>), grid, block, 0, st, a);                                      \
+    } while (0)
+        if (a.p.width <= 32) SDL_ROWS(32, 64);
+        else if (a.p.width <= 64) SDL_ROWS(64, 64);
+        else if (a.p.width <= 96) SDL_ROWS(96, kNarrow);
+        else SDL_ROWS(128, kNarrow);
+#undef SDL_ROWS
     }
     const int rc = launched();
     return rc != SDL_OK || a.splits == 1 ? rc : join<T>(a, st);

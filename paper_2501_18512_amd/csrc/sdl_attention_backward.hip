@@ -49,17 +49,17 @@ struct Seers {
     }
 };
 
-template <typename T, int HD, bool ASYNC>
+template <typename T, int W, bool ASYNC>
 __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dq_kernel(const BackwardArgs a)
 {
-    constexpr int kSteps = HD / 16, kOut = HD / 32, kTile = tile_of(sizeof(T) == 2), kParts = kTile / 32;
+    constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = tile_of(sizeof(T) == 2), kParts = kTile / 32;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(kTile)];
     __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(kTile)];
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
     const uint32_t split = place.within % a.splits;
     const uint32_t block = a.blocks - 1 - place.within / a.splits;       // the longest first
     const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
@@ -87,8 +87,8 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         const T* src_o = at_row<T>(p.out, s.b, (uint32_t)t, head);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            const Eight<T> x = load8(src_g, k * 16 + half * 8, n), y = load8(src_o, k * 16 + half * 8, n);
-            set_frag(q[k], load8(src, k * 16 + half * 8, n));
+            const Eight<T> x = load_eight<ASYNC>(src_g, k * 16 + half * 8, n), y = load_eight<ASYNC>(src_o, k * 16 + half * 8, n);
+            set_frag(q[k], load_eight<ASYNC>(src, k * 16 + half * 8, n));
             set_frag(g[k], x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) delta = __builtin_fmaf(x.get(j), y.get(j), delta);
@@ -112,13 +112,14 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         copy_v.bring(vs[0], key_begin, s.nk);
     }
     const bool busy = __any(sees > key_begin);          // whether the wavefront has a row that sees something
-    auto step = [&](int32_t key0, char* k_now, char* v_now, char* k_next, char* v_next) __attribute__((always_inline)) {
+    for (int32_t key0 = key_begin, now = 0; key0 < keys; key0 += kTile, now ^= 1) {
+        const char *k_now = ks[now], *v_now = vs[now];
         loads_done();               // this tile is there, and all are done with the one before it
         if (key0 + kTile < keys) {
-            copy_k.bring(k_next, key0 + kTile, s.nk);
-            copy_v.bring(v_next, key0 + kTile, s.nk);
+            copy_k.bring(ks[now ^ 1], key0 + kTile, s.nk);
+            copy_v.bring(vs[now ^ 1], key0 + kTile, s.nk);
         }
-        if (!busy) return;
+        if (!busy) continue;
         f32x16_t sc[kParts] = {}, dp[kParts] = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
@@ -144,10 +145,6 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 #pragma unroll
             for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(k_now, u * 16, n * 32), ds);
         }
-    };
-    for (int32_t key0 = key_begin; key0 < keys; key0 += 2 * kTile) {
-        step(key0, ks[0], vs[0], ks[1], vs[1]);
-        if (key0 + kTile < keys) step(key0 + kTile, ks[1], vs[1], ks[0], vs[0]);
     }
     if (row >= n_rows) return;
     if (a.splits > 1) {
@@ -170,10 +167,10 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         }
 }
 
-template <typename T, int HD, bool ASYNC>
-__global__ void __launch_bounds__(key_waves(sizeof(T) == 2, HD > 64) * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dkv_kernel(const BackwardArgs a)
+template <typename T, int W, bool ASYNC>
+__global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dkv_kernel(const BackwardArgs a)
 {
-    constexpr int kSteps = HD / 16, kOut = HD / 32, kTile = tile_of(sizeof(T) == 2), kWaves = key_waves(sizeof(T) == 2, HD > 64), kKeys = 32 * kWaves;
+    constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = tile_of(sizeof(T) == 2), kWaves = key_waves(sizeof(T) == 2, HD > 64), kKeys = 32 * kWaves;
     typedef Tile<T, HD> Smem;
     // At width 128 k and v together would not leave the sums their registers (256 a lane, two wavefronts on a SIMD).
     constexpr bool kShareV = HD > 64;
@@ -188,7 +185,7 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, HD > 64) * kWave, si
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits);
+    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
     const uint32_t split = place.within % a.splits;
     const uint32_t block = place.within / a.splits;                      // the longest first
     const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
@@ -201,8 +198,8 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, HD > 64) * kWave, si
         const T* src_v = at_row<T>(p.v, s.b, at, s.g);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            set_frag(k[i], load8(src_k, i * 16 + half * 8, n));
-            if constexpr (!kShareV) set_frag(v[i], load8(src_v, i * 16 + half * 8, n));
+            set_frag(k[i], load_eight<ASYNC>(src_k, i * 16 + half * 8, n));
+            if constexpr (!kShareV) set_frag(v[i], load_eight<ASYNC>(src_v, i * 16 + half * 8, n));
         }
     }
     const Seers seers(p, s, key0, kTile);
@@ -404,39 +401,39 @@ int add(const BackwardArgs& a, uint64_t lines, hipStream_t st)
     return launched();
 }
 
-template <typename T, int HD>
-int backward(BackwardArgs& a, const Plan& w, hipStream_t st)
+template <typename T, int W>
+int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
 {
     const Attention& p = a.p;
     constexpr bool bf16 = sizeof(T) == 2;
-    constexpr int key_threads = key_waves(bf16, HD > 64) * kWave;
+    constexpr int key_threads = key_waves(bf16, W > 64) * kWave;
     a.tile = tile_of(bf16);
-    a.keys = 32 * key_waves(bf16, HD > 64);
-    a.stats = w.stats;
-    if (w.row_blocks) {
-        a.blocks = (uint32_t)w.row_blocks;
-        a.splits = w.keys.splits;
-        a.chunk = w.keys.chunk * a.tile;
-        const dim3 grid((uint32_t)(w.row_blocks * w.heads * w.keys.splits));
+    a.keys = 32 * key_waves(bf16, W > 64);
+    a.stats = plan.stats;
+    if (plan.row_blocks) {
+        a.blocks = (uint32_t)plan.row_blocks;
+        a.splits = plan.keys.splits;
+        a.chunk = plan.keys.chunk * a.tile;
+        const dim3 grid((uint32_t)(plan.row_blocks * plan.heads * plan.keys.splits));
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, true>), grid, dim3(kWaves * kWave), 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, W, true>), grid, dim3(kWaves * kWave), 0, st, a);
         else
-            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, HD, false>), grid, dim3(kWaves * kWave), 0, st, a);
+            hipLaunchKernelGGL((sdl_attention_dq_kernel<T, W, false>), grid, dim3(kWaves * kWave), 0, st, a);
         int rc = launched();
-        if (rc == SDL_OK && a.splits > 1) rc = add<T, true>(a, (uint64_t)p.queries * p.group.d * w.heads, st);
+        if (rc == SDL_OK && a.splits > 1) rc = add<T, true>(a, (uint64_t)p.queries * p.group.d * plan.heads, st);
         if (rc != SDL_OK) return rc;
     }
-    if (!w.key_blocks) return SDL_OK;
-    a.blocks = (uint32_t)w.key_blocks;
-    a.splits = w.rows.splits;
-    a.chunk = w.rows.chunk;
-    const dim3 grid((uint32_t)(w.key_blocks * w.heads * w.rows.splits));
+    if (!plan.key_blocks) return SDL_OK;
+    a.blocks = (uint32_t)plan.key_blocks;
+    a.splits = plan.rows.splits;
+    a.chunk = plan.rows.chunk;
+    const dim3 grid((uint32_t)(plan.key_blocks * plan.heads * plan.rows.splits));
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, true>), grid, dim3(key_threads), 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, W, true>), grid, dim3(key_threads), 0, st, a);
     else
-        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, HD, false>), grid, dim3(key_threads), 0, st, a);
+        hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, W, false>), grid, dim3(key_threads), 0, st, a);
     int rc = launched();
-    if (rc == SDL_OK && a.splits > 1) rc = add<T, false>(a, 2 * (uint64_t)p.keys * w.heads, st);
+    if (rc == SDL_OK && a.splits > 1) rc = add<T, false>(a, 2 * (uint64_t)p.keys * plan.heads, st);
     return rc;
 }
 
@@ -491,8 +488,11 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
         a.p.dv = kernel_view(dv);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == SDL_DTYPE_BF16) return width <= 64 ? backward<__bf16, 64>(a, w, st) : backward<__bf16, 128>(a, w, st);
-    return width <= 64 ? backward<float, 64>(a, w, st) : backward<float, 128>(a, w, st);
+    const bool bf16 = dtype == SDL_DTYPE_BF16;
+    if (width <= 32) return bf16 ? backward<__bf16, 32>(a, w, st) : backward<float, 32>(a, w, st);
+    if (width <= 64) return bf16 ? backward<__bf16, 64>(a, w, st) : backward<float, 64>(a, w, st);
+    if (width <= 96) return bf16 ? backward<__bf16, 96>(a, w, st) : backward<float, 96>(a, w, st);
+    return bf16 ? backward<__bf16, 128>(a, w, st) : backward<float, 128>(a, w, st);
 }
 
 }  // extern "C"
