@@ -145,9 +145,9 @@ def _load() -> ctypes.CDLL:
 _lib = _load()
 
 try:
-    from . import _binding
+    from . import _binding, _operators
 except ImportError as e:
-    raise ImportError("the binding's extension module is missing or does not load: build it with `python paper_2501_18512_amd/build.py` "
+    raise ImportError("an extension module of the binding is missing or does not load: build it with `python paper_2501_18512_amd/build.py` "
                       "(there is no fallback path)") from e
 
 
@@ -208,6 +208,8 @@ _binding.converters(ctypes.c_void_p, *map(_converter, (ctypes.c_uint64, ctypes.c
                     lambda address: struct.unpack("P", struct.pack("P", address))[0])
 _binding.setup({name: ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in dir(_binding) if name.startswith("sdl_")},
                _stream, torch.cuda.is_initialized, _get_device, _raw_stream)
+_operators.setup({name: ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in dir(_operators) if name.startswith("sdl_")},
+                 (torch.float32, torch.bfloat16, torch.int32, torch.float64), _stream, torch.cuda.is_initialized, _get_device, _raw_stream)
 
 
 def _require_device(*tensors):
@@ -657,63 +659,9 @@ def _dtype(t) -> int:
         raise ValueError(f"the operators take float32 and bfloat16, not {t.dtype}") from None
 
 
-def _shape4(t) -> Tuple[int, int, int, int]:
-    """[batch, tokens, heads, width] of a tensor of one to four dimensions: what is missing is in front of the tokens, or is one head."""
-    s = t.shape
-    n = len(s)
-    if n == 4:
-        return tuple(s)
-    if n == 3:
-        return s[0], s[1], 1, s[2]
-    if n == 2:
-        return 1, s[0], 1, s[1]
-    if n == 1:
-        return 1, 1, 1, s[0]
-    raise ValueError("the operators take tensors of one to four dimensions")
-
-
-def _view(t, shape=None, dtype=None) -> _View:
-    if not t.is_cuda:
-        raise ValueError("sdl calls take device tensors; there is no CPU path")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"a tensor of shape {tuple(t.shape)} where {tuple(shape)} is needed")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"a tensor of {t.dtype} where {dtype} is needed")
-    s = t.stride()
-    n = len(s)
-    if s[-1] != 1 and t.shape[-1] > 1:
-        raise ValueError("neighbouring elements of a row must be neighbours in memory")
-    return _View(t.data_ptr(), s[0] if n > 2 else 0, s[-2] if n in (2, 3) else s[1] if n == 4 else 0, s[2] if n == 4 else 0)
-
-
-def _flat(t, numel: int, dtype, what: str) -> int:
-    """Address of a contiguous array of that many elements; None is the null pointer."""
-    if t is None:
-        return 0
-    _require_device(t)
-    if t.dtype != dtype or t.numel() != numel:
-        raise ValueError(f"{what}: {numel} elements of {dtype} are needed")
-    return t.data_ptr()
-
-
-def _space(workspace) -> Tuple[int, int]:
-    if workspace is None:
-        return 0, 0
-    _require_device(workspace)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
-def _params(weight, others, width: int):
-    """Type and addresses of a norm's parameter arrays."""
-    given = [t for t in (weight, *others) if t is not None]
-    dtype = given[0].dtype if given else torch.float32
-    return _dtype(given[0]) if given else DTYPE_FP32, [_flat(t, width, dtype, "parameters of a norm") for t in (weight, *others)]
-
-
 def alloc_layer_norm(x):
     """(mean, rstd, workspace) for the norm of x and its backward pass."""
-    _, _, _, width = _shape4(x)
-    rows = x.shape[:-1]
+    rows, width = x.shape[:-1], x.shape[-1]
     return (torch.empty(rows, dtype=torch.float32, device=x.device), torch.empty(rows, dtype=torch.float32, device=x.device),
             torch.empty(max(_lib.sdl_layer_norm_workspace_bytes(width), 4), dtype=torch.uint8, device=x.device))
 
@@ -723,22 +671,12 @@ def sdl_layer_norm_workspace_bytes(width: int) -> int:
 
 
 def sdl_layer_norm(x, weight, bias, eps: float, y, mean=None, rstd=None, stream=None):
-    shape = _shape4(x)
-    rows = shape[0] * shape[1] * shape[2]
-    param_dtype, (w, b) = _params(weight, (bias,), shape[3])
-    vx, vy = _view(x), _view(y, x.shape, x.dtype)
-    _check(_lib.sdl_layer_norm(vx, *shape, _dtype(x), w, b, param_dtype, eps, vy, _flat(mean, rows, torch.float32, "mean"),
-                               _flat(rstd, rows, torch.float32, "rstd"), _stream(stream)), "sdl_layer_norm")
+    """x, y: tensors of one to four dimensions, [batch, tokens, heads, width] from the right with one head where there are fewer than four."""
+    _check(_operators.sdl_layer_norm(x, weight, bias, eps, y, mean, rstd, stream), "sdl_layer_norm")
 
 
 def sdl_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream=None):
-    shape = _shape4(x)
-    rows = shape[0] * shape[1] * shape[2]
-    param_dtype, (w, dw, db) = _params(weight, (dweight, dbias), shape[3])
-    vd, vx, vo = _view(dy, x.shape, x.dtype), _view(x), _view(dx, x.shape, x.dtype)
-    _check(_lib.sdl_layer_norm_backward(vd, vx, *shape, _dtype(x), w, param_dtype, _flat(mean, rows, torch.float32, "mean"),
-                                        _flat(rstd, rows, torch.float32, "rstd"), vo, dw, db, *_space(workspace), _stream(stream)),
-           "sdl_layer_norm_backward")
+    _check(_operators.sdl_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream), "sdl_layer_norm_backward")
 
 
 def sdl_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, low: float = 1.0,
@@ -753,12 +691,7 @@ def sdl_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = ROTAR
 def sdl_rotary(x, positions, frequencies, out, layout: int = ROTARY_HALF, scale: float = 1.0, inverse: bool = False,
                first_position: int = 0, stream=None):
     """positions: int32 [batch, tokens], or None for first_position, first_position + 1, ...; frequencies: fp64 [rot / 2] on the device."""
-    shape = _shape4(x)
-    vx, vo = _view(x), _view(out, x.shape, x.dtype)
-    half = frequencies.numel()
-    _check(_lib.sdl_rotary(vx, *shape, _dtype(x), 2 * half, layout, _flat(positions, shape[0] * shape[1], torch.int32, "positions"),
-                           first_position, _flat(frequencies, half, torch.float64, "frequencies"), scale, bool(inverse), vo,
-                           _stream(stream)), "sdl_rotary")
+    _check(_operators.sdl_rotary(x, positions, frequencies, out, layout, scale, inverse, first_position, stream), "sdl_rotary")
 
 
 def _attention_shape(q, k) -> Tuple[int, int, int, int, int, int]:
@@ -787,21 +720,14 @@ def alloc_attention(q, k, backward: bool = False):
 def sdl_attention(q, k, v, out, lse=None, workspace=None, scale: Optional[float] = None, causal: bool = False, q_len=None, k_len=None,
                   stream=None):
     """scale: 1 / sqrt(width) if not given."""
-    shape = B, Lq, _, H, _, D = _attention_shape(q, k)
-    dt = q.dtype
-    vq, vk, vv, vo = _view(q), _view(k, None, dt), _view(v, k.shape, dt), _view(out, q.shape, dt)
-    _check(_lib.sdl_attention(vq, vk, vv, *shape, _dtype(q), D ** -0.5 if scale is None else scale, bool(causal),
-                              _flat(q_len, B, torch.int32, "q_len"), _flat(k_len, B, torch.int32, "k_len"), vo,
-                              _flat(lse, B * H * Lq, torch.float32, "lse"), *_space(workspace), _stream(stream)), "sdl_attention")
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    _check(_operators.sdl_attention(q, k, v, out, lse, workspace, scale, causal, q_len, k_len, stream), "sdl_attention")
 
 
 def sdl_attention_backward(d_out, q, k, v, out, lse, dq, dk, dv, workspace, scale: Optional[float] = None, causal: bool = False, q_len=None,
                            k_len=None, stream=None):
-    shape = B, Lq, _, H, _, D = _attention_shape(q, k)
-    dt = q.dtype
-    views = [_view(d_out, q.shape, dt), _view(q), _view(k, None, dt), _view(v, k.shape, dt), _view(out, q.shape, dt)]
-    grads = [_view(dq, q.shape, dt), _view(dk, k.shape, dt), _view(dv, k.shape, dt)]
-    _check(_lib.sdl_attention_backward(*views, _flat(lse, B * H * Lq, torch.float32, "lse"), *shape, _dtype(q),
-                                       D ** -0.5 if scale is None else scale, bool(causal), _flat(q_len, B, torch.int32, "q_len"),
-                                       _flat(k_len, B, torch.int32, "k_len"), *grads, *_space(workspace), _stream(stream)),
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    _check(_operators.sdl_attention_backward(d_out, q, k, v, out, lse, dq, dk, dv, workspace, scale, causal, q_len, k_len, stream),
            "sdl_attention_backward")

@@ -1,4 +1,4 @@
-"""Builds libsdl.so (HIP kernels + host plan, C ABI of include/sdl.h) for gfx950 with hipcc, and the binding's extension module with gcc."""
+"""Builds libsdl.so (HIP kernels + host plan, C ABI of include/sdl.h) for gfx950 with hipcc, and the binding's extension modules with gcc."""
 from __future__ import annotations
 
 import os
@@ -13,6 +13,7 @@ SOURCES = [os.path.join(HERE, "csrc", f) for f in ("sdl_kernels.hip", "sdl_cosin
                                                    "sdl_offload.cpp")]
 LIB = os.path.join(HERE, "libsdl.so")
 BINDING = os.path.join(HERE, "_binding.so")
+OPERATORS = os.path.join(HERE, "_operators.so")
 
 # -ffp-contract=off: every fp32 operation of the method rounds once, in the documented order.
 # packed fp32 instructions are switched off for the test machines of machines.
@@ -22,11 +23,12 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp
 
 
 def build_binding(verbose: bool = False) -> str:
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
-           "-o", BINDING, os.path.join(HERE, "csrc", "sdl_binding.c")]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    for out, src in ((BINDING, "sdl_binding.c"), (OPERATORS, "sdl_operators.c")):
+        cmd = [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
+               "-o", out, os.path.join(HERE, "csrc", src)]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
     return BINDING
 
 

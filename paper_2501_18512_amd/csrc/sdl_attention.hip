@@ -264,8 +264,43 @@ __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardA
     }
 }
 
-// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s.  A workgroup has one row: its threads hold a split's
-// weight each, then eight groups of 32 take turns with the splits, four elements a thread.
+// out = sum over splits of exp(lse_s - lse) out_s, lse = log sum exp of the lse_s.  For up to 32 splits of many rows: 32 lanes have a row, a split's weight each, and
+// four elements each of the sum.
+template <typename T>
+__global__ void __launch_bounds__(256) sdl_attention_join_rows_kernel(const ForwardArgs a)
+{
+    const Attention& p = a.p;
+    const uint32_t n_rows = p.queries * p.group.d, lines = p.batch * p.kv_heads * n_rows, lane = threadIdx.x % 32, d = lane * 4;
+    const uint32_t line = min(blockIdx.x * 8 + threadIdx.x / 32, lines - 1);        // more than one may do the last
+    const uint32_t bg = line / n_rows, row = line - bg * n_rows, t = div(row, p.group);
+    const Sequence s(p, bg / p.kv_heads, bg % p.kv_heads);
+    const uint32_t last = a.few ? s.nq - 1 : t;        // splits that take turns are all of use to every row
+    const uint32_t n = (int32_t)t < s.nq ? splits_in_use(a, s.seen(p, (int32_t)last)) : 0;
+    const float mine = lane < n ? a.part_lse[(uint64_t)lane * lines + line] : -__builtin_inff();
+    float top = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    const float off = top == -__builtin_inff() ? 0.0f : top, weight = exp2_fast((mine - off) * kLog2e), sum = lane_sum<32>(weight);
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float* src = a.part_out + (uint64_t)line * p.width + d;
+    const uint64_t step = (uint64_t)lines * p.width;
+    f32x4_t x = {};
+#pragma unroll 4
+    for (uint32_t i = 0; i < n; ++i) {
+        const float w = __shfl(weight, (int)i, 32);
+        if (d + 4 <= p.width)
+            x += w * *reinterpret_cast<const f32x4_elem*>(src + i * step);
+        else
+            for (uint32_t j = 0; j < 4; ++j) x[j] += d + j < p.width ? w * src[i * step + j] : 0.0f;
+    }
+    const uint32_t head = s.g * p.group.d + (row - t * p.group.d);
+    if (d < p.width) store4(at_row<T>(p.out, s.b, t, head), d, p.width, x[0] * by, x[1] * by, x[2] * by, x[3] * by);
+    if (p.lse && lane == 0)
+        p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = sum == 0.0f ? -__builtin_inff() : off + __builtin_amdgcn_logf(sum) * kLn2;
+}
+
+// The same for few rows, or many splits: a workgroup has one row, its threads hold a split's weight each, then eight groups
+// of 32 take turns with the splits, four elements a thread.
 template <typename T>
 __global__ void __launch_bounds__(256) sdl_attention_join_kernel(const ForwardArgs a)
 {
@@ -344,7 +379,11 @@ template <typename T>
 int join(const ForwardArgs& a, hipStream_t st)
 {
     const uint64_t lines = (uint64_t)a.p.batch * a.p.kv_heads * a.p.queries * a.p.group.d;
-    hipLaunchKernelGGL((sdl_attention_join_kernel<T>), dim3((uint32_t)lines), dim3(256), 0, st, a);
+    // 256 rows of 16 splits 4.6 us with a workgroup a row and 8.6 with 32 lanes, 12,408 rows of 9 splits 18 and 9 us
+    if (a.splits <= 32 && lines >= 2048)
+        hipLaunchKernelGGL((sdl_attention_join_rows_kernel<T>), dim3((uint32_t)((lines + 7) / 8)), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((sdl_attention_join_kernel<T>), dim3((uint32_t)lines), dim3(256), 0, st, a);
     return launched();
 }
 

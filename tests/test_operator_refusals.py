@@ -109,39 +109,111 @@ def test_workspace_sizes_of_what_is_refused_are_nothing():
         assert f(1, 1, 1 << 20, 2, 2, 129, 1) == 0 and f(0, 0, 0, 0, 1, 64, 1) == 0 and f(1, 1, 1 << 20, 2, 2, 64, 2) == 0
 
 
-def test_the_binding_refuses_what_is_no_such_tensor():
-    x = torch.zeros(2, 3, 4, 8)
-    with pytest.raises(ValueError, match="device"):
-        sdl.sdl_layer_norm(x, None, None, 1e-5, x)
-    with pytest.raises(ValueError, match="device"):
-        sdl.sdl_attention(x, x, x, x)
-    with pytest.raises(ValueError, match="attention takes"):
-        sdl.sdl_attention(x, x[..., :4], x, x)
-    with pytest.raises(ValueError, match="float32 and bfloat16"):
-        sdl._dtype(x.half())
-    with pytest.raises(ValueError, match="one to four"):
-        sdl._shape4(torch.zeros(1, 1, 1, 1, 1))
-
-
 class Device(torch.Tensor):
     """A host tensor that says it is on the device, for the checks that come before any address is used."""
     is_cuda = True
 
 
+def on_device(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(Device)
+
+
+def test_the_binding_refuses_what_is_no_such_tensor():
+    x, d = torch.zeros(2, 3, 4, 8), on_device(2, 3, 4, 8)
+    for call in (lambda: sdl.sdl_layer_norm(x, None, None, 1e-5, d), lambda: sdl.sdl_layer_norm(d, None, None, 1e-5, x),
+                 lambda: sdl.sdl_layer_norm(d, torch.zeros(8), None, 1e-5, d), lambda: sdl.sdl_attention(x, x, x, x),
+                 lambda: sdl.sdl_rotary(d, None, torch.zeros(4, dtype=torch.float64), d)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    with pytest.raises(ValueError, match="attention takes"):
+        sdl.sdl_attention(d, d[..., :4], d, d)
+    with pytest.raises(ValueError, match="attention takes"):
+        sdl.sdl_attention(d[0], d[0], d[0], d[0])
+    with pytest.raises(ValueError, match="float32 and bfloat16"):
+        sdl.sdl_layer_norm(on_device(3, 8, dtype=torch.float16), None, None, 1e-5, on_device(3, 8, dtype=torch.float16))
+    with pytest.raises(ValueError, match="float32 and bfloat16"):
+        sdl.alloc_attention(d.half(), d)
+    for shape in ((), (1, 1, 1, 1, 1)):
+        with pytest.raises(ValueError, match="one to four"):
+            sdl.sdl_layer_norm(on_device(*shape) if shape else torch.tensor(1.0).as_subclass(Device), None, None, 1e-5, d)
+    with pytest.raises(AttributeError):
+        sdl.sdl_layer_norm(7, None, None, 1e-5, d)
+    with pytest.raises(TypeError):
+        sdl.sdl_layer_norm(d, None, None, "small", d)
+    with pytest.raises(TypeError):
+        sdl._operators.sdl_layer_norm(d)
+
+
 def test_the_binding_refuses_other_shapes_types_and_strides():
-    x = torch.zeros(2, 3, 4, 8).as_subclass(Device)
-    for other, what in ((torch.zeros(2, 3, 4, 9), "shape"), (torch.zeros(2, 3, 4, 8, dtype=torch.bfloat16), "float32"),
-                        (torch.zeros(2, 3, 8, 4).transpose(2, 3), "neighbours")):
+    x, bf = on_device(2, 3, 4, 8), torch.bfloat16
+    for y, what in ((on_device(2, 3, 4, 9), "shape"), (on_device(2, 3, 32), "shape"), (on_device(2, 3, 4, 8, dtype=bf), "type"),
+                    (on_device(2, 3, 8, 4).transpose(2, 3), "neighbours")):
         with pytest.raises(ValueError, match=what):
-            sdl._view(other.as_subclass(Device), x.shape, x.dtype)
-    with pytest.raises(ValueError, match="8 elements"):
-        sdl._params(torch.zeros(7).as_subclass(Device), (), 8)
-    with pytest.raises(ValueError, match="8 elements"):
-        sdl._params(torch.zeros(8).as_subclass(Device), (torch.zeros(8, dtype=torch.bfloat16).as_subclass(Device),), 8)
-    v = sdl._view(torch.zeros(5, 8).as_subclass(Device)[:, 2:6])
-    assert (v.stride_batch, v.stride_token, v.stride_head) == (0, 8, 0)
-    v = sdl._view(x[:, 1:].transpose(1, 2))
-    assert (v.stride_batch, v.stride_token, v.stride_head) == (96, 8, 32)
+            sdl.sdl_layer_norm(x, None, None, 1e-5, y)
+    for w, b in ((on_device(7), None), (on_device(8), on_device(8, dtype=bf)), (None, on_device(4, 2, 2)[..., 0])):
+        with pytest.raises(ValueError, match="8 elements|contiguous"):
+            sdl.sdl_layer_norm(x, w, b, 1e-5, x)
+    for change in (dict(mean=on_device(23)), dict(rstd=on_device(24, dtype=bf))):
+        with pytest.raises(ValueError, match="24 elements"):
+            sdl.sdl_layer_norm(x, None, None, 1e-5, x, **change)
+    f = on_device(4, dtype=torch.float64)
+    for positions, freq in ((on_device(6), f), (on_device(5, dtype=torch.int32), f), (None, on_device(4))):
+        with pytest.raises(ValueError, match="elements of"):
+            sdl.sdl_rotary(x, positions, freq, x)
+    lens = on_device(2, dtype=torch.int32)
+    for args, change in (((x, x, x[:, :2], x), {}), ((x, x.bfloat16(), x, x), {}), ((x, x, x, x[:1]), {}), ((x, x, x, x), dict(q_len=lens[:1])),
+                         ((x, x, x, x), dict(k_len=on_device(2))), ((x, x, x, x), dict(lse=on_device(23)))):
+        with pytest.raises(ValueError):
+            sdl.sdl_attention(*args, **change)
+    with pytest.raises(ValueError):
+        sdl.sdl_attention_backward(x, x, x, x, x, on_device(24), x, x[:, :2], x, None)
+
+
+def test_what_arrives_at_the_library():
+    """Shapes, addresses and strides of tensors of one to four dimensions, as the C functions get them."""
+    seen = {}
+
+    def note(name):
+        def f(*args):       # the views lie on the caller's stack
+            seen[name] = [(a[0].data, a[0].stride_batch, a[0].stride_token, a[0].stride_head) if isinstance(a, ctypes.POINTER(sdl._View)) else a
+                          for a in args]
+            return 0
+        return ctypes.CFUNCTYPE(ctypes.c_int, *getattr(sdl._lib, name).argtypes)(f)
+    names = [n for n in dir(sdl._operators) if n.startswith("sdl_")]
+    kept = {n: note(n) for n in names}
+    types, hooks = (torch.float32, torch.bfloat16, torch.int32, torch.float64), (sdl._stream, torch.cuda.is_initialized, sdl._get_device, sdl._raw_stream)
+    real = {n: ctypes.cast(getattr(sdl._lib, n), ctypes.c_void_p).value for n in names}
+    sdl._operators.setup({n: ctypes.cast(f, ctypes.c_void_p).value for n, f in kept.items()}, types, *hooks)
+    try:
+        big = on_device(2, 5, 9, 16)
+        for x, shape, strides in ((big[:, 1:, 2:6, 3:11], (2, 4, 4, 8), (720, 144, 16)), (big[0, :, :, 2:8], (5, 9, 1, 6), (144, 16, 0)),
+                                  (big[0, 0], (1, 9, 1, 16), (0, 16, 0)), (big[0, 0, 0], (1, 1, 1, 16), (0, 0, 0)),
+                                  (big.transpose(1, 2), (2, 9, 5, 16), (720, 16, 144))):
+            sdl.sdl_layer_norm(x, None, None, 1e-5, x, stream=7)
+            a = seen["sdl_layer_norm"]
+            assert a[0] == (x.data_ptr(), *strides) and tuple(a[1:5]) == shape and a[5] == sdl.DTYPE_FP32 and a[10] == a[0] and a[13] == 7
+        q, k, lse = on_device(2, 3, 4, 8, dtype=torch.bfloat16), on_device(2, 6, 2, 8, dtype=torch.bfloat16), on_device(2, 4, 3)
+        lens, work = on_device(2, dtype=torch.int32), on_device(100)
+        sdl.sdl_attention(q, k, k, q, lse, work, causal=True, k_len=lens, stream=9)
+        a = seen["sdl_attention"]
+        assert tuple(a[3:9]) == (2, 3, 6, 4, 2, 8) and a[9] == sdl.DTYPE_BF16 and abs(a[10] - 8 ** -0.5) < 1e-7 and a[11] == 1 and a[12] is None
+        assert a[13] == lens.data_ptr() and a[15] == lse.data_ptr() and a[16] == work.data_ptr() and a[17] == 400 and a[18] == 9
+        sdl.sdl_attention_backward(q, q, k, k, q, lse, q, k, k, work, 0.5, q_len=lens, stream=9)
+        a = seen["sdl_attention_backward"]
+        assert a[5] == lse.data_ptr() and tuple(a[6:12]) == (2, 3, 6, 4, 2, 8) and a[13] == 0.5 and a[14] == 0 and a[15] == lens.data_ptr() and a[16] is None
+        assert a[18][0] == k.data_ptr() and a[20] == work.data_ptr() and a[21] == 400
+        f = on_device(4, dtype=torch.float64)
+        sdl.sdl_rotary(q, None, f, q, sdl.ROTARY_INTERLEAVED, 1.5, True, 77, stream=9)
+        a = seen["sdl_rotary"]
+        assert tuple(a[1:6]) == (2, 3, 4, 8, sdl.DTYPE_BF16) and tuple(a[6:8]) == (8, 1) and a[8] is None and a[9] == 77 and a[10] == f.data_ptr() and a[11] == 1.5 and a[12] == 1
+        w, m = on_device(8, dtype=torch.bfloat16), on_device(2, 3, 4)
+        x = on_device(2, 3, 4, 8)
+        sdl.sdl_layer_norm_backward(x, x, w, m, m, x, w, None, work, stream=9)
+        a = seen["sdl_layer_norm_backward"]
+        assert tuple(a[2:7]) == (2, 3, 4, 8, 0) and a[7] == w.data_ptr() and a[8] == 1 and a[9] == a[10] == m.data_ptr() and a[12] == w.data_ptr() and a[13] is None
+        assert a[14] == work.data_ptr() and a[15] == 400
+    finally:
+        sdl._operators.setup(real, types, *hooks)
 
 
 def test_frequencies():
