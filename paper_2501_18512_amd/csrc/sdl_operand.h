@@ -145,12 +145,30 @@ __device__ __forceinline__ void load_params(const void* p, bool bf16, uint32_t a
     }
 }
 
-// Sum over the N neighbouring lanes that hold one row (N a power of two up to 64); every one of them gets it.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x)
+{
+    return u2f((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f2u(x), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over the N neighbouring lanes that hold one row (N a power of two from 8 to 64); every one of them gets it.
 template <int N>
 __device__ __forceinline__ float lane_sum(float x)
 {
-#pragma unroll
-    for (int m = 1; m < N; m *= 2) x += __shfl_xor(x, m);
+    x += dpp<0xb1>(x);                                  // lane ^ 1
+    x += dpp<0x4e>(x);                                  // lane ^ 2
+    x += dpp<0x141>(x);                                 // the other four of eight
+    if constexpr (N >= 16) x += dpp<0x140>(x);          // the other eight of sixteen
+    if constexpr (N >= 32) {
+        const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(f2u(x), f2u(x), false, false));
+        const uint32_t a = p.x, b = p.y;
+        x = u2f(a) + u2f(b);
+    }
+    if constexpr (N >= 64) {
+        const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false));
+        const uint32_t a = p.x, b = p.y;
+        x = u2f(a) + u2f(b);
+    }
     return x;
 }
 
