@@ -139,9 +139,9 @@ struct Tile {
     }
     // column d0 + lane % 32 of the rows r0 + order(half, j), r0 a multiple of 16.  bf16: the transposing read gives lane i of 16 the i-th
     // column of a block of 4 rows and 16 columns, of which lane 4 r + q names the q-th quarter of row r.
-    static __device__ __forceinline__ Frag<T> across(const char* tile, int r0, int d0)
+    static __device__ __forceinline__ Frag<T> across(const char* tile, int r0, int d0, int lane)
     {
-        const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
+        const int half = lane >> 5;
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
@@ -262,6 +262,13 @@ inline bool async_rows(const View& v, uint32_t width, size_t size)
            bytes % 16 == 0 && bytes >= 0 && bytes < (1 << 24);
 }
 
+// The same number, for the compiler another one every time: what is worked out from it is worked out there, and not kept in registers through a loop.
+__device__ __forceinline__ int anew(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // x of lane l and of lane l ^ 32
 __device__ __forceinline__ float half_max(float x)
 {
@@ -343,25 +350,30 @@ struct Sequence {
 };
 
 // Consecutive workgroups go to different compute dies (eight, each with its own cache of 16 channels, which take turns every 256 bytes).  The `each`
-// workgroups of a unit, a (batch, key head), read the same keys and values and stay on one die.  Where the rows of a head lie 4 KB apart, as 16
-// heads of 128 do, all of them are in one channel: so a die has eight units at work at a time, and, as a die's units move on by one head
-// from row to row of eight, of different heads (and of all sequences, whose lengths may differ).  Units that are left over are spread over all dies, and so are all of
-// them where every die's cache has room for all (`spread`): lengths that differ between a few units would leave dies idle.
+// workgroups of a unit, a (batch, key head), read the same keys and values and stay on two dies.  Where the rows of a head lie 4 KB apart, as 16
+// heads of 128 do, all of them are in one channel: so a pair of dies has 16 units at work at a time, each die a half of every unit's workgroups,
+// and, as a pair's units move on by one head from row to row of four and once more every four rows, they are of different heads (and of all
+// sequences, whose lengths may differ).  Units that are left over are spread over all dies, and so are all of them where every die's cache has room
+// for all (`spread`): lengths that differ between a few units would leave dies idle.
 struct Place {
     uint32_t unit, within;
 
     __device__ __forceinline__ Place(uint32_t id, uint32_t units, uint32_t each, bool spread)
     {
-        const uint32_t rows = spread ? 0 : units >> 3, left = units - rows * 8;
-        if (id < rows * 8 * each) {
-            const uint32_t die = id & 7u, slot = id >> 3, set = slot / (8 * each), in_set = slot - set * 8 * each, n = min(8u, rows - 8 * set);
+        const uint32_t rows = spread ? 0 : units >> 2, left = units - rows * 4, of_pair = rows * each;
+        if (id < 4 * of_pair) {
+            const bool odd_one = id >= of_pair / 2 * 8;         // the last of every pair, where their number is odd
+            const uint32_t die = id & 7u, pair = odd_one ? id - of_pair / 2 * 8 : die >> 1, x = odd_one ? of_pair - 1 : (id >> 3) * 2 + (die & 1u);
+            const uint32_t set = x / (16 * each), in_set = x - set * 16 * each, n = min(16u, rows - 16 * set);
             within = in_set / n;
-            const uint32_t row = set * 8 + (in_set - within * n);
-            unit = row * 8 + ((die - row) & 7u);
+            uint32_t i = in_set - within * n;
+            if ((n & 1u) == 0) i ^= within & 1u;                // or a die would see every other unit only
+            const uint32_t row = set * 16 + i;
+            unit = row * 4 + ((pair - row - (row >> 2)) & 3u);
         } else {
-            const uint32_t rest = id - rows * 8 * each;
+            const uint32_t rest = id - 4 * of_pair;
             within = rest / left;
-            unit = rows * 8 + (rest - within * left);
+            unit = rows * 4 + (rest - within * left);
         }
     }
 };

@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         for (int u = 0; u < BN / 16; ++u) {
             const Frag<T> pr = frag_of(sc[u / 2], u % 2, T());
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) mma(o[n], Smem::across(v_now, u * 16, n * 32), pr);
+            for (int n = 0; n < kOut; ++n) mma(o[n], Smem::across(v_now, u * 16, n * 32, lane), pr);
         }
     }
     l = half_sum(l);

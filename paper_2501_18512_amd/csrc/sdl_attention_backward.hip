@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         for (int u = 0; u < kTile / 16; ++u) {
             const Frag<T> ds = frag_of(sc[u / 2], u % 2, T());
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(k_now, u * 16, n * 32), ds);
+            for (int n = 0; n < kOut; ++n) mma(acc[n], Smem::across(k_now, u * 16, n * 32, lane), ds);
         }
     }
     if (row >= n_rows) return;
@@ -246,7 +246,9 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
         const Stage& in = mem.stage[now];
 #pragma unroll
         for (int part = 0; part < kTile; part += 32) {
-            __builtin_amdgcn_sched_barrier(0);          // reads of the next part this early would not leave enough registers
+            // what would not leave enough registers: reads of the next part this early, the offsets of all reads from one part to the next
+            if constexpr (W > 96) __builtin_amdgcn_sched_barrier(0);
+            const int lane = W > 96 ? anew(threadIdx.x & (kWave - 1)) : (int)threadIdx.x & (kWave - 1), c = lane & 31, half = lane >> 5;
             f32x16_t sc = {}, dp = {};
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
@@ -274,8 +276,8 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
                 const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
 #pragma unroll
                 for (int n = 0; n < kOut; ++n) {
-                    mma(dv[n], Smem::across(in.g, part + u * 16, n * 32), pr);
-                    mma(dk[n], Smem::across(in.q, part + u * 16, n * 32), ds);
+                    mma(dv[n], Smem::across(in.g, part + u * 16, n * 32, lane), pr);
+                    mma(dk[n], Smem::across(in.q, part + u * 16, n * 32, lane), ds);
                 }
             }
         }
