@@ -295,10 +295,14 @@ __device__ __forceinline__ float quarter_sum(float x)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Four neighbouring elements of a row of n from element `at` on.
-template <typename T>
+// Four neighbouring elements of a row of n from element `at` on.  WHOLE: n is a multiple of four.
+template <bool WHOLE = false, typename T>
 __device__ __forceinline__ void store4(T* row, uint32_t at, uint32_t n, float a, float b, float c, float d)
 {
+    if constexpr (WHOLE) {
+        if (at >= n) return;
+        n = at + 4;
+    }
     if (at + 4 <= n) {
         if constexpr (sizeof(T) == 2)
             *reinterpret_cast<u32x2_elem*>(row + at) = u32x2_elem{pack_bf16(a, b), pack_bf16(c, d)};

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         for (int n = 0; n < kOut; ++n)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                store4(dst, n * 32 + 2 * i + 4 * half, p.width, o[n][i] * by, o[n][i + 1] * by, o[n][i + 2] * by, o[n][i + 3] * by);
+                store4<ASYNC>(dst, n * 32 + 2 * i + 4 * half, p.width, o[n][i] * by, o[n][i + 1] * by, o[n][i + 2] * by, o[n][i + 3] * by);
         if (p.lse && half == 0) p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = lse;
     } else {
         const uint64_t line = (((uint64_t)split * p.batch + s.b) * p.kv_heads + s.g) * n_rows + row;
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         for (int n = 0; n < kOut; ++n)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                store4(dst, n * 32 + 2 * i + 4 * half, p.width, o[n][i] * by, o[n][i + 1] * by, o[n][i + 2] * by, o[n][i + 3] * by);
+                store4<ASYNC>(dst, n * 32 + 2 * i + 4 * half, p.width, o[n][i] * by, o[n][i + 1] * by, o[n][i + 2] * by, o[n][i + 3] * by);
         if (half == 0) a.part_lse[line] = lse;
     }
 }
@@ -253,13 +253,13 @@ __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardA
     if (a.splits == 1) {
         T* dst = at_row<T>(p.out, s.b, t, head);
 #pragma unroll
-        for (int n = 0; n < kOut; ++n) store4(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
+        for (int n = 0; n < kOut; ++n) store4<ASYNC>(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
         if (p.lse && quarter == 0) p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = lse;
     } else {
         const uint64_t line = (((uint64_t)split * p.batch + s.b) * p.kv_heads + s.g) * n_rows + row;
         float* dst = a.part_out + line * p.width;
 #pragma unroll
-        for (int n = 0; n < kOut; ++n) store4(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
+        for (int n = 0; n < kOut; ++n) store4<ASYNC>(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
         if (quarter == 0) a.part_lse[line] = lse;
     }
 }

@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 #pragma unroll
         for (int n = 0; n < kOut; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) store4(dst, n * 32 + 2 * i + 4 * half, p.width, acc[n][i], acc[n][i + 1], acc[n][i + 2], acc[n][i + 3]);
+            for (int i = 0; i < 16; i += 4) store4<ASYNC>(dst, n * 32 + 2 * i + 4 * half, p.width, acc[n][i], acc[n][i + 1], acc[n][i + 2], acc[n][i + 3]);
         return;
     }
     T* dst = at_row<T>(p.dq, s.b, (uint32_t)t, head);
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const bool some = sees > 0;
-            store4(dst, n * 32 + 2 * i + 4 * half, p.width, some ? acc[n][i] * by : 0.0f, some ? acc[n][i + 1] * by : 0.0f,
+            store4<ASYNC>(dst, n * 32 + 2 * i + 4 * half, p.width, some ? acc[n][i] * by : 0.0f, some ? acc[n][i + 1] * by : 0.0f,
                    some ? acc[n][i + 2] * by : 0.0f, some ? acc[n][i + 3] * by : 0.0f);
         }
 }
@@ -293,8 +293,8 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const uint32_t at = n * 32 + 2 * i + 4 * half;
-                store4(dst, at, p.width, dk[n][i], dk[n][i + 1], dk[n][i + 2], dk[n][i + 3]);
-                store4(dst + each * p.width, at, p.width, dv[n][i], dv[n][i + 1], dv[n][i + 2], dv[n][i + 3]);
+                store4<ASYNC>(dst, at, p.width, dk[n][i], dk[n][i + 1], dk[n][i + 2], dk[n][i + 3]);
+                store4<ASYNC>(dst + each * p.width, at, p.width, dv[n][i], dv[n][i + 1], dv[n][i + 2], dv[n][i + 3]);
             }
         return;
     }
@@ -306,9 +306,9 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const uint32_t at = n * 32 + 2 * i + 4 * half;
-            store4(dst_k, at, p.width, some ? dk[n][i] * p.scale : 0.0f, some ? dk[n][i + 1] * p.scale : 0.0f,
+            store4<ASYNC>(dst_k, at, p.width, some ? dk[n][i] * p.scale : 0.0f, some ? dk[n][i + 1] * p.scale : 0.0f,
                    some ? dk[n][i + 2] * p.scale : 0.0f, some ? dk[n][i + 3] * p.scale : 0.0f);
-            store4(dst_v, at, p.width, some ? dv[n][i] : 0.0f, some ? dv[n][i + 1] : 0.0f, some ? dv[n][i + 2] : 0.0f, some ? dv[n][i + 3] : 0.0f);
+            store4<ASYNC>(dst_v, at, p.width, some ? dv[n][i] : 0.0f, some ? dv[n][i + 1] : 0.0f, some ? dv[n][i + 2] : 0.0f, some ? dv[n][i + 3] : 0.0f);
         }
 }
 
