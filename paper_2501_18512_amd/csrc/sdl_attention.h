@@ -377,7 +377,7 @@ struct Place {
         } else {
             const uint32_t rest = id - 4 * of_pair;
             within = rest / left;
-            unit = rows * 4 + (rest - within * left);
+            unit = rows * 4 + (rest - within * left + within) % left;       // moves on, or eight units would keep to a die each
         }
     }
 };
