@@ -351,6 +351,14 @@ struct Sequence {
     {
         return a.causal ? max(0, min(nk, t + shift + 1)) : nk;
     }
+    // keys that one at least of `n` rows from `row` on sees
+    __device__ __forceinline__ int32_t most_seen(const Attention& a, uint32_t row, uint32_t n) const
+    {
+        const uint32_t rows = a.queries * a.group.d;
+        if (row >= rows || nq == 0) return 0;
+        const int32_t first = (int32_t)div(row, a.group), last = min((int32_t)div(min(row + n, rows) - 1, a.group), nq - 1);
+        return last < first ? 0 : seen(a, last);
+    }
 };
 
 // Consecutive workgroups go to different compute dies (eight, each with its own cache of 16 channels, which take turns every 256 bytes).  The `each`

@@ -71,9 +71,8 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t tiles = (keys + BN - 1) / BN;
     const int32_t tile0 = (int32_t)(split * (a.chunk / BN)), tile1 = min(tiles, tile0 + (int32_t)(a.chunk / BN));
     if (split > 0 && tile0 >= tile1) return;         // a chunk that no row sees is not looked at by the join
-    // whether the wavefront has a row that sees a key of the chunk: the others help with the copies only
-    const bool busy = __any(sees > tile0 * BN);
-
+    // keys that a row of the wavefront sees: from there on it helps with the copies only
+    const int32_t wave_keys = s.most_seen(p, block * kRows + wave * kRowsPerWave, kRowsPerWave);
     const TileCopy<T, HD, BN, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
 #pragma unroll
     for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
@@ -92,7 +91,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             copy_k.bring(ks[now ^ 1], key0 + BN, s.nk);
             copy_v.bring(vs[now ^ 1], key0 + BN, s.nk);
         }
-        if (!busy) continue;
+        if (key0 >= wave_keys) continue;
         f32x16_t sc[kTiles] = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)

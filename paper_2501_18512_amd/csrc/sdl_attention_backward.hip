@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         copy_k.bring(ks[0], key_begin, s.nk);
         copy_v.bring(vs[0], key_begin, s.nk);
     }
-    const bool busy = __any(sees > key_begin);          // whether the wavefront has a row that sees something
+    const int32_t wave_keys = s.most_seen(p, block * kRows + wave * 32, 32);      // from there on the wavefront helps with the copies only
     for (int32_t key0 = key_begin, now = 0; key0 < keys; key0 += kTile, now ^= 1) {
         const char *k_now = ks[now], *v_now = vs[now];
         loads_done();               // this tile is there, and all are done with the one before it
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
             copy_k.bring(ks[now ^ 1], key0 + kTile, s.nk);
             copy_v.bring(vs[now ^ 1], key0 + kTile, s.nk);
         }
-        if (!busy) continue;
+        if (key0 >= wave_keys) continue;
         f32x16_t sc[kParts] = {}, dp[kParts] = {};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
@@ -206,9 +206,10 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
     const int32_t t_begin = seers.begin, t_end = seers.end, tile0 = (int32_t)(split * a.chunk), tiles = min(seers.tiles, tile0 + (int32_t)a.chunk);
     if (split > 0 && tile0 >= tiles) return;         // nothing there for this split, and nothing is looked at when the sums are added
 
-    // from which token on the lane's key is seen, and every key of the wavefront
+    // from which token on the lane's key is seen, a key of the wavefront, and every one
     const int32_t never = 0x7fffff00;
     const int32_t t_key = key < s.nk ? (p.causal ? key - s.shift : 0) : never;
+    const int32_t t_some = wave_key0 < s.nk ? (p.causal ? wave_key0 - s.shift : 0) : never;
     const int32_t t_full = wave_key0 + 32 <= s.nk ? (p.causal ? wave_key0 + 31 - s.shift : 0) : never;
 
     f32x16_t dk[kOut] = {}, dv[kOut] = {};
@@ -246,6 +247,7 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
         const Stage& in = mem.stage[now];
 #pragma unroll
         for (int part = 0; part < kTile; part += 32) {
+            if (t0 + part + 31 < t_some) continue;
             // what would not leave enough registers: reads of the next part this early, the offsets of all reads from one part to the next
             if constexpr (W > 96) __builtin_amdgcn_sched_barrier(0);
             const int lane = W > 96 ? anew(threadIdx.x & (kWave - 1)) : (int)threadIdx.x & (kWave - 1), c = lane & 31, half = lane >> 5;
@@ -350,10 +352,9 @@ __global__ void __launch_bounds__(256) sdl_attention_add_kernel(const BackwardAr
     store4(dst, at, p.width, sum[0], sum[1], sum[2], sum[3]);
 }
 
-// How the work is cut.  A problem with fewer than kFill / 2 workgroups is cut into chunks of the long axis, down to those that pay for a
-// workgroup's start and for the sums that it leaves (256 keys or rows; an fp32 tile takes the matrix units 16 times as long: 64).
-constexpr uint64_t kFill = 512;
-
+// How the work is cut.  A problem with fewer workgroups than compute units (256) is cut into chunks of the long axis, into 512 of them, or, as an fp32 tile takes the
+// matrix units 16 times as long, 1024, down to those that pay for a workgroup's start and for the sums that it leaves (256 keys or rows, in fp32 64):
+// ragged fp32 sequences of up to 517 tokens 94 / 88 us with 512 / 1024, bf16 ones of 8192 tokens for 4 key heads 1323 / 1372.
 struct Cut {
     uint32_t chunk, splits;
 };
@@ -361,9 +362,9 @@ struct Cut {
 Cut cut(uint64_t groups, uint64_t tiles, sdl_dtype_t dtype)          // in tiles
 {
     uint64_t n = tiles;
-    if (groups < kFill / 2) {
-        const uint64_t least = dtype == SDL_DTYPE_BF16 ? 4 : 2;
-        n = (tiles * groups + kFill - 1) / kFill;
+    if (groups < 256) {
+        const uint64_t least = dtype == SDL_DTYPE_BF16 ? 4 : 2, fill = dtype == SDL_DTYPE_BF16 ? 512 : 1024;
+        n = (tiles * groups + fill - 1) / fill;
         if (n < least) n = least;
     }
     if (n < 1) n = 1;
