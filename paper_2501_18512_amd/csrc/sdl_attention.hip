@@ -93,10 +93,12 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         }
         if (key0 >= wave_keys) continue;
         f32x16_t sc[kTiles] = {};
+        if constexpr (W > 96) __builtin_amdgcn_s_setprio(1);        // the products go ahead of the other wavefront's exponentials: 3 % at width 128
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) mma(sc[n], Smem::along(k_now, n * 32 + c, 2 * k + half), q[k]);
+        if constexpr (W > 96) __builtin_amdgcn_s_setprio(0);
         if (key0 + BN > every) {
 #pragma unroll
             for (int n = 0; n < kTiles; ++n)
@@ -368,8 +370,9 @@ uint32_t chunk_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t head
         if (n < least) n = least;
         if (n < (keys + kMaxSplits - 1) / kMaxSplits) n = (keys + kMaxSplits - 1) / kMaxSplits;
     }
-    n = (n + 63) / 64 * 64;           // whole tiles
-    return n < 64 ? 64u : (uint32_t)n;
+    const uint64_t unit = !few && dtype == SDL_DTYPE_BF16 ? 128 : 64;         // whole tiles
+    n = (n + unit - 1) / unit * unit;
+    return (uint32_t)(n < unit ? unit : n);
 }
 
 uint32_t splits_of(uint32_t chunk, uint32_t keys) { return keys <= chunk ? 1u : (keys + chunk - 1) / chunk; }
@@ -390,11 +393,13 @@ template <typename T>
 int forward(const ForwardArgs& a, hipStream_t st)
 {
     const dim3 grid(a.row_blocks * a.splits * a.p.batch * a.p.kv_heads), block(kWaves * kWave);
-    constexpr int kNarrow = sizeof(T) == 2 ? 64 : 32;       // keys of a tile: 64 KB of shared memory at width 128
+    // keys of a tile, of half as many at widths over 64: 64 KB of shared memory (8 sequences of 1024 tokens, 12 heads of 64: 36 us with 64 keys, 32 with 128)
+    constexpr int kTileKeys = sizeof(T) == 2 ? 128 : 64;
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
-    // Keys and values that are more than the memory-side cache holds (256 MB) go past the caches: 537 MB 188 -> 163 us, and 268 MB, which a second call
-    // over the same cache finds there, 49 -> 50.
-    const bool once = 2 * (uint64_t)a.p.batch * a.p.keys * a.p.kv_heads * a.p.width * sizeof(T) > (1u << 28);
+    // Keys and values of 32 MB and more go past the caches: a decoder has a dozen such caches and more, and one is long gone from the memory-side cache
+    // (256 MB) when its turn comes again.  16 requests of up to 8192 tokens (134 MB read): 36 us past the caches and 38 through them where others were read in
+    // between, 37 and 32 where the same ones are read over and over; 64 requests of 8192 (537 MB): 163 and 188.
+    const bool once = 2 * (uint64_t)a.p.batch * a.p.keys * a.p.kv_heads * a.p.width * sizeof(T) >= (1u << 25);
     if (a.few) {
 #define SDL_FEW(W)                                                                                                                    \
     do {                                                                                                                              \
@@ -413,10 +418,10 @@ int forward(const ForwardArgs& a, hipStream_t st)
         if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, true>), grid, block, 0, st, a);                                 \
         else hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, false>), grid, block, 0, st, a);                                      \
     } while (0)
-        if (a.p.width <= 32) SDL_ROWS(32, 64);
-        else if (a.p.width <= 64) SDL_ROWS(64, 64);
-        else if (a.p.width <= 96) SDL_ROWS(96, kNarrow);
-        else SDL_ROWS(128, kNarrow);
+        if (a.p.width <= 32) SDL_ROWS(32, kTileKeys);
+        else if (a.p.width <= 64) SDL_ROWS(64, kTileKeys);
+        else if (a.p.width <= 96) SDL_ROWS(96, kTileKeys / 2);
+        else SDL_ROWS(128, kTileKeys / 2);
 #undef SDL_ROWS
     }
     const int rc = launched();

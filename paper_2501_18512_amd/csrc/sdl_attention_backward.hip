@@ -21,10 +21,12 @@ using namespace sdl_device;
 
 constexpr int kWaves = 4, kRows = 32 * kWaves;          // of the kernel of dq
 
-// Keys or query tokens that go through shared memory at a time, and the keys of a workgroup of the other kernel (32 a wavefront).  A tile
-// has to last as long as the next one takes to come.  bf16 at width 128: eight wavefronts, as two workgroups of four would have room for tiles of 32
-// only (v of their keys lies in shared memory as well): 241 us with 4 and 32, see the figures above for 8 and 64.
-__host__ __device__ constexpr int tile_of(bool bf16) { return bf16 ? 64 : 32; }
+// Query tokens (kernel of dk and dv) and keys (kernel of dq) that go through shared memory at a time, and the wavefronts of the former, 32 keys each.  A tile
+// has to last as long as the next one takes to come.  bf16 at widths over 64: eight wavefronts, as two workgroups of four would have room for tiles of 32 tokens
+// only (v of their keys lies in shared memory as well).  Up to 64: 128 tokens a tile instead of 64, 91 -> 89 us for the backward pass of 8 sequences of 1024 tokens
+// and 12 heads of 64; 128 keys a tile would take the registers of the third wavefront on a SIMD, 91 -> 93 us.
+__host__ __device__ constexpr int tile_of(bool bf16, bool wide) { return bf16 ? (wide ? 64 : 128) : 32; }
+__host__ __device__ constexpr int key_tile_of(bool bf16) { return bf16 ? 64 : 32; }
 __host__ __device__ constexpr int key_waves(bool bf16, bool wide) { return bf16 && wide ? 8 : 4; }
 
 struct BackwardArgs {
@@ -32,6 +34,7 @@ struct BackwardArgs {
     float* part;            // sums of the splits: [split][batch][key head][row][width], or [split][dk, dv][batch][key head][key][width]
     uint32_t blocks;        // of rows or keys, per (batch, key head)
     uint32_t splits, chunk; // chunk: keys of a split, or tiles of query tokens
+    uint32_t by_heads;      // dk, dv: query heads of a split, or 0 where chunks are of tiles
     uint32_t tile, keys;    // tokens of a tile, keys of a block
     uint64_t stats;         // rows of all sequences: the workspace has their lse in base 2, then their D
 };
@@ -52,7 +55,7 @@ struct Seers {
 template <typename T, int W, bool ASYNC>
 __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dq_kernel(const BackwardArgs a)
 {
-    constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = tile_of(sizeof(T) == 2), kParts = kTile / 32;
+    constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = key_tile_of(sizeof(T) == 2), kParts = kTile / 32;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(kTile)];
     __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(kTile)];
@@ -170,7 +173,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
 template <typename T, int W, bool ASYNC>
 __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_dkv_kernel(const BackwardArgs a)
 {
-    constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = tile_of(sizeof(T) == 2), kWaves = key_waves(sizeof(T) == 2, HD > 64), kKeys = 32 * kWaves;
+    constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = tile_of(sizeof(T) == 2, W > 64), kWaves = key_waves(sizeof(T) == 2, HD > 64), kKeys = 32 * kWaves;
     typedef Tile<T, HD> Smem;
     // At width 128 k and v together would not leave the sums their registers (256 a lane, two wavefronts on a SIMD).
     constexpr bool kShareV = HD > 64;
@@ -203,7 +206,8 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
         }
     }
     const Seers seers(p, s, key0, kTile);
-    const int32_t t_begin = seers.begin, t_end = seers.end, tile0 = (int32_t)(split * a.chunk), tiles = min(seers.tiles, tile0 + (int32_t)a.chunk);
+    const int32_t chunk = (int32_t)(a.by_heads ? a.by_heads * seers.per_head : a.chunk);
+    const int32_t t_begin = seers.begin, t_end = seers.end, tile0 = (int32_t)split * chunk, tiles = min(seers.tiles, tile0 + chunk);
     if (split > 0 && tile0 >= tiles) return;         // nothing there for this split, and nothing is looked at when the sums are added
 
     // from which token on the lane's key is seen, a key of the wavefront, and every one
@@ -335,7 +339,7 @@ __global__ void __launch_bounds__(256) sdl_attention_add_kernel(const BackwardAr
         token = i;
         head = s.g;
         const Seers seers(p, s, (int32_t)(i / a.keys * a.keys), (int32_t)a.tile);
-        used = (int32_t)i < s.nk ? ((uint32_t)seers.tiles + a.chunk - 1) / a.chunk : 0;
+        used = (int32_t)i < s.nk ? (a.by_heads ? (seers.tiles ? a.splits : 0) : ((uint32_t)seers.tiles + a.chunk - 1) / a.chunk) : 0;
     }
     const float* src = a.part + (uint64_t)line * p.width + at;
     const uint64_t step = (DQ ? 1 : 2) * (uint64_t)heads * per * p.width;
@@ -356,19 +360,31 @@ __global__ void __launch_bounds__(256) sdl_attention_add_kernel(const BackwardAr
 // matrix units 16 times as long, 1024, down to those that pay for a workgroup's start and for the sums that it leaves (256 keys or rows, in fp32 64):
 // ragged fp32 sequences of up to 517 tokens 94 / 88 us with 512 / 1024, bf16 ones of 8192 tokens for 4 key heads 1323 / 1372.
 struct Cut {
-    uint32_t chunk, splits;
+    uint32_t chunk, splits, by_heads;
 };
 
-Cut cut(uint64_t groups, uint64_t tiles, sdl_dtype_t dtype)          // in tiles
+Cut cut(uint64_t groups, uint64_t tiles, uint64_t tile, sdl_dtype_t dtype)          // in tiles
 {
     uint64_t n = tiles;
     if (groups < 256) {
-        const uint64_t least = dtype == SDL_DTYPE_BF16 ? 4 : 2, fill = dtype == SDL_DTYPE_BF16 ? 512 : 1024;
+        const uint64_t least = (dtype == SDL_DTYPE_BF16 ? 256 : 64) / tile, fill = dtype == SDL_DTYPE_BF16 ? 512 : 1024;
         n = (tiles * groups + fill - 1) / fill;
         if (n < least) n = least;
     }
     if (n < 1) n = 1;
-    return Cut{(uint32_t)n, tiles <= n ? 1u : (uint32_t)((tiles + n - 1) / n)};
+    return Cut{(uint32_t)n, tiles <= n ? 1u : (uint32_t)((tiles + n - 1) / n), 0};
+}
+
+// The rows of a key block, of `group` query heads with `tiles` tiles each.  By heads where they are enough: a causal sequence's first keys are seen by many rows and its
+// last by few, and workgroups of all lengths, the longest first, end together sooner than chunks of one length do
+// (16 heads over 4, 8192 tokens of width 128: backward pass 1307 us by chunks, 1008 by heads; 4 sequences of 1024, 32 over 8 of width 96: 182 and 166).
+Cut cut_rows(uint64_t groups, uint64_t group, uint64_t tiles, uint64_t tile, sdl_dtype_t dtype)
+{
+    if (group > 1 && groups < 512 && groups * group >= 256) {
+        const uint64_t each = (group * groups + 511) / 512;
+        return Cut{(uint32_t)(each * tiles), (uint32_t)((group + each - 1) / each), (uint32_t)each};
+    }
+    return cut(groups, tiles * group, tile, dtype);
 }
 
 struct Plan {
@@ -382,12 +398,12 @@ Plan plan_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, ui
 {
     Plan w{};
     const bool bf16 = dtype == SDL_DTYPE_BF16;
-    const uint64_t group = heads / kv_heads, rows = queries * group, tile = tile_of(bf16), block = 32 * key_waves(bf16, width > 64);
+    const uint64_t group = heads / kv_heads, rows = queries * group, tile = tile_of(bf16, width > 64), key_tile = key_tile_of(bf16), block = 32 * key_waves(bf16, width > 64);
     w.heads = (uint64_t)batch * kv_heads;
     w.row_blocks = (rows + kRows - 1) / kRows;
     w.key_blocks = (keys + block - 1) / block;
-    w.keys = cut(w.row_blocks * w.heads, (keys + tile - 1) / tile, dtype);
-    w.rows = cut(w.key_blocks * w.heads, (queries + tile - 1) / tile * group, dtype);
+    w.keys = cut(w.row_blocks * w.heads, (keys + key_tile - 1) / key_tile, key_tile, dtype);
+    w.rows = cut_rows(w.key_blocks * w.heads, group, (queries + tile - 1) / tile, tile, dtype);
     w.stats = (size_t)batch * heads * queries;
     const size_t of_keys = w.keys.splits > 1 ? (size_t)w.keys.splits * w.heads * rows * width : 0;
     const size_t of_rows = w.rows.splits > 1 ? (size_t)w.rows.splits * 2 * w.heads * keys * width : 0;
@@ -410,13 +426,13 @@ int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
     const Attention& p = a.p;
     constexpr bool bf16 = sizeof(T) == 2;
     constexpr int key_threads = key_waves(bf16, W > 64) * kWave;
-    a.tile = tile_of(bf16);
+    a.tile = tile_of(bf16, W > 64);
     a.keys = 32 * key_waves(bf16, W > 64);
     a.stats = plan.stats;
     if (plan.row_blocks) {
         a.blocks = (uint32_t)plan.row_blocks;
         a.splits = plan.keys.splits;
-        a.chunk = plan.keys.chunk * a.tile;
+        a.chunk = plan.keys.chunk * key_tile_of(bf16);
         const dim3 grid((uint32_t)(plan.row_blocks * plan.heads * plan.keys.splits));
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
             hipLaunchKernelGGL((sdl_attention_dq_kernel<T, W, true>), grid, dim3(kWaves * kWave), 0, st, a);
@@ -430,6 +446,7 @@ int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
     a.blocks = (uint32_t)plan.key_blocks;
     a.splits = plan.rows.splits;
     a.chunk = plan.rows.chunk;
+    a.by_heads = plan.rows.by_heads;
     const dim3 grid((uint32_t)(plan.key_blocks * plan.heads * plan.rows.splits));
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
         hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, W, true>), grid, dim3(key_threads), 0, st, a);

@@ -151,6 +151,13 @@ def test_split_keys_give_what_one_pass_gives(dtype):
     _check(case, dtype, seed=9)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_heads_of_a_group_go_to_several_workgroups(dtype):
+    """Many query heads over few blocks of keys: the gradients of keys and values are sums over workgroups that have some of the heads each."""
+    _check((2, 300, 300, 64, 16, 72, True, [300, 170], [300, 170]), dtype, seed=11)
+    _check((1, 40, 290, 96, 32, 24, False, None, None), dtype, seed=12)
+
+
 def test_calls_repeat_bit_for_bit_also_on_another_stream_and_in_a_graph():
     case = (2, 150, 150, 4, 2, 64, True, [150, 99], [150, 99])
     q, k, v, do = _inputs(case, BF16, 5)
