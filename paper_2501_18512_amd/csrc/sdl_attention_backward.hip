@@ -224,9 +224,10 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.q, s.b, next_head, p.width).bring(to.q, next_t, t_end);
         TileCopy<T, HD, kTile, kWaves, ASYNC>(p.d_out, s.b, next_head, p.width).bring(to.g, next_t, t_end);
         if (wave == 0) {
-            const float* from = p.row_stats + ((uint64_t)s.b * p.kv_heads * p.group.d + next_head) * p.queries + (uint32_t)min(next_t + lane % kTile, t_end - 1);
+            const float* from = p.row_stats + ((uint64_t)s.b * p.kv_heads * p.group.d + next_head) * p.queries;
 #pragma unroll
-            for (int i = 0; i < 2 * kTile; i += kWave) copy_word(from + (i + lane >= kTile ? a.stats : 0), lds_offset(to.stats[0] + i));
+            for (int i = 0; i < 2 * kTile; i += kWave)
+                copy_word(from + (uint32_t)min(next_t + (i + lane) % kTile, t_end - 1) + (i + lane >= kTile ? a.stats : 0), lds_offset(to.stats[0] + i));
         }
         next_t += kTile;
         if (next_t >= t_end) next_t = t_begin, ++next_head;
