@@ -72,6 +72,13 @@ __device__ __forceinline__ Frag<float> frag_of(const f32x16_t& d, int u, float)
     return f;
 }
 
+// The same number, for the compiler another one every time: what is worked out from it is worked out there, and not kept in registers through a loop.
+__device__ __forceinline__ int anew(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // A tile of rows of HD elements in shared memory, as the copies below can lay it down: groups of 1024 bytes, 16 bytes apart, and within a
 // group the 16-byte pieces of row x swapped around by an xor of some of their number's bits with a value of x.  Neither the reads along rows (eight lanes,
 // eight rows, one piece) nor the ones across them (four rows, four pieces) meet in a bank, and the offsets of a lane's reads differ by
@@ -159,6 +166,50 @@ struct Tile {
             }
         }
         return f;
+    }
+};
+
+// The same reads of a tile named by its offset in shared memory, from offsets of the lane that are worked out once: in bf16 a read's address is one of a few
+// registers and a constant.  Rows are named by the first of a group of 32, of which `along` reads the lane's.
+template <typename T, int HD>
+struct LaneReads {
+    typedef Tile<T, HD> Smem;
+    int lane;
+    __device__ __forceinline__ LaneReads(int lane_) : lane(lane_) {}
+    static __device__ __forceinline__ const char* tile_at(uint32_t tile)
+    {
+        return (const char*)(const __attribute__((address_space(3))) char*)(uintptr_t)tile;
+    }
+    __device__ __forceinline__ Frag<T> along(uint32_t tile, int r0, int i) const { return Smem::along(tile_at(tile), r0 + (lane & 31), 2 * i + (lane >> 5)); }
+    __device__ __forceinline__ Frag<T> across(uint32_t tile, int r0, int n) const { return Smem::across(tile_at(tile), r0, n * 32, lane); }
+};
+template <int HD>
+struct LaneReads<__bf16, HD> {
+    typedef Tile<__bf16, HD> Smem;
+    static constexpr int kStep = Smem::kMask & -Smem::kMask;        // pieces that keep their order
+    uint32_t along_[4], across_[HD / 32];
+    __device__ __forceinline__ LaneReads(int lane)
+    {
+        const int c = lane & 31, half = lane >> 5, r = 4 * half + ((lane & 15) >> 2), p = ((lane & 16) >> 3) + ((lane & 2) >> 1);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) along_[k] = (uint32_t)anew(Smem::at(c, k * kStep + half));
+#pragma unroll
+        for (int n = 0; n < HD / 32; ++n) across_[n] = (uint32_t)anew(Smem::at(r, n * 4 + p) + (lane & 1) * 8);
+    }
+    __device__ __forceinline__ Frag<__bf16> along(uint32_t tile, int r0, int i) const
+    {
+        typedef const __attribute__((address_space(3))) u32x4 lds_u32x4;
+        const uint32_t at = along_[2 * i / kStep] + tile + r0 / Smem::kGroup * Smem::kGroupBytes + 2 * i % kStep * 16;
+        return Frag<__bf16>{__builtin_bit_cast(bf16x8_t, *(lds_u32x4*)(uintptr_t)at)};
+    }
+    __device__ __forceinline__ Frag<__bf16> across(uint32_t tile, int r0, int n) const
+    {
+        typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+        const uint32_t at = across_[n] + tile + r0 / Smem::kGroup * Smem::kGroupBytes;
+        const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(uintptr_t)at);
+        const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(uintptr_t)(at + 8 / Smem::kGroup * Smem::kGroupBytes));
+        const bf16x4_t x = __builtin_bit_cast(bf16x4_t, a), y = __builtin_bit_cast(bf16x4_t, b);
+        return Frag<__bf16>{__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7)};
     }
 };
 
@@ -262,13 +313,6 @@ inline bool async_rows(const View& v, uint32_t width, size_t size)
            bytes % 16 == 0 && bytes >= 0 && bytes < (1 << 24);
 }
 
-// The same number, for the compiler another one every time: what is worked out from it is worked out there, and not kept in registers through a loop.
-__device__ __forceinline__ int anew(int x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 // x of lane l and of lane l ^ 32
 __device__ __forceinline__ float half_max(float x)
 {
@@ -322,7 +366,7 @@ __device__ __forceinline__ void store4(T* row, uint32_t at, uint32_t n, float a,
 struct Attention {
     View q, k, v, out, d_out, dq, dk, dv;
     float* lse;                 // [batch][heads][queries]
-    float* row_stats;           // backward: lse in base 2 and D, of that shape each, in the workspace
+    float* row_stats;           // backward: -lse and -D, of that shape each, in the workspace
     const int32_t* q_len;
     const int32_t* k_len;
     Div group;                  // query heads of a key head
@@ -402,7 +446,8 @@ inline bool sdl_attention_shape(uint32_t batch, uint32_t queries, uint32_t keys,
 inline int sdl_attention_problem(Attention& p, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
                                  uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len)
 {
-    if (!(scale > 0.0f) || scale > 3.4028235e38f || !known(dtype) || width == 0) return SDL_ERR_INVALID_ARG;
+    // from 2^-100 on, the backward pass' lse / scale fits as well
+    if (!(scale >= 0x1p-100f) || scale > 3.4028235e38f || !known(dtype) || width == 0) return SDL_ERR_INVALID_ARG;
     if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return SDL_ERR_INVALID_ARG;
     if (heads && !sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return SDL_ERR_UNSUPPORTED;
     if (!aligned_to(q_len, 4) || !aligned_to(k_len, 4)) return SDL_ERR_ALIGNMENT;

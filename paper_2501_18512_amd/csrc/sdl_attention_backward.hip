@@ -29,6 +29,10 @@ __host__ __device__ constexpr int tile_of(bool bf16, bool wide) { return bf16 ? 
 __host__ __device__ constexpr int key_tile_of(bool bf16) { return bf16 ? 64 : 32; }
 __host__ __device__ constexpr int key_waves(bool bf16, bool wide) { return bf16 && wide ? 8 : 4; }
 
+// In bf16 the sums of a tile's products S and dP of the kernel of dk and dv start from -lse / scale and -D, in place of subtractions of them afterwards: the reads go straight
+// to the registers of the sums.  In fp32 a sum of 128 products of its own size beside a large number would lose digits that are wanted.
+__host__ __device__ constexpr bool from_stats(bool bf16) { return bf16; }
+
 struct BackwardArgs {
     Attention p;
     float* part;            // sums of the splits: [split][batch][key head][row][width], or [split][dk, dv][batch][key head][key][width]
@@ -36,7 +40,7 @@ struct BackwardArgs {
     uint32_t splits, chunk; // chunk: keys of a split, or tiles of query tokens
     uint32_t by_heads;      // dk, dv: query heads of a split, or 0 where chunks are of tiles
     uint32_t tile, keys;    // tokens of a tile, keys of a block
-    uint64_t stats;         // rows of all sequences: the workspace has their lse in base 2, then their D
+    uint64_t stats;         // rows of all sequences: the workspace has their -lse (base 2, or over the scale), then their -D
 };
 
 // The query tokens that see a key of a block, in tiles, head by head of the group.
@@ -136,8 +140,8 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         delta = half_sum(delta);
     }
     if (row < n_rows && half == 0 && split == 0) {
-        p.row_stats[stat] = lse2;
-        p.row_stats[a.stats + stat] = delta;
+        p.row_stats[stat] = from_stats(sizeof(T) == 2) ? -lse2 / p.scale_log2 : -lse2;
+        p.row_stats[a.stats + stat] = -delta;
     }
 
     f32x16_t acc[kOut] = {};
@@ -201,11 +205,12 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
 {
     constexpr int HD = tile_width(W), kSteps = W / 16, kOut = W / 32, kTile = tile_of(sizeof(T) == 2, W > 64), kWaves = key_waves(sizeof(T) == 2, HD > 64), kKeys = 32 * kWaves;
     typedef Tile<T, HD> Smem;
+    constexpr bool kFromStats = from_stats(sizeof(T) == 2);
     // At width 128 k and v together would not leave the sums their registers (256 a lane, two wavefronts on a SIMD).
     constexpr bool kShareV = HD > 64;
     struct Stage {
         char q[Smem::bytes(kTile)], g[Smem::bytes(kTile)];
-        float stats[2][kTile];          // lse in base 2, D
+        float stats[2][kTile];          // -lse (base 2, or over the scale), -D
     };
     __shared__ __attribute__((aligned(16))) struct {
         Stage stage[2];
@@ -272,45 +277,51 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
         }
         bring(mem.stage[0]);
     }
+    const LaneReads<T, HD> reads(lane);
     for (int32_t tile = tile0, now = 0; tile < tiles; ++tile, now ^= 1) {
         loads_done();               // this tile is there, and all are done with the one before it
         if (tile + 1 < tiles) bring(mem.stage[now ^ 1]);
         const Stage& in = mem.stage[now];
+        const uint32_t in_q = lds_offset(in.q), in_g = lds_offset(in.g);
 #pragma unroll
         for (int part = 0; part < kTile; part += 32) {
             if (t0 + part + 31 < t_some) continue;
-            // what would not leave enough registers: reads of the next part this early, the offsets of all reads from one part to the next
-            if constexpr (W > 96) __builtin_amdgcn_sched_barrier(0);
-            const int lane = W > 96 ? anew(threadIdx.x & (kWave - 1)) : (int)threadIdx.x & (kWave - 1), c = lane & 31, half = lane >> 5;
+                    // reads of the next part this early would not leave enough registers
+            uint32_t v_at = lds_offset(mem.v) + wave * 32 / Smem::kGroup * Smem::kGroupBytes;
+            asm volatile("" : "+s"(v_at));         // the lane's addresses in it would take four registers through the loop
             f32x16_t sc = {}, dp = {};
+            if constexpr (kFromStats) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[i] = in.stats[0][part + 8 * (i / 4) + 4 * half + i % 4], dp[i] = in.stats[1][part + 8 * (i / 4) + 4 * half + i % 4];
+            }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                mma(sc, Smem::along(in.q, part + c, 2 * i + half), k[i]);
+                mma(sc, reads.along(in_q, part, i), k[i]);
                 if constexpr (kShareV)
-                    mma(dp, Smem::along(in.g, part + c, 2 * i + half), Smem::along(mem.v, wave * 32 + c, 2 * i + half));
+                    mma(dp, reads.along(in_g, part, i), reads.along(v_at, 0, i));
                 else
-                    mma(dp, Smem::along(in.g, part + c, 2 * i + half), v[i]);
+                    mma(dp, reads.along(in_g, part, i), v[i]);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int r = part + 8 * (i / 4) + 4 * half + i % 4;
-                sc[i] = exp2_fast(__builtin_fmaf(sc[i], p.scale_log2, -in.stats[0][r]));
-                dp[i] = sc[i] * (dp[i] - in.stats[1][r]);
+                sc[i] = exp2_fast(kFromStats ? sc[i] * p.scale_log2 : __builtin_fmaf(sc[i], p.scale_log2, in.stats[0][r]));
+                dp[i] = sc[i] * (kFromStats ? dp[i] : dp[i] + in.stats[1][r]);
             }
             // unless every row of the tile sees every key of the wavefront
             if (t0 < t_full || t0 + kTile > t_end) {
-                const int32_t t = t0 + part + 4 * half;
+                const int32_t t = t0 + part + 4 * half, first = t_key - t, end = t_end - t;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (t < t_key - (8 * (i / 4) + i % 4) || t >= t_end - (8 * (i / 4) + i % 4)) sc[i] = 0.0f, dp[i] = 0.0f;
+                    if (8 * (i / 4) + i % 4 < first || 8 * (i / 4) + i % 4 >= end) sc[i] = 0.0f, dp[i] = 0.0f;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const Frag<T> pr = frag_of(sc, u, T()), ds = frag_of(dp, u, T());
 #pragma unroll
                 for (int n = 0; n < kOut; ++n) {
-                    mma(dv[n], Smem::across(in.g, part + u * 16, n * 32, lane), pr);
-                    mma(dk[n], Smem::across(in.q, part + u * 16, n * 32, lane), ds);
+                    mma(dv[n], reads.across(in_g, part + u * 16, n), pr);
+                    mma(dk[n], reads.across(in_q, part + u * 16, n), ds);
                 }
             }
         }

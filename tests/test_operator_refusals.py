@@ -44,7 +44,7 @@ NORM = [
 ATTENTION = [
     (INVALID, dict(q=None)), (INVALID, dict(k=None)), (INVALID, dict(v=view(0))), (INVALID, dict(out=view(0))), (INVALID, dict(dtype=2)),
     (INVALID, dict(width=0)), (INVALID, dict(heads=3)), (INVALID, dict(kv_heads=0)), (INVALID, dict(scale=0.0)), (INVALID, dict(scale=-1.0)),
-    (INVALID, dict(scale=NAN)), (INVALID, dict(scale=INF)), (UNSUPPORTED, dict(width=129)), (UNSUPPORTED, dict(keys=(1 << 30) + 1)),
+    (INVALID, dict(scale=NAN)), (INVALID, dict(scale=INF)), (INVALID, dict(scale=7e-31)), (UNSUPPORTED, dict(width=129)), (UNSUPPORTED, dict(keys=(1 << 30) + 1)),
     (UNSUPPORTED, dict(queries=1 << 31, heads=1 << 30, kv_heads=1)), (UNSUPPORTED, dict(batch=1 << 30, queries=1)), (ALIGNMENT, dict(q=view(0x10001))),
     (ALIGNMENT, dict(v=view(0x10001))), (ALIGNMENT, dict(q_len=0x10002)), (ALIGNMENT, dict(k_len=0x10001)), (ALIGNMENT, dict(lse=0x10002)),
 ]
