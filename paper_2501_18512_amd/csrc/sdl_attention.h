@@ -434,6 +434,40 @@ struct Place {
     }
 };
 
+// A small problem that is cut into splits: the workgroups that have something to do come first, or two of them would share a compute unit while others had none
+// (a unit that is done with an empty one takes the next).  How many splits of a (unit, block) are of use depends on the lengths, so every wavefront counts them for
+// itself, 64 pairs at a time, until it comes to workgroup `id`; false: there are fewer.
+template <typename Count>
+__device__ __forceinline__ bool pick_item(uint32_t id, uint32_t units, uint32_t blocks, Count count, uint32_t& unit, uint32_t& nth_block, uint32_t& split)
+{
+    const uint32_t lane = threadIdx.x & (kWave - 1), pairs = units * blocks;
+    for (uint32_t first = 0; first < pairs; first += kWave) {
+        const uint32_t i = min(first + lane, pairs - 1), b = i / units, u = i - b * units;
+        const uint32_t n = first + lane < pairs ? count(u, b) : 0;
+        uint32_t upto = n;
+#pragma unroll
+        for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2) {
+            const uint32_t before = __shfl_up(upto, d);
+            if (lane >= d) upto += before;
+        }
+        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
+        if (id < all) {
+            const int who = __builtin_popcountll(__ballot(upto <= id));
+            unit = (uint32_t)__builtin_amdgcn_readlane((int)u, who);
+            nth_block = (uint32_t)__builtin_amdgcn_readlane((int)b, who);
+            split = id - (uint32_t)__builtin_amdgcn_readlane((int)(upto - n), who);
+            return true;
+        }
+        id -= all;
+    }
+    return false;
+}
+// Host: where that pays.
+inline bool pick_items(const Attention& p, uint64_t blocks, uint32_t splits)
+{
+    return p.spread && splits > 1 && (p.causal || p.q_len || p.k_len) && blocks * p.batch * p.kv_heads <= 256;
+}
+
 // Host: whether the kernels take such a problem.
 inline bool sdl_attention_shape(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype)
 {

@@ -26,13 +26,11 @@ struct ForwardArgs {
     float* part_lse;        // [split][batch][key head][row]
     uint32_t row_blocks, splits, chunk;         // chunk: keys of a split
     uint32_t few;                               // few rows: the splits take turns
+    uint32_t pick;                              // splits of no use come last
 };
 
-// Splits that keys make: one at least, which says that there are none.
-__device__ __forceinline__ int32_t splits_in_use(const ForwardArgs& a, int32_t keys)
-{
-    return max(1, (int32_t)(((uint32_t)keys + a.chunk - 1) / a.chunk));
-}
+// Splits that keys make.
+__device__ __forceinline__ uint32_t splits_in_use(const ForwardArgs& a, int32_t keys) { return ((uint32_t)keys + a.chunk - 1) / a.chunk; }
 
 template <typename T, int W, int BN, bool ASYNC>
 __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_kernel(const ForwardArgs a)
@@ -44,10 +42,20 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.row_blocks * a.splits, p.spread);
-    const uint32_t split = place.within % a.splits;
-    const uint32_t block = a.row_blocks - 1 - place.within / a.splits;      // the longest first
-    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
+    uint32_t unit, nth, split;
+    if (a.pick) {
+        const auto splits = [&](uint32_t u, uint32_t n) {
+            return splits_in_use(a, Sequence(p, u / p.kv_heads, 0).most_seen(p, (a.row_blocks - 1 - n) * kRows, kRows));
+        };
+        if (!pick_item(blockIdx.x, p.batch * p.kv_heads, a.row_blocks, splits, unit, nth, split)) return;
+    } else {
+        const Place place(blockIdx.x, p.batch * p.kv_heads, a.row_blocks * a.splits, p.spread);
+        unit = place.unit;
+        nth = place.within / a.splits;
+        split = place.within % a.splits;
+    }
+    const uint32_t block = a.row_blocks - 1 - nth;          // the longest first
+    const Sequence s(p, unit / p.kv_heads, unit % p.kv_heads);
 
     const uint32_t n_rows = p.queries * p.group.d;
     const uint32_t row = block * kRows + wave * kRowsPerWave + c;
@@ -70,7 +78,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t every = t_last < t_first ? 0 : s.seen(p, t_first);    // keys that all valid rows see
     const int32_t tiles = (keys + BN - 1) / BN;
     const int32_t tile0 = (int32_t)(split * (a.chunk / BN)), tile1 = min(tiles, tile0 + (int32_t)(a.chunk / BN));
-    if (split > 0 && tile0 >= tile1) return;         // a chunk that no row sees is not looked at by the join
+    if (a.splits > 1 && tile0 >= tile1) return;      // a chunk that no row sees is not looked at by the join
     // keys that a row of the wavefront sees: from there on it helps with the copies only
     const int32_t wave_keys = s.most_seen(p, block * kRows + wave * kRowsPerWave, kRowsPerWave);
     const TileCopy<T, HD, BN, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
@@ -95,9 +103,11 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         f32x16_t sc[kTiles] = {};
         if constexpr (W > 96) __builtin_amdgcn_s_setprio(1);        // the products go ahead of the other wavefront's exponentials: 3 % at width 128
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k)
+        for (int k = 0; k < kSteps; ++k) {
+            if (sizeof(T) == 4 && W <= 96 && k * 16 >= (int)p.width) break;        // eight instructions of 64 cycles each for nothing
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) mma(sc[n], Smem::along(k_now, n * 32 + c, 2 * k + half), q[k]);
+        }
         if constexpr (W > 96) __builtin_amdgcn_s_setprio(0);
         if (key0 + BN > every) {
 #pragma unroll
@@ -178,8 +188,8 @@ __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardA
     const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits, p.spread);
     const uint32_t split = place.within;
     const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
-    const int32_t keys = s.nq > 0 ? s.seen(p, s.nq - 1) : 0, splits = splits_in_use(a, keys);
-    if ((int32_t)split >= splits) return;               // not looked at by the join
+    const int32_t keys = s.nq > 0 ? s.seen(p, s.nq - 1) : 0, splits = (int32_t)splits_in_use(a, keys);
+    if (a.splits > 1 && (int32_t)split >= splits) return;       // not looked at by the join
     const TileCopy<T, HD, BN, 1, ASYNC, ONCE> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
 #pragma unroll
     for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
@@ -463,6 +473,7 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
     const uint64_t rows = (uint64_t)queries * a.p.group.d;
     a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
     a.few = rows <= kFewRows;
+    a.pick = !a.few && pick_items(a.p, a.row_blocks, a.splits);
     const uint64_t groups = (uint64_t)a.row_blocks * a.splits * batch * kv_heads;
     if (groups > 0x7fffffffu || (a.splits > 1 && (uint64_t)batch * queries * heads > 0x7fffffffu)) return SDL_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);

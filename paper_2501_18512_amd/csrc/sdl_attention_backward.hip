@@ -39,6 +39,7 @@ struct BackwardArgs {
     uint32_t blocks;        // of rows or keys, per (batch, key head)
     uint32_t splits, chunk; // chunk: keys of a split, or tiles of query tokens
     uint32_t by_heads;      // dk, dv: query heads of a split, or 0 where chunks are of tiles
+    uint32_t pick;          // splits of no use come last
     uint32_t tile, keys;    // tokens of a tile, keys of a block
     uint64_t stats;         // rows of all sequences: the workspace has their -lse (base 2, or over the scale), then their -D
 };
@@ -66,10 +67,20 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
-    const uint32_t split = place.within % a.splits;
-    const uint32_t block = a.blocks - 1 - place.within / a.splits;       // the longest first
-    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
+    uint32_t unit, nth, split;
+    if (a.pick) {
+        const auto splits = [&](uint32_t u, uint32_t n) {
+            return ((uint32_t)Sequence(p, u / p.kv_heads, 0).most_seen(p, (a.blocks - 1 - n) * kRows, kRows) + a.chunk - 1) / a.chunk;
+        };
+        if (!pick_item(blockIdx.x, p.batch * p.kv_heads, a.blocks, splits, unit, nth, split)) return;
+    } else {
+        const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
+        unit = place.unit;
+        nth = place.within / a.splits;
+        split = place.within % a.splits;
+    }
+    const uint32_t block = a.blocks - 1 - nth;           // the longest first
+    const Sequence s(p, unit / p.kv_heads, unit % p.kv_heads);
 
     const uint32_t n_rows = p.queries * p.group.d;
     const uint32_t row = block * kRows + wave * 32 + c;
@@ -83,7 +94,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     const int32_t key_begin = (int32_t)(split * a.chunk);
     const int32_t keys = min(t_last < t_first ? 0 : s.seen(p, t_last), key_begin + (int32_t)a.chunk);     // of this split: [key_begin, keys)
     const int32_t every = t_last < t_first ? 0 : s.seen(p, t_first);
-    if (split > 0 && key_begin >= keys) return;          // a chunk that no row sees is not looked at when the sums are added
+    if (a.splits > 1 && key_begin >= keys) return;       // a chunk that no row sees is not looked at when the sums are added
 
     Frag<T> q[kSteps], g[kSteps];
     float delta = 0.0f;
@@ -155,12 +166,14 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         if (key0 >= wave_keys) continue;
         f32x16_t sc[kParts] = {}, dp[kParts] = {};
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k)
+        for (int k = 0; k < kSteps; ++k) {
+            if (sizeof(T) == 4 && W <= 96 && k * 16 >= (int)p.width) break;
 #pragma unroll
             for (int n = 0; n < kParts; ++n) {
                 mma(sc[n], Smem::along(k_now, n * 32 + c, 2 * k + half), q[k]);
                 mma(dp[n], Smem::along(v_now, n * 32 + c, 2 * k + half), g[k]);
             }
+        }
 #pragma unroll
         for (int n = 0; n < kParts; ++n)
 #pragma unroll
@@ -219,10 +232,21 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
     const Attention& p = a.p;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, half = lane >> 5;
 
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
-    const uint32_t split = place.within % a.splits;
-    const uint32_t block = place.within / a.splits;                      // the longest first
-    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
+    uint32_t unit, block, split;                         // the longest first
+    if (a.pick) {
+        const auto splits = [&](uint32_t u, uint32_t n) {
+            const Seers of(p, Sequence(p, u / p.kv_heads, 0), (int32_t)(n * kKeys), kTile);
+            const int32_t chunk = (int32_t)(a.by_heads ? a.by_heads * of.per_head : a.chunk);
+            return of.tiles ? (uint32_t)((of.tiles + chunk - 1) / chunk) : 0u;
+        };
+        if (!pick_item(blockIdx.x, p.batch * p.kv_heads, a.blocks, splits, unit, block, split)) return;
+    } else {
+        const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
+        unit = place.unit;
+        block = place.within / a.splits;
+        split = place.within % a.splits;
+    }
+    const Sequence s(p, unit / p.kv_heads, unit % p.kv_heads);
 
     const int32_t key0 = (int32_t)(block * kKeys), wave_key0 = key0 + wave * 32, key = wave_key0 + c;
     Frag<T> k[kSteps], v[kShareV ? 1 : kSteps];
@@ -239,7 +263,7 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
     const Seers seers(p, s, key0, kTile);
     const int32_t chunk = (int32_t)(a.by_heads ? a.by_heads * seers.per_head : a.chunk);
     const int32_t t_begin = seers.begin, t_end = seers.end, tile0 = (int32_t)split * chunk, tiles = min(seers.tiles, tile0 + chunk);
-    if (split > 0 && tile0 >= tiles) return;         // nothing there for this split, and nothing is looked at when the sums are added
+    if (a.splits > 1 && tile0 >= tiles) return;      // nothing there for this split, and nothing is looked at when the sums are added
 
     // from which token on the lane's key is seen, a key of the wavefront, and every one
     const int32_t never = 0x7fffff00;
@@ -296,6 +320,7 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
             }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
+                if (sizeof(T) == 4 && W <= 96 && i * 16 >= (int)p.width) break;
                 mma(sc, reads.along(in_q, part, i), k[i]);
                 if constexpr (kShareV)
                     mma(dp, reads.along(in_g, part, i), reads.along(v_at, 0, i));
@@ -471,6 +496,7 @@ int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
         a.blocks = (uint32_t)plan.row_blocks;
         a.splits = plan.keys.splits;
         a.chunk = plan.keys.chunk * key_tile_of(bf16);
+        a.pick = pick_items(p, plan.row_blocks, a.splits);
         const dim3 grid((uint32_t)(plan.row_blocks * plan.heads * plan.keys.splits));
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
             hipLaunchKernelGGL((sdl_attention_dq_kernel<T, W, true>), grid, dim3(kWaves * kWave), 0, st, a);
@@ -485,6 +511,7 @@ int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
     a.splits = plan.rows.splits;
     a.chunk = plan.rows.chunk;
     a.by_heads = plan.rows.by_heads;
+    a.pick = pick_items(p, plan.key_blocks, a.splits);
     const dim3 grid((uint32_t)(plan.key_blocks * plan.heads * plan.rows.splits));
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
         hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, W, true>), grid, dim3(key_threads), 0, st, a);
