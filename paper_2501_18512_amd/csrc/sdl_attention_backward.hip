@@ -9,6 +9,10 @@
 //   dk, dv   keys are a wavefront's own: S = q k^T and dP = d_out v^T leave P and dS where dv^T = d_out^T P and dk^T = q^T dS want them
 // D is worked out by the first and read by the second.  Where the workgroups are too few to fill the chip, a chunk of the keys (or of the
 // rows) goes to a workgroup each, which leaves its sums in the workspace, and a third kernel adds them up in order.
+//
+// In bf16 the registers allow two wavefronts on a SIMD, which keep the matrix units busy for about two fifths of the cycles.  2 sequences of 4096 tokens, 16 heads of
+// 128, no mask: 868 us, 792 TFLOP/s of the five products that count, 1110 of the seven; 4 causal ones of 2048: 128 us for dq and 185 for dk and dv; 8 of 1024, 12 heads of 64:
+// 45 and 52.  In fp32 the matrix instructions bound it: 119 TFLOP/s of seven products at width 128.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -23,14 +27,16 @@ constexpr int kWaves = 4, kRows = 32 * kWaves;          // of the kernel of dq
 
 // Query tokens (kernel of dk and dv) and keys (kernel of dq) that go through shared memory at a time, and the wavefronts of the former, 32 keys each.  A tile
 // has to last as long as the next one takes to come.  bf16 at widths over 64: eight wavefronts, as two workgroups of four would have room for tiles of 32 tokens
-// only (v of their keys lies in shared memory as well).  Up to 64: 128 tokens a tile instead of 64, 91 -> 89 us for the backward pass of 8 sequences of 1024 tokens
-// and 12 heads of 64; 128 keys a tile would take the registers of the third wavefront on a SIMD, 91 -> 93 us.
+// only (v of their keys lies in shared memory as well).  Up to 64: 128 tokens a tile instead of 64, 96 -> 91 us for the backward pass of 8 sequences of 1024 tokens
+// and 12 heads of 64 (three workgroups a compute unit, which tiles of 64 leave room for, are no faster); 128 keys a tile would take the registers of the third wavefront
+// on a SIMD, 91 -> 93 us.  At width 96 v would have room in the registers, with four wavefronts a workgroup: 159 -> 170 us for 4 sequences of 1024, 32 heads over 8.
 __host__ __device__ constexpr int tile_of(bool bf16, bool wide) { return bf16 ? (wide ? 64 : 128) : 32; }
 __host__ __device__ constexpr int key_tile_of(bool bf16) { return bf16 ? 64 : 32; }
 __host__ __device__ constexpr int key_waves(bool bf16, bool wide) { return bf16 && wide ? 8 : 4; }
 
 // In bf16 the sums of a tile's products S and dP of the kernel of dk and dv start from -lse / scale and -D, in place of subtractions of them afterwards: the reads go straight
-// to the registers of the sums.  In fp32 a sum of 128 products of its own size beside a large number would lose digits that are wanted.
+// to the registers of the sums (with the addresses of LaneReads, 4 sequences of 2048 tokens, 16 heads of 128: 200 -> 185 us).  In fp32 a sum of up to 128 products beside a
+// larger number would lose digits that are wanted.
 __host__ __device__ constexpr bool from_stats(bool bf16) { return bf16; }
 
 struct BackwardArgs {
@@ -421,7 +427,8 @@ __global__ void __launch_bounds__(256) sdl_attention_add_kernel(const BackwardAr
 
 // How the work is cut.  A problem with fewer workgroups than compute units (256) is cut into chunks of the long axis, into 512 of them, or, as an fp32 tile takes the
 // matrix units 16 times as long, 1024, down to those that pay for a workgroup's start and for the sums that it leaves (256 keys or rows, in fp32 64):
-// ragged fp32 sequences of up to 517 tokens 94 / 88 us with 512 / 1024, bf16 ones of 8192 tokens for 4 key heads 1323 / 1372.
+// backward pass of four ragged fp32 sequences of up to 517 tokens 77 / 62 us with 512 / 1024, and 77 with 128 rows at least; of 8192 bf16 tokens for 4 heads 432 / 464,
+// of 1024 for 8 heads 55 and, with 128 rows at least, 63.
 struct Cut {
     uint32_t chunk, splits, by_heads;
 };

@@ -131,20 +131,6 @@ __device__ __forceinline__ void store8(float* row, uint32_t at, uint32_t n, cons
         if (at + j < n) row[at + j] = v[j];
 }
 
-// Elements [at, at + 8) of a parameter array of either type.
-__device__ __forceinline__ void load_params(const void* p, bool bf16, uint32_t at, uint32_t n, float* out)
-{
-    if (bf16) {
-        const Eight<__bf16> x = load8(static_cast<const __bf16*>(p), at, n);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) out[j] = x.get(j);
-    } else {
-        const Eight<float> x = load8(static_cast<const float*>(p), at, n);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) out[j] = x.get(j);
-    }
-}
-
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x)
 {

@@ -5,6 +5,8 @@
 // Memory bounds it: every element is read and written once.  A thread has eight pairs (i .. i+7) of one token and walks over heads, so that the
 // angles, the dear part, are worked out once for them all.  An angle is held in turns in 64 bits until its whole turns are off: at position
 // 10^5 an fp32 angle would be good to three digits.
+//
+// 8192 tokens of 32 heads of 128 in bf16 (134 MB): 24 us, 5.5 TB/s.  16 tokens of 20 heads: 4.2 us, of which the launch is 3 and the angles are the rest.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -141,8 +143,10 @@ int sdl_rotary(const sdl_view_t* x, uint32_t batch, uint32_t tokens, uint32_t he
     if (chunks == 0) return SDL_OK;
     const uint64_t bt = (uint64_t)batch * tokens;
     if (bt * chunks * heads > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
-    // heads a thread walks over: as many as leave the chip full (262,144 threads)
-    uint64_t parts = (262144 + bt * chunks - 1) / (bt * chunks);
+    // Heads a thread walks over: as many as leave 131,072 threads, a wavefront and more for every SIMD, and no more than eight of them up to four times as many: 4096
+    // tokens of 8 heads of 128, two heads a thread 6.0 us and one 7.4 (the angles); 32,768 of 16, eight a thread 49 us and sixteen 53.
+    uint64_t parts = (131072 + bt * chunks - 1) / (bt * chunks);
+    while (heads > 8 * parts && bt * chunks * parts < 524288) parts *= 2;
     if (parts > heads) parts = heads;
     a.heads_each = (uint32_t)((heads + parts - 1) / parts);
     parts = (heads + a.heads_each - 1) / a.heads_each;
