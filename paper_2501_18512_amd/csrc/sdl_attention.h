@@ -446,12 +446,7 @@ __device__ __forceinline__ bool pick_item(uint32_t id, uint32_t units, uint32_t 
     for (uint32_t first = 0; first < pairs; first += kWave) {
         const uint32_t i = min(first + lane, pairs - 1), b = i / units, u = i - b * units;
         const uint32_t n = first + lane < pairs ? count(u, b) : 0;
-        uint32_t upto = n;
-#pragma unroll
-        for (uint32_t d = 1; d < (uint32_t)kWave; d *= 2) {
-            const uint32_t before = __shfl_up(upto, d);
-            if (lane >= d) upto += before;
-        }
+        const uint32_t upto = lane_scan(n);
         const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
         if (id < all) {
             const int who = __builtin_popcountll(__ballot(upto <= id));

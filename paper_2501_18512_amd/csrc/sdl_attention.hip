@@ -24,6 +24,8 @@ using namespace sdl_device;
 
 constexpr int kRowsPerWave = 32, kWaves = 4, kRows = kRowsPerWave * kWaves;
 constexpr uint32_t kMaxSplits = 256;           // the join has one a thread
+constexpr uint32_t kFewRows = 16, kFewLeast = 128, kFewUnits = 256;
+template <typename T> constexpr uint32_t kFewTile = sizeof(T) == 2 ? 32 : 16;      // keys of a tile of the kernel for few rows
 
 struct ForwardArgs {
     Attention p;
@@ -32,6 +34,7 @@ struct ForwardArgs {
     uint32_t row_blocks, splits, chunk;         // chunk: keys of a split
     uint32_t few;                               // few rows: the splits take turns
     uint32_t pick;                              // splits of no use come last
+    uint32_t slots;                             // few rows: workgroups among which all sequences' tiles are shared out, whose results lie one behind the other; or 0
 };
 
 // Splits that keys make.
@@ -178,23 +181,83 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     }
 }
 
+// Few rows over caches of different lengths: chunks of one size would leave a half of the workgroups without work and compute units with one of them or three.  The lengths
+// are in device memory, so every wavefront adds up the tiles for itself: the least number of tiles each with which the workgroups are enough.  16 requests of 1 to
+// 8192 tokens, 4 key heads of 128: 36 us with chunks of one size and 30 so, in fp32 77 and 53, 64 requests 106 and 95; 16 of 8192 each 48 and 49.
+struct Shares {
+    uint32_t n[kFewUnits / kWave];          // workgroups of unit 64 j + lane
+
+    static __device__ __forceinline__ uint32_t sum(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)lane_scan(x), kWave - 1); }
+    __device__ __forceinline__ Shares(const ForwardArgs& a, uint32_t tile)
+    {
+        const Attention& p = a.p;
+        const uint32_t lane = threadIdx.x & (kWave - 1), units = p.batch * p.kv_heads;
+        uint32_t all = 0, most = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kFewUnits / kWave; ++j) {
+            const uint32_t u = j * kWave + lane;
+            n[j] = u < units ? ((uint32_t)Sequence(p, u / p.kv_heads, 0).most_seen(p, 0, kFewRows) + tile - 1) / tile : 0;
+            all += n[j];
+            most = max(most, n[j]);
+        }
+        // no unit has more than the join has threads
+        uint32_t each = max(kFewLeast / tile, (sum(all) + a.slots - 1) / a.slots);
+        while (__any(most > each * kMaxSplits)) each += max(1u, each / 16);
+        for (;; each += max(1u, each / 16)) {            // ends where a workgroup has a whole sequence, if not before: there are as many as units
+            uint32_t taken = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < kFewUnits / kWave; ++j) taken += (n[j] + each - 1) / each;
+            if (sum(taken) <= a.slots) break;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kFewUnits / kWave; ++j) n[j] = (n[j] + each - 1) / each;
+    }
+    __device__ __forceinline__ uint32_t mine(uint32_t u) const
+    {
+        uint32_t x = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kFewUnits / kWave; ++j) x |= u / kWave == j ? n[j] : 0;
+        return x;
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t unit) const
+    {
+        return (uint32_t)__builtin_amdgcn_readlane((int)mine(unit), (int)(unit % kWave));
+    }
+    __device__ __forceinline__ uint32_t before(uint32_t unit) const
+    {
+        const uint32_t lane = threadIdx.x & (kWave - 1);
+        uint32_t x = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kFewUnits / kWave; ++j) x += j * kWave + lane < unit ? n[j] : 0;
+        return sum(x);
+    }
+};
+
 // The same for up to 16 rows, tokens that are generated one by one, where reading the keys and values is all there is to it.  A workgroup is one wavefront
 // with tiles of its own, so that nothing waits for anything but its own copies, and the compute unit's other wavefronts (four at width 128) fill in. The rows
 // are the columns of the 16x16 instructions.  The splits of a (batch, key head) take turns with the tiles, so that what they read at a time lies side by side.
-// 64 requests of 8192 tokens, 16 heads over 4 of width 128 (1.07 GB): 163 us, 6.6 TB/s; 16 of up to 8192 (134 MB): 31 us with the launch, and 4 for the join.
+// 64 requests of 8192 tokens, 16 heads over 4 of width 128 (1.07 GB): 166 us, 6.5 TB/s; 16 of up to 8192 (134 MB): 30 us, 4.5 TB/s, of which the join is 4.
 template <typename T, int W, bool ASYNC, bool ONCE>
 __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardArgs a)
 {
-    constexpr int HD = tile_width(W), BN = sizeof(T) == 2 ? 32 : 16, kTiles = BN / 16, kSteps = W / 32, kOut = W / 16;
+    constexpr int HD = tile_width(W), BN = kFewTile<T>, kTiles = BN / 16, kSteps = W / 32, kOut = W / 16;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(BN)];
     __shared__ __attribute__((aligned(16))) char vs[2][Smem::bytes(BN)];
     const Attention& p = a.p;
     const int lane = threadIdx.x, c = lane & 15, quarter = lane >> 4;
-    const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits, p.spread);
-    const uint32_t split = place.within;
-    const Sequence s(p, place.unit / p.kv_heads, place.unit % p.kv_heads);
-    const int32_t keys = s.nq > 0 ? s.seen(p, s.nq - 1) : 0, splits = (int32_t)splits_in_use(a, keys);
+    uint32_t unit, nth, split, shares = 0;
+    if (a.slots) {
+        const Shares of(a, BN);
+        if (!pick_item(blockIdx.x, p.batch * p.kv_heads, 1, [&](uint32_t u, uint32_t) { return of.mine(u); }, unit, nth, split)) return;
+        shares = of.of(unit);
+    } else {
+        const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits, p.spread);
+        unit = place.unit;
+        split = place.within;
+    }
+    const Sequence s(p, unit / p.kv_heads, unit % p.kv_heads);
+    const int32_t keys = s.nq > 0 ? s.seen(p, s.nq - 1) : 0, splits = (int32_t)(a.slots ? shares : splits_in_use(a, keys));
     if (a.splits > 1 && (int32_t)split >= splits) return;       // not looked at by the join
     const TileCopy<T, HD, BN, 1, ASYNC, ONCE> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
 #pragma unroll
@@ -273,7 +336,7 @@ __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardA
         for (int n = 0; n < kOut; ++n) store4<ASYNC>(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
         if (p.lse && quarter == 0) p.lse[((uint64_t)s.b * p.kv_heads * p.group.d + head) * p.queries + t] = lse;
     } else {
-        const uint64_t line = (((uint64_t)split * p.batch + s.b) * p.kv_heads + s.g) * n_rows + row;
+        const uint64_t line = (a.slots ? blockIdx.x : (uint64_t)split * p.batch * p.kv_heads + unit) * n_rows + row;
         float* dst = a.part_out + line * p.width;
 #pragma unroll
         for (int n = 0; n < kOut; ++n) store4<ASYNC>(dst, n * 16 + 4 * quarter, p.width, o[n][0] * by, o[n][1] * by, o[n][2] * by, o[n][3] * by);
@@ -329,11 +392,19 @@ __global__ void __launch_bounds__(256) sdl_attention_join_kernel(const ForwardAr
     const uint32_t bg = line / n_rows, row = line - bg * n_rows, t = div(row, p.group);
     const Sequence s(p, bg / p.kv_heads, bg % p.kv_heads);
     const uint32_t last = a.few ? s.nq - 1 : t;        // splits that take turns are all of use to every row
-    const uint32_t n = (int32_t)t < s.nq ? splits_in_use(a, s.seen(p, (int32_t)last)) : 0;
+    uint32_t n = 0, first = line, next = lines;           // rows of results: the first split's, and from one split to the next
+    if (a.slots) {
+        const Shares of(a, kFewTile<T>);
+        first = of.before(bg) * n_rows + row;
+        next = n_rows;
+        if ((int32_t)t < s.nq) n = of.of(bg);
+    } else if ((int32_t)t < s.nq) {
+        n = splits_in_use(a, s.seen(p, (int32_t)last));
+    }
     const uint32_t group = threadIdx.x / 32, d = threadIdx.x % 32 * 4;
-    const float* src = a.part_out + (uint64_t)line * p.width + d;
-    const uint64_t step = (uint64_t)lines * p.width;
-    const float mine = threadIdx.x < n ? a.part_lse[(uint64_t)threadIdx.x * lines + line] : -__builtin_inff();
+    const float* src = a.part_out + (uint64_t)first * p.width + d;
+    const uint64_t step = (uint64_t)next * p.width;
+    const float mine = threadIdx.x < n ? a.part_lse[(uint64_t)threadIdx.x * next + first] : -__builtin_inff();
     float top = mine;
 #pragma unroll
     for (int m = 1; m < kWave; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
@@ -372,14 +443,12 @@ __global__ void __launch_bounds__(256) sdl_attention_join_kernel(const ForwardAr
 //                                   matrix units 16 times as long: 64)
 //   few rows, of one wavefront      1024 are what the shared memory holds at width 128, of 128 keys at least: 16 caches of 8192 tokens for 4 heads
 //                                   56 / 49 / 50 / 54 us with 512 / 1024 / 2048 / 4096
-constexpr uint32_t kFewRows = 16;
-
 uint32_t chunk_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, sdl_dtype_t dtype)
 {
     const uint64_t rows = (uint64_t)queries * (heads / kv_heads);
     const bool few = rows <= kFewRows;
     const uint64_t groups = (rows + kRows - 1) / kRows * batch * kv_heads, fill = 1024, enough = few ? 1024 : 512;
-    const uint64_t least = few ? 128 : dtype == SDL_DTYPE_BF16 ? 256 : 64;
+    const uint64_t least = few ? kFewLeast : dtype == SDL_DTYPE_BF16 ? 256 : 64;
     uint64_t n = keys;
     if (groups < enough) {
         n = keys * groups / fill;
@@ -391,6 +460,15 @@ uint32_t chunk_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t head
     return (uint32_t)(n < unit ? unit : n);
 }
 
+// Workgroups among which the tiles of few rows' caches are shared out, where the units are few enough to be counted through by each, and their tiles no more than 32 bits
+// hold.  Caches that go into 1024 chunks of the least size are all at work at once as it is.
+uint32_t slots_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads)
+{
+    const uint64_t units = (uint64_t)batch * kv_heads;
+    const bool pays = (uint64_t)queries * (heads / kv_heads) <= kFewRows && units <= kFewUnits && units * ((keys + kFewLeast - 1) / kFewLeast) > 1024;
+    return pays && units * keys < (1ull << 35) ? 1024u : 0u;
+}
+
 uint32_t splits_of(uint32_t chunk, uint32_t keys) { return keys <= chunk ? 1u : (keys + chunk - 1) / chunk; }
 
 template <typename T>
@@ -398,7 +476,7 @@ int join(const ForwardArgs& a, hipStream_t st)
 {
     const uint64_t lines = (uint64_t)a.p.batch * a.p.kv_heads * a.p.queries * a.p.group.d;
     // 256 rows of 16 splits 4.6 us with a workgroup a row and 8.6 with 32 lanes, 12,408 rows of 9 splits 18 and 9 us
-    if (a.splits <= 32 && lines >= 2048)
+    if (!a.slots && a.splits <= 32 && lines >= 2048)
         hipLaunchKernelGGL((sdl_attention_join_rows_kernel<T>), dim3((uint32_t)((lines + 7) / 8)), dim3(256), 0, st, a);
     else
         hipLaunchKernelGGL((sdl_attention_join_kernel<T>), dim3((uint32_t)lines), dim3(256), 0, st, a);
@@ -408,7 +486,7 @@ int join(const ForwardArgs& a, hipStream_t st)
 template <typename T>
 int forward(const ForwardArgs& a, hipStream_t st)
 {
-    const dim3 grid(a.row_blocks * a.splits * a.p.batch * a.p.kv_heads), block(kWaves * kWave);
+    const dim3 grid(a.slots ? a.slots : a.row_blocks * a.splits * a.p.batch * a.p.kv_heads), block(kWaves * kWave);
     // keys of a tile, of half as many at widths over 64: 64 KB of shared memory (8 sequences of 1024 tokens, 12 heads of 64: 36 us with 64 keys, 32 with 128)
     constexpr int kTileKeys = sizeof(T) == 2 ? 128 : 64;
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
@@ -452,7 +530,9 @@ size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t 
 {
     if (!sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return 0;
     const uint32_t n = splits_of(chunk_of(batch, queries, keys, heads, kv_heads, dtype), keys);
-    return n == 1 ? 0 : (size_t)n * batch * heads * queries * (width + 1) * sizeof(float);
+    if (n == 1) return 0;
+    const size_t lines = (size_t)n * batch * heads * queries, shared = (size_t)slots_of(batch, queries, keys, heads, kv_heads) * (heads / kv_heads) * queries;
+    return (lines > shared ? lines : shared) * (width + 1) * sizeof(float);
 }
 
 int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v, uint32_t batch, uint32_t queries, uint32_t keys,
@@ -475,8 +555,9 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
     a.chunk = chunk_of(batch, queries, keys, heads, kv_heads, dtype);
     a.splits = splits_of(a.chunk, keys);
     a.part_out = static_cast<float*>(workspace);
-    a.part_lse = a.part_out + (size_t)a.splits * batch * heads * queries * width;
+    if (k_len && a.splits > 1) a.slots = slots_of(batch, queries, keys, heads, kv_heads);
     const uint64_t rows = (uint64_t)queries * a.p.group.d;
+    a.part_lse = a.part_out + (a.slots ? a.slots * rows : (size_t)a.splits * batch * heads * queries) * width;
     a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
     a.few = rows <= kFewRows;
     a.pick = !a.few && pick_items(a.p, a.row_blocks, a.splits);

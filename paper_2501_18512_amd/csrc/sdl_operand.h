@@ -158,6 +158,20 @@ __device__ __forceinline__ float lane_sum(float x)
     return x;
 }
 
+// The sum of the lanes up to and including this one, over a whole wavefront.
+__device__ __forceinline__ uint32_t lane_scan(uint32_t x)
+{
+#define SDL_SCAN(CTRL, ROWS) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false)
+    SDL_SCAN(0x111, 0xf);       // from one lane down in a row of 16, then 2, 4, 8
+    SDL_SCAN(0x112, 0xf);
+    SDL_SCAN(0x114, 0xf);
+    SDL_SCAN(0x118, 0xf);
+    SDL_SCAN(0x142, 0xa);       // the last of rows 0 and 2 to rows 1 and 3
+    SDL_SCAN(0x143, 0xc);       // the last of row 1 to rows 2 and 3
+#undef SDL_SCAN
+    return x;
+}
+
 // ------------------------------------------------------------------------------------------------- host side
 
 inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }

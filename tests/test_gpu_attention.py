@@ -152,6 +152,18 @@ def test_split_keys_give_what_one_pass_gives(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_few_rows_over_caches_of_different_lengths(dtype):
+    """The tiles of many keys' caches are shared out evenly among the workgroups; those of fewer keys, and of more than 256 sequences times key heads, go another way."""
+    for i, (B, Lq, Lk, H, G, D, causal, lens) in enumerate([
+            (7, 1, 6300, 6, 3, 128, True, [0, 1, 128, 129, 6300, 31, 4700]), (40, 1, 2000, 4, 2, 32, True, [(7 * b * b) % 2001 for b in range(40)]),
+            (70, 1, 700, 3, 3, 16, True, [(11 * b) % 701 for b in range(70)]), (128, 2, 600, 2, 2, 24, True, [(37 * b) % 601 for b in range(128)]),
+            (1, 3, 140000, 2, 1, 16, True, [139999]), (3, 5, 50000, 3, 1, 8, False, [50000, 2, 0]), (2, 1, 66000, 16, 1, 64, True, [0, 0]),
+            (130, 1, 600, 2, 2, 24, True, [(13 * b) % 601 for b in range(130)]), (3, 2, 900, 8, 2, 64, True, [900, 2, 0])]):
+        print(f"few rows {B} {Lq} {Lk} {H} {G} {D} {dtype}", flush=True)
+        _check((B, Lq, Lk, H, G, D, causal, None, lens), dtype, seed=400 + 10 * i)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_heads_of_a_group_go_to_several_workgroups(dtype):
     """Many query heads over few blocks of keys: the gradients of keys and values are sums over workgroups that have some of the heads each."""
     _check((2, 300, 300, 64, 16, 72, True, [300, 170], [300, 170]), dtype, seed=11)
