@@ -1,6 +1,6 @@
 // Attention, forward (gfx950):  S = scale q k^T, masked;  P = softmax(S);  out = P v;  lse = log sum exp S.
 //
-// One pass over the keys with the running maximum m and sum l of every row.  A workgroup has 4 wavefronts of 32 rows; a tile of
+// One pass over the keys with the running maximum m and sum l of every row.  A workgroup has 4 or 8 wavefronts of 32 rows; a tile of
 // keys and values goes through shared memory.  S^T = k q^T has a row's scores in the registers of two lanes, and P^T as it stands is the
 // operand of out^T = v^T P^T (sdl_attention.h), so that m, l and the rescaling of the result are a lane's own.
 // Where there are too few rows to fill the chip, the keys are cut into chunks for a workgroup each, which leave normalised results and their
@@ -8,8 +8,8 @@
 // long ones leave no one waiting.
 //
 // In bf16 at width 128 the matrix units are busy for a third of the cycles and the vector units for two fifths (exponentials, the rounding of P), the two for the
-// most part not at once: a workgroup's wavefronts do the same at the same time, and the registers hold two workgroups a compute unit.  2 sequences of 4096
-// tokens, 16 heads, no mask: 296 us, 930 TFLOP/s (a library product of 8192^3: 1294); 8192 causal tokens: 282 us, 975; 4 of 2048: 106 us, 650, where a
+// most part not at once: a workgroup's wavefronts do the same at the same time, and the registers hold two of them on a SIMD.  2 sequences of 4096
+// tokens, 16 heads, no mask: 280 us, 980 TFLOP/s (a library product of 8192^3: 1294); 8192 causal tokens: 275 us, 1000; 4 of 2048: 106 us, 650, where a
 // workgroup's start and end are a sixth of its life.  In fp32 the matrix instructions bound it: 121 to 128 of 155 TFLOP/s.
 #include <hip/hip_runtime.h>
 
@@ -22,7 +22,7 @@ namespace {
 
 using namespace sdl_device;
 
-constexpr int kRowsPerWave = 32, kWaves = 4, kRows = kRowsPerWave * kWaves;
+constexpr int kRowsPerWave = 32, kRows = 4 * kRowsPerWave;      // of a wavefront, of a workgroup of four
 constexpr uint32_t kMaxSplits = 256;           // the join has one a thread
 constexpr uint32_t kFewRows = 16, kFewLeast = 128, kFewUnits = 256;
 template <typename T> constexpr uint32_t kFewTile = sizeof(T) == 2 ? 32 : 16;      // keys of a tile of the kernel for few rows
@@ -40,9 +40,10 @@ struct ForwardArgs {
 // Splits that keys make.
 __device__ __forceinline__ uint32_t splits_in_use(const ForwardArgs& a, int32_t keys) { return ((uint32_t)keys + a.chunk - 1) / a.chunk; }
 
-template <typename T, int W, int BN, bool ASYNC>
-__global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_kernel(const ForwardArgs a)
+template <typename T, int W, int BN, int WAVES, bool ASYNC>
+__global__ void __launch_bounds__(WAVES * kWave, sizeof(T) == 2 ? 2 : 1) sdl_attention_kernel(const ForwardArgs a)
 {
+    constexpr int kRows = kRowsPerWave * WAVES;
     constexpr int HD = tile_width(W), kTiles = BN / 32, kSteps = W / 16, kOut = W / 32;
     typedef Tile<T, HD> Smem;
     __shared__ __attribute__((aligned(16))) char ks[2][Smem::bytes(BN)];
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
     if (a.splits > 1 && tile0 >= tile1) return;      // a chunk that no row sees is not looked at by the join
     // keys that a row of the wavefront sees: from there on it helps with the copies only
     const int32_t wave_keys = s.most_seen(p, block * kRows + wave * kRowsPerWave, kRowsPerWave);
-    const TileCopy<T, HD, BN, kWaves, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
+    const TileCopy<T, HD, BN, WAVES, ASYNC> copy_k(p.k, s.b, s.g, p.width), copy_v(p.v, s.b, s.g, p.width);
 #pragma unroll
     for (int i = 0; i < 2; ++i) copy_k.clear(ks[i]), copy_v.clear(vs[i]);
 
@@ -471,6 +472,15 @@ uint32_t slots_of(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t head
 
 uint32_t splits_of(uint32_t chunk, uint32_t keys) { return keys <= chunk ? 1u : (keys + chunk - 1) / chunk; }
 
+// Widths over 64 in bf16: eight wavefronts a workgroup and tiles of 128 keys, half as many waits for one another, where such workgroups are two for every compute unit, or one
+// and all alike.  2 sequences of 4096 tokens, 16 heads of 128, no mask: 304 us with four wavefronts and 64 keys, 280 so (one sequence 145 and 135); 8192 causal
+// tokens of 16 heads over 4: 292 and 275; 2 causal sequences of 2048, which are 256 workgroups of different lengths: 65 and 66.
+bool is_tall(uint32_t batch, uint32_t queries, uint32_t heads, uint32_t kv_heads, uint32_t width, sdl_dtype_t dtype, bool causal, uint32_t splits)
+{
+    const uint64_t rows = (uint64_t)queries * (heads / kv_heads), groups = (rows + 2 * kRows - 1) / (2 * kRows) * batch * kv_heads;
+    return dtype == SDL_DTYPE_BF16 && width > 64 && splits == 1 && rows > kFewRows && groups >= (causal ? 512 : 256);
+}
+
 template <typename T>
 int join(const ForwardArgs& a, hipStream_t st)
 {
@@ -484,9 +494,9 @@ int join(const ForwardArgs& a, hipStream_t st)
 }
 
 template <typename T>
-int forward(const ForwardArgs& a, hipStream_t st)
+int forward(const ForwardArgs& a, bool tall, hipStream_t st)
 {
-    const dim3 grid(a.slots ? a.slots : a.row_blocks * a.splits * a.p.batch * a.p.kv_heads), block(kWaves * kWave);
+    const dim3 grid(a.slots ? a.slots : a.row_blocks * a.splits * a.p.batch * a.p.kv_heads);
     // keys of a tile, of half as many at widths over 64: 64 KB of shared memory (8 sequences of 1024 tokens, 12 heads of 64: 36 us with 64 keys, 32 with 128)
     constexpr int kTileKeys = sizeof(T) == 2 ? 128 : 64;
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
@@ -507,15 +517,20 @@ int forward(const ForwardArgs& a, hipStream_t st)
         else SDL_FEW(128);
 #undef SDL_FEW
     } else {
-#define SDL_ROWS(W, BN)                                                                                                               \
+#define SDL_ROWS(W, BN, WAVES)                                                                                                        \
     do {                                                                                                                              \
-        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, true>), grid, block, 0, st, a);                                 \
-        else hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, false>), grid, block, 0, st, a);                                      \
+        if (async) hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, WAVES, true>), grid, dim3(WAVES * kWave), 0, st, a);            \
+        else hipLaunchKernelGGL((sdl_attention_kernel<T, W, BN, WAVES, false>), grid, dim3(WAVES * kWave), 0, st, a);                 \
     } while (0)
-        if (a.p.width <= 32) SDL_ROWS(32, kTileKeys);
-        else if (a.p.width <= 64) SDL_ROWS(64, kTileKeys);
-        else if (a.p.width <= 96) SDL_ROWS(96, kTileKeys / 2);
-        else SDL_ROWS(128, kTileKeys / 2);
+        if (a.p.width <= 32) SDL_ROWS(32, kTileKeys, 4);
+        else if (a.p.width <= 64) SDL_ROWS(64, kTileKeys, 4);
+        else if (sizeof(T) == 2 && tall) {
+            if constexpr (sizeof(T) == 2) {
+                if (a.p.width <= 96) SDL_ROWS(96, 128, 8);
+                else SDL_ROWS(128, 128, 8);
+            }
+        } else if (a.p.width <= 96) SDL_ROWS(96, kTileKeys / 2, 4);
+        else SDL_ROWS(128, kTileKeys / 2, 4);
 #undef SDL_ROWS
     }
     const int rc = launched();
@@ -558,13 +573,14 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
     if (k_len && a.splits > 1) a.slots = slots_of(batch, queries, keys, heads, kv_heads);
     const uint64_t rows = (uint64_t)queries * a.p.group.d;
     a.part_lse = a.part_out + (a.slots ? a.slots * rows : (size_t)a.splits * batch * heads * queries) * width;
-    a.row_blocks = (uint32_t)((rows + kRows - 1) / kRows);
+    const bool tall = is_tall(batch, queries, heads, kv_heads, width, dtype, a.p.causal, a.splits);
+    a.row_blocks = (uint32_t)((rows + (tall ? 2 : 1) * kRows - 1) / ((tall ? 2 : 1) * kRows));
     a.few = rows <= kFewRows;
     a.pick = !a.few && pick_items(a.p, a.row_blocks, a.splits);
     const uint64_t groups = (uint64_t)a.row_blocks * a.splits * batch * kv_heads;
     if (groups > 0x7fffffffu || (a.splits > 1 && (uint64_t)batch * queries * heads > 0x7fffffffu)) return SDL_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return dtype == SDL_DTYPE_BF16 ? forward<__bf16>(a, st) : forward<float>(a, st);
+    return dtype == SDL_DTYPE_BF16 ? forward<__bf16>(a, tall, st) : forward<float>(a, tall, st);
 }
 
 }  // extern "C"

@@ -164,6 +164,14 @@ def test_few_rows_over_caches_of_different_lengths(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_many_heads_at_once(dtype):
+    """As many (sequence, key head) as fill the chip with workgroups of 256 rows."""
+    _check((8, 200, 300, 32, 32, 128, False, None, [300, 0, 1, 127, 128, 129, 256, 290]), dtype, seed=13)
+    _check((16, 70, 190, 32, 32, 104, True, [70, 0, 1, 33, 70, 64, 31, 32] * 2, [190, 100, 0, 20, 128, 129, 31, 190] * 2), dtype, seed=14)
+    _check((16, 20, 140, 96, 32, 90, True, None, None), dtype, seed=15)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_heads_of_a_group_go_to_several_workgroups(dtype):
     """Many query heads over few blocks of keys: the gradients of keys and values are sums over workgroups that have some of the heads each."""
     _check((2, 300, 300, 64, 16, 72, True, [300, 170], [300, 170]), dtype, seed=11)
