@@ -300,7 +300,7 @@ struct TileCopy {
             for (int i = threadIdx.x; i < ROWS * (HD / 8); i += WAVES * kWave) {
                 const int r = i / (HD / 8), c8 = i % (HD / 8);
                 const T* from = reinterpret_cast<const T*>(base + (int64_t)min(row0 + r, rows - 1) * stride);
-                Smem::put(tile, r, c8, load8(from, c8 * 8, width));
+                Smem::put(tile, r, c8, load8_ends(from, c8 * 8, width));
             }
         }
     }
