@@ -142,7 +142,8 @@ int sdl_rotary(const sdl_view_t* x, uint32_t batch, uint32_t tokens, uint32_t he
     const uint32_t chunks = (a.half + 7) / 8 + (in_place ? 0u : (width - rot + 7) / 8);
     if (chunks == 0) return SDL_OK;
     const uint64_t bt = (uint64_t)batch * tokens;
-    if (bt * chunks * heads > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
+    // step by step: a product of all four may be a multiple of 2^64
+    if (bt > 0x7fffffffu || bt * chunks > 0x7fffffffu || bt * chunks * heads > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
     // Heads a thread walks over: as many as leave 131,072 threads, a wavefront and more for every SIMD, and no more than eight of them up to four times as many: 4096
     // tokens of 8 heads of 128, two heads a thread 6.0 us and one 7.4 (the angles); 32,768 of 16, eight a thread 49 us and sixteen 53.
     uint64_t parts = (131072 + bt * chunks - 1) / (bt * chunks);
