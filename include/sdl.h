@@ -543,7 +543,7 @@ int sdl_layer_norm_backward(const sdl_view_t* dy, const sdl_view_t* x, uint32_t 
  * (2 i, 2 i + 1) in the interleaved one; the elements behind them are copied.  With p the token's position:
  *     (a, b) -> scale * (a cos(p f[i]) - b sin(p f[i]),  a sin(p f[i]) + b cos(p f[i]))
  * inverse != 0 turns the other way, with the same scale, which is the gradient's way back.  positions: int32
- * [batch][tokens] in device memory, or NULL for first_position + token.  frequencies: fp64 [rot / 2] in device memory, radians a
+ * [batch][tokens] in device memory, or NULL for first_position + token (which may be more than 32 bits hold).  frequencies: fp64 [rot / 2] in device memory, radians a
  * position; the angle is reduced in 64 bits, so that positions far into a long context lose nothing.  out may be x itself, with the same
  * strides.  Queries and keys that lie side by side in a fused projection's output are one call.
  * Errors: SDL_ERR_INVALID_ARG (missing array, bad enum, odd rot, rot above width, scale not finite), SDL_ERR_UNSUPPORTED

@@ -25,7 +25,7 @@ struct RotaryArgs {
     Div chunks, parts, tokens;      // thread -> (batch, token, share of the heads, eight pairs), the last fastest
     uint64_t n;
     uint32_t heads, heads_each, width, half;
-    int32_t first;
+    int32_t first;                  // counted on from in 64 bits
     float scale, sign;
 };
 
@@ -54,11 +54,11 @@ __global__ void __launch_bounds__(256) sdl_rotary_kernel(const RotaryArgs a)
         }
         return;
     }
-    const int32_t pos = a.positions ? a.positions[(uint64_t)b * a.tokens.d + t] : a.first + (int32_t)t;
+    const double pos = a.positions ? (double)a.positions[(uint64_t)b * a.tokens.d + t] : (double)a.first + (double)t;
     float c[8], s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const double turns = (double)pos * (i0 + j < a.half ? a.f[i0 + j] * 0.15915494309189535 : 0.0);
+        const double turns = pos * (i0 + j < a.half ? a.f[i0 + j] * 0.15915494309189535 : 0.0);
         float sj, cj;
         sincospif(2.0f * (float)(turns - rint(turns)), &sj, &cj);
         c[j] = cj * a.scale;
