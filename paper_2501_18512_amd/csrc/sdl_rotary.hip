@@ -4,7 +4,8 @@
 //
 // Memory bounds it: every element is read and written once.  A thread has eight pairs (i .. i+7) of one token and walks over heads, so that the
 // angles, the dear part, are worked out once for them all.  An angle is held in turns in 64 bits until its whole turns are off: at position
-// 10^5 an fp32 angle would be good to three digits.
+// 10^5 an fp32 angle would be good to three digits.  What is left is a pair of fp32 numbers, so that the sines and cosines next to whole quarter turns keep their digits as well:
+// error in fp32 (root mean square, 2048 positions, width 128) 5.6e-8 with the first of the two only and 4.5e-8 so, for 1 % of the time, 3 % in small fp32 calls.
 //
 // 8192 tokens of 32 heads of 128 in bf16 (134 MB): 24 us, 5.5 TB/s.  16 tokens of 20 heads: 4.2 us, of which the launch is 3 and the angles are the rest.
 #include <hip/hip_runtime.h>
@@ -59,10 +60,13 @@ __global__ void __launch_bounds__(256) sdl_rotary_kernel(const RotaryArgs a)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const double turns = pos * (i0 + j < a.half ? a.f[i0 + j] * 0.15915494309189535 : 0.0);
+        const double rest = 2.0 * (turns - rint(turns));            // half turns, in [-1, 1]
+        const float near = (float)rest, off = (float)(rest - (double)near) * 3.14159265f;
         float sj, cj;
-        sincospif(2.0f * (float)(turns - rint(turns)), &sj, &cj);
-        c[j] = cj * a.scale;
-        s[j] = sj * a.scale * a.sign;
+        sincospif(near, &sj, &cj);
+        // what the rounding of the angle to fp32 left out, at most 2^-25 of a half turn: the next terms are under 2^-47
+        c[j] = __builtin_fmaf(-sj, off, cj) * a.scale;
+        s[j] = __builtin_fmaf(cj, off, sj) * a.scale * a.sign;
     }
     for (uint32_t h = h0; h < h1; ++h) {
         const T* xr = x + (int64_t)h * a.x.head;

@@ -24,3 +24,24 @@ def test_counted_positions_go_on_behind_the_last_of_32_bits(first, dtype):
     X = x.double().abs()
     pair = (X[..., :4] + X[..., 4:]).repeat(1, 1, 1, 2)
     close(out, want, U[dtype] * want.abs() + (8 * U32 + 4 * 2.0 ** 31 * 2.0 ** -53) * pair, f"first {first}")
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_small_sines_and_cosines_keep_their_digits(interleaved):
+    """Pairs (1, 0) give cosine and sine themselves, held against 64 bits relatively, where one of them is small: around whole quarter turns.
+
+    The function of an fp32 number of turns is good to two units in the last place (4 u), a remainder that is added to it may halve it (8 u), the
+    sum and the scale are a rounding each: 12 u, and the angle's own error in 64 bits, four roundings of it."""
+    near = [0.0] + [s * d for d in (1e-1, 1e-2, 1e-3, 1e-4, 1e-5, 1e-6, 1e-7, 1e-8) for s in (-1, 1)]
+    f = torch.tensor([k * math.pi / 2 + d for k in range(1, 9) for d in near], dtype=torch.float64)
+    half = len(f)
+    positions = torch.tensor([[1, 3, -1, 5, 1001]], dtype=torch.int32)
+    x, scale = torch.zeros(1, 5, 1, 2 * half), 1.25
+    first, second = (slice(0, None, 2), slice(1, None, 2)) if interleaved else (slice(0, half), slice(half, None))
+    x[..., first] = 1.0
+    out = torch.empty_like(x, device="cuda")
+    sdl.sdl_rotary(x.cuda(), positions.cuda(), f.cuda(), out, sdl.ROTARY_INTERLEAVED if interleaved else sdl.ROTARY_HALF, scale)
+    torch.cuda.synchronize()
+    angle = positions.double()[..., None, None] * f
+    for part, want in ((first, scale * torch.cos(angle)), (second, scale * torch.sin(angle))):
+        close(out[..., part], want, 12 * U32 * want.abs() + 4 * scale * 2.0 ** -53 * angle.abs(), "cosine" if part == first else "sine")
