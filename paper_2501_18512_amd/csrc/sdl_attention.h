@@ -477,8 +477,8 @@ inline bool sdl_attention_shape(uint32_t batch, uint32_t queries, uint32_t keys,
 inline int sdl_attention_problem(Attention& p, uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads,
                                  uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len)
 {
-    // from 2^-100 on, the backward pass' lse / scale fits as well
-    if (!(scale >= 0x1p-100f) || scale > 3.4028235e38f || !known(dtype) || width == 0) return SDL_ERR_INVALID_ARG;
+    // from 2^-100 on, the backward pass' lse / scale fits as well; up to 2^127, the scale times log2(e)
+    if (!(scale >= 0x1p-100f) || scale > 0x1p127f || !known(dtype) || width == 0) return SDL_ERR_INVALID_ARG;
     if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return SDL_ERR_INVALID_ARG;
     if (heads && !sdl_attention_shape(batch, queries, keys, heads, kv_heads, width, dtype)) return SDL_ERR_UNSUPPORTED;
     if (!aligned_to(q_len, 4) || !aligned_to(k_len, 4)) return SDL_ERR_ALIGNMENT;
