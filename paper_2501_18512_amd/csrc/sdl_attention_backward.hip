@@ -547,6 +547,7 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
                            const sdl_view_t* dq, const sdl_view_t* dk, const sdl_view_t* dv, void* workspace, size_t workspace_bytes,
                            void* stream)
 {
+    if (heads == 0) heads = kv_heads, queries = 0;          // keys that no head reads: their gradients are written all the same
     BackwardArgs a{};
     int rc = sdl_attention_problem(a.p, batch, queries, keys, heads, kv_heads, width, dtype, scale, causal, q_len, k_len);
     if (rc != SDL_OK) return rc;
