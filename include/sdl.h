@@ -577,7 +577,7 @@ int sdl_rotary_frequencies(uint32_t rot, double base, sdl_rotary_scaling_t scali
  * do not depend on anything but the arguments.
  * Errors: SDL_ERR_INVALID_ARG (missing array, bad type, width 0, heads no multiple of kv_heads, scale below 2^-100, above
  * 2^127 or NaN, workspace too small), SDL_ERR_UNSUPPORTED (width above SDL_ATTENTION_MAX_WIDTH; more than 2^30 keys, queries times heads or
- * batch times heads), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+ * batch times heads; 2^31 and more blocks of 128 rows, or of 128 keys, of a sequence and key head), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
 #define SDL_ATTENTION_MAX_WIDTH 128u
 size_t sdl_attention_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width,
                                      sdl_dtype_t dtype);

@@ -406,6 +406,12 @@ struct Sequence {
     }
 };
 
+// A launch takes less than 2^32 threads along x.  Workgroups are numbered through rows of kGridX of them (a multiple of the dies, and 2^31 threads at 512 each); those of the last
+// row that are too many have nothing to do.
+constexpr uint32_t kGridX = 1u << 22;
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridX + blockIdx.x; }
+inline dim3 grid_of(uint64_t groups) { return groups <= kGridX ? dim3((uint32_t)groups) : dim3(kGridX, (uint32_t)((groups + kGridX - 1) / kGridX)); }
+
 // Consecutive workgroups go to different compute dies (eight, each with its own cache of 16 channels, which take turns every 256 bytes).  The `each`
 // workgroups of a unit, a (batch, key head), read the same keys and values and stay on two dies.  Where the rows of a head lie 4 KB apart, as 16
 // heads of 128 do, all of them are in one channel: so a pair of dies has 16 units at work at a time, each die a half of every unit's workgroups,

@@ -58,7 +58,9 @@ __global__ void __launch_bounds__(WAVES * kWave, sizeof(T) == 2 ? 2 : 1) sdl_att
         };
         if (!pick_item(blockIdx.x, p.batch * p.kv_heads, a.row_blocks, splits, unit, nth, split)) return;
     } else {
-        const Place place(blockIdx.x, p.batch * p.kv_heads, a.row_blocks * a.splits, p.spread);
+        const uint32_t units = p.batch * p.kv_heads, each = a.row_blocks * a.splits;
+        if (workgroup() >= units * each) return;
+        const Place place(workgroup(), units, each, p.spread);
         unit = place.unit;
         nth = place.within / a.splits;
         split = place.within % a.splits;
@@ -253,7 +255,9 @@ __global__ void __launch_bounds__(kWave) sdl_attention_few_kernel(const ForwardA
         if (!pick_item(blockIdx.x, p.batch * p.kv_heads, 1, [&](uint32_t u, uint32_t) { return of.mine(u); }, unit, nth, split)) return;
         shares = of.of(unit);
     } else {
-        const Place place(blockIdx.x, p.batch * p.kv_heads, a.splits, p.spread);
+        const uint32_t units = p.batch * p.kv_heads;
+        if (workgroup() >= units * a.splits) return;
+        const Place place(workgroup(), units, a.splits, p.spread);
         unit = place.unit;
         split = place.within;
     }
@@ -496,7 +500,7 @@ int join(const ForwardArgs& a, hipStream_t st)
 template <typename T>
 int forward(const ForwardArgs& a, bool tall, hipStream_t st)
 {
-    const dim3 grid(a.slots ? a.slots : a.row_blocks * a.splits * a.p.batch * a.p.kv_heads);
+    const dim3 grid = grid_of(a.slots ? a.slots : a.row_blocks * a.splits * a.p.batch * a.p.kv_heads);
     // keys of a tile, of half as many at widths over 64: 64 KB of shared memory (8 sequences of 1024 tokens, 12 heads of 64: 36 us with 64 keys, 32 with 128)
     constexpr int kTileKeys = sizeof(T) == 2 ? 128 : 64;
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));

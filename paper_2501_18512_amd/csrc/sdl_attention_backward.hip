@@ -80,7 +80,9 @@ __global__ void __launch_bounds__(kWaves * kWave, sizeof(T) == 2 ? 2 : 1) sdl_at
         };
         if (!pick_item(blockIdx.x, p.batch * p.kv_heads, a.blocks, splits, unit, nth, split)) return;
     } else {
-        const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
+        const uint32_t units = p.batch * p.kv_heads, each = a.blocks * a.splits;
+        if (workgroup() >= units * each) return;
+        const Place place(workgroup(), units, each, p.spread);
         unit = place.unit;
         nth = place.within / a.splits;
         split = place.within % a.splits;
@@ -247,7 +249,9 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
         };
         if (!pick_item(blockIdx.x, p.batch * p.kv_heads, a.blocks, splits, unit, block, split)) return;
     } else {
-        const Place place(blockIdx.x, p.batch * p.kv_heads, a.blocks * a.splits, p.spread);
+        const uint32_t units = p.batch * p.kv_heads, each = a.blocks * a.splits;
+        if (workgroup() >= units * each) return;
+        const Place place(workgroup(), units, each, p.spread);
         unit = place.unit;
         block = place.within / a.splits;
         split = place.within % a.splits;
@@ -504,7 +508,7 @@ int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
         a.splits = plan.keys.splits;
         a.chunk = plan.keys.chunk * key_tile_of(bf16);
         a.pick = pick_items(p, plan.row_blocks, a.splits);
-        const dim3 grid((uint32_t)(plan.row_blocks * plan.heads * plan.keys.splits));
+        const dim3 grid = grid_of(plan.row_blocks * plan.heads * plan.keys.splits);
         if (async_rows(p.k, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
             hipLaunchKernelGGL((sdl_attention_dq_kernel<T, W, true>), grid, dim3(kWaves * kWave), 0, st, a);
         else
@@ -519,7 +523,7 @@ int backward(BackwardArgs& a, const Plan& plan, hipStream_t st)
     a.chunk = plan.rows.chunk;
     a.by_heads = plan.rows.by_heads;
     a.pick = pick_items(p, plan.key_blocks, a.splits);
-    const dim3 grid((uint32_t)(plan.key_blocks * plan.heads * plan.rows.splits));
+    const dim3 grid = grid_of(plan.key_blocks * plan.heads * plan.rows.splits);
     if (async_rows(p.q, p.width, sizeof(T)) && async_rows(p.d_out, p.width, sizeof(T)) && async_rows(p.v, p.width, sizeof(T)))
         hipLaunchKernelGGL((sdl_attention_dkv_kernel<T, W, true>), grid, dim3(key_threads), 0, st, a);
     else
@@ -553,7 +557,7 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
     if (rc != SDL_OK) return rc;
     if (batch == 0 || heads == 0 || (queries == 0 && keys == 0)) return SDL_OK;
     const Plan w = plan_of(batch, queries, keys, heads, kv_heads, width, dtype);
-    // numbers of workgroups, and of threads that add sums up, that a launch can have
+    // numbers of workgroups, and of threads that add sums up, that fit 31 bits
     constexpr uint64_t kMost = 0x7fffffffu;
     if (w.row_blocks * w.heads > kMost / w.keys.splits || w.key_blocks * w.heads > kMost / w.rows.splits) return SDL_ERR_UNSUPPORTED;
     if (w.keys.splits > 1 && (uint64_t)batch * queries * heads * ((width + 3) / 4) > kMost) return SDL_ERR_UNSUPPORTED;
