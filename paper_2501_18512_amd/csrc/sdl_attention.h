@@ -231,11 +231,13 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
 template <bool ONCE>
 __device__ __forceinline__ void copy_piece(const char* base, uint32_t offset, uint32_t to)
 {
-    // a write of m0 needs one wait state before the instruction that reads it; nothing else in these kernels uses m0
+    // Five wait states between a vector instruction that writes a scalar register (the base may come from a lane) and the load that reads it, of which the write of m0 is one: the
+    // compiler does not look in here.  m0 itself needs one; the compiler holds nothing in that register from one instruction to the next (naming it as overwritten is warned
+    // of for that reason), and these kernels have no other instruction that reads it.  The wait costs 0 to 1 % of a kernel.
     if constexpr (ONCE)
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(to) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(to) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");
 }
 // Four bytes a lane, from any addresses.
 __device__ __forceinline__ void copy_word(const float* from, uint32_t to)
