@@ -42,3 +42,41 @@ def test_chunks_of_keys_against_one_pass(dtype, queries, lens):
         close(out, w["out"], e, "out")
     close(got[0][0], got[1][0].cpu().double(), 2 * e, "chunks and one pass")
     close(got[0][1], got[1][1].cpu().double(), 2 * (d + U32 * w["lse"].abs().nan_to_num(0, 0, 0)), "lse of chunks and one pass")
+
+
+@pytest.mark.parametrize("case", [(2, 5, 5, 2, 2, 64, False, None, None), (2, 100, 100, 4, 2, 128, True, None, None), (1, 128, 128, 2, 1, 40, True, [111], [120]),
+                                  (3, 60, 64, 2, 1, 96, True, None, [64, 1, 0]), (2, 128, 128, 3, 3, 30, False, None, None)])
+def test_short_rows_take_the_sum_of_p_dp_and_not_the_rounded_result(case):
+    """Values with a large part in common: d_out out and d_out v agree in it, and the rounding of the stored result would be many times larger than what is left.
+
+    As in the module that the other bounds are from, with D's error from its own sum: P |dP| off by d each and by u a term, and dP's products."""
+    B, Lq, Lk, H, G, D = case[:6]
+    q, k, v, do = _inputs(case, BF16, 41)
+    v = (v.float() + 128.0).bfloat16()
+    lens = [None if n is None else torch.tensor(n, dtype=torch.int32) for n in case[7:9]]
+    qg, kg, vg, dg = (placed(t) for t in (q, k, v, do))
+    out, lse = torch.empty_like(qg), torch.empty(B, H, Lq, device="cuda")
+    mask = dict(causal=case[6], q_len=None if lens[0] is None else lens[0].cuda(), k_len=None if lens[1] is None else lens[1].cuda())
+    space = sdl.alloc_attention(qg, kg, backward=True)
+    sdl.sdl_attention(qg, kg, vg, out, lse, space, **mask)
+    dq, dk, dv = (torch.empty_like(t) for t in (qg, kg, vg))
+    sdl.sdl_attention_backward(dg, qg, kg, vg, out, lse, dq, dk, dv, space, **mask)
+    torch.cuda.synchronize()
+    s, r = D ** -0.5, U[BF16]
+    w = ref.attention(q, k, v, s, case[6], *lens, d_out=do)
+    some = w["lse"][torch.isfinite(w["lse"])]
+    d = 2 * U32 * ((D + 4) * w["score_abs"] + 8 * (1 + float(some.abs().max())) + 8 + Lk)
+    e_q, e_k, a_q, a_k = (torch.zeros(t.shape, dtype=torch.float64) for t in (q, k, q, k))
+    for b, h, g, nq, nk, p in w["p"]:
+        qq, kk, vv, dd = (t.double() for t in (q[b, :nq, h], k[b, :nk, g], v[b, :nk, g], do[b, :nq, h]))
+        dp, size = dd @ vv.T, dd.abs() @ vv.abs().T
+        ds = p * (dp - (p * dp).sum(1, keepdim=True))
+        e_d = (p * ((d + Lk * U32) * dp.abs() + (D + 4) * U32 * size)).sum(1, keepdim=True)
+        # dk and dv start a sum from -D, of D's size: a rounding of |D| for every 16 products of it
+        e = 1.01 * (d * ds.abs() + p * ((D + 4) * U32 * (size + (p * dp).sum(1, keepdim=True).abs()) + e_d)) + r * ds.abs()
+        e_q[b, :nq, h] = s * (e @ kk.abs())
+        a_q[b, :nq, h] = s * (ds.abs() @ kk.abs())
+        e_k[b, :nk, g] += s * (e.T @ qq.abs())
+        a_k[b, :nk, g] += s * (ds.abs().T @ qq.abs())
+    close(dq, w["dq"], r * w["dq"].abs() + 1.01 * (e_q + U32 * (Lk + 2) * a_q), "dq")
+    close(dk, w["dk"], r * w["dk"].abs() + 1.01 * (e_k + U32 * (Lq * (H // G) + 2) * a_k), "dk")
