@@ -80,3 +80,18 @@ def test_short_rows_take_the_sum_of_p_dp_and_not_the_rounded_result(case):
         a_k[b, :nk, g] += s * (ds.abs().T @ qq.abs())
     close(dq, w["dq"], r * w["dq"].abs() + 1.01 * (e_q + U32 * (Lk + 2) * a_q), "dq")
     close(dk, w["dk"], r * w["dk"].abs() + 1.01 * (e_k + U32 * (Lq * (H // G) + 2) * a_k), "dk")
+
+
+def test_calls_on_another_stream_that_waits_for_their_arrays():
+    case = (2, 150, 150, 4, 2, 64, True, None, None)
+    q, k, v, do = (t.cuda() for t in _inputs(case, BF16, 5))
+    res = []
+    for stream in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        out, dq, dk, dv = (torch.full_like(t, float("nan")) for t in (q, q, k, v))
+        lse, space = torch.full((2, 4, 150), float("nan"), device="cuda"), sdl.alloc_attention(q, k, backward=True)
+        stream.wait_stream(torch.cuda.current_stream())         # everything the calls read and write is there
+        sdl.sdl_attention(q, k, v, out, lse, space, causal=True, stream=stream)
+        sdl.sdl_attention_backward(do, q, k, v, out, lse, dq, dk, dv, space, causal=True, stream=stream)
+        torch.cuda.synchronize()
+        res.append((out, lse, dq, dk, dv))
+    assert all(torch.equal(a, b) for a, b in zip(*res)) and not any(torch.isnan(t.float()).any() for t in res[0])
