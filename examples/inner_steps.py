@@ -26,15 +26,16 @@ class LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight):
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean, rstd, workspace = sdl.alloc_layer_norm(x)
+        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2))
         sdl.sdl_layer_norm(x, weight, None, EPS, y, mean, rstd)
-        ctx.save_for_backward(x, weight, mean, rstd, workspace)
+        ctx.save_for_backward(x, weight, mean, rstd)
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x, weight, mean, rstd, workspace = ctx.saved_tensors
+        x, weight, mean, rstd = ctx.saved_tensors
         dx, dweight = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty_like(weight)
+        workspace = torch.empty(sdl.sdl_layer_norm_workspace_bytes(x.shape[-1]), dtype=torch.uint8, device=x.device)
         sdl.sdl_layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, dx, dweight, None, workspace)
         return dx, dweight
 
@@ -60,16 +61,15 @@ class Attention(torch.autograd.Function):
     def forward(ctx, q, k, v):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-        workspace = sdl.alloc_attention(q, k, backward=True)
-        sdl.sdl_attention(q, k, v, out, lse, workspace, causal=True)
-        ctx.save_for_backward(q, k, v, out, lse, workspace)
+        sdl.sdl_attention(q, k, v, out, lse, sdl.alloc_attention(q, k), causal=True)
+        ctx.save_for_backward(q, k, v, out, lse)
         return out
 
     @staticmethod
     def backward(ctx, d_out):
-        q, k, v, out, lse, workspace = ctx.saved_tensors
+        q, k, v, out, lse = ctx.saved_tensors
         dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
-        sdl.sdl_attention_backward(d_out.contiguous(), q, k, v, out, lse, dq, dk, dv, workspace, causal=True)
+        sdl.sdl_attention_backward(d_out.contiguous(), q, k, v, out, lse, dq, dk, dv, sdl.alloc_attention(q, k, backward=True), causal=True)
         return dq, dk, dv
 
 
