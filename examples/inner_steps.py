@@ -3,7 +3,7 @@
 The replicas are the flat bf16 arrays that the outer step works on; the decoder's parameters are views of them.  One inner step of a
 replica: embedding, blocks of [norm, q k v projection, norm of q and k per head, rotary positions, attention, output projection; norm,
 feed-forward], final norm, head, cross entropy, backward, Adam.  Norms, rotary positions and attention are this library's calls, the
-products torch's.  The engine sends and receives what its schedule says after every step.  Then the outer parameters answer a
+products torch's.  The engine sends and receives what its schedule says after every step.  Then the mean of the replicas answers a
 prompt: once as a whole, and once token by token over a cache of keys and values.
 
     python examples/inner_steps.py [--steps 60] [--replicas 2]
@@ -170,7 +170,7 @@ def answer(shape, params, prompt, frequencies, new):
 
 
 def train(steps=60, replicas=2, batch=16, length=65, H=20, tau=2, lr=3e-3, seed=0, say=print):
-    """Returns the losses [steps][replicas], the shape, the outer parameters as bf16 and the frequencies."""
+    """Returns the losses [steps][replicas], the shape, the mean of the replicas as bf16 and the frequencies."""
     shape = Shape()
     plan = sdl.sdl_fragment_plan(shape.numel, [u for _, _, u in shape.groups], shape.blocks, 2, sdl.PATTERN_STRIDED, H, tau)
     total = plan.total_numel
