@@ -504,10 +504,11 @@ int forward(const ForwardArgs& a, bool tall, hipStream_t st)
     // keys of a tile, of half as many at widths over 64: 64 KB of shared memory (8 sequences of 1024 tokens, 12 heads of 64: 36 us with 64 keys, 32 with 128)
     constexpr int kTileKeys = sizeof(T) == 2 ? 128 : 64;
     const bool async = async_rows(a.p.k, a.p.width, sizeof(T)) && async_rows(a.p.v, a.p.width, sizeof(T));
-    // Keys and values of 32 MB and more go past the caches: a decoder has a dozen such caches and more, and one is long gone from the memory-side cache
-    // (256 MB) when its turn comes again.  16 requests of up to 8192 tokens (134 MB read): 36 us past the caches and 38 through them where others were read in
-    // between, 37 and 32 where the same ones are read over and over; 64 requests of 8192 (537 MB): 163 and 188.
-    const bool once = 2 * (uint64_t)a.p.batch * a.p.keys * a.p.kv_heads * a.p.width * sizeof(T) >= (1u << 25);
+    // Keys and values of 128 MB and more go past the caches: two of them are more than the memory-side cache (256 MB) holds, and a decoder has one a block.  Single tokens, 16 heads over 4
+    // of 128, through the caches and past them, a dozen caches in turn and the same one over and over: 34 MB 17.4 and 17.1 us, 15.0 and 17.2; 67 MB 21.3 and 20.7, 18.8 and 20.0; 134 MB
+    // 35.0 and 31.9, 29.6 and 30.5; 268 MB 58 and 52, 48 and 49.  The valid lengths are in device memory, so it goes by what the caches have room for; half of it valid, 134 MB
+    // 24.2 and 23.1, 20.7 and 21.2; 268 MB 35.5 and 33.1, 30.5 and 30.8.
+    const bool once = 2 * (uint64_t)a.p.batch * a.p.keys * a.p.kv_heads * a.p.width * sizeof(T) >= (1u << 27);
     if (a.few) {
 #define SDL_FEW(W)                                                                                                                    \
     do {                                                                                                                              \

@@ -37,3 +37,14 @@ def test_rows_of_every_kind_of_width(dtype):
             print(f"attention width {width} {how} {dtype}", flush=True)
             _check((2, 70, 75, 2, 1, width, True, [70, 33], [75, 40]), dtype, how, seed=500 + i)
             _check((1, 1, 200, 4, 2, width, True, None, [131]), dtype, how, seed=600 + i)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("case", [
+    (8, 1, 8300, 8, 4, 128, True, None, [8300, 1, 0, 4000, 31, 32, 33, 8299]), (8, 2, 11000, 4, 4, 96, True, None, None),
+    (8, 1, 16500, 4, 4, 64, False, None, [16500, 5, 0, 128, 129, 9000, 12345, 64]), (9, 1, 33000, 4, 4, 32, True, None, None)])
+def test_caches_that_go_past_the_devices_own(dtype, case):
+    """Single tokens over keys and values of 128 MB and more."""
+    assert 2 * case[0] * case[2] * case[4] * case[5] * 2 >= 1 << 27
+    for how in ("dense", "heads"):
+        _check(case, dtype, how, seed=23)
