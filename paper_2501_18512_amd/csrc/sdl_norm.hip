@@ -285,7 +285,8 @@ __global__ void __launch_bounds__(1024) sdl_norm_sum_kernel(const SumArgs a)
 }
 
 // Workgroups of a backward launch, at most: one for every compute unit, as each leaves a line of sums; two for rows that are little to wait for and still keep most of a
-// wavefront's lanes (16,384 rows of 300 in bf16, with the column sums: 22.3 us with 256 and 19.9 with 768; 98,304 of 64: 12.6 and 14.2).
+// wavefront's lanes.  With the column sums, in us, 256 / 512 / 768 of them: 16,384 rows in bf16 of 128 6.7 / 7.1 / 7.1, of 192 10.6 / 9.6 / 11.8, of 300 19.9 / 16.1 / 18.6 (fp32 20.2 /
+// 16.9 / 18.6), of 512 13.9 / 13.6 / 13.9, of 520 21.1 / 22.9 / 24.8; 98,304 of 64 11.2 / 11.0 / 11.5; 8192 of 768 13.9 / 15.8 / 17.9.
 constexpr uint32_t most_lines(uint32_t width) { return width > 128 && width <= 512 ? 512 : 256; }
 // Of a forward launch: four for every compute unit, and eight of those with two rows at a time.  Two wavefronts a row at widths over 1024, 8192 rows of 2048 in bf16
 // 14.3 us with one and 13.1 with two, 16,384 of 1500 29 and 26; 8192 rows of 768, of one wavefront, 8.8 us with 1024 workgroups and 9.8 with 2048.
