@@ -690,7 +690,7 @@ def sdl_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = ROTAR
 
 def sdl_rotary(x, positions, frequencies, out, layout: int = ROTARY_HALF, scale: float = 1.0, inverse: bool = False,
                first_position: int = 0, stream=None):
-    """positions: int32 [batch, tokens], or None for first_position, first_position + 1, ...; frequencies: fp64 [rot / 2] on the device."""
+    """positions: int32 [batch, tokens], contiguous, or None for first_position, first_position + 1, ...; frequencies: fp64 [rot / 2] on the device."""
     _check(_operators.sdl_rotary(x, positions, frequencies, out, layout, scale, inverse, first_position, stream), "sdl_rotary")
 
 

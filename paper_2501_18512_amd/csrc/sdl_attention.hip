@@ -7,10 +7,10 @@
 // log sums in the workspace, and a second kernel joins them.  Chunks have one size whatever a sequence's length, so that short sequences beside
 // long ones leave no one waiting.
 //
-// In bf16 at width 128 the matrix units are busy for a third of the cycles and the vector units for two fifths (exponentials, the rounding of P), the two for the
+// In bf16 at width 128 the matrix units are busy for 34 to 45 % of the cycles and the vector units for 38 to 43 % (exponentials, the rounding of P), the two for the
 // most part not at once: a workgroup's wavefronts do the same at the same time, and the registers hold two of them on a SIMD.  2 sequences of 4096
-// tokens, 16 heads, no mask: 280 us, 980 TFLOP/s (a library product of 8192^3: 1294); 8192 causal tokens: 275 us, 1000; 4 of 2048: 106 us, 650, where a
-// workgroup's start and end are a sixth of its life.  In fp32 the matrix instructions bound it: 121 to 128 of 155 TFLOP/s.
+// tokens, 16 heads, no mask: 269 us, 1020 TFLOP/s (a library product of 8192^3: 1294); 8192 causal tokens: 275 us, 1000; 4 of 2048: 93 us, 740 (104 on another card), where a
+// workgroup's start and end are a sixth of its life.  In fp32 the matrix instructions bound it: 122 to 126 of 155 TFLOP/s without a mask, 107 in 4 causal sequences of 2048.
 #include <hip/hip_runtime.h>
 
 #include <cmath>

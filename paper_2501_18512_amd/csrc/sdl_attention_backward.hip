@@ -10,9 +10,10 @@
 // D is worked out by the first and read by the second.  Where the workgroups are too few to fill the chip, a chunk of the keys (or of the
 // rows) goes to a workgroup each, which leaves its sums in the workspace, and a third kernel adds them up in order.
 //
-// In bf16 the registers allow two wavefronts on a SIMD, which keep the matrix units busy for about two fifths of the cycles.  2 sequences of 4096 tokens, 16 heads of
-// 128, no mask: 868 us, 792 TFLOP/s of the five products that count, 1110 of the seven; 4 causal ones of 2048: 128 us for dq and 185 for dk and dv; 8 of 1024, 12 heads of 64:
-// 45 and 52.  In fp32 the matrix instructions bound it: 119 TFLOP/s of seven products at width 128.
+// In bf16 the registers allow two wavefronts on a SIMD, which keep the matrix units busy for half of the cycles in long sequences and for 37 % in 4 causal ones of 2048 tokens.  2 sequences
+// of 4096 tokens, 16 heads of 128, no mask: 384 us for dq and 495 for dk and dv, 780 TFLOP/s of the five products that count, 1090 of the seven; 4 causal ones of 2048: 127 and 166 (140 and 187 on
+// another card); 8 of 1024, 12 heads of 64: 44 and 50.  In fp32 the matrix instructions bound it: 118 to 125 TFLOP/s of seven products at width 128 and no mask, 109 to 113 in 4 causal
+// sequences of 2048 (a library product 155).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -320,7 +321,6 @@ __global__ void __launch_bounds__(key_waves(sizeof(T) == 2, W > 64) * kWave, siz
 #pragma unroll
         for (int part = 0; part < kTile; part += 32) {
             if (t0 + part + 31 < t_some) continue;
-                    // reads of the next part this early would not leave enough registers
             uint32_t v_at = lds_offset(mem.v) + wave * 32 / Smem::kGroup * Smem::kGroupBytes;
             asm volatile("" : "+s"(v_at));         // the lane's addresses in it would take four registers through the loop
             f32x16_t sc = {}, dp = {};

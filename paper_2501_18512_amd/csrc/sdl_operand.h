@@ -22,7 +22,7 @@ struct View {
     int64_t batch, token, head;
 };
 
-// n / d for n < 2^31 by one multiplication: with 2^l the least power of two >= d, n/d = (floor(m n / 2^32) + n) >> l
+// n / d for n < 2^31 by one multiplication (T. Granlund, P. L. Montgomery, Division by invariant integers using multiplication, 1994): with 2^l the least power of two >= d, n/d = (floor(m n / 2^32) + n) >> l
 // for m = floor(2^32 (2^l - d) / d) + 1.
 struct Div {
     uint32_t m, l, d;
