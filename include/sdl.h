@@ -589,8 +589,9 @@ int sdl_attention(const sdl_view_t* q, const sdl_view_t* k, const sdl_view_t* v,
  *     D = sum over the width of d_out out,  dS = P (d_out v^T - D),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T d_out
  * dk and dv of a key head are the sums over its query heads.  Rows behind a length, and of queries that see nothing, are 0.  The order of
  * every sum is fixed by the arguments: two calls give the same bits.  dq, dk, dv are written, not added to; they may lie in one array.
- * bf16: P and dS are rounded to bf16 before they meet d_out, q and k; D is taken from the stored out, which is rounded, and in
- * rows of few keys, where that would count, as the sum over the keys of P (d_out v^T), which is the same number.
+ * bf16: P and dS are rounded to bf16 before they meet d_out, q and k; D is taken from the stored out, and has its rounding in it (2^-9 of
+ * d_out out on average, which counts where all values have a large part in common), but in blocks of 128 rows that see up to 128 keys, where it would count most, as the
+ * sum over the keys of P (d_out v^T), which is the same number.
  * workspace: as above, sdl_attention_backward_workspace_bytes(...) bytes.  Errors as above. */
 size_t sdl_attention_backward_workspace_bytes(uint32_t batch, uint32_t queries, uint32_t keys, uint32_t heads, uint32_t kv_heads, uint32_t width,
                                               sdl_dtype_t dtype);
