@@ -17,7 +17,8 @@
  * diagnostics on the same arrays.  sdl_fragment_outer_step_plan_static is the fused step
  * for callers that cannot allocate; sdl_flat_layout says where to put the flat arrays and
  * sdl_memory_probe measures what the memory system gives (neither is part of the method).
- * sdl_layer_norm*, sdl_rotary* and sdl_attention* are the operators of the decoder between two outer steps.
+ * sdl_layer_norm*, sdl_rotary* and sdl_attention* are the operators of the decoder between two outer steps, sdl_embedding* and
+ * sdl_cross_entropy* those at its two ends; sdl_orthogonalize makes an update of its matrices.
  * The M replicas ("workers") are M parameter arrays
  * resident in one GPU's memory; no call communicates with another device.
  *
@@ -600,6 +601,62 @@ int sdl_attention_backward(const sdl_view_t* d_out, const sdl_view_t* q, const s
                            uint32_t width, sdl_dtype_t dtype, float scale, int causal, const int32_t* q_len, const int32_t* k_len,
                            const sdl_view_t* dq, const sdl_view_t* dk, const sdl_view_t* dv, void* workspace, size_t workspace_bytes,
                            void* stream);
+
+/* ---- The decoder's two ends, and the update of its matrices ---------------------------
+ *
+ * Conventions as for the operators above.  Arrays of rows are views whose stride_head is not looked at: [batch][tokens][width]. */
+
+/* Type of arrays of tokens: [batch][tokens], contiguous, in device memory. */
+typedef enum { SDL_INDEX_INT32 = 0, SDL_INDEX_INT64 = 1 } sdl_index_t;
+
+/* Embedding: out[b][t] = scale * table[tokens[b][t]].  table: [vocab][width], its rows table_stride elements apart.  A token that is
+ * not in [0, vocab), as padding, gives a row of zeros.  The product is fp32, rounded once to dtype, which need not be the table's.
+ * Errors: SDL_ERR_INVALID_ARG (missing array, bad type, width 0, scale not finite), SDL_ERR_UNSUPPORTED (width above SDL_EMBEDDING_MAX_WIDTH,
+ * 2^31 rows and more, of the table or of out), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+#define SDL_EMBEDDING_MAX_WIDTH 65536u
+int sdl_embedding(const void* table, int64_t table_stride, uint32_t vocab, uint32_t width, sdl_dtype_t table_dtype, const void* tokens, sdl_index_t index,
+                  uint32_t batch, uint32_t tokens_of_batch, float scale, const sdl_view_t* out, sdl_dtype_t dtype, void* stream);
+
+/* The gradient of its table: d_table[v] = scale * the sum of d_out[b][t] over the places with tokens[b][t] = v, in fp32, rounded once to table_dtype.
+ * All rows are written, not added to; those of tokens that do not come are zeros.  The order of the sums is fixed by the arguments: two calls give the
+ * same bits.  workspace: device memory, 8-byte aligned, of at least sdl_embedding_workspace_bytes(batch * tokens_of_batch, width) bytes, contents
+ * irrelevant.  Errors as above, and SDL_ERR_INVALID_ARG (workspace too small), SDL_ERR_UNSUPPORTED (more than SDL_EMBEDDING_MAX_PLACES tokens). */
+#define SDL_EMBEDDING_MAX_PLACES 268435456u
+size_t sdl_embedding_workspace_bytes(uint64_t places, uint32_t width);
+int sdl_embedding_backward(const sdl_view_t* d_out, sdl_dtype_t dtype, const void* tokens, sdl_index_t index, uint32_t batch, uint32_t tokens_of_batch,
+                           float scale, void* d_table, int64_t table_stride, uint32_t vocab, uint32_t width, sdl_dtype_t table_dtype, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Cross entropy of logits x [batch][tokens][vocab] with one target a row, smoothed, and with the z term that keeps lse near 0 (Section 3.2 of the paper trains
+ * with z = 1e-4):
+ *     lse = log sum exp(x),  loss = lse - (1 - smoothing) x[target] - smoothing * mean(x) + z lse^2
+ *     d_x = d_loss ((1 + 2 z lse) exp(x - lse) - smoothing / vocab - (1 - smoothing) [target])
+ * loss, lse, d_loss: fp32 [batch][tokens].  A row whose target is not in [0, vocab) has loss 0, lse 0 and a gradient of zeros, whatever its logits are (they are not
+ * read).  A logit of -infinity is a token that cannot come (its loss as a target is infinite); a row with NaN or +infinity, or with nothing but -infinity, gives NaN, to itself only.
+ * d_logits: NULL, or the gradient in the same pass, in the logits' type; it may be logits itself, with the same strides.  d_loss: NULL for 1.  loss, lse: NULL where
+ * not wanted.  Errors: SDL_ERR_INVALID_ARG (missing array, bad type, vocab 0, smoothing outside [0, 1], z negative or not finite, nothing to write),
+ * SDL_ERR_UNSUPPORTED (vocab above SDL_CROSS_ENTROPY_MAX_VOCAB, 2^31 rows and more), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+#define SDL_CROSS_ENTROPY_MAX_VOCAB 16777216u
+int sdl_cross_entropy(const sdl_view_t* logits, uint32_t batch, uint32_t tokens, uint32_t vocab, sdl_dtype_t dtype, const void* targets, sdl_index_t index,
+                      float smoothing, float z, float* loss, float* lse, const float* d_loss, const sdl_view_t* d_logits, void* stream);
+/* The gradient alone, from the forward pass' lse. */
+int sdl_cross_entropy_backward(const sdl_view_t* logits, uint32_t batch, uint32_t tokens, uint32_t vocab, sdl_dtype_t dtype, const void* targets, sdl_index_t index,
+                               float smoothing, float z, const float* lse, const float* d_loss, const sdl_view_t* d_logits, void* stream);
+
+/* Orthogonalised matrices, as an update by Newton-Schulz steps takes them: of every matrix x [rows][cols] of a batch, with X = x / (norm(x) + eps) (the root of the sum
+ * of squares; of a matrix with more rows than columns, the transpose),
+ *     for every (a, b, c):  A = X X^T,  X = a X + (b A + c A^2) X          out = scale X
+ * which takes every singular value s of X to a s + b s^3 + c s^5 and leaves the singular vectors.  x, out: views [batch][rows][cols] (stride_token between rows).
+ * coefficients: HOST array [steps][3], read during the call; the polynomials, one after the other, may take no s in [0, 1] beyond 2.  out may be x itself, with the same
+ * strides and type.  Products have 11 bits of each operand and fp32 sums where out is bf16, 22 bits where it is fp32; X, norms and what is added to a X are fp32 (norms
+ * 64 bits).  A matrix of zeros gives zeros; one with NaN or infinity gives NaN, to itself only.  workspace: device memory, 16-byte aligned, of at least
+ * sdl_orthogonalize_workspace_bytes(...) bytes, contents irrelevant.
+ * Errors: SDL_ERR_INVALID_ARG (missing array, bad type, no steps, coefficients, eps negative or not finite, scale not finite, workspace too small), SDL_ERR_UNSUPPORTED
+ * (a side above SDL_ORTHOGONALIZE_MAX_SIDE, 2^16 matrices and more, more than 2^22 tiles of 64 by 64), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */
+#define SDL_ORTHOGONALIZE_MAX_SIDE 65536u
+size_t sdl_orthogonalize_workspace_bytes(uint32_t batch, uint32_t rows, uint32_t cols, sdl_dtype_t out_dtype);
+int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32_t cols, sdl_dtype_t dtype, const float* coefficients, uint32_t steps, float eps,
+                      float scale, const sdl_view_t* out, sdl_dtype_t out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* sdl_status_string(int status);
 

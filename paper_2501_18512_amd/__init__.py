@@ -137,6 +137,16 @@ def _load() -> ctypes.CDLL:
         getattr(lib, name).restype = ctypes.c_size_t
     lib.sdl_attention.argtypes = [pv, pv, pv, *shape6, ctypes.c_int, f32, ctypes.c_int, vp, vp, pv, vp, vp, ctypes.c_size_t, vp]
     lib.sdl_attention_backward.argtypes = [pv] * 5 + [vp, *shape6, ctypes.c_int, f32, ctypes.c_int, vp, vp, pv, pv, pv, vp, ctypes.c_size_t, vp]
+    pf = ctypes.POINTER(f32)
+    lib.sdl_embedding.argtypes = [vp, ctypes.c_int64, u32, u32, ctypes.c_int, vp, ctypes.c_int, u32, u32, f32, pv, ctypes.c_int, vp]
+    lib.sdl_embedding_workspace_bytes.argtypes = [u64, u32]
+    lib.sdl_embedding_workspace_bytes.restype = ctypes.c_size_t
+    lib.sdl_embedding_backward.argtypes = [pv, ctypes.c_int, vp, ctypes.c_int, u32, u32, f32, vp, ctypes.c_int64, u32, u32, ctypes.c_int, vp, ctypes.c_size_t, vp]
+    lib.sdl_cross_entropy.argtypes = [pv, u32, u32, u32, ctypes.c_int, vp, ctypes.c_int, f32, f32, vp, vp, vp, pv, vp]
+    lib.sdl_cross_entropy_backward.argtypes = [pv, u32, u32, u32, ctypes.c_int, vp, ctypes.c_int, f32, f32, vp, vp, pv, vp]
+    lib.sdl_orthogonalize_workspace_bytes.argtypes = [u32, u32, u32, ctypes.c_int]
+    lib.sdl_orthogonalize_workspace_bytes.restype = ctypes.c_size_t
+    lib.sdl_orthogonalize.argtypes = [pv, u32, u32, u32, ctypes.c_int, pf, u32, f32, f32, pv, ctypes.c_int, vp, ctypes.c_size_t, vp]
     lib.sdl_status_string.argtypes = [ctypes.c_int]
     lib.sdl_status_string.restype = ctypes.c_char_p
     return lib
@@ -145,7 +155,7 @@ def _load() -> ctypes.CDLL:
 _lib = _load()
 
 try:
-    from . import _binding, _operators
+    from . import _binding, _operators, _training
 except ImportError as e:
     raise ImportError("an extension module of the binding is missing or does not load: build it with `python paper_2501_18512_amd/build.py` "
                       "(there is no fallback path)") from e
@@ -210,6 +220,8 @@ _binding.setup({name: ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value fo
                _stream, torch.cuda.is_initialized, _get_device, _raw_stream)
 _operators.setup({name: ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in dir(_operators) if name.startswith("sdl_")},
                  (torch.float32, torch.bfloat16, torch.int32, torch.float64), _stream, torch.cuda.is_initialized, _get_device, _raw_stream)
+_training.setup({name: ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in dir(_training) if name.startswith("sdl_")},
+                (torch.float32, torch.bfloat16, torch.int32, torch.int64), _stream, torch.cuda.is_initialized, _get_device, _raw_stream)
 
 
 def _require_device(*tensors):
@@ -731,3 +743,56 @@ def sdl_attention_backward(d_out, q, k, v, out, lse, dq, dk, dv, workspace, scal
         scale = q.shape[-1] ** -0.5
     _check(_operators.sdl_attention_backward(d_out, q, k, v, out, lse, dq, dk, dv, workspace, scale, causal, q_len, k_len, stream),
            "sdl_attention_backward")
+
+
+# ------------------------------------------------------------------ the decoder's two ends, and the update of its matrices
+
+INDEX_INT32, INDEX_INT64 = 0, 1
+EMBEDDING_MAX_WIDTH, EMBEDDING_MAX_PLACES, CROSS_ENTROPY_MAX_VOCAB, ORTHOGONALIZE_MAX_SIDE = 65536, 1 << 28, 1 << 24, 65536
+# Five steps of the Muon optimizer's polynomial (K. Jordan et al., 2024), which lifts small singular values fast and leaves all of them between about 0.7 and 1.2, and
+# of Newton and Schulz's cubic one, which goes to 1 itself, slowly.
+ORTHOGONALIZE_QUINTIC = ((3.4445, -4.7750, 2.0315),) * 5
+ORTHOGONALIZE_CUBIC = ((1.5, -0.5, 0.0),) * 12
+
+
+def sdl_embedding(table, tokens, out, scale: float = 1.0, stream=None):
+    """table: [vocab, width]; tokens: int32 or int64, contiguous, one for every row of out [batch, tokens, width] (fewer dimensions from the right)."""
+    _check(_training.sdl_embedding(table, tokens, out, scale, stream), "sdl_embedding")
+
+
+def sdl_embedding_workspace_bytes(places: int, width: int) -> int:
+    return _lib.sdl_embedding_workspace_bytes(places, width)
+
+
+def alloc_embedding(tokens, width: int):
+    """Workspace for sdl_embedding_backward of these tokens."""
+    return torch.empty(max(_lib.sdl_embedding_workspace_bytes(tokens.numel(), width), 8), dtype=torch.uint8, device=tokens.device)
+
+
+def sdl_embedding_backward(d_out, tokens, d_table, workspace, scale: float = 1.0, stream=None):
+    _check(_training.sdl_embedding_backward(d_out, tokens, d_table, workspace, scale, stream), "sdl_embedding_backward")
+
+
+def sdl_cross_entropy(logits, targets, loss, lse=None, d_logits=None, d_loss=None, smoothing: float = 0.0, z: float = 0.0, stream=None):
+    """logits: [batch, tokens, vocab] (fewer dimensions from the right); targets: int32 or int64, contiguous, one for every row; loss, lse, d_loss: fp32, as many.
+    d_logits: the gradient in the same pass, None where it is not wanted; d_loss: None for 1."""
+    _check(_training.sdl_cross_entropy(logits, targets, loss, lse, d_logits, d_loss, smoothing, z, stream), "sdl_cross_entropy")
+
+
+def sdl_cross_entropy_backward(logits, targets, lse, d_logits, d_loss=None, smoothing: float = 0.0, z: float = 0.0, stream=None):
+    _check(_training.sdl_cross_entropy_backward(logits, targets, lse, d_logits, d_loss, smoothing, z, stream), "sdl_cross_entropy_backward")
+
+
+def sdl_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, out_dtype: int) -> int:
+    return _lib.sdl_orthogonalize_workspace_bytes(batch, rows, cols, out_dtype)
+
+
+def alloc_orthogonalize(x, out):
+    """Workspace for sdl_orthogonalize of a matrix or a batch of them."""
+    batch, rows, cols = (1, *x.shape) if x.dim() == 2 else x.shape
+    return torch.empty(max(_lib.sdl_orthogonalize_workspace_bytes(batch, rows, cols, _dtype(out)), 16), dtype=torch.uint8, device=x.device)
+
+
+def sdl_orthogonalize(x, out, workspace, coefficients=ORTHOGONALIZE_QUINTIC, eps: float = 1e-7, scale: float = 1.0, stream=None):
+    """x, out: [rows, cols] or [batch, rows, cols], of one shape; coefficients: (a, b, c) of every step."""
+    _check(_training.sdl_orthogonalize(x, out, workspace, coefficients, eps, scale, stream), "sdl_orthogonalize")

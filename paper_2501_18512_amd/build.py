@@ -9,11 +9,12 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("sdl_kernels.hip", "sdl_cosine.hip", "sdl_eval.hip", "sdl_norm.hip", "sdl_rotary.hip",
-                                                   "sdl_attention.hip", "sdl_attention_backward.hip", "sdl_plan.cpp", "sdl_engine.cpp",
-                                                   "sdl_offload.cpp")]
+                                                   "sdl_attention.hip", "sdl_attention_backward.hip", "sdl_embedding.hip", "sdl_cross_entropy.hip",
+                                                   "sdl_orthogonalize.hip", "sdl_plan.cpp", "sdl_engine.cpp", "sdl_offload.cpp")]
 LIB = os.path.join(HERE, "libsdl.so")
 BINDING = os.path.join(HERE, "_binding.so")
 OPERATORS = os.path.join(HERE, "_operators.so")
+TRAINING = os.path.join(HERE, "_training.so")
 
 # -ffp-contract=off: every fp32 operation of the method rounds once, in the documented order.
 # packed fp32 instructions are switched off for the test machines of machines.
@@ -23,7 +24,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp
 
 
 def build_binding(verbose: bool = False) -> str:
-    for out, src in ((BINDING, "sdl_binding.c"), (OPERATORS, "sdl_operators.c")):
+    for out, src in ((BINDING, "sdl_binding.c"), (OPERATORS, "sdl_operators.c"), (TRAINING, "sdl_training.c")):
         cmd = [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
                "-o", out, os.path.join(HERE, "csrc", src)]
         if verbose:

@@ -1,0 +1,480 @@
+// Embedding lookup and the gradient of its table (gfx950).
+//
+// Forward: out[t] = scale * table[token[t]], a gather of rows: bound by memory, every element is touched once.
+//
+// Backward: d_table[v] = scale * sum of d_out[t] over the places t with token[t] = v.  Every row of the table is written, most of
+// them as zeros, and every row of d_out is read once; no atomics, one order of every sum.  What is done:
+//   1. sort   chunks of 2048 places are sorted by (token, place) in shared memory; meanwhile other workgroups write zeros
+//   2. merge  (more than one chunk) the rank of a place is its rank in its chunk and, by bisection, in the others: up to 32 sorted
+//             runs become one, again and again until one is left
+//   3. reduce the sorted places are cut into segments of equal length, whatever the tokens are.  A run of one token that lies within a segment is
+//             added up and written; one that goes on over an end leaves a line of fp32 sums
+//   4. join   adds up the lines of every run that crosses an end, in order
+// So a token that is every second one costs what others do.  The zeros are most of the bytes: written beside the sorting, which few
+// workgroups do and which waits most of its time, they hide it.
+#include "sdl_operand.h"
+
+namespace {
+
+using namespace sdl_device;
+
+constexpr uint32_t kNone = 0xffffffffu;     // token of a place that is not in the table: behind all others
+
+struct Tokens {
+    const void* at;
+    uint32_t wide, vocab;       // 64 bits each; rows of the table
+    // the token, or kNone
+    __device__ __forceinline__ uint32_t get(uint32_t i) const
+    {
+        const int64_t t = wide ? static_cast<const int64_t*>(at)[i] : (int64_t) static_cast<const int32_t*>(at)[i];
+        return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : kNone;
+    }
+};
+
+struct Places {
+    Div tokens;                 // n = batch * tokens places
+    uint32_t n, width;
+    View rows;                  // out or d_out
+};
+
+template <typename T>
+__device__ __forceinline__ T* place_row(const Places& p, uint32_t i)
+{
+    const uint32_t b = div(i, p.tokens), t = i - b * p.tokens.d;
+    return reinterpret_cast<T*>(p.rows.data) + ((int64_t)b * p.rows.batch + (int64_t)t * p.rows.token);
+}
+
+struct LookupArgs {
+    Places places;
+    Tokens tokens;
+    const char* table;
+    int64_t stride;
+    float scale;
+};
+
+// LPR lanes a row, ROWS rows at a time each, so that their loads are under way together.
+template <typename P, typename T, int LPR, int ROWS>
+__global__ void __launch_bounds__(256) sdl_embedding_kernel(const LookupArgs a)
+{
+    constexpr uint32_t kTeams = 256 / LPR;
+    const uint32_t lane = threadIdx.x % LPR, W = a.places.width;
+    const uint32_t first = (workgroup() * kTeams + threadIdx.x / LPR) * ROWS;
+    uint32_t v[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) v[r] = first + r < a.places.n ? a.tokens.get(first + r) : kNone;
+    for (uint32_t at = lane * 8; at < W; at += LPR * 8) {
+        Eight<P> e[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            e[r] = Eight<P>{};
+            if (v[r] != kNone) e[r] = load8(reinterpret_cast<const P*>(a.table) + (int64_t)v[r] * a.stride, at, W);
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (first + r >= a.places.n) break;
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = v[r] == kNone ? 0.0f : e[r].get(j) * a.scale;
+            store8(place_row<T>(a.places, first + r), at, W, x);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ backward
+
+constexpr uint32_t kChunk = 2048;           // places that a workgroup sorts
+constexpr uint32_t kFan = 32;               // sorted runs that become one
+constexpr uint32_t kFill = 1024 * 8;        // elements of a table without gaps that a workgroup clears at a time
+
+struct Table {
+    char* data;
+    int64_t stride;
+    uint32_t vocab, width;
+};
+
+// A share of the table's zeros: pieces [lo, hi) of a table without gaps, or rows.
+struct Fill {
+    Table table;
+    uint64_t lo, hi;
+    uint32_t dense;
+};
+
+template <typename P>
+__device__ __forceinline__ void fill(const Fill& f, uint32_t group, uint32_t groups)
+{
+    const float zero[8] = {};
+    if (f.dense) {
+        const uint64_t numel = (uint64_t)f.table.vocab * f.table.width;
+        for (uint64_t i = f.lo + group; i < f.hi; i += groups) {
+            const uint64_t at = i * kFill;
+            const uint32_t n = (uint32_t)min((uint64_t)kFill, numel - at);
+            if (threadIdx.x * 8 < n) store8(reinterpret_cast<P*>(f.table.data) + at, threadIdx.x * 8, n, zero);
+        }
+    } else {
+        for (uint64_t i = f.lo + group; i < f.hi; i += groups)
+            for (uint32_t at = threadIdx.x * 8; at < f.table.width; at += 1024 * 8)
+                store8(reinterpret_cast<P*>(f.table.data) + (int64_t)i * f.table.stride, at, f.table.width, zero);
+    }
+}
+
+struct SortArgs {
+    Tokens tokens;
+    uint32_t n, chunks;
+    uint64_t* keys;             // token << 32 | place
+    Fill fill;
+};
+
+// Bitonic sort of one chunk (K. E. Batcher, Sorting networks and their applications, 1968): keys differ, so that equal tokens keep their order.
+template <typename P>
+__global__ void __launch_bounds__(1024) sdl_embedding_sort_kernel(const SortArgs a)
+{
+    __shared__ uint64_t k[kChunk];
+    if (blockIdx.x >= a.chunks) {
+        fill<P>(a.fill, blockIdx.x - a.chunks, gridDim.x - a.chunks);
+        return;
+    }
+    const uint32_t base = blockIdx.x * kChunk, n = min(kChunk, a.n - base);
+    uint32_t size = 2;
+    while (size < n) size *= 2;
+    for (uint32_t i = threadIdx.x; i < size; i += 1024) k[i] = i < n ? ((uint64_t)a.tokens.get(base + i) << 32) | (base + i) : ~0ull;
+    __syncthreads();
+    for (uint32_t s = 2; s <= size; s *= 2) {
+        for (uint32_t j = s / 2; j; j /= 2) {
+            const uint32_t t = threadIdx.x;
+            if (t < size / 2) {
+                const uint32_t i = 2 * t - (t & (j - 1));
+                const uint64_t x = k[i], y = k[i + j];
+                if ((x > y) == ((i & s) == 0)) {
+                    k[i] = y;
+                    k[i + j] = x;
+                }
+            }
+            __syncthreads();
+        }
+    }
+    for (uint32_t i = threadIdx.x; i < n; i += 1024) a.keys[base + i] = k[i];
+}
+
+struct MergeArgs {
+    const uint64_t* from;
+    uint64_t* to;
+    uint32_t n, run, groups;    // length of the sorted runs; workgroups that merge
+    Fill fill;
+};
+
+// Keys of runs[r] that are less than `key`, for SEARCHES runs at a time: bisections that wait for memory together.
+template <typename P>
+__global__ void __launch_bounds__(1024) sdl_embedding_merge_kernel(const MergeArgs a)
+{
+    if (blockIdx.x >= a.groups) {
+        fill<P>(a.fill, blockIdx.x - a.groups, gridDim.x - a.groups);
+        return;
+    }
+    // four lanes share a place: each looks it up in every fourth run
+    const uint32_t share = threadIdx.x % 4;
+    const uint64_t p64 = (uint64_t)blockIdx.x * 256 + threadIdx.x / 4;
+    const bool mine = p64 < a.n;
+    const uint32_t p = mine ? (uint32_t)p64 : a.n - 1;
+    const uint32_t own = p / a.run, first = own / kFan * kFan, runs = (a.n - 1) / a.run + 1;
+    const uint64_t key = a.from[p];
+    uint32_t rank = share == 0 ? p - own * a.run : 0;
+    constexpr int kSearches = 8;
+    static_assert(kSearches * 4 == kFan, "all of a group's runs at once");
+    uint32_t lo[kSearches], len[kSearches];
+#pragma unroll
+    for (int i = 0; i < kSearches; ++i) {
+        const uint32_t r = first + i * 4 + share;
+        const bool there = r < runs && r != own;
+        lo[i] = there ? r * a.run : 0;
+        len[i] = there ? min(a.run, a.n - r * a.run) : 0;
+    }
+    for (uint32_t left = a.run; left; left /= 2) {        // lengths fall below their half, rounded down, or come to it
+#pragma unroll
+        for (int i = 0; i < kSearches; ++i) {
+            if (!len[i]) continue;
+            const uint32_t half = len[i] / 2;
+            const bool less = a.from[lo[i] + half] < key;
+            rank += less ? half + 1 : 0;
+            lo[i] += less ? half + 1 : 0;
+            len[i] = less ? len[i] - half - 1 : half;
+        }
+    }
+    rank += __shfl_xor(rank, 1);
+    rank += __shfl_xor(rank, 2);
+    if (mine && share == 0) a.to[first * a.run + rank] = key;
+}
+
+struct ReduceArgs {
+    Places places;
+    Table table;
+    const uint64_t* keys;
+    float* lines;               // [segments][2][width]: sums of the run that comes in over a segment's start, and of the one that leaves over its end
+    Div slices;                 // parts of LPR * 8 columns
+    uint32_t segments, length;
+    float scale;
+};
+
+__device__ __forceinline__ uint32_t token_of(uint64_t key) { return (uint32_t)(key >> 32); }
+
+template <typename P>
+__device__ __forceinline__ void write_row(const Table& t, uint32_t v, uint32_t at, float scale, const float* acc)
+{
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = acc[j] * scale;
+    store8(reinterpret_cast<P*>(t.data) + (int64_t)v * t.stride, at, t.width, x);
+}
+
+// LPR lanes have eight columns each of one segment; eight rows are under way at a time.
+template <typename T, typename P, int LPR>
+__global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceArgs a)
+{
+    constexpr uint32_t kTeams = 256 / LPR;
+    const uint32_t unit = blockIdx.x * kTeams + threadIdx.x / LPR, seg = div(unit, a.slices);
+    const uint32_t at = ((unit - seg * a.slices.d) * LPR + threadIdx.x % LPR) * 8, W = a.table.width;
+    if (seg >= a.segments || at >= W) return;
+    const uint32_t s0 = seg * a.length, s1 = min(s0 + a.length, a.places.n);
+    uint32_t cur = token_of(a.keys[s0]);
+    if (cur == kNone) return;
+    bool open = s0 > 0 && token_of(a.keys[s0 - 1]) == cur;        // begun in front of this segment
+    float acc[8] = {};
+    for (uint32_t p = s0; p < s1; p += 8) {
+        uint64_t k[8];
+        Eight<T> e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] = p + j < s1 ? a.keys[p + j] : ~0ull;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            e[j] = Eight<T>{};
+            if (token_of(k[j]) != kNone) e[j] = load8(place_row<const T>(a.places, (uint32_t)k[j]), at, W);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (p + j >= s1) break;
+            const uint32_t v = token_of(k[j]);
+            if (v != cur) {
+                if (cur != kNone) {
+                    if (open)
+                        store8(a.lines + (uint64_t)seg * 2 * W, at, W, acc);
+                    else
+                        write_row<P>(a.table, cur, at, a.scale, acc);
+                }
+                open = false;
+                cur = v;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += e[j].get(i);
+        }
+    }
+    if (cur == kNone) return;
+    const bool on = s1 < a.places.n && token_of(a.keys[s1]) == cur;
+    if (open || on)
+        store8(a.lines + ((uint64_t)seg * 2 + (open ? 0 : 1)) * W, at, W, acc);
+    else
+        write_row<P>(a.table, cur, at, a.scale, acc);
+}
+
+// The lines of a run that leaves its first segment: eight wavefronts add up a share each, in order, then the shares.
+template <typename P>
+__global__ void __launch_bounds__(512) sdl_embedding_join_kernel(const ReduceArgs a)
+{
+    __shared__ float sums[8][kWave][9];
+    const uint32_t seg = div(blockIdx.x, a.slices), lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const uint32_t at = ((blockIdx.x - seg * a.slices.d) * kWave + lane) * 8, W = a.table.width;
+    const uint32_t s0 = seg * a.length, s1 = s0 + a.length;
+    const uint32_t v = token_of(a.keys[s1 - 1]);           // there is a segment behind this one
+    if (v == kNone || token_of(a.keys[s1]) != v) return;
+    if (s0 > 0 && token_of(a.keys[s0 - 1]) == v) return;   // all of this segment is one run from further up
+    uint32_t lo = s1, hi = a.places.n;                      // first place behind the run
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (token_of(a.keys[mid]) > v) hi = mid;
+        else lo = mid + 1;
+    }
+    const uint32_t lines = (lo - 1) / a.length - seg + 1;   // this segment's second line and the others' first ones
+    const uint32_t each = (lines + 7) / 8, from = min(wave * each, lines), to = min(from + each, lines);
+    float acc[8] = {};
+    if (at < W) {
+        const float* line = a.lines + (uint64_t)seg * 2 * W;
+#pragma unroll 4
+        for (uint32_t l = from; l < to; ++l) {
+            const Eight<float> e = load8(line + ((uint64_t)l * 2 + (l == 0)) * W, at, W);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += e.get(j);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[wave][lane][j] = acc[j];
+    __syncthreads();
+    if (wave != 0 || at >= W) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += sums[w][lane][j];
+    write_row<P>(a.table, v, at, a.scale, acc);
+}
+
+// -------------------------------------------------------------------------------------------------------- host
+
+constexpr uint32_t kSlice = kWave * 8;      // columns of a wavefront
+
+// Places of a segment: enough of them that a device has work for all its compute units, and not so many that the join of one token's lines
+// takes longer than the reading.
+uint32_t segment_length(uint64_t n)
+{
+    const uint64_t each = (n + 1023) / 1024;
+    return (uint32_t)(each <= 16 ? 16 : (each + 7) / 8 * 8);
+}
+
+struct Space {
+    size_t keys, lines, bytes;
+    uint32_t length, segments;
+};
+
+Space space_of(uint64_t n, uint32_t width)
+{
+    Space s{};
+    s.length = segment_length(n);
+    s.segments = (uint32_t)((n + s.length - 1) / s.length);
+    s.keys = ((size_t)n * sizeof(uint64_t) + 15) / 16 * 16;
+    s.lines = s.segments > 1 ? (size_t)s.segments * 2 * width * sizeof(float) : 0;
+    s.bytes = (n > kChunk ? 2 : 1) * s.keys + s.lines;
+    return s;
+}
+
+int check_shape(uint32_t batch, uint32_t tokens, uint32_t vocab, uint32_t width, sdl_dtype_t dtype, sdl_dtype_t table_dtype, sdl_index_t index)
+{
+    if (!known(dtype) || !known(table_dtype) || (index != SDL_INDEX_INT32 && index != SDL_INDEX_INT64) || width == 0) return SDL_ERR_INVALID_ARG;
+    if (width > SDL_EMBEDDING_MAX_WIDTH || vocab > 0x7fffffffu || (uint64_t)batch * tokens > 0x7fffffffu) return SDL_ERR_UNSUPPORTED;
+    return SDL_OK;
+}
+
+size_t index_size(sdl_index_t t) { return t == SDL_INDEX_INT64 ? 8 : 4; }
+bool finite(float x) { return x - x == 0.0f; }
+
+template <typename P, typename T>
+int lookup(const LookupArgs& a, hipStream_t st)
+{
+    const uint32_t n = a.places.n, W = a.places.width;
+    const auto groups = [n](uint32_t rows) { return grid_of(((uint64_t)n + rows - 1) / rows); };
+    // one row at a time while there are few, as they have the device to themselves
+    const bool few = n <= 1024;
+    if (W <= 64)
+        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 8, 1>), groups(32), dim3(256), 0, st, a);
+    else if (W <= 256)
+        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 32, 1>), groups(8), dim3(256), 0, st, a);
+    else if (few)
+        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 256, 1>), groups(1), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 64, 2>), groups(8), dim3(256), 0, st, a);
+    return launched();
+}
+
+// Workgroups that clear while others sort or merge.
+constexpr uint32_t kFillGroups = 1024;
+
+template <typename T, typename P>
+int gradient(const Places& places, const Tokens& tokens, const Table& table, float scale, char* workspace, hipStream_t st)
+{
+    const uint32_t n = places.n, chunks = (n + kChunk - 1) / kChunk;
+    const Space s = space_of(n, table.width);
+    uint64_t *keys = reinterpret_cast<uint64_t*>(workspace), *other = reinterpret_cast<uint64_t*>(workspace + s.keys);
+    float* lines = reinterpret_cast<float*>(workspace + (n > kChunk ? 2 : 1) * s.keys);
+    const bool dense = table.stride == (int64_t)table.width || table.vocab <= 1;
+    const uint64_t pieces = dense ? ((uint64_t)table.vocab * table.width + kFill - 1) / kFill : table.vocab;
+    const uint64_t half = chunks > 1 ? pieces / 2 : pieces;
+    const auto fillers = [](uint64_t share) { return (uint32_t)(share < kFillGroups ? share : kFillGroups); };
+    if (chunks || half) {
+        const SortArgs a{tokens, n, chunks, keys, Fill{table, 0, half, dense}};
+        hipLaunchKernelGGL((sdl_embedding_sort_kernel<P>), dim3(chunks + fillers(half)), dim3(1024), 0, st, a);
+        if (launched() != SDL_OK) return SDL_ERR_DEVICE;
+    }
+    if (n == 0) return SDL_OK;
+    uint64_t rest = half;
+    for (uint64_t run = kChunk; run < n; run *= kFan) {
+        const uint32_t groups = (n + 255) / 256;
+        const MergeArgs a{keys, other, n, (uint32_t)run, groups, Fill{table, rest, pieces, dense}};
+        hipLaunchKernelGGL((sdl_embedding_merge_kernel<P>), dim3(groups + fillers(pieces - rest)), dim3(1024), 0, st, a);
+        if (launched() != SDL_OK) return SDL_ERR_DEVICE;
+        rest = pieces;
+        uint64_t* t = keys;
+        keys = other;
+        other = t;
+    }
+    ReduceArgs r{places, table, keys, lines, make_div(1), s.segments, s.length, scale};
+    const uint32_t W = table.width;
+#define SDL_LAUNCH(LPR)                                                                                                     \
+    do {                                                                                                                    \
+        r.slices = make_div((W + LPR * 8 - 1) / (LPR * 8));                                                                 \
+        const uint32_t teams = 256 / LPR, units = r.slices.d * s.segments;                                                  \
+        hipLaunchKernelGGL((sdl_embedding_reduce_kernel<T, P, LPR>), dim3((units + teams - 1) / teams), dim3(256), 0, st, r); \
+    } while (0)
+    if (W <= 64) SDL_LAUNCH(8);
+    else if (W <= 256) SDL_LAUNCH(32);
+    else SDL_LAUNCH(64);
+#undef SDL_LAUNCH
+    if (launched() != SDL_OK) return SDL_ERR_DEVICE;
+    if (s.segments > 1) {
+        r.slices = make_div((W + kSlice - 1) / kSlice);
+        hipLaunchKernelGGL((sdl_embedding_join_kernel<P>), dim3(r.slices.d * (s.segments - 1)), dim3(512), 0, st, r);
+    }
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int sdl_embedding(const void* table, int64_t table_stride, uint32_t vocab, uint32_t width, sdl_dtype_t table_dtype, const void* tokens, sdl_index_t index,
+                  uint32_t batch, uint32_t tokens_of_batch, float scale, const sdl_view_t* out, sdl_dtype_t dtype, void* stream)
+{
+    int rc = check_shape(batch, tokens_of_batch, vocab, width, dtype, table_dtype, index);
+    if (rc != SDL_OK) return rc;
+    if (!finite(scale)) return SDL_ERR_INVALID_ARG;
+    if (batch == 0 || tokens_of_batch == 0) return SDL_OK;
+    if (!tokens || (vocab && !table)) return SDL_ERR_INVALID_ARG;
+    if ((rc = check_output(out, dtype, batch, tokens_of_batch, 1)) != SDL_OK) return rc;
+    if (!aligned_to(table, dtype_size(table_dtype)) || !aligned_to(tokens, index_size(index))) return SDL_ERR_ALIGNMENT;
+    const LookupArgs a{Places{make_div(tokens_of_batch), batch * tokens_of_batch, width, kernel_view(out)},
+                       Tokens{tokens, index == SDL_INDEX_INT64, vocab}, static_cast<const char*>(table), table_stride, scale};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (table_dtype == SDL_DTYPE_BF16) return dtype == SDL_DTYPE_BF16 ? lookup<__bf16, __bf16>(a, st) : lookup<__bf16, float>(a, st);
+    return dtype == SDL_DTYPE_BF16 ? lookup<float, __bf16>(a, st) : lookup<float, float>(a, st);
+}
+
+size_t sdl_embedding_workspace_bytes(uint64_t places, uint32_t width)
+{
+    return places == 0 || places > SDL_EMBEDDING_MAX_PLACES || width > SDL_EMBEDDING_MAX_WIDTH ? 0 : space_of(places, width).bytes;
+}
+
+int sdl_embedding_backward(const sdl_view_t* d_out, sdl_dtype_t dtype, const void* tokens, sdl_index_t index, uint32_t batch, uint32_t tokens_of_batch,
+                           float scale, void* d_table, int64_t table_stride, uint32_t vocab, uint32_t width, sdl_dtype_t table_dtype, void* workspace,
+                           size_t workspace_bytes, void* stream)
+{
+    int rc = check_shape(batch, tokens_of_batch, vocab, width, dtype, table_dtype, index);
+    if (rc != SDL_OK) return rc;
+    if (!finite(scale)) return SDL_ERR_INVALID_ARG;
+    if (vocab == 0) return SDL_OK;
+    if (!d_table || (vocab > 1 && table_stride == 0)) return SDL_ERR_INVALID_ARG;
+    if (!aligned_to(d_table, dtype_size(table_dtype))) return SDL_ERR_ALIGNMENT;
+    if ((uint64_t)batch * tokens_of_batch > SDL_EMBEDDING_MAX_PLACES) return SDL_ERR_UNSUPPORTED;
+    const uint32_t n = batch * tokens_of_batch;
+    Places places{make_div(tokens_of_batch ? tokens_of_batch : 1), n, width, View{}};
+    if (n) {
+        if (!tokens || !workspace || workspace_bytes < sdl_embedding_workspace_bytes(n, width)) return SDL_ERR_INVALID_ARG;
+        if ((rc = check_view(d_out, dtype)) != SDL_OK) return rc;
+        if (!aligned_to(tokens, index_size(index)) || !aligned_to(workspace, 8)) return SDL_ERR_ALIGNMENT;
+        places.rows = kernel_view(d_out);
+    }
+    const Tokens t{tokens, index == SDL_INDEX_INT64, vocab};
+    const Table table{static_cast<char*>(d_table), table_stride, vocab, width};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(workspace);
+    if (dtype == SDL_DTYPE_BF16)
+        return table_dtype == SDL_DTYPE_BF16 ? gradient<__bf16, __bf16>(places, t, table, scale, w, st) : gradient<__bf16, float>(places, t, table, scale, w, st);
+    return table_dtype == SDL_DTYPE_BF16 ? gradient<float, __bf16>(places, t, table, scale, w, st) : gradient<float, float>(places, t, table, scale, w, st);
+}
+
+}  // extern "C"

@@ -150,6 +150,12 @@ __device__ __forceinline__ void store8(float* row, uint32_t at, uint32_t n, cons
         if (at + j < n) row[at + j] = v[j];
 }
 
+// A launch takes less than 2^32 threads along x.  Workgroups are numbered through rows of kGridX of them (a multiple of the dies, and 2^31 threads at 1024 each); those of the last
+// row that are too many have nothing to do.
+constexpr uint32_t kGridX = 1u << 21;
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridX + blockIdx.x; }
+inline dim3 grid_of(uint64_t groups) { return groups <= kGridX ? dim3((uint32_t)groups) : dim3(kGridX, (uint32_t)((groups + kGridX - 1) / kGridX)); }
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x)
 {
