@@ -8,12 +8,14 @@
 // The products run on fp16 matrix instructions with fp32 sums.  X lies within the unit ball (the coefficients are checked on the host), so a power of
 // two keeps its elements in the middle of fp16's range: X 2^14, A 2^12, and b A + c A^2 by what its bound allows.
 //   - X itself is kept in fp32 beside its fp16 image, and a X is taken from there.  What the images lose is then a factor near 1 on what a
-//     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.
+//     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.  A matrix whose norm is far under eps
+//     keeps its digits too, where its products are nothing beside a X.
 //   - results in bf16: one image, 11 bits.  An error of 2^-12 an element, 0.0003 to 0.0005 of the result after five steps, under the 0.0017 of its own rounding.
 //   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include <utility>
 
 #include "sdl_operand.h"
@@ -25,8 +27,10 @@ using namespace sdl_device;
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f;
+constexpr uint32_t kDies = 8;
 
 // One matrix in the workspace, of which the next lies `each` bytes further.  Both sides are filled up with zeros to whole tiles.
 struct Work {
@@ -38,47 +42,34 @@ struct Work {
     __host__ __device__ uint32_t pitch(uint32_t k) const { return k * (split ? 4u : 2u); }     // bytes of a row of k elements of an image
 };
 
-// Image of v at element k of a row.
-template <bool SPLIT>
-__device__ __forceinline__ void put(char* row, uint32_t k, float v)
+// Eight elements of an image, from element k of its row on, a multiple of eight.
+struct Parts {
+    f16x8_t hi, lo;
+};
+__device__ __forceinline__ Parts parts_of(const float* v)
 {
-    const _Float16 hi = (_Float16)v;
-    if constexpr (SPLIT) {
-        char* at = row + (k / 32) * 128 + (k % 32) * 2;
-        *reinterpret_cast<_Float16*>(at) = hi;
-        *reinterpret_cast<_Float16*>(at + 64) = (_Float16)(v - (float)hi);
-    } else {
-        *reinterpret_cast<_Float16*>(row + k * 2) = hi;
-    }
-}
-// N elements from k on, a multiple of N
-template <bool SPLIT, int N>
-__device__ __forceinline__ void put_many(char* row, uint32_t k, const float* v)
-{
-    typedef _Float16 vec __attribute__((ext_vector_type(N)));
-    vec hi, lo;
+    typedef float f32x8_t __attribute__((ext_vector_type(8)));
+    f32x8_t x, rest;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        hi[i] = (_Float16)v[i];
-        lo[i] = (_Float16)(v[i] - (float)hi[i]);
-    }
-    if constexpr (SPLIT) {
-        char* at = row + (k / 32) * 128 + (k % 32) * 2;
-        *reinterpret_cast<vec*>(at) = hi;
-        *reinterpret_cast<vec*>(at + 64) = lo;
-    } else {
-        *reinterpret_cast<vec*>(row + k * 2) = hi;
-    }
+    for (int i = 0; i < 8; ++i) x[i] = v[i];
+    Parts p;
+    p.hi = __builtin_convertvector(x, f16x8_t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = v[i] - (float)p.hi[i];
+    p.lo = __builtin_convertvector(rest, f16x8_t);
+    return p;
 }
 template <bool SPLIT>
-__device__ __forceinline__ float take(const char* row, uint32_t k)
+__device__ __forceinline__ f16x8_t* piece(char* row, uint32_t k)
 {
-    if constexpr (SPLIT) {
-        const char* at = row + (k / 32) * 128 + (k % 32) * 2;
-        return (float)*reinterpret_cast<const _Float16*>(at) + (float)*reinterpret_cast<const _Float16*>(at + 64);
-    } else {
-        return (float)*reinterpret_cast<const _Float16*>(row + k * 2);
-    }
+    return reinterpret_cast<f16x8_t*>(row + (SPLIT ? (k / 32) * 128 + (k % 32) * 2 : k * 2));
+}
+template <bool SPLIT>
+__device__ __forceinline__ void put(char* row, uint32_t k, const Parts& p)
+{
+    f16x8_t* at = piece<SPLIT>(row, k);
+    at[0] = p.hi;
+    if constexpr (SPLIT) at[4] = p.lo;
 }
 
 // ------------------------------------------------------------------------------------------- norm, first images
@@ -116,7 +107,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_norm_kernel(const First
     if (threadIdx.x == 0) a.squares[(size_t)matrix * a.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// x over its norm, in fp32 and as images of both orders, in tiles of 64 by 64 of what the workspace holds.
+// x over its norm, as images of both orders, in tiles of 64 by 64 of what the workspace holds.
 template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(256) sdl_orthogonalize_first_kernel(const FirstArgs a)
 {
@@ -153,27 +144,31 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_first_kernel(const Firs
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = tile[r][c + j], s[j] = v[j] * kScaleX;
         store8(reinterpret_cast<float*>(base + a.w.x32) + (size_t)(i0 + r) * a.w.m + j0, c, c + 8, v);
-        put_many<SPLIT, 8>(base + a.w.x16 + (size_t)(i0 + r) * a.w.pitch(a.w.m), j0 + c, s);
+        put<SPLIT>(base + a.w.x16 + (size_t)(i0 + r) * a.w.pitch(a.w.m), j0 + c, parts_of(s));
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[j] = tile[c + j][r] * kScaleX;
-        put_many<SPLIT, 8>(base + a.w.xt16 + (size_t)(j0 + r) * a.w.pitch(a.w.n), i0 + c, s);
+        put<SPLIT>(base + a.w.xt16 + (size_t)(j0 + r) * a.w.pitch(a.w.n), i0 + c, parts_of(s));
     }
 }
 
 // ----------------------------------------------------------------------------------------------------- products
 
 enum { GRAM, POLY, UPDATE };
+// A symmetric product has few tiles, and with one long matrix few compute units are at work: then every tile's sum is cut into slices, whose partial sums go
+// through memory (PART), and are added up in order by a launch that goes on as the other way does (JOIN).
+enum { WHOLE, PART, JOIN };
 
 struct ProductArgs {
     Work w;
     size_t p, q, t;             // offsets of the two operands' images, and of what is written: images (UPDATE: of the transpose)
     uint32_t pitch_p, pitch_q, steps;
+    Div slice_of;               // slices of a sum, and the partial sums of each:
+    f32x4_t* partial;           // [workgroup][slice][4 registers][thread]
     Div tiles, across;          // of a matrix; UPDATE: along m
-    float on_sum, on_old, image;    // result = on_old * old + on_sum * product; factor of its image
+    float on_sum, on_old;       // result = on_old * old + on_sum * product
     // the last update: where to
     View out;
     uint32_t last, tall, rows, cols;
-    float scale;
 };
 
 // 64 pieces of 16 bytes into shared memory, past the registers: they land one behind the other.  Five wait states between a vector instruction that writes a
@@ -187,20 +182,32 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// TILE by TILE of C = P Q^T, both operands with k along their rows, by W by W wavefronts.  In shared memory a row's step is 128 bytes, its eight
+// TILE by TILE of C = P Q^T, both operands with k along their rows, by 2 by 2 wavefronts.  In shared memory a row's step is 128 bytes, its eight
 // pieces swapped around by an xor with bits 1 to 3 of the row's number: neither the copies nor the reads (16 rows, one piece) meet in a bank.
-// Two steps' tiles in turn: the next one's copies are under way while one is multiplied.
+// Two steps' tiles in turn.  A step is G groups of products; a group's operands are read while the one before is multiplied, and the wait for the next step's tile
+// comes in front of the last group, whose operands are in registers by then: its products run while the next step's first operands are read and the copies of the one after
+// that are started.
 //
 // Layouts of the 32x32x16 instruction, lane l, half = l / 32, c = l % 32:  A row c, k = 8 half + j;  B column c, k = 8 half + j;
 // D column c, rows 8 (i / 4) + 4 half + i % 4.
-template <int TILE, int W, bool SPLIT, int MODE, typename O>
-__global__ void __launch_bounds__(W * W * kWave) sdl_orthogonalize_product_kernel(const ProductArgs a)
+//
+// The columns of D are the rows of C, of which a lane so has four neighbours at a time.  Results go through shared memory in blocks of a wavefront's own, so that they are written (and
+// what they are added to is read) in pieces of 16 bytes, and their images once more: transposing reads give the other half of what is symmetric, and X's transpose.
+template <int TILE, bool SPLIT, int MODE, int HOW, typename O>
+__global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const ProductArgs a)
 {
-    constexpr int kBytes = TILE * 128, kSide = TILE / W, kParts = kSide / 32, kCopies = TILE / 8 / (W * W);
-    static_assert(kParts * 32 == kSide && kCopies * 8 * W * W == TILE, "whole instructions");
-    __shared__ __attribute__((aligned(128))) char lds[2][2][kBytes];
+    constexpr int kBytes = TILE * 128, kSide = TILE / 2, kParts = kSide / 32, kCopies = TILE / 32, kGroups = SPLIT ? 2 : 4;
+    // Of a block, bytes from row to row of fp32 and of an image: a row's pieces are four banks further than those of the row before.
+    constexpr int kBlock = kSide < 64 ? kSide : 64, kPitch = kBlock * 4 + 16, kImagePitch = kBlock * 2 + 16;
+    constexpr int kOwn = kBlock * (kPitch > 2 * kImagePitch ? kPitch : 2 * kImagePitch);      // of a wavefront: a block, or both of its images
+    constexpr int kLds = 4 * (kBytes > kOwn ? kBytes : kOwn);
+    __shared__ __attribute__((aligned(128))) char lds[kLds];
     const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32, c = lane % 32;
-    const uint32_t matrix = div(blockIdx.x, a.tiles), t = blockIdx.x - matrix * a.tiles.d;
+    // consecutive workgroups go to different dies: each die takes tiles that follow each other, which share rows in its cache
+    const uint32_t die = blockIdx.x % kDies, each = gridDim.x / kDies, more = gridDim.x % kDies;
+    const uint32_t number = die * each + min(die, more) + blockIdx.x / kDies;
+    const uint32_t at = HOW == PART ? div(number, a.slice_of) : number, matrix = div(at, a.tiles), t = at - matrix * a.tiles.d;
+    const uint32_t slice = HOW == PART ? number - at * a.slice_of.d : 0;
     uint32_t ti, tj;
     if constexpr (MODE == UPDATE) {
         ti = div(t, a.across);
@@ -213,132 +220,278 @@ __global__ void __launch_bounds__(W * W * kWave) sdl_orthogonalize_product_kerne
         tj = t - ti * (ti + 1) / 2;
     }
     char* base = a.w.base + matrix * a.w.each;
-    const char* from_p = base + a.p + (size_t)(ti * TILE + wave * kCopies * 8) * a.pitch_p;
-    const char* from_q = base + a.q + (size_t)(tj * TILE + wave * kCopies * 8) * a.pitch_q;
+    const uint32_t first = HOW == PART ? slice * a.steps / a.slice_of.d : 0, steps = (HOW == PART ? (slice + 1) * a.steps / a.slice_of.d : a.steps) - first;
+    const char* from_p = base + a.p + (size_t)(ti * TILE + wave * kCopies * 8) * a.pitch_p + (size_t)first * 128;
+    const char* from_q = base + a.q + (size_t)(tj * TILE + wave * kCopies * 8) * a.pitch_q + (size_t)first * 128;
     // the piece that comes to lie where the lane's 16 bytes land, in the even instructions; 4 further, by xor, in the odd ones
-    const uint32_t piece = ((lane % 8) ^ (lane / 16)) * 16;
-    const uint32_t off_p = lane / 8 * a.pitch_p + piece, off_q = lane / 8 * a.pitch_q + piece;
-    const auto bring = [&](uint32_t step) {
-        const uint32_t to = lds_offset(lds[step % 2][0]) + wave * kCopies * 1024;
+    const uint32_t piece_at = ((lane % 8) ^ (lane / 16)) * 16;
+    const uint32_t off_p = lane / 8 * a.pitch_p + piece_at, off_q = lane / 8 * a.pitch_q + piece_at;
+    static_assert(kCopies % 2 == 0, "an instruction's parity is its number's within the wavefront's");
+    uint32_t offs_p[kCopies], offs_q[kCopies];
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            // an instruction's parity is its number's: kCopies is even, or there is one wavefront's parity to count
-            const uint32_t odd = ((wave * kCopies + i) & 1) * 64;
-            copy_pieces(from_p + (size_t)i * 8 * a.pitch_p + step * 128, off_p ^ odd, to + i * 1024);
-            copy_pieces(from_q + (size_t)i * 8 * a.pitch_q + step * 128, off_q ^ odd, to + kBytes + i * 1024);
-        }
+    for (int i = 0; i < kCopies; ++i) {
+        offs_p[i] = (off_p ^ (i % 2 * 64)) + i * 8 * a.pitch_p;
+        offs_q[i] = (off_q ^ (i % 2 * 64)) + i * 8 * a.pitch_q;
+    }
+    // the i-th of a wavefront's copies of a step's tiles
+    const auto copy = [&](uint32_t step, int i) {
+        const uint32_t to = lds_offset(lds) + (step % 2) * (2 * kBytes) + wave * kCopies * 1024;
+        if (i % 2 == 0) copy_pieces(from_p + step * 128, offs_p[i / 2], to + i / 2 * 1024);
+        else copy_pieces(from_q + step * 128, offs_q[i / 2], to + kBytes + i / 2 * 1024);
+    };
+    const uint32_t i0 = wave / 2 * kSide, j0 = wave % 2 * kSide, mix = (c >> 1) & 7;
+    constexpr int kImages = SPLIT ? 2 : 1, kReads = 2 * kParts * kImages, kProducts = kParts * kParts * (SPLIT ? 3 : 1);     // of a group
+    f16x8_t p[2][kImages][kParts], q[2][kImages][kParts];
+    // the r-th of the reads of a group's operands
+    const auto read = [&](uint32_t step, int g, int to, int r) {
+        const char* rows = lds + (step % 2) * (2 * kBytes) + c * 128;
+        const int image = r / (2 * kParts), i = r % (2 * kParts) / 2;
+        const uint32_t at = ((4 * image + 2 * g + half) ^ mix) * 16;
+        if (r % 2 == 0) p[to][image][i] = *reinterpret_cast<const f16x8_t*>(rows + (i0 + i * 32) * 128 + at);
+        else q[to][image][i] = *reinterpret_cast<const f16x8_t*>(rows + kBytes + (j0 + i * 32) * 128 + at);
     };
     f32x16_t acc[kParts][kParts] = {};
-    const uint32_t i0 = wave / W * kSide, j0 = wave % W * kSide, mix = (c >> 1) & 7;
-    bring(0);
-    for (uint32_t step = 0; step < a.steps; ++step) {
+    // the m-th of a group's products: hi hi of all, hi lo of all, lo hi of all
+    const auto multiply = [&](int from, int m) {
+        const int way = m / (kParts * kParts), i = m / kParts % kParts, j = m % kParts;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(q[from][way == 1][j], p[from][way == 2][i], acc[i][j], 0, 0, 0);
+    };
+    const auto arrived = [&]() {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" : : : "memory");
-        if (step + 1 < a.steps) bring(step + 1);
-        const char *rows_p = lds[step % 2][0] + (i0 + c) * 128, *rows_q = lds[step % 2][1] + (j0 + c) * 128;
-        const auto frag = [&](const char* rows, int part, uint32_t p) {
-            return *reinterpret_cast<const f16x8_t*>(rows + part * 4096 + ((p ^ mix) * 16));
-        };
+    };
+    // The order of the instructions is the one that is written: between two products one read or copy or two.  The last two steps have nothing to copy.
+    const auto multiply_step = [&](uint32_t step, auto copies) {
 #pragma unroll
-        for (int k = 0; k < (SPLIT ? 2 : 4); ++k) {
-            f16x8_t p[kParts], q[kParts];
+        for (int g = 0; g < kGroups - 1; ++g) {
 #pragma unroll
-            for (int i = 0; i < kParts; ++i) p[i] = frag(rows_p, i, 2 * k + half), q[i] = frag(rows_q, i, 2 * k + half);
+            for (int m = 0; m < kProducts; ++m) {
+                multiply(g % 2, m);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = kReads * m / kProducts; r < kReads * (m + 1) / kProducts; ++r) read(step, g + 1, (g + 1) % 2, r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        arrived();
+        constexpr int kAll = kReads + decltype(copies)::value * 2 * kCopies;
+#pragma unroll
+        for (int m = 0; m < kProducts; ++m) {
+            multiply((kGroups - 1) % 2, m);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int r = kAll * m / kProducts; r < kAll * (m + 1) / kProducts; ++r) {
+                if (r < kReads) read(step + 1, 0, 0, r);        // behind the last step what lies there, for nothing
+                else copy(step + 2, r - kReads);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // the partial sums of a slice, a register of four at a time
+    const auto partial_of = [&](uint32_t which) { return a.partial + ((size_t)at * a.slice_of.d + which) * (kParts * kParts * 4 * 256) + threadIdx.x; };
+    if constexpr (HOW != JOIN) {
+#pragma unroll
+        for (int i = 0; i < 2 * kCopies; ++i) copy(0, i);
+        arrived();
+        if (steps > 1) {
+#pragma unroll
+            for (int i = 0; i < 2 * kCopies; ++i) copy(1, i);
+        }
+#pragma unroll
+        for (int r = 0; r < kReads; ++r) read(0, 0, 0, r);
+        uint32_t step = 0;
+        for (; step + 2 < steps; ++step) multiply_step(step, std::integral_constant<int, 1>());
+#pragma unroll 1
+        for (; step < steps; ++step) multiply_step(step, std::integral_constant<int, 0>());
+    } else {
+        for (uint32_t which = 0; which < a.slice_of.d; ++which) {
+            const f32x4_t* from = partial_of(which);
 #pragma unroll
             for (int i = 0; i < kParts; ++i)
 #pragma unroll
-                for (int j = 0; j < kParts; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[i], q[j], acc[i][j], 0, 0, 0);
-            if constexpr (SPLIT) {
-                f16x8_t low[kParts];
+                for (int j = 0; j < kParts; ++j)
 #pragma unroll
-                for (int j = 0; j < kParts; ++j) low[j] = frag(rows_q, j, 4 + 2 * k + half);
+                    for (int u = 0; u < 4; ++u) {
+                        const f32x4_t v = from[((i * kParts + j) * 4 + u) * 256];
 #pragma unroll
-                for (int i = 0; i < kParts; ++i)
-#pragma unroll
-                    for (int j = 0; j < kParts; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[i], low[j], acc[i][j], 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < kParts; ++i) low[i] = frag(rows_p, i, 4 + 2 * k + half);
-#pragma unroll
-                for (int i = 0; i < kParts; ++i)
-#pragma unroll
-                    for (int j = 0; j < kParts; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(low[i], q[j], acc[i][j], 0, 0, 0);
-            }
+                        for (int r = 0; r < 4; ++r) acc[i][j][4 * u + r] += v[r];
+                    }
         }
     }
-    const uint32_t n = a.w.n, m = a.w.m;
+    if constexpr (HOW == PART) {
+        f32x4_t* to = partial_of(slice);
 #pragma unroll
-    for (int pi = 0; pi < kParts; ++pi)
+        for (int i = 0; i < kParts; ++i)
 #pragma unroll
-        for (int pj = 0; pj < kParts; ++pj) {
-            const uint32_t j = tj * TILE + j0 + pj * 32 + c;
+            for (int j = 0; j < kParts; ++j)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t i = ti * TILE + i0 + pi * 32 + 8 * u + 4 * half;
-                float v[4];
-                if constexpr (MODE == GRAM) {
-                    char* out = base + a.t;
+                for (int u = 0; u < 4; ++u) {
+                    f32x4_t v;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        v[r] = acc[pi][pj][4 * u + r] * a.on_sum;
-                        put<SPLIT>(out + (size_t)(i + r) * a.w.pitch(n), j, v[r]);
-                    }
-                    if (ti != tj) put_many<SPLIT, 4>(out + (size_t)j * a.w.pitch(n), i, v);
-                } else if constexpr (MODE == POLY) {
-                    char* out = base + a.t;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float old = take<SPLIT>(base + a.w.a16 + (size_t)(i + r) * a.w.pitch(n), j);
-                        v[r] = (a.on_old * old + acc[pi][pj][4 * u + r] * a.on_sum) * a.image;
-                        put<SPLIT>(out + (size_t)(i + r) * a.w.pitch(n), j, v[r]);
-                    }
-                    if (ti != tj) put_many<SPLIT, 4>(out + (size_t)j * a.w.pitch(n), i, v);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float* x = reinterpret_cast<float*>(base + a.w.x32) + (size_t)(i + r) * m + j;
-                        v[r] = a.on_old * *x + acc[pi][pj][4 * u + r] * a.on_sum;
-                        if (!a.last) *x = v[r];
-                    }
-                    if (!a.last) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) put<SPLIT>(base + a.w.x16 + (size_t)(i + r) * a.w.pitch(m), j, v[r] *= kScaleX);
-                        put_many<SPLIT, 4>(base + a.t + (size_t)j * a.w.pitch(n), i, v);
-                    } else {
-                        O* out = reinterpret_cast<O*>(a.out.data) + (int64_t)matrix * a.out.batch;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint32_t row = a.tall ? j : i + r, col = a.tall ? i + r : j;
-                            if (row < a.rows && col < a.cols) out[(int64_t)row * a.out.token + col] = (O)(v[r] * a.scale);
-                        }
-                    }
+                    for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * u + r];
+                    to[((i * kParts + j) * 4 + u) * 256] = v;
                 }
+        return;
+    }
+    __syncthreads();        // the tiles' memory becomes the blocks'
+    const uint32_t n = a.w.n, m = a.w.m;
+    char* block = lds + wave * kOwn;
+    // The transposing read: lane 4 r + q of 16 names the q-th quarter of row r of 4, and gets the four rows of its column of 16.
+    const auto across = [](const char* at) {
+        typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+        const i16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 4 * kImagePitch));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    constexpr int kSpan = kBlock / 8, kRows = kWave / kSpan, kPasses = kBlock / kRows, kIn = kBlock / 32;     // lanes of a row; rows of a pass
+    const uint32_t r0 = lane / kSpan, c0 = lane % kSpan * 8;
+#pragma unroll
+    for (int bi = 0; bi < kParts / kIn; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < kParts / kIn; ++bj) {
+            const uint32_t i = ti * TILE + i0 + bi * kBlock, j = tj * TILE + j0 + bj * kBlock;     // the block's first row and column
+            Parts old[MODE == POLY ? kPasses : 1];
+            Eight<float> x[MODE == UPDATE ? kPasses : 1];
+            if constexpr (MODE == POLY) {
+#pragma unroll
+                for (int k = 0; k < kPasses; ++k) {
+                    const f16x8_t* at = piece<SPLIT>(base + a.w.a16 + (size_t)(i + k * kRows + r0) * a.w.pitch(n), j + c0);
+                    old[k].hi = at[0];
+                    old[k].lo = SPLIT ? at[4] : f16x8_t{};
+                }
+            }
+            if constexpr (MODE == UPDATE) {
+#pragma unroll
+                for (int k = 0; k < kPasses; ++k)
+                    x[k] = load8(reinterpret_cast<const float*>(base + a.w.x32) + (size_t)(i + k * kRows + r0) * m + j, c0, c0 + 8);
+            }
+#pragma unroll
+            for (int pi = 0; pi < kIn; ++pi)
+#pragma unroll
+                for (int pj = 0; pj < kIn; ++pj)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        f32x4_t v;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = acc[bi * kIn + pi][bj * kIn + pj][4 * u + r];
+                        *reinterpret_cast<f32x4_t*>(block + (pi * 32 + c) * kPitch + (pj * 32 + 8 * u + 4 * half) * 4) = v;
+                    }
+            float v[kPasses][8];
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const char* at = block + (k * kRows + r0) * kPitch + c0 * 4;
+                const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(at), hi = *reinterpret_cast<const f32x4_t*>(at + 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float s = e < 4 ? lo[e & 3] : hi[e & 3];
+                    if constexpr (MODE == GRAM) v[k][e] = s * a.on_sum;
+                    if constexpr (MODE == POLY) v[k][e] = fmaf(s, a.on_sum, a.on_old * (SPLIT ? (float)old[k].hi[e] + (float)old[k].lo[e] : (float)old[k].hi[e]));
+                    if constexpr (MODE == UPDATE) v[k][e] = fmaf(s, a.on_sum, a.on_old * x[k].get(e));
+                }
+            }
+            if constexpr (MODE == UPDATE) {
+                if (a.last) {
+                    O* out = reinterpret_cast<O*>(a.out.data) + (int64_t)matrix * a.out.batch;
+                    if (!a.tall) {
+#pragma unroll
+                        for (int k = 0; k < kPasses; ++k) {
+                            const uint32_t row = i + k * kRows + r0;
+                            if (row < a.rows && j + c0 < a.cols) store8(out + (int64_t)row * a.out.token, j + c0, a.cols, v[k]);
+                        }
+                        continue;
+                    }
+#pragma unroll
+                    for (int k = 0; k < kPasses; ++k)
+                        store8(reinterpret_cast<float*>(block + (k * kRows + r0) * kPitch), c0, c0 + 8, v[k]);
+#pragma unroll
+                    for (int k = 0; k < kPasses; ++k) {
+                        const uint32_t row = lane % kBlock, col = (k * (kWave / kBlock) + lane / kBlock) * 8;
+                        float t[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) t[e] = *reinterpret_cast<const float*>(block + (col + e) * kPitch + row * 4);
+                        if (j + row < a.rows && i + col < a.cols) store8(out + (int64_t)(j + row) * a.out.token, i + col, a.cols, t);
+                    }
+                    continue;
+                }
+#pragma unroll
+                for (int k = 0; k < kPasses; ++k) {
+                    store8(reinterpret_cast<float*>(base + a.w.x32) + (size_t)(i + k * kRows + r0) * m + j, c0, c0 + 8, v[k]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[k][e] *= kScaleX;
+                }
+            }
+            const bool turned = MODE == UPDATE || ti != tj;
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const uint32_t row = k * kRows + r0;
+                const Parts image = parts_of(v[k]);
+                put<SPLIT>(base + (MODE == UPDATE ? a.w.x16 : a.t) + (size_t)(i + row) * a.w.pitch(MODE == UPDATE ? m : n), j + c0, image);
+                if (turned) {
+                    *reinterpret_cast<f16x8_t*>(block + row * kImagePitch + c0 * 2) = image.hi;
+                    if constexpr (SPLIT) *reinterpret_cast<f16x8_t*>(block + (kBlock + row) * kImagePitch + c0 * 2) = image.lo;
+                }
+            }
+            if (!turned) continue;
+            // lanes of a group of 16 have a column each, of 16; the groups have eight rows each, of 32
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const uint32_t col = k % (kBlock / 16) * 16, row = k / (kBlock / 16) * 32 + lane / 16 * 8;
+                const char* at = block + (row + lane % 16 / 4) * kImagePitch + col * 2 + lane % 4 * 8;
+                Parts image;
+                image.hi = across(at);
+                if constexpr (SPLIT) image.lo = across(at + kBlock * kImagePitch);
+                put<SPLIT>(base + a.t + (size_t)(j + col + lane % 16) * a.w.pitch(n), i + row, image);
             }
         }
 }
 
 // -------------------------------------------------------------------------------------------------------- host
 
-// Side of a product's tiles.
-uint32_t tile_of(uint32_t batch, uint32_t n, uint32_t m)
+// Workgroups that are at work at a time.
+constexpr uint32_t slots_of(uint32_t tile) { return tile == 256 ? 256 : tile == 128 ? 512 : 1024; }
+
+// Slices of a symmetric product's sums over k values.
+uint32_t slices_of(uint32_t batch, uint32_t tile, uint32_t n, uint32_t k, bool split)
 {
-    const uint64_t tiles = (uint64_t)batch * ((n + 127) / 128) * ((m + 127) / 128);
-    return tiles >= 128 ? 128 : 64;
+    if (tile == 256) return 1;
+    const uint64_t side = (n + tile - 1) / tile, tiles = batch * (side * (side + 1) / 2), steps = k / (split ? 32 : 64);
+    const uint64_t want = std::max<uint64_t>(1, slots_of(tile) / tiles), most = std::max<uint64_t>(1, steps / 8);
+    return (uint32_t)std::min(want, most);
 }
 
-constexpr uint32_t kParts = 64;     // sums of squares of a matrix
+// Side of the products' tiles: the one whose rounds of workgroups take least. Larger tiles read less for every product, smaller ones leave fewer compute units without
+// one at the end.
+uint32_t tile_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
+{
+    uint32_t best = 0;
+    double least = 0.0;
+    for (const uint32_t tile : {256u, 128u, 64u}) {
+        const uint64_t rows = (n + tile - 1) / tile, cols = (m + tile - 1) / tile, symmetric = batch * (rows * (rows + 1) / 2);
+        const auto rounds = [&](uint64_t tiles, uint32_t slices) {
+            return (double)((tiles * slices + slots_of(tile) - 1) / slots_of(tile)) / slices;
+        };
+        const double k = rounds(symmetric, slices_of(batch, tile, n, m, split)) * m + rounds(symmetric, slices_of(batch, tile, n, n, split)) * n + rounds(batch * rows * cols, 1) * n;
+        const double cost = k * (tile == 256 ? 256.0 * 256.0 : tile == 128 ? 2.5 * 128.0 * 128.0 : 6.8 * 64.0 * 64.0);
+        if (best == 0 || cost < least) best = tile, least = cost;
+    }
+    return best;
+}
+
+// Sums of squares of a matrix: enough workgroups for all compute units.
+uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(256u, 2048u / batch)); }
 
 struct Layout {
     Work w;
     uint32_t tile;
-    size_t squares, bytes;
+    size_t squares, partial, bytes;
+    uint32_t parts, gram_slices, poly_slices;
 };
 
 Layout layout_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
 {
     Layout l{};
     const uint32_t n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    l.tile = tile_of(batch, n, m);
+    l.tile = tile_of(batch, n, m, split);
     Work& w = l.w;
     w.split = split;
     w.n = (n + l.tile - 1) / l.tile * l.tile;
@@ -349,15 +502,20 @@ Layout layout_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
         at += (bytes + 127) / 128 * 128;
         return here;
     };
-    w.x32 = place((size_t)w.n * w.m * 4);
     w.x16 = place((size_t)w.n * w.pitch(w.m));
+    w.x32 = place((size_t)w.n * w.m * 4);
     w.xt16 = place((size_t)w.m * w.pitch(w.n));
     w.xt16_other = place((size_t)w.m * w.pitch(w.n));
     w.a16 = place((size_t)w.n * w.pitch(w.n));
     w.b16 = place((size_t)w.n * w.pitch(w.n));
     w.each = at;
+    l.parts = parts_of(batch);
     l.squares = (size_t)batch * w.each;
-    l.bytes = l.squares + (size_t)batch * kParts * sizeof(double);
+    l.partial = l.squares + ((size_t)batch * l.parts * sizeof(double) + 127) / 128 * 128;
+    l.gram_slices = slices_of(batch, l.tile, w.n, w.m, split);
+    l.poly_slices = slices_of(batch, l.tile, w.n, w.n, split);
+    const uint32_t slices = std::max(l.gram_slices, l.poly_slices), side = w.n / l.tile;
+    l.bytes = l.partial + (slices > 1 ? (size_t)batch * (side * (side + 1) / 2) * slices * l.tile * l.tile * sizeof(float) : 0);
     return l;
 }
 
@@ -382,14 +540,23 @@ double reach(double a, double b, double c, double h)
     return most;
 }
 
-template <int TILE, int W, bool SPLIT, int MODE, typename O>
+template <int TILE, bool SPLIT, int MODE, typename O>
 int product(const ProductArgs& a, uint32_t batch, hipStream_t st)
 {
-    hipLaunchKernelGGL((sdl_orthogonalize_product_kernel<TILE, W, SPLIT, MODE, O>), dim3(batch * a.tiles.d), dim3(W * W * kWave), 0, st, a);
+    const uint32_t groups = batch * a.tiles.d;
+    if constexpr (MODE != UPDATE && TILE != 256) {
+        if (a.slice_of.d > 1) {
+            hipLaunchKernelGGL((sdl_orthogonalize_product_kernel<TILE, SPLIT, MODE, PART, O>), dim3(groups * a.slice_of.d), dim3(256), 0, st, a);
+            if (launched() != SDL_OK) return SDL_ERR_DEVICE;
+            hipLaunchKernelGGL((sdl_orthogonalize_product_kernel<TILE, SPLIT, MODE, JOIN, O>), dim3(groups), dim3(256), 0, st, a);
+            return launched();
+        }
+    }
+    hipLaunchKernelGGL((sdl_orthogonalize_product_kernel<TILE, SPLIT, MODE, WHOLE, O>), dim3(groups), dim3(256), 0, st, a);
     return launched();
 }
 
-template <int TILE, int W, bool SPLIT, typename O>
+template <int TILE, bool SPLIT, typename O>
 int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, const float* coefficients, uint32_t steps, float scale, const sdl_view_t* out,
              hipStream_t st)
 {
@@ -405,35 +572,37 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         h = reach(ca, cb, cc, h);
         ProductArgs a{};
         a.w = w;
+        a.partial = reinterpret_cast<f32x4_t*>(w.base + l.partial);
+        a.slice_of = make_div(l.gram_slices);
         a.p = a.q = w.x16;
         a.t = w.a16;
         a.pitch_p = a.pitch_q = w.pitch(w.m);
         a.steps = w.m / per;
         a.tiles = make_div(n * (n + 1) / 2);
         a.on_sum = kScaleA / (kScaleX * kScaleX);
-        if (product<TILE, W, SPLIT, GRAM, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<TILE, SPLIT, GRAM, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        a.slice_of = make_div(l.poly_slices);
         a.p = a.q = w.a16;
         a.t = w.b16;
         a.pitch_p = a.pitch_q = w.pitch(w.n);
         a.steps = w.n / per;
-        a.on_old = (float)(cb / kScaleA);
-        a.on_sum = (float)(cc / ((double)kScaleA * kScaleA));
-        a.image = scale_b;
-        if (product<TILE, W, SPLIT, POLY, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        a.on_old = (float)(cb / kScaleA * scale_b);
+        a.on_sum = (float)(cc / ((double)kScaleA * kScaleA) * scale_b);
+        if (product<TILE, SPLIT, POLY, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         a.p = w.b16;
         a.q = xt;
         a.t = other;
         a.tiles = make_div(n * m);
         a.across = make_div(m);
-        a.on_old = (float)ca;
-        a.on_sum = 1.0f / (scale_b * kScaleX);
         a.last = s + 1 == steps;
+        const double to = a.last ? scale : 1.0;
+        a.on_old = (float)(ca * to);
+        a.on_sum = (float)(to / ((double)scale_b * kScaleX));
         a.out = kernel_view(out);
         a.tall = rows > cols;
         a.rows = rows;
         a.cols = cols;
-        a.scale = scale;
-        if (product<TILE, W, SPLIT, UPDATE, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<TILE, SPLIT, UPDATE, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         std::swap(xt, other);
     }
     return SDL_OK;
@@ -488,7 +657,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     a.rows = rows;
     a.cols = cols;
     a.tall = rows > cols;
-    a.parts = kParts;
+    a.parts = l.parts;
     a.squares = reinterpret_cast<double*>(l.w.base + l.squares);
     a.eps = (double)eps;
     a.w = l.w;
@@ -496,10 +665,10 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (dtype == SDL_DTYPE_BF16) rc = split ? first<__bf16, true>(a, batch, st) : first<__bf16, false>(a, batch, st);
     else rc = split ? first<float, true>(a, batch, st) : first<float, false>(a, batch, st);
     if (rc != SDL_OK) return rc;
-#define SDL_STEPS(TILE, W)                                                                                             \
-    (split ? steps_of<TILE, W, true, float>(l, batch, rows, cols, coefficients, steps, scale, out, st)                 \
-           : steps_of<TILE, W, false, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st))
-    return l.tile == 128 ? SDL_STEPS(128, 2) : SDL_STEPS(64, 2);
+#define SDL_STEPS(TILE)                                                                                                \
+    (split ? steps_of<TILE, true, float>(l, batch, rows, cols, coefficients, steps, scale, out, st)                 \
+           : steps_of<TILE, false, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st))
+    return l.tile == 256 ? SDL_STEPS(256) : l.tile == 128 ? SDL_STEPS(128) : SDL_STEPS(64);
 #undef SDL_STEPS
 }
 
