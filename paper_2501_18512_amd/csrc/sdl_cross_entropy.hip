@@ -41,112 +41,127 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 // exp(x - m) where m is at least x
 __device__ __forceinline__ float exp_under(float x, float m) { return exp2_of((x - m) * kLog2e); }
 
-// Maximum, sum of exp(x - maximum), sum of x, and the target's logit (0 in the lanes that do not have it).
+// Maximum, sum of exp(x - maximum), and sum of x of some of a row's elements.
 struct Part {
-    float m, s, sum, hit;
+    float m, s, sum;
 };
 
-// exp(from - to) for the joining of two parts; a part of nothing but -infinity has s = 0.
+// A part of nothing but -infinity has s = 0.
 __device__ __forceinline__ Part join(const Part& a, const Part& b)
 {
     const float m = fmaxf(a.m, b.m);
     const float base = m == -__builtin_inff() ? 0.0f : m;
-    return Part{m, a.s * exp_under(a.m, base) + b.s * exp_under(b.m, base), a.sum + b.sum, a.hit + b.hit};
+    return Part{m, a.s * exp_under(a.m, base) + b.s * exp_under(b.m, base), a.sum + b.sum};
 }
 
-__device__ __forceinline__ Part wave_join(Part p)
+__device__ __forceinline__ float wave_max(float x)
 {
+    x = fmaxf(x, dpp<0xb1>(x));
+    x = fmaxf(x, dpp<0x4e>(x));
+    x = fmaxf(x, dpp<0x141>(x));
+    x = fmaxf(x, dpp<0x140>(x));
+    u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(f2u(x), f2u(x), false, false));
+    x = fmaxf(u2f(p[0]), u2f(p[1]));
+    p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(f2u(x), f2u(x), false, false));
+    return fmaxf(u2f(p[0]), u2f(p[1]));
+}
+
+// The lanes' parts as one, in all of them.
+__device__ __forceinline__ Part wave_join(const Part& p, bool smooth)
+{
+    const float m = wave_max(p.m), base = m == -__builtin_inff() ? 0.0f : m;
+    return Part{m, lane_sum<kWave>(p.s * exp_under(p.m, base)), smooth ? lane_sum<kWave>(p.sum) : 0.0f};
+}
+
+// The same bits, for the compiler others, that it has when `now` is worked out: else it would keep eight numbers instead of the four words that they come in, for all that
+// a thread holds (104 registers instead of 70 for eight groups, and memory for sixteen).
+__device__ __forceinline__ void forget(Eight<__bf16>& e, float& now) { asm volatile("" : "+v"(e.w), "+v"(now)); }
+__device__ __forceinline__ void forget(Eight<float>&, float&) {}
+
+// Where the eight elements lie that stand for [at, at + 8) of a row of n: in their place, or at the row's end, where the ones before `at` are someone else's too.
+// All of a thread's loads are whole accesses that wait for nothing, and what two threads write to one place is the same.  (TINY rows, which may have less than eight, go element by
+// element, with -infinity behind the row.)
+template <bool TINY>
+__device__ __forceinline__ uint32_t from_of(uint32_t at, uint32_t n)
+{
+    return TINY ? at : min(at, n - 8);
+}
+template <bool TINY, typename T>
+__device__ __forceinline__ Eight<T> load_logits(const T* row, uint32_t at, uint32_t n)
+{
+    if constexpr (TINY) {
+        const T low = (T)-__builtin_inff();
+        T v[8];
 #pragma unroll
-    for (int k = 32; k; k /= 2) {
-        const Part q{__shfl_xor(p.m, k), __shfl_xor(p.s, k), __shfl_xor(p.sum, k), __shfl_xor(p.hit, k)};
-        p = join(p, q);         // the same bits in both lanes: sums of two do not go by their order
+        for (int j = 0; j < 8; ++j) v[j] = at + j < n ? row[at + j] : low;
+        return __builtin_bit_cast(Eight<T>, v);
+    } else {
+        return load8(row, from_of<TINY>(at, n), ~0u);
     }
-    return p;
 }
 
-// Elements [at, at + 8) of a row of n; what is behind the row is -infinity.
-__device__ __forceinline__ Eight<__bf16> load_logits(const __bf16* row, uint32_t at, uint32_t n)
+// What K groups of eight elements, TPR groups apart, are as a part of their row.  No branch goes by an element: a thread's groups stay in the words they came in.
+template <bool TINY, typename T, int K, int TPR>
+__device__ __forceinline__ Part part_of(Eight<T> (&e)[K], uint32_t first, uint32_t n, bool smooth)
 {
-    if (at + 8 <= n) return load8(row, at, n);
-    const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
-    uint32_t h[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = at + j < n ? p[at + j] : 0xff80u;
-    return Eight<__bf16>{u32x4{h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16)}};
-}
-__device__ __forceinline__ Eight<float> load_logits(const float* row, uint32_t at, uint32_t n)
-{
-    if (at + 8 <= n) return load8(row, at, n);
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(row);
-    Eight<float> r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        r.lo[j] = at + j < n ? p[at + j] : 0xff800000u;
-        r.hi[j] = at + 4 + j < n ? p[at + 4 + j] : 0xff800000u;
-    }
-    return r;
-}
-
-// What K groups of eight elements, TPR groups apart, are as a part of their row.
-template <typename T, int K, int TPR>
-__device__ __forceinline__ Part part_of(const Eight<T> (&e)[K], uint32_t first, uint32_t n, int32_t target, bool smooth)
-{
-    float m[K];
+    Part p{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        m[k] = e[k].get(0);
+        float m = e[k].get(0);
 #pragma unroll
-        for (int j = 1; j < 8; ++j) m[k] = fmaxf(m[k], e[k].get(j));
+        for (int j = 1; j < 8; ++j) m = fmaxf(m, e[k].get(j));
+        p.m = fmaxf(p.m, m);
+        forget(e[k], p.m);
     }
-    Part p{m[0], 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int k = 1; k < K; ++k) p.m = fmaxf(p.m, m[k]);
     const float base = p.m == -__builtin_inff() ? 0.0f : p.m;
-    float s[4] = {};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
+        const uint32_t at = first + k * TPR * 8, from = from_of<TINY>(at, n);
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j % 4] += exp_under(e[k].get(j), base);
-        const uint32_t at = first + k * TPR * 8;
-        if (smooth && at < n) {
+        for (int j = 0; j < 8; ++j) v[j] = from + j >= at ? exp_under(e[k].get(j), base) : 0.0f;
+        p.s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        forget(e[k], p.s);
+    }
+    if (smooth) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const uint32_t at = first + k * TPR * 8, from = from_of<TINY>(at, n);
             float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += at + j < n ? e[k].get(j) : 0.0f;
+            for (int j = 0; j < 8; ++j) sum += (TINY ? at + j < n : from + j >= at) ? e[k].get(j) : 0.0f;
             p.sum += sum;
-        }
-        if (at == ((uint32_t)target & ~7u)) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p.hit = j == (target & 7) ? e[k].get(j) : p.hit;
+            forget(e[k], p.sum);
         }
     }
-    p.s = (s[0] + s[1]) + (s[2] + s[3]);
     return p;
 }
 
-// The row's loss and lse, from its whole part.
-__device__ __forceinline__ void write_loss(const LossArgs& a, uint32_t row, const Part& p)
+// What a row's gradient is made of: factor exp(x - m) - even, and `hit` less at the target.
+struct Slope {
+    float m, factor, even, hit;
+};
+
+template <bool TINY, typename T, int K, int TPR>
+__device__ __forceinline__ void write_gradient(T* row, uint32_t first, uint32_t n, Eight<T> (&e)[K], const Slope& g)
 {
-    const float log_s = logf(p.s);
-    const float lse = p.m + log_s;
-    float loss = log_s + a.hit * (p.m - p.hit);
-    if (a.smoothing > 0.0f) loss += a.smoothing * (p.m - p.sum / (float)a.vocab);
-    if (a.z != 0.0f) loss += a.z * lse * lse;
-    if (a.loss) a.loss[row] = loss;
-    if (a.lse) a.lse[row] = lse;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint32_t at = first + k * TPR * 8;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = g.factor * exp_under(e[k].get(j), g.m) - g.even;
+        if (at < n) store8(row, from_of<TINY>(at, n), TINY ? n : ~0u, v);
+    }
 }
 
-// Gradient of eight elements: factor exp(x - m) - even, and `hit` less at the target.
-template <typename T>
-__device__ __forceinline__ void write_gradient(T* row, uint32_t at, uint32_t n, const Eight<T>& e, float m, float factor, float even, float hit, int32_t target)
+// The target's element, once more by every thread that has written it: a wavefront's stores to one place keep their order.
+template <bool TINY, typename T, int TPR>
+__device__ __forceinline__ void write_target(T* row, uint32_t first, uint32_t n, int32_t target, float x, const Slope& g)
 {
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = factor * exp_under(e.get(j), m) - even;
-    if (at == ((uint32_t)target & ~7u)) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] -= j == (target & 7) ? hit : 0.0f;
-    }
-    store8(row, at, n, v);
+    bool mine = (uint32_t)target / 8 % TPR == first / 8;
+    if constexpr (!TINY) mine |= (uint32_t)target >= n - 8 && (n - 1) / 8 % TPR == first / 8;      // the last group has reached back for its eight
+    if (mine) row[target] = (T)(g.factor * exp_under(x, g.m) - g.even - g.hit);
 }
 
 template <typename T, int TPR>
@@ -157,12 +172,13 @@ __device__ __forceinline__ void write_zeros(T* row, uint32_t first, uint32_t n)
 }
 
 // TPR threads a row, K groups of eight elements each; FIT: a row is that long at most and stays in the registers, else it is read again for its gradient.
-template <typename T, int BLOCK, int TPR, int K, bool FIT>
+template <typename T, int BLOCK, int TPR, int K, bool FIT, bool TINY = false>
 __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs a)
 {
     constexpr int kWaves = TPR / kWave;
     static_assert(TPR == kWave || TPR == BLOCK, "a row is a wavefront's or a workgroup's");
-    const uint32_t row = workgroup() * (BLOCK / TPR) + threadIdx.x / TPR, n = a.vocab, first = threadIdx.x % TPR * 8;
+    const uint32_t row = TPR == BLOCK ? workgroup() : workgroup() * (BLOCK / TPR) + threadIdx.x / TPR, n = a.vocab;
+    uint32_t first = threadIdx.x % TPR * 8;
     if (row >= a.rows) return;
     const int32_t target = target_of(a, row);
     T* d = a.d.data ? row_of<T>(a, a.d, row) : nullptr;
@@ -176,20 +192,23 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
     }
     const T* x = row_of<const T>(a, a.x, row);
     const bool smooth = a.smoothing > 0.0f;
+    const float at_target = (float)x[target], g = d && a.d_loss ? a.d_loss[row] : 1.0f;
     Eight<T> e[K];
-    Part p{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+    Part p{-__builtin_inff(), 0.0f, 0.0f};
     if constexpr (FIT) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) e[k] = load_logits(x, first + k * TPR * 8, n);
-        p = part_of<T, K, TPR>(e, first, n, target, smooth);
+        for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, first + k * TPR * 8, n);
+        p = part_of<TINY, T, K, TPR>(e, first, n, smooth);
     } else {
         for (uint32_t at = first; at < n; at += TPR * 8 * K) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = load_logits(x, at + k * TPR * 8, n);
-            p = join(p, part_of<T, K, TPR>(e, at, n, target, smooth));
+            for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, at + k * TPR * 8, n);
+            p = join(p, part_of<TINY, T, K, TPR>(e, at, n, smooth));
         }
     }
-    p = wave_join(p);
+    p = wave_join(p, smooth);
+    // all of the row is read before any of it is written, which may be in its place
+    asm volatile("" : : "v"(at_target) : "memory");
     if constexpr (kWaves > 1) {
         __shared__ Part parts[kWaves];
         if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = p;
@@ -198,32 +217,35 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) p = join(p, parts[w]);
     }
-    if (threadIdx.x % TPR == 0) write_loss(a, row, p);
+    const float log_s = logf(p.s), lse = p.m + log_s;
+    if (threadIdx.x % TPR == 0) {
+        float loss = log_s + a.hit * (p.m - at_target);
+        if (smooth) loss += a.smoothing * (p.m - p.sum / (float)n);
+        if (a.z != 0.0f) loss += a.z * lse * lse;
+        if (a.loss) a.loss[row] = loss;
+        if (a.lse) a.lse[row] = lse;
+    }
     if (!d) return;
-    const float g = a.d_loss ? a.d_loss[row] : 1.0f;
-    const float factor = g * (1.0f + 2.0f * a.z * (p.m + logf(p.s))) / p.s, even = g * a.share, hit = g * a.hit;
+    const Slope slope{p.m, g * (1.0f + 2.0f * a.z * lse) / p.s, g * a.share, g * a.hit};
+    asm volatile("" : "+v"(first));         // places are worked out again, and not kept
     if constexpr (FIT) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const uint32_t at = first + k * TPR * 8;
-            if (at < n) write_gradient(d, at, n, e[k], p.m, factor, even, hit, target);
-        }
+        write_gradient<TINY, T, K, TPR>(d, first, n, e, slope);
     } else {
         for (uint32_t at = first; at < n; at += TPR * 8 * K) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = load_logits(x, at + k * TPR * 8, n);
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (at + k * TPR * 8 < n) write_gradient(d, at + k * TPR * 8, n, e[k], p.m, factor, even, hit, target);
+            for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, at + k * TPR * 8, n);
+            write_gradient<TINY, T, K, TPR>(d, at, n, e, slope);
         }
     }
+    write_target<TINY, T, TPR>(d, first, n, target, at_target, slope);
 }
 
 // The gradient alone, from the forward pass' lse.
-template <typename T, int BLOCK, int TPR, int K>
+template <typename T, int BLOCK, int TPR, int K, bool TINY>
 __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_backward_kernel(const LossArgs a)
 {
-    const uint32_t row = workgroup() * (BLOCK / TPR) + threadIdx.x / TPR, n = a.vocab, first = threadIdx.x % TPR * 8;
+    const uint32_t row = TPR == BLOCK ? workgroup() : workgroup() * (BLOCK / TPR) + threadIdx.x / TPR, n = a.vocab;
+    uint32_t first = threadIdx.x % TPR * 8;
     if (row >= a.rows) return;
     const int32_t target = target_of(a, row);
     T* d = row_of<T>(a, a.d, row);
@@ -232,28 +254,24 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_backward_kernel(const
         return;
     }
     const T* x = row_of<const T>(a, a.x, row);
-    const float lse = a.lse[row], g = a.d_loss ? a.d_loss[row] : 1.0f;
-    const float factor = g * (1.0f + 2.0f * a.z * lse), even = g * a.share, hit = g * a.hit;
+    const float at_target = (float)x[target], lse = a.lse[row], g = a.d_loss ? a.d_loss[row] : 1.0f;
+    const Slope slope{lse, g * (1.0f + 2.0f * a.z * lse), g * a.share, g * a.hit};
     for (uint32_t at = first; at < n; at += TPR * 8 * K) {
         Eight<T> e[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            e[k] = Eight<T>{};
-            if (at + k * TPR * 8 < n) e[k] = load8(x, at + k * TPR * 8, n);
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (at + k * TPR * 8 < n) write_gradient(d, at + k * TPR * 8, n, e[k], lse, factor, even, hit, target);
+        for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, at + k * TPR * 8, n);
+        write_gradient<TINY, T, K, TPR>(d, at, n, e, slope);
     }
+    write_target<TINY, T, TPR>(d, first, n, target, at_target, slope);
 }
 
 template <typename T>
 int loss(const LossArgs& a, hipStream_t st)
 {
     const uint32_t V = a.vocab;
-#define SDL_LAUNCH(BLOCK, TPR, K, FIT) \
-    hipLaunchKernelGGL((sdl_cross_entropy_kernel<T, BLOCK, TPR, K, FIT>), grid_of((a.rows - 1) / (BLOCK / TPR) + 1), dim3(BLOCK), 0, st, a)
-    if (V <= 512) SDL_LAUNCH(256, 64, 1, true);
+#define SDL_LAUNCH(BLOCK, TPR, K, ...) \
+    hipLaunchKernelGGL((sdl_cross_entropy_kernel<T, BLOCK, TPR, K, __VA_ARGS__>), grid_of((a.rows - 1) / (BLOCK / TPR) + 1), dim3(BLOCK), 0, st, a)
+    if (V <= 512) SDL_LAUNCH(256, 64, 1, true, true);
     else if (V <= 1024) SDL_LAUNCH(256, 64, 2, true);
     else if (V <= 2048) SDL_LAUNCH(256, 64, 4, true);
     else if (V <= 4096) SDL_LAUNCH(256, 256, 2, true);
@@ -261,8 +279,15 @@ int loss(const LossArgs& a, hipStream_t st)
     else if (V <= 16384) SDL_LAUNCH(512, 512, 4, true);
     else if (V <= 32768) SDL_LAUNCH(512, 512, 8, true);
     else if (V <= 65536) SDL_LAUNCH(1024, 1024, 8, true);
-    else if (V <= 131072 && sizeof(T) == 2) SDL_LAUNCH(1024, 1024, 16, true);
-    else SDL_LAUNCH(1024, 1024, 4, false);
+    else {
+        if constexpr (sizeof(T) == 2) {
+            if (V <= 131072) {
+                SDL_LAUNCH(1024, 1024, 16, true);
+                return launched();
+            }
+        }
+        SDL_LAUNCH(1024, 1024, 4, false);
+    }
 #undef SDL_LAUNCH
     return launched();
 }
@@ -270,10 +295,12 @@ int loss(const LossArgs& a, hipStream_t st)
 template <typename T>
 int gradient(const LossArgs& a, hipStream_t st)
 {
-    if (a.vocab <= 2048)
-        hipLaunchKernelGGL((sdl_cross_entropy_backward_kernel<T, 256, 64, 4>), grid_of((a.rows - 1) / 4 + 1), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((sdl_cross_entropy_backward_kernel<T, 256, 256, 4>), grid_of(a.rows), dim3(256), 0, st, a);
+#define SDL_LAUNCH(TPR, K, TINY) \
+    hipLaunchKernelGGL((sdl_cross_entropy_backward_kernel<T, 256, TPR, K, TINY>), grid_of((a.rows - 1) / (256 / TPR) + 1), dim3(256), 0, st, a)
+    if (a.vocab <= 512) SDL_LAUNCH(64, 1, true);
+    else if (a.vocab <= 2048) SDL_LAUNCH(64, 2, false);
+    else SDL_LAUNCH(256, 4, false);
+#undef SDL_LAUNCH
     return launched();
 }
 
