@@ -78,31 +78,80 @@ __device__ __forceinline__ Part wave_join(const Part& p, bool smooth)
 __device__ __forceinline__ void forget(Eight<__bf16>& e, float& now) { asm volatile("" : "+v"(e.w), "+v"(now)); }
 __device__ __forceinline__ void forget(Eight<float>&, float&) {}
 
-// Where the eight elements lie that stand for [at, at + 8) of a row of n: in their place, or at the row's end, where the ones before `at` are someone else's too.
-// All of a thread's loads are whole accesses that wait for nothing, and what two threads write to one place is the same.  (TINY rows, which may have less than eight, go element by
-// element, with -infinity behind the row.)
+// A row of n elements in groups of eight that start on 16 bytes: group g stands for [8 g - lead, 8 g - lead + 8).  The first and the last, which may stick out, are the eight
+// elements at the row's end instead, so that others' are among them too: those are not counted, and what two threads write to one place is the same.  All of a thread's accesses are
+// whole ones that wait for nothing.  Rows of 32001 in bf16 instead of 32000: 219 us with groups that start with the row, 179 so.  (TINY rows, which may have less than eight
+// elements, go element by element.)
 template <bool TINY>
-__device__ __forceinline__ uint32_t from_of(uint32_t at, uint32_t n)
-{
-    return TINY ? at : min(at, n - 8);
-}
-template <bool TINY, typename T>
-__device__ __forceinline__ Eight<T> load_logits(const T* row, uint32_t at, uint32_t n)
+struct Groups {
+    uint32_t n;
+    int32_t lead;
+
+    template <typename T>
+    __device__ __forceinline__ Groups(uint32_t n_, const T* row) : n(n_), lead(TINY ? 0 : (int32_t)((uintptr_t)row % 16 / sizeof(T))) {}
+    __device__ __forceinline__ bool there(uint32_t first) const { return first < n + lead; }      // first = 8 g
+    __device__ __forceinline__ uint32_t from(uint32_t first) const
+    {
+        return TINY ? first : (uint32_t)min(max((int32_t)first - lead, 0), (int32_t)n - 8);
+    }
+    // whether the j-th element from from(first) on is the group's
+    __device__ __forceinline__ bool has(uint32_t first, int j) const
+    {
+        return TINY ? first + j < n : from(first) + j + lead - first < 8;
+    }
+    // whether a group that this thread, whose first one is 8 g, has of every TPR touches the element
+    template <int TPR>
+    __device__ __forceinline__ bool touches(uint32_t first, uint32_t element) const
+    {
+        const uint32_t own = first / 8;
+        if (TINY) return element / 8 % TPR == own;
+        return (element + lead) / 8 % TPR == own || (element < 8 && own == 0) || (element >= n - 8 && (n - 1 + lead) / 8 % TPR == own);
+    }
+    template <typename T>
+    __device__ __forceinline__ Eight<T> load(const T* row, uint32_t first) const;
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, uint32_t first, const float* v) const;
+};
+
+// In bf16, where an access of a wavefront's is whole cache lines, rows go past the caches: 8192 of 32000 with their gradient 195 us with cached accesses, 179 so; 256 of them 10.4
+// and 9.0.  In fp32 it is two halves of every 32 bytes: 4096 rows 203 us and 216, 1551 of 5003 13.0 and 16.1.
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+
+template <bool TINY>
+template <typename T>
+__device__ __forceinline__ Eight<T> Groups<TINY>::load(const T* row, uint32_t first) const
 {
     if constexpr (TINY) {
         const T low = (T)-__builtin_inff();
         T v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = at + j < n ? row[at + j] : low;
+        for (int j = 0; j < 8; ++j) v[j] = first + j < n ? row[first + j] : low;
         return __builtin_bit_cast(Eight<T>, v);
+    } else if constexpr (sizeof(T) == 2) {
+        const u32x4_at2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_at2*>(row + from(first)));
+        return Eight<T>{u32x4{w.x, w.y, w.z, w.w}};
     } else {
-        return load8(row, from_of<TINY>(at, n), ~0u);
+        return load8(row, from(first), ~0u);
+    }
+}
+
+template <bool TINY>
+template <typename T>
+__device__ __forceinline__ void Groups<TINY>::store(T* row, uint32_t first, const float* v) const
+{
+    if constexpr (TINY) {
+        store8(row, first, n, v);
+    } else if constexpr (sizeof(T) == 2) {
+        const u32x4_at2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4_at2*>(row + from(first)));
+    } else {
+        store8(row, from(first), ~0u, v);
     }
 }
 
 // What K groups of eight elements, TPR groups apart, are as a part of their row.  No branch goes by an element: a thread's groups stay in the words they came in.
 template <bool TINY, typename T, int K, int TPR>
-__device__ __forceinline__ Part part_of(Eight<T> (&e)[K], uint32_t first, uint32_t n, bool smooth)
+__device__ __forceinline__ Part part_of(Eight<T> (&e)[K], uint32_t first, const Groups<TINY>& groups, bool smooth)
 {
     Part p{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
@@ -116,20 +165,18 @@ __device__ __forceinline__ Part part_of(Eight<T> (&e)[K], uint32_t first, uint32
     const float base = p.m == -__builtin_inff() ? 0.0f : p.m;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const uint32_t at = first + k * TPR * 8, from = from_of<TINY>(at, n);
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = from + j >= at ? exp_under(e[k].get(j), base) : 0.0f;
+        for (int j = 0; j < 8; ++j) v[j] = groups.has(first + k * TPR * 8, j) ? exp_under(e[k].get(j), base) : 0.0f;
         p.s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         forget(e[k], p.s);
     }
     if (smooth) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const uint32_t at = first + k * TPR * 8, from = from_of<TINY>(at, n);
             float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += (TINY ? at + j < n : from + j >= at) ? e[k].get(j) : 0.0f;
+            for (int j = 0; j < 8; ++j) sum += groups.has(first + k * TPR * 8, j) ? e[k].get(j) : 0.0f;
             p.sum += sum;
             forget(e[k], p.sum);
         }
@@ -143,32 +190,29 @@ struct Slope {
 };
 
 template <bool TINY, typename T, int K, int TPR>
-__device__ __forceinline__ void write_gradient(T* row, uint32_t first, uint32_t n, Eight<T> (&e)[K], const Slope& g)
+__device__ __forceinline__ void write_gradient(T* row, uint32_t first, const Groups<TINY>& groups, Eight<T> (&e)[K], const Slope& g)
 {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const uint32_t at = first + k * TPR * 8;
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = g.factor * exp_under(e[k].get(j), g.m) - g.even;
-        if (at < n) store8(row, from_of<TINY>(at, n), TINY ? n : ~0u, v);
+        if (groups.there(first + k * TPR * 8)) groups.store(row, first + k * TPR * 8, v);
     }
 }
 
 // The target's element, once more by every thread that has written it: a wavefront's stores to one place keep their order.
 template <bool TINY, typename T, int TPR>
-__device__ __forceinline__ void write_target(T* row, uint32_t first, uint32_t n, int32_t target, float x, const Slope& g)
+__device__ __forceinline__ void write_target(T* row, uint32_t first, const Groups<TINY>& groups, int32_t target, float x, const Slope& g)
 {
-    bool mine = (uint32_t)target / 8 % TPR == first / 8;
-    if constexpr (!TINY) mine |= (uint32_t)target >= n - 8 && (n - 1) / 8 % TPR == first / 8;      // the last group has reached back for its eight
-    if (mine) row[target] = (T)(g.factor * exp_under(x, g.m) - g.even - g.hit);
+    if (groups.template touches<TPR>(first, (uint32_t)target)) row[target] = (T)(g.factor * exp_under(x, g.m) - g.even - g.hit);
 }
 
-template <typename T, int TPR>
-__device__ __forceinline__ void write_zeros(T* row, uint32_t first, uint32_t n)
+template <bool TINY, typename T, int TPR>
+__device__ __forceinline__ void write_zeros(T* row, uint32_t first, const Groups<TINY>& groups)
 {
     const float zero[8] = {};
-    for (uint32_t at = first; at < n; at += TPR * 8) store8(row, at, n, zero);
+    for (uint32_t at = first; groups.there(at); at += TPR * 8) groups.store(row, at, zero);
 }
 
 // TPR threads a row, K groups of eight elements each; FIT: a row is that long at most and stays in the registers, else it is read again for its gradient.
@@ -187,23 +231,24 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
             if (a.loss) a.loss[row] = 0.0f;
             if (a.lse) a.lse[row] = 0.0f;
         }
-        if (d) write_zeros<T, TPR>(d, first, n);
+        if (d) write_zeros<TINY, T, TPR>(d, first, Groups<TINY>(n, d));
         return;
     }
     const T* x = row_of<const T>(a, a.x, row);
     const bool smooth = a.smoothing > 0.0f;
     const float at_target = (float)x[target], g = d && a.d_loss ? a.d_loss[row] : 1.0f;
+    const Groups<TINY> groups(n, d ? d : x);
     Eight<T> e[K];
     Part p{-__builtin_inff(), 0.0f, 0.0f};
     if constexpr (FIT) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, first + k * TPR * 8, n);
-        p = part_of<TINY, T, K, TPR>(e, first, n, smooth);
+        for (int k = 0; k < K; ++k) e[k] = groups.load(x, first + k * TPR * 8);
+        p = part_of<TINY, T, K, TPR>(e, first, groups, smooth);
     } else {
-        for (uint32_t at = first; at < n; at += TPR * 8 * K) {
+        for (uint32_t at = first; groups.there(at); at += TPR * 8 * K) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, at + k * TPR * 8, n);
-            p = join(p, part_of<TINY, T, K, TPR>(e, at, n, smooth));
+            for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * 8);
+            p = join(p, part_of<TINY, T, K, TPR>(e, at, groups, smooth));
         }
     }
     p = wave_join(p, smooth);
@@ -229,15 +274,15 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
     const Slope slope{p.m, g * (1.0f + 2.0f * a.z * lse) / p.s, g * a.share, g * a.hit};
     asm volatile("" : "+v"(first));         // places are worked out again, and not kept
     if constexpr (FIT) {
-        write_gradient<TINY, T, K, TPR>(d, first, n, e, slope);
+        write_gradient<TINY, T, K, TPR>(d, first, groups, e, slope);
     } else {
-        for (uint32_t at = first; at < n; at += TPR * 8 * K) {
+        for (uint32_t at = first; groups.there(at); at += TPR * 8 * K) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, at + k * TPR * 8, n);
-            write_gradient<TINY, T, K, TPR>(d, at, n, e, slope);
+            for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * 8);
+            write_gradient<TINY, T, K, TPR>(d, at, groups, e, slope);
         }
     }
-    write_target<TINY, T, TPR>(d, first, n, target, at_target, slope);
+    write_target<TINY, T, TPR>(d, first, groups, target, at_target, slope);
 }
 
 // The gradient alone, from the forward pass' lse.
@@ -250,19 +295,20 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_backward_kernel(const
     const int32_t target = target_of(a, row);
     T* d = row_of<T>(a, a.d, row);
     if (target < 0) {
-        write_zeros<T, TPR>(d, first, n);
+        write_zeros<TINY, T, TPR>(d, first, Groups<TINY>(n, d));
         return;
     }
     const T* x = row_of<const T>(a, a.x, row);
     const float at_target = (float)x[target], lse = a.lse[row], g = a.d_loss ? a.d_loss[row] : 1.0f;
+    const Groups<TINY> groups(n, d);
     const Slope slope{lse, g * (1.0f + 2.0f * a.z * lse), g * a.share, g * a.hit};
-    for (uint32_t at = first; at < n; at += TPR * 8 * K) {
+    for (uint32_t at = first; groups.there(at); at += TPR * 8 * K) {
         Eight<T> e[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) e[k] = load_logits<TINY>(x, at + k * TPR * 8, n);
-        write_gradient<TINY, T, K, TPR>(d, at, n, e, slope);
+        for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * 8);
+        write_gradient<TINY, T, K, TPR>(d, at, groups, e, slope);
     }
-    write_target<TINY, T, TPR>(d, first, n, target, at_target, slope);
+    write_target<TINY, T, TPR>(d, first, groups, target, at_target, slope);
 }
 
 template <typename T>
@@ -271,17 +317,22 @@ int loss(const LossArgs& a, hipStream_t st)
     const uint32_t V = a.vocab;
 #define SDL_LAUNCH(BLOCK, TPR, K, ...) \
     hipLaunchKernelGGL((sdl_cross_entropy_kernel<T, BLOCK, TPR, K, __VA_ARGS__>), grid_of((a.rows - 1) / (BLOCK / TPR) + 1), dim3(BLOCK), 0, st, a)
+    const View& rows = a.d.data ? a.d : a.x;
+    const bool even = aligned_to(rows.data, 16) && rows.batch * (int64_t)sizeof(T) % 16 == 0 && rows.token * (int64_t)sizeof(T) % 16 == 0;
+    const uint32_t room = even ? V : V + 7;         // a row's groups are one more where it does not start on 16 bytes
     if (V <= 512) SDL_LAUNCH(256, 64, 1, true, true);
-    else if (V <= 1024) SDL_LAUNCH(256, 64, 2, true);
-    else if (V <= 2048) SDL_LAUNCH(256, 64, 4, true);
-    else if (V <= 4096) SDL_LAUNCH(256, 256, 2, true);
-    else if (V <= 8192) SDL_LAUNCH(256, 256, 4, true);
-    else if (V <= 16384) SDL_LAUNCH(512, 512, 4, true);
-    else if (V <= 32768) SDL_LAUNCH(512, 512, 8, true);
-    else if (V <= 65536) SDL_LAUNCH(1024, 1024, 8, true);
+    else if (room <= 1024) SDL_LAUNCH(256, 64, 2, true);
+    else if (room <= 2048) SDL_LAUNCH(256, 64, 4, true);
+    else if (room <= 4096) SDL_LAUNCH(256, 256, 2, true);
+    else if (room <= 8192) SDL_LAUNCH(256, 256, 4, true);
+    else if (room <= 16384) SDL_LAUNCH(512, 512, 4, true);
+    // without a gradient, fewer threads a row and more rows at a time: 8192 of 32000, half of them without a target, 51.7 us with 512 and 47.1 with 256; with one 179 and 185
+    else if (room <= 32768 && !a.d.data) SDL_LAUNCH(256, 256, 16, true);
+    else if (room <= 32768) SDL_LAUNCH(512, 512, 8, true);
+    else if (room <= 65536) SDL_LAUNCH(512, 512, 16, true);
     else {
         if constexpr (sizeof(T) == 2) {
-            if (V <= 131072) {
+            if (room <= 131072) {
                 SDL_LAUNCH(1024, 1024, 16, true);
                 return launched();
             }
