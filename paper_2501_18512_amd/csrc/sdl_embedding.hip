@@ -4,7 +4,7 @@
 //
 // Backward: d_table[v] = scale * sum of d_out[t] over the places t with token[t] = v.  Every row of the table is written, most of
 // them as zeros, and every row of d_out is read once; no atomics, one order of every sum.  What is done:
-//   1. sort   chunks of 2048 places are sorted by (token, place) in shared memory; meanwhile other workgroups write zeros
+//   1. sort   chunks of 1024 places are sorted by (token, place) in shared memory; meanwhile other workgroups write zeros
 //   2. merge  (more than one chunk) the rank of a place is its rank in its chunk and, by bisection, in the others: up to 32 sorted
 //             runs become one, again and again until one is left
 //   3. reduce the sorted places are cut into segments of equal length, whatever the tokens are.  A run of one token that lies within a segment is
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(256) sdl_embedding_kernel(const LookupArgs a)
 
 // ------------------------------------------------------------------------------------------------------ backward
 
-constexpr uint32_t kChunk = 2048;           // places that a workgroup sorts
+constexpr uint32_t kChunk = 1024;           // places that a workgroup sorts, one a thread
 constexpr uint32_t kFan = 32;               // sorted runs that become one
 constexpr uint32_t kFill = 1024 * 8;        // elements of a table without gaps that a workgroup clears at a time
 
@@ -124,84 +124,162 @@ struct SortArgs {
     Fill fill;
 };
 
+// x of lane ^ J
+template <int J>
+__device__ __forceinline__ uint32_t of_lane(uint32_t x)
+{
+#define SDL_DPP(v, ctrl) (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v), ctrl, 0xf, 0xf, true)
+    if constexpr (J == 1) return SDL_DPP(x, 0xb1);
+    else if constexpr (J == 2) return SDL_DPP(x, 0x4e);
+    else if constexpr (J == 4) return SDL_DPP(SDL_DPP(x, 0x141), 0x1b);      // the other end of eight, and of four
+    else if constexpr (J == 8) return SDL_DPP(x, 0x128);                      // half of sixteen around
+    else if constexpr (J == 16) {
+        const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, x, false, false));
+        return threadIdx.x & 16 ? p[0] : p[1];
+    } else {
+        static_assert(J == 32, "a lane of the wavefront");
+        const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, x, false, false));
+        return threadIdx.x & 32 ? p[0] : p[1];
+    }
+#undef SDL_DPP
+}
+
+constexpr uint32_t log2_of(uint32_t x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
+
+// One exchange of a bitonic sort: places J apart, in runs of S that go up and down in turn.
+template <uint32_t S, uint32_t J>
+__device__ __forceinline__ void exchange(uint64_t& key, uint64_t (*lds)[kChunk])
+{
+    uint64_t other;
+    if constexpr (J >= (uint32_t)kWave) {
+        // two arrays in turn, so that one barrier is enough: the exchanges of S = 128, 256, .. through shared memory are 1, 2, .., counted from the first
+        constexpr uint32_t kStage = log2_of(S) - 7, kNumber = kStage * (kStage + 1) / 2 + log2_of(S / 2) - log2_of(J);
+        uint64_t* at = lds[kNumber % 2];
+        at[threadIdx.x] = key;
+        __syncthreads();
+        other = at[threadIdx.x ^ J];
+    } else {
+        other = (uint64_t)of_lane<(int)J>((uint32_t)(key >> 32)) << 32 | of_lane<(int)J>((uint32_t)key);
+    }
+    const bool least = ((threadIdx.x & J) == 0) == ((threadIdx.x & S) == 0);
+    key = (other < key) == least ? other : key;
+    if constexpr (J > 1) exchange<S, J / 2>(key, lds);
+}
+
 // Bitonic sort of one chunk (K. E. Batcher, Sorting networks and their applications, 1968): keys differ, so that equal tokens keep their order.
+template <uint32_t S>
+__device__ __forceinline__ void sort_runs(uint64_t& key, uint32_t n, uint64_t (*lds)[kChunk])
+{
+    exchange<S, S / 2>(key, lds);
+    if constexpr (S < kChunk)
+        if (S < n) sort_runs<2 * S>(key, n, lds);
+}
+
 template <typename P>
 __global__ void __launch_bounds__(1024) sdl_embedding_sort_kernel(const SortArgs a)
 {
-    __shared__ uint64_t k[kChunk];
+    __shared__ uint64_t lds[2][kChunk];
     if (blockIdx.x >= a.chunks) {
         fill<P>(a.fill, blockIdx.x - a.chunks, gridDim.x - a.chunks);
         return;
     }
-    const uint32_t base = blockIdx.x * kChunk, n = min(kChunk, a.n - base);
-    uint32_t size = 2;
-    while (size < n) size *= 2;
-    for (uint32_t i = threadIdx.x; i < size; i += 1024) k[i] = i < n ? ((uint64_t)a.tokens.get(base + i) << 32) | (base + i) : ~0ull;
-    __syncthreads();
-    for (uint32_t s = 2; s <= size; s *= 2) {
-        for (uint32_t j = s / 2; j; j /= 2) {
-            const uint32_t t = threadIdx.x;
-            if (t < size / 2) {
-                const uint32_t i = 2 * t - (t & (j - 1));
-                const uint64_t x = k[i], y = k[i + j];
-                if ((x > y) == ((i & s) == 0)) {
-                    k[i] = y;
-                    k[i + j] = x;
-                }
-            }
-            __syncthreads();
-        }
-    }
-    for (uint32_t i = threadIdx.x; i < n; i += 1024) a.keys[base + i] = k[i];
+    const uint32_t i = blockIdx.x * kChunk + threadIdx.x, n = min(kChunk, a.n - blockIdx.x * kChunk);
+    uint64_t key = threadIdx.x < n ? ((uint64_t)a.tokens.get(i) << 32) | i : ~0ull;
+    sort_runs<2>(key, n, lds);
+    if (threadIdx.x < n) a.keys[i] = key;
 }
 
 struct MergeArgs {
     const uint64_t* from;
     uint64_t* to;
-    uint32_t n, run, groups;    // length of the sorted runs; workgroups that merge
+    uint32_t n, run, groups;    // length of the sorted runs, a power of two; workgroups that merge
     Fill fill;
 };
 
-// Keys of runs[r] that are less than `key`, for SEARCHES runs at a time: bisections that wait for memory together.
+// A place's rank is its place in its run and the number of lesser keys in each of the others, by bisection; four lanes share a place, each with every fourth run.
+// Chunks are looked through in shared memory, eight of them at a time: a search in memory waits ten times, for 1 us each.
 template <typename P>
 __global__ void __launch_bounds__(1024) sdl_embedding_merge_kernel(const MergeArgs a)
 {
+    constexpr uint32_t kHeld = 8;
+    __shared__ uint64_t held[kHeld * kChunk];
     if (blockIdx.x >= a.groups) {
         fill<P>(a.fill, blockIdx.x - a.groups, gridDim.x - a.groups);
         return;
     }
-    // four lanes share a place: each looks it up in every fourth run
-    const uint32_t share = threadIdx.x % 4;
-    const uint64_t p64 = (uint64_t)blockIdx.x * 256 + threadIdx.x / 4;
-    const bool mine = p64 < a.n;
-    const uint32_t p = mine ? (uint32_t)p64 : a.n - 1;
-    const uint32_t own = p / a.run, first = own / kFan * kFan, runs = (a.n - 1) / a.run + 1;
-    const uint64_t key = a.from[p];
-    uint32_t rank = share == 0 ? p - own * a.run : 0;
-    constexpr int kSearches = 8;
-    static_assert(kSearches * 4 == kFan, "all of a group's runs at once");
-    uint32_t lo[kSearches], len[kSearches];
+    // a workgroup's places are of one chunk
+    const uint32_t share = threadIdx.x % 4, p = blockIdx.x * 256 + threadIdx.x / 4, own = blockIdx.x * 256 / kChunk, first = own / kFan * kFan;
+    const uint32_t runs = min((a.n - 1) / kChunk + 1 - first, kFan);
+    const uint64_t key = a.from[min(p, a.n - 1)];
+    uint32_t rank = share == 0 ? p - own * kChunk : 0;
+    for (uint32_t r0 = first; r0 < first + runs; r0 += kHeld) {
+        if (r0 > first) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSearches; ++i) {
-        const uint32_t r = first + i * 4 + share;
-        const bool there = r < runs && r != own;
-        lo[i] = there ? r * a.run : 0;
-        len[i] = there ? min(a.run, a.n - r * a.run) : 0;
-    }
-    for (uint32_t left = a.run; left; left /= 2) {        // lengths fall below their half, rounded down, or come to it
+        for (uint32_t i = 0; i < kHeld; ++i) {
+            const uint64_t k = (uint64_t)(r0 + i) * kChunk + threadIdx.x;
+            held[i * kChunk + threadIdx.x] = k < a.n ? a.from[k] : ~0ull;
+        }
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kSearches; ++i) {
-            if (!len[i]) continue;
-            const uint32_t half = len[i] / 2;
-            const bool less = a.from[lo[i] + half] < key;
-            rank += less ? half + 1 : 0;
-            lo[i] += less ? half + 1 : 0;
-            len[i] = less ? len[i] - half - 1 : half;
+        for (uint32_t i = 0; i < kHeld; i += 4) {
+            const uint32_t r = r0 + i + share;
+            if (r == own || r >= first + runs) continue;
+            const uint64_t* run = held + (i + share) * kChunk;
+            uint32_t lesser = 0;
+#pragma unroll
+            for (uint32_t step = kChunk / 2; step; step /= 2) lesser += run[lesser + step - 1] < key ? step : 0;
+            rank += lesser + (run[lesser] < key);
         }
     }
     rank += __shfl_xor(rank, 1);
     rank += __shfl_xor(rank, 2);
-    if (mine && share == 0) a.to[first * a.run + rank] = key;
+    if (p < a.n && share == 0) a.to[first * kChunk + rank] = key;
+}
+
+// The same for longer runs, in memory: eight searches a lane wait together, and take three keys at a time, which divide what is left by four.
+__global__ void __launch_bounds__(1024) sdl_embedding_merge_long_kernel(const MergeArgs a)
+{
+    const uint32_t share = threadIdx.x % 4;
+    const uint32_t p = blockIdx.x * 256 + threadIdx.x / 4, own = blockIdx.x * 256 / a.run, first = own / kFan * kFan;
+    const uint32_t runs = min((a.n - 1) / a.run + 1 - first, kFan);
+    const uint64_t key = a.from[min(p, a.n - 1)];
+    uint32_t rank = share == 0 ? p - own * a.run : 0;
+    constexpr int kSearches = 8;
+    static_assert(kSearches * 4 == kFan, "all of a group's runs at once");
+    uint32_t at[kSearches];         // keys in front of it are lesser ones
+#pragma unroll
+    for (int i = 0; i < kSearches; ++i) at[i] = (first + i * 4 + share) * a.run;
+    // no load waits for a comparison: a last run that is shorter goes on with what counts as more than all
+    const auto load = [&](int i, uint32_t offset) { return a.from[min(at[i] + offset, a.n - 1)]; };
+    const auto less = [&](int i, uint32_t offset, uint64_t k) { return (uint32_t)(k < key && at[i] + offset < a.n); };
+    uint32_t left = a.run;
+    for (; left >= 4; left /= 4) {
+        uint64_t k[kSearches][3];
+#pragma unroll
+        for (int i = 0; i < kSearches; ++i)
+            if (i * 4u < runs)
+#pragma unroll
+                for (int q = 0; q < 3; ++q) k[i][q] = load(i, left / 4 * (q + 1) - 1);
+#pragma unroll
+        for (int i = 0; i < kSearches; ++i)
+            if (i * 4u < runs) {
+                uint32_t lesser = 0;
+#pragma unroll
+                for (int q = 0; q < 3; ++q) lesser += less(i, left / 4 * (q + 1) - 1, k[i][q]);
+                at[i] += lesser * (left / 4);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < kSearches; ++i) {
+        const uint32_t r = first + i * 4 + share;
+        if (i * 4u >= runs) break;
+        if (left == 2) at[i] += less(i, 0, load(i, 0));
+        at[i] += less(i, 0, load(i, 0));
+        if (r != own && i * 4 + share < runs) rank += at[i] - r * a.run;
+    }
+    rank += __shfl_xor(rank, 1);
+    rank += __shfl_xor(rank, 2);
+    if (p < a.n && share == 0) a.to[first * a.run + rank] = key;
 }
 
 struct ReduceArgs {
@@ -234,20 +312,25 @@ __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceA
     const uint32_t at = ((unit - seg * a.slices.d) * LPR + threadIdx.x % LPR) * 8, W = a.table.width;
     if (seg >= a.segments || at >= W) return;
     const uint32_t s0 = seg * a.length, s1 = min(s0 + a.length, a.places.n);
-    uint32_t cur = token_of(a.keys[s0]);
+    // the keys around the segment with those of its first places: nothing waits for one after the other
+    const uint64_t before = s0 > 0 ? a.keys[s0 - 1] : ~0ull, behind = s1 < a.places.n ? a.keys[s1] : ~0ull;
+    uint64_t k[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = s0 + j < s1 ? a.keys[s0 + j] : ~0ull;
+    uint32_t cur = token_of(k[0]);
     if (cur == kNone) return;
-    bool open = s0 > 0 && token_of(a.keys[s0 - 1]) == cur;        // begun in front of this segment
+    bool open = s0 > 0 && token_of(before) == cur;        // begun in front of this segment
     float acc[8] = {};
     for (uint32_t p = s0; p < s1; p += 8) {
-        uint64_t k[8];
+        uint64_t next[8];
         Eight<T> e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) k[j] = p + j < s1 ? a.keys[p + j] : ~0ull;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             e[j] = Eight<T>{};
             if (token_of(k[j]) != kNone) e[j] = load8(place_row<const T>(a.places, (uint32_t)k[j]), at, W);
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) next[j] = p + 8 + j < s1 ? a.keys[p + 8 + j] : ~0ull;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (p + j >= s1) break;
@@ -267,53 +350,81 @@ __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceA
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i] += e[j].get(i);
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] = next[j];
     }
     if (cur == kNone) return;
-    const bool on = s1 < a.places.n && token_of(a.keys[s1]) == cur;
+    const bool on = token_of(behind) == cur;
     if (open || on)
         store8(a.lines + ((uint64_t)seg * 2 + (open ? 0 : 1)) * W, at, W, acc);
     else
         write_row<P>(a.table, cur, at, a.scale, acc);
 }
 
-// The lines of a run that leaves its first segment: eight wavefronts add up a share each, in order, then the shares.
+// The lines of the runs that leave their first segments: a wavefront a segment, which adds up a few lines in order; of many, all sixteen of the workgroup a share each, and
+// then the shares.  (A workgroup a segment and part of the columns: 17 us for 4000 that have nothing to do.)
+constexpr uint32_t kJoined = 16, kFew = 16;
+
 template <typename P>
-__global__ void __launch_bounds__(512) sdl_embedding_join_kernel(const ReduceArgs a)
+__global__ void __launch_bounds__(1024) sdl_embedding_join_kernel(const ReduceArgs a)
 {
-    __shared__ float sums[8][kWave][9];
-    const uint32_t seg = div(blockIdx.x, a.slices), lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const uint32_t at = ((blockIdx.x - seg * a.slices.d) * kWave + lane) * 8, W = a.table.width;
-    const uint32_t s0 = seg * a.length, s1 = s0 + a.length;
-    const uint32_t v = token_of(a.keys[s1 - 1]);           // there is a segment behind this one
-    if (v == kNone || token_of(a.keys[s1]) != v) return;
-    if (s0 > 0 && token_of(a.keys[s0 - 1]) == v) return;   // all of this segment is one run from further up
-    uint32_t lo = s1, hi = a.places.n;                      // first place behind the run
-    while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (token_of(a.keys[mid]) > v) hi = mid;
-        else lo = mid + 1;
-    }
-    const uint32_t lines = (lo - 1) / a.length - seg + 1;   // this segment's second line and the others' first ones
-    const uint32_t each = (lines + 7) / 8, from = min(wave * each, lines), to = min(from + each, lines);
-    float acc[8] = {};
-    if (at < W) {
-        const float* line = a.lines + (uint64_t)seg * 2 * W;
-#pragma unroll 4
+    __shared__ float sums[kJoined][kWave][9];
+    __shared__ uint32_t many[kJoined];          // lines, where they are many
+    const uint32_t group = div(blockIdx.x, a.slices), lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t at = ((blockIdx.x - group * a.slices.d) * kWave + lane) * 8, W = a.table.width, seg = group * kJoined + wave;
+    const auto add = [&](uint32_t s, uint32_t from, uint32_t to, float* acc) {
+        const float* line = a.lines + (uint64_t)s * 2 * W;
+#pragma unroll 8
         for (uint32_t l = from; l < to; ++l) {
             const Eight<float> e = load8(line + ((uint64_t)l * 2 + (l == 0)) * W, at, W);
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] += e.get(j);
         }
+    };
+    uint32_t lines = 0;
+    if (seg + 1 < a.segments) {
+        const uint32_t s0 = seg * a.length, s1 = s0 + a.length;
+        const uint64_t before = s0 > 0 ? a.keys[s0 - 1] : ~0ull, last = a.keys[s1 - 1];
+        // first tokens of the segments that follow, one a lane: the run goes on through those that have its own
+        uint32_t other = seg + 1 + lane < a.segments ? token_of(a.keys[(seg + 1 + lane) * a.length]) : kNone;
+        const uint32_t v = token_of(last);
+        // (all of a segment may be one run from further up)
+        if (v != kNone && !(s0 > 0 && token_of(before) == v)) {
+            for (lines = 1;;) {                 // this segment's second line, and the others' first ones
+                const uint32_t more = (uint32_t)__popcll(__ballot(other == v));
+                lines += more;
+                if (more < (uint32_t)kWave) break;
+                other = seg + lines + lane < a.segments ? token_of(a.keys[(seg + lines + lane) * a.length]) : kNone;
+            }
+            if (lines > 1 && lines <= kFew && at < W) {
+                float acc[8] = {};
+                add(seg, 0, lines, acc);
+                write_row<P>(a.table, v, at, a.scale, acc);
+            }
+        }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sums[wave][lane][j] = acc[j];
+    if (lane == 0) many[wave] = lines > kFew ? lines : 0;
     __syncthreads();
-    if (wave != 0 || at >= W) return;
+    for (uint32_t k = 0; k < kJoined; ++k) {
+        const uint32_t n = many[k], s = group * kJoined + k;
+        if (n == 0) continue;
+        const uint32_t each = (n + kJoined - 1) / kJoined, from = min(wave * each, n);
+        float acc[8] = {};
+        if (at < W) add(s, from, min(from + each, n), acc);
 #pragma unroll
-    for (int w = 1; w < 8; ++w)
+        for (int j = 0; j < 8; ++j) sums[wave][lane][j] = acc[j];
+        __syncthreads();
+        if (wave == k && at < W) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += sums[w][lane][j];
-    write_row<P>(a.table, v, at, a.scale, acc);
+            for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+#pragma unroll
+            for (uint32_t w = 0; w < kJoined; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += sums[w][lane][j];
+            write_row<P>(a.table, token_of(a.keys[(s + 1) * a.length]), at, a.scale, acc);
+        }
+        __syncthreads();
+    }
 }
 
 // -------------------------------------------------------------------------------------------------------- host
@@ -325,7 +436,7 @@ constexpr uint32_t kSlice = kWave * 8;      // columns of a wavefront
 uint32_t segment_length(uint64_t n)
 {
     const uint64_t each = (n + 1023) / 1024;
-    return (uint32_t)(each <= 16 ? 16 : (each + 7) / 8 * 8);
+    return each <= 8 ? 8 : (uint32_t)((each + 7) / 8 * 8);
 }
 
 struct Space {
@@ -392,13 +503,14 @@ int gradient(const Places& places, const Tokens& tokens, const Table& table, flo
         if (launched() != SDL_OK) return SDL_ERR_DEVICE;
     }
     if (n == 0) return SDL_OK;
-    uint64_t rest = half;
     for (uint64_t run = kChunk; run < n; run *= kFan) {
         const uint32_t groups = (n + 255) / 256;
-        const MergeArgs a{keys, other, n, (uint32_t)run, groups, Fill{table, rest, pieces, dense}};
-        hipLaunchKernelGGL((sdl_embedding_merge_kernel<P>), dim3(groups + fillers(pieces - rest)), dim3(1024), 0, st, a);
+        const MergeArgs a{keys, other, n, (uint32_t)run, groups, Fill{table, half, pieces, dense}};
+        if (run == kChunk)
+            hipLaunchKernelGGL((sdl_embedding_merge_kernel<P>), dim3(groups + fillers(pieces - half)), dim3(1024), 0, st, a);
+        else
+            hipLaunchKernelGGL(sdl_embedding_merge_long_kernel, dim3(groups), dim3(1024), 0, st, a);
         if (launched() != SDL_OK) return SDL_ERR_DEVICE;
-        rest = pieces;
         uint64_t* t = keys;
         keys = other;
         other = t;
@@ -418,7 +530,7 @@ int gradient(const Places& places, const Tokens& tokens, const Table& table, flo
     if (launched() != SDL_OK) return SDL_ERR_DEVICE;
     if (s.segments > 1) {
         r.slices = make_div((W + kSlice - 1) / kSlice);
-        hipLaunchKernelGGL((sdl_embedding_join_kernel<P>), dim3(r.slices.d * (s.segments - 1)), dim3(512), 0, st, r);
+        hipLaunchKernelGGL((sdl_embedding_join_kernel<P>), dim3(r.slices.d * ((s.segments + kJoined - 1) / kJoined)), dim3(1024), 0, st, r);
     }
     return launched();
 }
