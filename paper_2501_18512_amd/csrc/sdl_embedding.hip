@@ -52,8 +52,26 @@ struct LookupArgs {
     float scale;
 };
 
+// Eight columns of a row of W: the last ones of a row come as the eight at its end, whose first ones a neighbour has too (and makes the same of).  A load that takes what is
+// there element by element is waited for on the spot.  TINY: rows of less than eight.
+template <bool TINY>
+__device__ __forceinline__ uint32_t columns(uint32_t at, uint32_t W)
+{
+    return TINY ? at : min(at, W - 8);
+}
+template <bool TINY, typename T>
+__device__ __forceinline__ Eight<T> load_columns(const T* row, uint32_t at, uint32_t W)
+{
+    return load8(row, at, TINY ? W : ~0u);
+}
+template <bool TINY, typename T>
+__device__ __forceinline__ void store_columns(T* row, uint32_t at, uint32_t W, const float* v)
+{
+    store8(row, at, TINY ? W : ~0u, v);
+}
+
 // LPR lanes a row, ROWS rows at a time each, so that their loads are under way together.
-template <typename P, typename T, int LPR, int ROWS>
+template <typename P, typename T, int LPR, int ROWS, bool TINY>
 __global__ void __launch_bounds__(256) sdl_embedding_kernel(const LookupArgs a)
 {
     constexpr uint32_t kTeams = 256 / LPR;
@@ -62,12 +80,13 @@ __global__ void __launch_bounds__(256) sdl_embedding_kernel(const LookupArgs a)
     uint32_t v[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) v[r] = first + r < a.places.n ? a.tokens.get(first + r) : kNone;
-    for (uint32_t at = lane * 8; at < W; at += LPR * 8) {
+    for (uint32_t from = lane * 8; from < W; from += LPR * 8) {
+        const uint32_t at = columns<TINY>(from, W);
         Eight<P> e[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             e[r] = Eight<P>{};
-            if (v[r] != kNone) e[r] = load8(reinterpret_cast<const P*>(a.table) + (int64_t)v[r] * a.stride, at, W);
+            if (v[r] != kNone) e[r] = load_columns<TINY>(reinterpret_cast<const P*>(a.table) + (int64_t)v[r] * a.stride, at, W);
         }
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -75,7 +94,7 @@ __global__ void __launch_bounds__(256) sdl_embedding_kernel(const LookupArgs a)
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = v[r] == kNone ? 0.0f : e[r].get(j) * a.scale;
-            store8(place_row<T>(a.places, first + r), at, W, x);
+            store_columns<TINY>(place_row<T>(a.places, first + r), at, W, x);
         }
     }
 }
@@ -294,23 +313,23 @@ struct ReduceArgs {
 
 __device__ __forceinline__ uint32_t token_of(uint64_t key) { return (uint32_t)(key >> 32); }
 
-template <typename P>
+template <bool TINY, typename P>
 __device__ __forceinline__ void write_row(const Table& t, uint32_t v, uint32_t at, float scale, const float* acc)
 {
     float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = acc[j] * scale;
-    store8(reinterpret_cast<P*>(t.data) + (int64_t)v * t.stride, at, t.width, x);
+    store_columns<TINY>(reinterpret_cast<P*>(t.data) + (int64_t)v * t.stride, at, t.width, x);
 }
 
 // LPR lanes have eight columns each of one segment; eight rows are under way at a time.
-template <typename T, typename P, int LPR>
+template <typename T, typename P, int LPR, bool TINY>
 __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceArgs a)
 {
     constexpr uint32_t kTeams = 256 / LPR;
     const uint32_t unit = blockIdx.x * kTeams + threadIdx.x / LPR, seg = div(unit, a.slices);
-    const uint32_t at = ((unit - seg * a.slices.d) * LPR + threadIdx.x % LPR) * 8, W = a.table.width;
-    if (seg >= a.segments || at >= W) return;
+    const uint32_t lane_at = ((unit - seg * a.slices.d) * LPR + threadIdx.x % LPR) * 8, W = a.table.width, at = columns<TINY>(lane_at, W);
+    if (seg >= a.segments || lane_at >= W) return;
     const uint32_t s0 = seg * a.length, s1 = min(s0 + a.length, a.places.n);
     // the keys around the segment with those of its first places: nothing waits for one after the other
     const uint64_t before = s0 > 0 ? a.keys[s0 - 1] : ~0ull, behind = s1 < a.places.n ? a.keys[s1] : ~0ull;
@@ -327,7 +346,7 @@ __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceA
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             e[j] = Eight<T>{};
-            if (token_of(k[j]) != kNone) e[j] = load8(place_row<const T>(a.places, (uint32_t)k[j]), at, W);
+            if (token_of(k[j]) != kNone) e[j] = load_columns<TINY>(place_row<const T>(a.places, (uint32_t)k[j]), at, W);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) next[j] = p + 8 + j < s1 ? a.keys[p + 8 + j] : ~0ull;
@@ -338,9 +357,9 @@ __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceA
             if (v != cur) {
                 if (cur != kNone) {
                     if (open)
-                        store8(a.lines + (uint64_t)seg * 2 * W, at, W, acc);
+                        store_columns<TINY>(a.lines + (uint64_t)seg * 2 * W, at, W, acc);
                     else
-                        write_row<P>(a.table, cur, at, a.scale, acc);
+                        write_row<TINY, P>(a.table, cur, at, a.scale, acc);
                 }
                 open = false;
                 cur = v;
@@ -356,72 +375,93 @@ __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceA
     if (cur == kNone) return;
     const bool on = token_of(behind) == cur;
     if (open || on)
-        store8(a.lines + ((uint64_t)seg * 2 + (open ? 0 : 1)) * W, at, W, acc);
+        store_columns<TINY>(a.lines + ((uint64_t)seg * 2 + (open ? 0 : 1)) * W, at, W, acc);
     else
-        write_row<P>(a.table, cur, at, a.scale, acc);
+        write_row<TINY, P>(a.table, cur, at, a.scale, acc);
 }
 
 // The lines of the runs that leave their first segments: a wavefront a segment, which adds up a few lines in order; of many, all sixteen of the workgroup a share each, and
 // then the shares.  (A workgroup a segment and part of the columns: 17 us for 4000 that have nothing to do.)
 constexpr uint32_t kJoined = 16, kFew = 16;
 
-template <typename P>
+template <typename P, bool TINY>
 __global__ void __launch_bounds__(1024) sdl_embedding_join_kernel(const ReduceArgs a)
 {
-    __shared__ float sums[kJoined][kWave][9];
-    __shared__ uint32_t many[kJoined];          // lines, where they are many
+    __shared__ f32x4_t sums[kJoined][kWave];
+    __shared__ uint32_t many[kJoined], tokens[kJoined];          // lines, where they are many
     const uint32_t group = div(blockIdx.x, a.slices), lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const uint32_t at = ((blockIdx.x - group * a.slices.d) * kWave + lane) * 8, W = a.table.width, seg = group * kJoined + wave;
-    const auto add = [&](uint32_t s, uint32_t from, uint32_t to, float* acc) {
-        const float* line = a.lines + (uint64_t)s * 2 * W;
-#pragma unroll 8
-        for (uint32_t l = from; l < to; ++l) {
-            const Eight<float> e = load8(line + ((uint64_t)l * 2 + (l == 0)) * W, at, W);
+    const uint32_t lane_at = ((blockIdx.x - group * a.slices.d) * kWave + lane) * 4, W = a.table.width, seg = group * kJoined + wave;
+    const uint32_t at = TINY ? lane_at : min(lane_at, W - 4);
+    const auto add = [&](uint32_t s, uint32_t from, uint32_t to) {
+        const float* line = a.lines + (uint64_t)s * 2 * W + at;
+        f32x4_t acc = {};
+        for (uint32_t l = from; l < to; l += 8) {
+            f32x4_t e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += e.get(j);
+            for (int j = 0; j < 8; ++j) {
+                e[j] = f32x4_t{};
+                if (l + j < to) {
+                    const float* p = line + ((uint64_t)(l + j) * 2 + (l + j == 0)) * W;
+                    if constexpr (TINY) {
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) e[j][i] = at + i < W ? p[i] : 0.0f;
+                    } else {
+                        const f32x4_elem x = *reinterpret_cast<const f32x4_elem*>(p);
+                        e[j] = f32x4_t{x.x, x.y, x.z, x.w};
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc += e[j];
         }
+        return acc;
     };
-    uint32_t lines = 0;
+    const auto write = [&](uint32_t v, const f32x4_t& x) {
+        P* row = reinterpret_cast<P*>(a.table.data) + (int64_t)v * a.table.stride + at;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (!TINY || at + i < W) row[i] = (P)(x[i] * a.scale);
+    };
+    uint32_t lines = 0, v = kNone;
     if (seg + 1 < a.segments) {
         const uint32_t s0 = seg * a.length, s1 = s0 + a.length;
         const uint64_t before = s0 > 0 ? a.keys[s0 - 1] : ~0ull, last = a.keys[s1 - 1];
-        // first tokens of the segments that follow, one a lane: the run goes on through those that have its own
-        uint32_t other = seg + 1 + lane < a.segments ? token_of(a.keys[(seg + 1 + lane) * a.length]) : kNone;
-        const uint32_t v = token_of(last);
+        // first tokens of the segments that follow, four a lane: the run goes on through those that have its own
+        const auto follow = [&](uint32_t s) { return s < a.segments ? token_of(a.keys[s * a.length]) : kNone; };
+        uint32_t other[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[i] = follow(seg + 1 + i * kWave + lane);
+        v = token_of(last);
         // (all of a segment may be one run from further up)
         if (v != kNone && !(s0 > 0 && token_of(before) == v)) {
             for (lines = 1;;) {                 // this segment's second line, and the others' first ones
-                const uint32_t more = (uint32_t)__popcll(__ballot(other == v));
+                uint32_t more = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) more += (uint32_t)__popcll(__ballot(other[i] == v));
                 lines += more;
-                if (more < (uint32_t)kWave) break;
-                other = seg + lines + lane < a.segments ? token_of(a.keys[(seg + lines + lane) * a.length]) : kNone;
+                if (more < 4u * kWave) break;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) other[i] = follow(seg + lines + i * kWave + lane);
             }
-            if (lines > 1 && lines <= kFew && at < W) {
-                float acc[8] = {};
-                add(seg, 0, lines, acc);
-                write_row<P>(a.table, v, at, a.scale, acc);
-            }
+            if (lines > 1 && lines <= kFew && lane_at < W) write(v, add(seg, 0, lines));
         }
     }
-    if (lane == 0) many[wave] = lines > kFew ? lines : 0;
+    if (lane == 0) {
+        many[wave] = lines > kFew ? lines : 0;
+        tokens[wave] = v;
+    }
     __syncthreads();
     for (uint32_t k = 0; k < kJoined; ++k) {
-        const uint32_t n = many[k], s = group * kJoined + k;
+        const uint32_t n = many[k];
         if (n == 0) continue;
         const uint32_t each = (n + kJoined - 1) / kJoined, from = min(wave * each, n);
-        float acc[8] = {};
-        if (at < W) add(s, from, min(from + each, n), acc);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sums[wave][lane][j] = acc[j];
+        sums[wave][lane] = lane_at < W ? add(group * kJoined + k, from, min(from + each, n)) : f32x4_t{};
         __syncthreads();
-        if (wave == k && at < W) {
+        if (wave == k && lane_at < W) {
+            f32x4_t acc = {};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
-#pragma unroll
-            for (uint32_t w = 0; w < kJoined; ++w)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += sums[w][lane][j];
-            write_row<P>(a.table, token_of(a.keys[(s + 1) * a.length]), at, a.scale, acc);
+            for (uint32_t w = 0; w < kJoined; ++w) acc += sums[w][lane];
+            write(tokens[k], acc);
         }
         __syncthreads();
     }
@@ -429,7 +469,7 @@ __global__ void __launch_bounds__(1024) sdl_embedding_join_kernel(const ReduceAr
 
 // -------------------------------------------------------------------------------------------------------- host
 
-constexpr uint32_t kSlice = kWave * 8;      // columns of a wavefront
+constexpr uint32_t kSlice = kWave * 4;      // columns of a wavefront that joins
 
 // Places of a segment: enough of them that a device has work for all its compute units, and not so many that the join of one token's lines
 // takes longer than the reading.
@@ -472,14 +512,13 @@ int lookup(const LookupArgs& a, hipStream_t st)
     const auto groups = [n](uint32_t rows) { return grid_of(((uint64_t)n + rows - 1) / rows); };
     // one row at a time while there are few, as they have the device to themselves
     const bool few = n <= 1024;
-    if (W <= 64)
-        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 8, 1>), groups(32), dim3(256), 0, st, a);
-    else if (W <= 256)
-        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 32, 1>), groups(8), dim3(256), 0, st, a);
-    else if (few)
-        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 256, 1>), groups(1), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((sdl_embedding_kernel<P, T, 64, 2>), groups(8), dim3(256), 0, st, a);
+#define SDL_LAUNCH(LPR, ROWS, TINY) hipLaunchKernelGGL((sdl_embedding_kernel<P, T, LPR, ROWS, TINY>), groups(256 / LPR * ROWS), dim3(256), 0, st, a)
+    if (W < 8) SDL_LAUNCH(8, 1, true);
+    else if (W <= 64) SDL_LAUNCH(8, 1, false);
+    else if (W <= 256) SDL_LAUNCH(32, 1, false);
+    else if (few) SDL_LAUNCH(256, 1, false);
+    else SDL_LAUNCH(64, 2, false);
+#undef SDL_LAUNCH
     return launched();
 }
 
@@ -517,20 +556,25 @@ int gradient(const Places& places, const Tokens& tokens, const Table& table, flo
     }
     ReduceArgs r{places, table, keys, lines, make_div(1), s.segments, s.length, scale};
     const uint32_t W = table.width;
-#define SDL_LAUNCH(LPR)                                                                                                     \
-    do {                                                                                                                    \
-        r.slices = make_div((W + LPR * 8 - 1) / (LPR * 8));                                                                 \
-        const uint32_t teams = 256 / LPR, units = r.slices.d * s.segments;                                                  \
-        hipLaunchKernelGGL((sdl_embedding_reduce_kernel<T, P, LPR>), dim3((units + teams - 1) / teams), dim3(256), 0, st, r); \
+#define SDL_LAUNCH(LPR, TINY)                                                                                                     \
+    do {                                                                                                                          \
+        r.slices = make_div((W + LPR * 8 - 1) / (LPR * 8));                                                                       \
+        const uint32_t teams = 256 / LPR, units = r.slices.d * s.segments;                                                        \
+        hipLaunchKernelGGL((sdl_embedding_reduce_kernel<T, P, LPR, TINY>), dim3((units + teams - 1) / teams), dim3(256), 0, st, r); \
     } while (0)
-    if (W <= 64) SDL_LAUNCH(8);
-    else if (W <= 256) SDL_LAUNCH(32);
-    else SDL_LAUNCH(64);
+    if (W < 8) SDL_LAUNCH(8, true);
+    else if (W <= 64) SDL_LAUNCH(8, false);
+    else if (W <= 256) SDL_LAUNCH(32, false);
+    else SDL_LAUNCH(64, false);
 #undef SDL_LAUNCH
     if (launched() != SDL_OK) return SDL_ERR_DEVICE;
     if (s.segments > 1) {
         r.slices = make_div((W + kSlice - 1) / kSlice);
-        hipLaunchKernelGGL((sdl_embedding_join_kernel<P>), dim3(r.slices.d * ((s.segments + kJoined - 1) / kJoined)), dim3(1024), 0, st, r);
+        const dim3 groups(r.slices.d * ((s.segments + kJoined - 1) / kJoined));
+        if (W < 8)
+            hipLaunchKernelGGL((sdl_embedding_join_kernel<P, true>), groups, dim3(1024), 0, st, r);
+        else
+            hipLaunchKernelGGL((sdl_embedding_join_kernel<P, false>), groups, dim3(1024), 0, st, r);
     }
     return launched();
 }
