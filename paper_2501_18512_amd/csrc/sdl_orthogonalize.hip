@@ -15,6 +15,7 @@
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 #include <type_traits>
 #include <utility>
 
@@ -31,6 +32,7 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f;
 constexpr uint32_t kDies = 8;
+constexpr uint32_t kMostSmallSteps = 32;
 
 // One matrix in the workspace, of which the next lies `each` bytes further.  Both sides are filled up with zeros to whole tiles.
 struct Work {
@@ -445,6 +447,213 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
         }
 }
 
+// --------------------------------------------------------------------------------------------- small matrices
+
+struct SmallArgs {
+    View x, out;
+    Div across;                                  // tiles along m
+    uint32_t tall, n, m, steps;                  // n <= m
+    double eps;
+    float scale;
+    float a[kMostSmallSteps], b[kMostSmallSteps], c[kMostSmallSteps], image[kMostSmallSteps];     // image: the scale of b A + c A^2
+};
+
+// A matrix whose images fit the shared memory of a workgroup is worked on there from its norm to its last step: with a launch for every product it would be the launches, 80 us for
+// five steps of 100 x 131.  Tiles of 16 by 16 go round among the wavefronts; those of X stay in the registers of theirs, in fp32, and what a step makes of them is what the next one
+// starts from.
+//
+// Layouts of the 16x16x32 instruction, lane l, q = l / 16, c = l % 16:  A row c, k = 8 q + j;  B column c, k = 8 q + j;  D column c, rows 4 q + i.  X's tile
+// has its rows along c, so that a lane has four neighbours of a row: A = the columns of X, by transposing reads, B = the rows of b A + c A^2.
+template <typename T, bool SPLIT, typename O, int WAVES, int SLOTS, int BYTES>
+__global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(const SmallArgs a)
+{
+    constexpr int kImages = SPLIT ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) char lds[BYTES];
+    __shared__ double sums[WAVES];
+    const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), q = lane / 16, c = lane % 16, matrix = blockIdx.x;
+    const uint32_t down = (a.n + 15) / 16, across = a.across.d, nk = (a.n + 31) / 32 * 32, mk = (a.m + 31) / 32 * 32;
+    const uint32_t pitch_x = mk * 2 + 16, pitch_a = nk * 2 + 16, bytes_x = nk * pitch_x, bytes_a = nk * pitch_a;
+    char *const image_x = lds, *const image_a = lds + kImages * bytes_x;
+    // what no tile writes is zero
+    for (uint32_t i = threadIdx.x * 16; i < kImages * (bytes_x + bytes_a); i += WAVES * kWave * 16) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
+
+    // X's tiles of this wavefront, the s-th of them.  Worked out anew wherever it is asked for: kept for all of them they would take the registers.
+    const uint32_t tiles = down * across;
+    const auto tile = [&](int s, uint32_t* i, uint32_t* j) {
+        uint32_t t = wave;
+        asm volatile("" : "+s"(t));
+        t += s * WAVES;
+        const uint32_t row = div(t, a.across);
+        *i = row * 16;
+        *j = (t - row * across) * 16;
+        return t < tiles;
+    };
+    f32x4_t x[SLOTS];
+    const T* from = reinterpret_cast<const T*>(a.x.data) + (int64_t)matrix * a.x.batch;
+    double squares = 0.0;
+    // no load waits for another: what is not there is the last element, and not counted
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        uint32_t i, j;
+        tile(s, &i, &j);
+        const uint32_t row = min(i + c, a.n - 1);
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) {
+            const uint32_t col = min(j + 4 * q + r, a.m - 1);
+            x[s][r] = (float)from[a.tall ? (int64_t)col * a.x.token + row : (int64_t)row * a.x.token + col];
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        uint32_t i, j;
+        const bool there = tile(s, &i, &j);
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) {
+            x[s][r] = there && i + c < a.n && j + 4 * q + r < a.m ? x[s][r] : 0.0f;
+            squares += (double)x[s][r] * (double)x[s][r];
+        }
+    }
+#pragma unroll
+    for (int k = 32; k; k /= 2) squares += __shfl_xor(squares, k);
+    if (lane == 0) sums[wave] = squares;
+    __syncthreads();
+    squares = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) squares += sums[w];
+    const double norm = sqrt(squares) + a.eps, inverse = norm == 0.0 ? 0.0 : 1.0 / norm;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[s][r] = (float)((double)x[s][r] * inverse);
+
+    // four neighbours of a row of an image, hi and lo
+    const auto put4 = [&](char* image, uint32_t bytes, uint32_t pitch, uint32_t row, uint32_t k, const f32x4_t& v) {
+        const f16x4_t hi = __builtin_convertvector(v, f16x4_t);
+        *reinterpret_cast<f16x4_t*>(image + row * pitch + k * 2) = hi;
+        if constexpr (SPLIT) {
+            f32x4_t rest;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) rest[r] = v[r] - (float)hi[r];
+            *reinterpret_cast<f16x4_t*>(image + bytes + row * pitch + k * 2) = __builtin_convertvector(rest, f16x4_t);
+        }
+    };
+    const auto put1 = [&](char* image, uint32_t bytes, uint32_t pitch, uint32_t row, uint32_t k, float v) {
+        const _Float16 hi = (_Float16)v;
+        *reinterpret_cast<_Float16*>(image + row * pitch + k * 2) = hi;
+        if constexpr (SPLIT) *reinterpret_cast<_Float16*>(image + bytes + row * pitch + k * 2) = (_Float16)(v - (float)hi);
+    };
+    const auto along = [&](const char* image, uint32_t pitch, uint32_t row, uint32_t k) {
+        return *reinterpret_cast<const f16x8_t*>(image + (row + c) * pitch + (k + 8 * q) * 2);
+    };
+    const auto across_rows = [&](const char* image, uint32_t pitch, uint32_t k, uint32_t col) {
+        typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+        const char* at = image + (k + 8 * q + c / 4) * pitch + (col + c % 4 * 4) * 2;
+        const i16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at), v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 4 * pitch));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // one tile of rows i of an image times rows j of the same one
+    const auto symmetric = [&](const char* image, uint32_t bytes, uint32_t pitch, uint32_t i, uint32_t j, uint32_t kk) {
+        f32x4_t d = {};
+#pragma unroll 2
+        for (uint32_t k = 0; k < kk; k += 32) {
+            const f16x8_t p = along(image, pitch, i, k), r = along(image, pitch, j, k);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, r, d, 0, 0, 0);
+            if constexpr (SPLIT) {
+                const f16x8_t pl = along(image + bytes, pitch, i, k), rl = along(image + bytes, pitch, j, k);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, rl, d, 0, 0, 0);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, r, d, 0, 0, 0);
+            }
+        }
+        return d;
+    };
+    // D of rows i and columns j, in its place and in the one across
+    const auto put_symmetric = [&](uint32_t i, uint32_t j, const f32x4_t& v) {
+        put4(image_a, bytes_a, pitch_a, j + c, i + 4 * q, v);
+        if (i != j)
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r) put1(image_a, bytes_a, pitch_a, i + 4 * q + r, j + c, v[r]);
+    };
+    // tiles on and under the diagonal: the t-th of them
+    const auto place = [](uint32_t t, uint32_t* i, uint32_t* j) {
+        uint32_t row = 0;
+        while ((row + 1) * (row + 2) / 2 <= t) ++row;
+        *i = row * 16;
+        *j = (t - row * (row + 1) / 2) * 16;
+    };
+    const uint32_t halves = down * (down + 1) / 2;
+    constexpr int kHalves = 5;                  // of a wavefront
+    for (uint32_t step = 0; step < a.steps; ++step) {
+        // X's image, once everyone has read the one before
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            uint32_t i, j;
+            if (tile(s, &i, &j)) put4(image_x, bytes_x, pitch_x, i + c, j + 4 * q, x[s] * kScaleX);
+        }
+        __syncthreads();
+        for (uint32_t t = wave; t < halves; t += WAVES) {
+            uint32_t i, j;
+            place(t, &i, &j);
+            put_symmetric(i, j, symmetric(image_x, bytes_x, pitch_x, i, j, mk) * (kScaleA / (kScaleX * kScaleX)));
+        }
+        __syncthreads();
+        f32x4_t mix[kHalves];
+#pragma unroll
+        for (int s = 0; s < kHalves; ++s) {
+            const uint32_t t = s * WAVES + wave;
+            if (t >= halves) continue;
+            uint32_t i, j;
+            place(t, &i, &j);
+            const f32x4_t square = symmetric(image_a, bytes_a, pitch_a, i, j, nk);
+            const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(image_a + (j + c) * pitch_a + (i + 4 * q) * 2);
+            f16x4_t lo = {};
+            if constexpr (SPLIT) lo = *reinterpret_cast<const f16x4_t*>(image_a + bytes_a + (j + c) * pitch_a + (i + 4 * q) * 2);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                mix[s][r] = fmaf(square[r], a.c[step] * a.image[step] / (kScaleA * kScaleA), a.b[step] * a.image[step] / kScaleA * ((float)hi[r] + (float)lo[r]));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kHalves; ++s) {
+            const uint32_t t = s * WAVES + wave;
+            if (t >= halves) continue;
+            uint32_t i, j;
+            place(t, &i, &j);
+            put_symmetric(i, j, mix[s]);
+        }
+        __syncthreads();
+        const float on_sum = 1.0f / (a.image[step] * kScaleX);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            uint32_t i, j;
+            if (!tile(s, &i, &j)) continue;
+            f32x4_t d = {};
+#pragma unroll 2
+            for (uint32_t k = 0; k < nk; k += 32) {
+                const f16x8_t p = across_rows(image_x, pitch_x, k, j), r = along(image_a, pitch_a, i, k);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, r, d, 0, 0, 0);
+                if constexpr (SPLIT) {
+                    const f16x8_t pl = across_rows(image_x + bytes_x, pitch_x, k, j), rl = along(image_a + bytes_a, pitch_a, i, k);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, rl, d, 0, 0, 0);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, r, d, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, a.a[step] * x[s][r]);
+        }
+    }
+    O* out = reinterpret_cast<O*>(a.out.data) + (int64_t)matrix * a.out.batch;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        uint32_t i, j;
+        if (!tile(s, &i, &j) || i + c >= a.n) continue;
+        const uint32_t row = i + c, col = j + 4 * q;
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r)
+            if (col + r < a.m) out[a.tall ? (int64_t)(col + r) * a.out.token + row : (int64_t)row * a.out.token + col + r] = (O)(x[s][r] * a.scale);
+    }
+}
+
 // -------------------------------------------------------------------------------------------------------- host
 
 // Workgroups that are at work at a time.
@@ -540,6 +749,13 @@ double reach(double a, double b, double c, double h)
     return most;
 }
 
+// Of the matrix b A + c A^2, where no singular value of X is above h: as much as fp16 has room for.
+float image_scale(double b, double c, double h)
+{
+    const double bound = std::fabs(b) * h * h + std::fabs(c) * h * h * h * h;
+    return (float)std::exp2(std::min(14.0, std::floor(std::log2(32768.0 / std::max(bound, 1e-30)))));
+}
+
 template <int TILE, bool SPLIT, int MODE, typename O>
 int product(const ProductArgs& a, uint32_t batch, hipStream_t st)
 {
@@ -566,9 +782,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
     double h = 1.0;
     for (uint32_t s = 0; s < steps; ++s) {
         const double ca = coefficients[3 * s], cb = coefficients[3 * s + 1], cc = coefficients[3 * s + 2];
-        // what the polynomial's matrix can be decides its image's scale
-        const double bound = std::fabs(cb) * h * h + std::fabs(cc) * h * h * h * h;
-        const float scale_b = (float)std::exp2(std::min(14.0, std::floor(std::log2(32768.0 / std::max(bound, 1e-30)))));
+        const float scale_b = image_scale(cb, cc, h);
         h = reach(ca, cb, cc, h);
         ProductArgs a{};
         a.w = w;
@@ -606,6 +820,36 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         std::swap(xt, other);
     }
     return SDL_OK;
+}
+
+// Wavefronts of a workgroup, tiles of X that each of them keeps, and shared memory of the kernels of small matrices: four workgroups of the first find room on a compute unit.
+struct Small {
+    uint32_t waves, slots, bytes;
+};
+constexpr Small kSmall[] = {{4, 4, 39 * 1024}, {4, 12, 39 * 1024}, {16, 6, 159 * 1024}, {16, 12, 159 * 1024}};
+
+bool fits(const Small& k, uint32_t n, uint32_t m, bool split)
+{
+    const uint64_t down = (n + 15) / 16, across = (m + 15) / 16, nk = (n + 31) / 32 * 32, mk = (m + 31) / 32 * 32;
+    return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) <= k.bytes && down * across <= k.waves * k.slots && down * (down + 1) / 2 <= k.waves * 5;
+}
+
+bool is_small(uint32_t n, uint32_t m, uint32_t steps, bool split)
+{
+    return steps <= kMostSmallSteps && std::any_of(std::begin(kSmall), std::end(kSmall), [=](const Small& k) { return fits(k, n, m, split); });
+}
+
+template <typename T, bool SPLIT, typename O>
+int small(const SmallArgs& a, uint32_t batch, hipStream_t st)
+{
+#define SDL_LAUNCH(N)                                                                                                                                  \
+    hipLaunchKernelGGL((sdl_orthogonalize_small_kernel<T, SPLIT, O, kSmall[N].waves, kSmall[N].slots, kSmall[N].bytes>), dim3(batch), dim3(kSmall[N].waves * kWave), 0, st, a)
+    if (fits(kSmall[0], a.n, a.m, SPLIT)) SDL_LAUNCH(0);
+    else if (fits(kSmall[1], a.n, a.m, SPLIT)) SDL_LAUNCH(1);
+    else if (fits(kSmall[2], a.n, a.m, SPLIT)) SDL_LAUNCH(2);
+    else SDL_LAUNCH(3);
+#undef SDL_LAUNCH
+    return launched();
 }
 
 template <typename T, bool SPLIT>
@@ -650,6 +894,21 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     const Layout l0 = layout_of(batch, rows, cols, split);
     if (!workspace || workspace_bytes < l0.bytes) return SDL_ERR_INVALID_ARG;
     if (!aligned_to(workspace, 16)) return SDL_ERR_ALIGNMENT;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const uint32_t n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
+    if (is_small(n, m, steps, split)) {
+        SmallArgs a{kernel_view(x), kernel_view(out), make_div((m + 15) / 16), rows > cols, n, m, steps, (double)eps, scale, {}, {}, {}, {}};
+        h = 1.0;
+        for (uint32_t s = 0; s < steps; ++s) {
+            a.a[s] = coefficients[3 * s];
+            a.b[s] = coefficients[3 * s + 1];
+            a.c[s] = coefficients[3 * s + 2];
+            a.image[s] = image_scale(a.b[s], a.c[s], h);
+            h = reach(a.a[s], a.b[s], a.c[s], h);
+        }
+        if (dtype == SDL_DTYPE_BF16) return split ? small<__bf16, true, float>(a, batch, st) : small<__bf16, false, __bf16>(a, batch, st);
+        return split ? small<float, true, float>(a, batch, st) : small<float, false, __bf16>(a, batch, st);
+    }
     Layout l = l0;
     l.w.base = static_cast<char*>(workspace);
     FirstArgs a{};
@@ -661,7 +920,6 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     a.squares = reinterpret_cast<double*>(l.w.base + l.squares);
     a.eps = (double)eps;
     a.w = l.w;
-    hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == SDL_DTYPE_BF16) rc = split ? first<__bf16, true>(a, batch, st) : first<__bf16, false>(a, batch, st);
     else rc = split ? first<float, true>(a, batch, st) : first<float, false>(a, batch, st);
     if (rc != SDL_OK) return rc;

@@ -55,9 +55,10 @@ def test_momentum(dtype, out):
 
 
 @pytest.mark.parametrize("out", [BF16, FP32])
-def test_tiles_of_128(out):
-    """Batches that are large enough for them."""
-    for i, shape in enumerate([(40, 200, 250), (36, 255, 129), (2, 1024, 1100)]):
+def test_every_launch_shape(out):
+    """A workgroup a matrix of all four kinds, up to what they hold; tiles of 64, of 128 and of 256; sums in slices."""
+    for i, shape in enumerate([(3, 48, 80), (2, 16, 500), (3, 90, 90), (2, 112, 176), (1, 17, 1000), (2, 160, 180), (1, 32, 1300), (2, 200, 300), (1, 300, 520), (1, 180, 2100),
+                               (40, 200, 400), (36, 385, 129), (2, 1024, 1100), (1, 513, 4000), (6, 700, 1600)]):
         print(f"orthogonalize {shape} {out}", flush=True)
         check(momentum(shape, FP32, 10 * i), out)
 
@@ -117,7 +118,7 @@ def test_zeros_and_what_is_not_finite():
             assert torch.equal(got[[0, 1, 4]], want[[0, 1, 4]])
 
 
-@pytest.mark.parametrize("shape", [(3, 100, 130), (40, 256, 130)])
+@pytest.mark.parametrize("shape", [(3, 100, 130), (300, 20, 30), (40, 256, 430), (1, 200, 2100)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_in_place_repeatable_on_another_stream_and_in_a_graph(shape, dtype):
     x = momentum(shape, dtype, 6).cuda()
