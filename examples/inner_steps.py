@@ -2,11 +2,11 @@
 
 The replicas are the flat bf16 arrays that the outer step works on; the decoder's parameters are views of them.  One inner step of a
 replica: embedding, blocks of [norm, q k v projection, norm of q and k per head, rotary positions, attention, output projection; norm,
-feed-forward], final norm, head, cross entropy, backward, Adam.  Norms, rotary positions and attention are this library's calls, the
-products torch's.  The engine sends and receives what its schedule says after every step.  Then the mean of the replicas answers a
+feed-forward], final norm, head, cross entropy with the z term, backward, Adam, or, for the blocks' matrices, momentum whose orthogonalised form is the step.  Embedding, norms,
+rotary positions, attention, cross entropy and the orthogonalised updates are this library's calls, the products torch's.  The engine sends and receives what its schedule says after every step.  Then the mean of the replicas answers a
 prompt: once as a whole, and once token by token over a cache of keys and values.
 
-    python examples/inner_steps.py [--steps 60] [--replicas 2]
+    python examples/inner_steps.py [--steps 60] [--replicas 2] [--update adam|orthogonal]
 """
 import argparse
 import os
@@ -18,9 +18,45 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2501_18512_amd as sdl  # noqa: E402
 
 EPS = 1e-5
+Z = 1e-4        # of the loss' z term
 
 
 # ---------------------------------------------------------------- the operators, as torch's autograd sees them
+
+class Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, tokens):
+        out = torch.empty((*tokens.shape, table.shape[1]), dtype=table.dtype, device=table.device)
+        sdl.sdl_embedding(table, tokens, out)
+        ctx.save_for_backward(tokens)
+        ctx.table = table.shape
+        return out
+
+    @staticmethod
+    def backward(ctx, d_out):
+        tokens, = ctx.saved_tensors
+        d_table = torch.empty(ctx.table, dtype=d_out.dtype, device=d_out.device)
+        sdl.sdl_embedding_backward(d_out.contiguous(), tokens, d_table, sdl.alloc_embedding(tokens, ctx.table[1]))
+        return d_table, None
+
+
+class CrossEntropy(torch.autograd.Function):
+    """The loss of every row, in fp32."""
+
+    @staticmethod
+    def forward(ctx, logits, targets):
+        loss, lse = (torch.empty(targets.shape, dtype=torch.float32, device=logits.device) for _ in range(2))
+        sdl.sdl_cross_entropy(logits, targets, loss, lse, z=Z)
+        ctx.save_for_backward(logits, targets, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, d_loss):
+        logits, targets, lse = ctx.saved_tensors
+        d_logits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        sdl.sdl_cross_entropy_backward(logits, targets, lse, d_logits, d_loss.contiguous(), z=Z)
+        return d_logits, None
+
 
 class LayerNorm(torch.autograd.Function):
     @staticmethod
@@ -102,7 +138,7 @@ def decoder(shape, params, tokens, frequencies, positions, cache=None):
     """Logits of tokens [batch, tokens].  cache: (keys, values, lengths) per block; the new tokens are put behind the valid ones."""
     B, L = tokens.shape
     H, G, D = shape.heads, shape.kv_heads, shape.head
-    x = params["embed"][tokens]
+    x = Embedding.apply(params["embed"], tokens.contiguous())
     for b in range(shape.blocks):
         p = {n: params[f"{b}.{n}"] for n in ("norm", "qkv", "q_norm", "k_norm", "out", "ffn_norm", "up", "down")}
         qkv = (LayerNorm.apply(x, p["norm"]) @ p["qkv"].T).view(B, L, H + 2 * G, D)
@@ -125,24 +161,40 @@ def decoder(shape, params, tokens, frequencies, positions, cache=None):
 
 
 class Replica:
-    """One worker's inner optimizer over a flat bf16 array (Adam's moments in fp32)."""
+    """One worker's inner optimizer over a flat bf16 array, moments in fp32: Adam, and with update="orthogonal" for the matrices of the blocks momentum, orthogonalised."""
 
-    def __init__(self, shape, flat, lr):
-        self.shape, self.flat, self.lr, self.t = shape, flat, lr, 0
+    def __init__(self, shape, flat, lr, update="adam"):
+        self.shape, self.flat, self.lr, self.update, self.t = shape, flat, lr, update, 0
         self.m, self.v = (torch.zeros(flat.numel(), dtype=torch.float32, device=flat.device) for _ in range(2))
 
-    def step(self, tokens, frequencies, positions):
+    def gradient(self, tokens, frequencies, positions):
         flat = self.flat.detach().requires_grad_()
         logits = decoder(self.shape, self.shape.views(flat), tokens[:, :-1], frequencies, positions)
-        loss = torch.nn.functional.cross_entropy(logits.float().flatten(0, 1), tokens[:, 1:].flatten())
-        grad = torch.autograd.grad(loss, flat)[0].float()
+        loss = CrossEntropy.apply(logits, tokens[:, 1:].contiguous()).mean()
+        return loss.detach(), torch.autograd.grad(loss, flat)[0].float()
+
+    def step(self, tokens, frequencies, positions):
+        loss, grad = self.gradient(tokens, frequencies, positions)
         self.t += 1
         self.m.lerp_(grad, 0.1)
         self.v.lerp_(grad * grad, 0.05)
         step = (self.m / (1 - 0.9 ** self.t)) / ((self.v / (1 - 0.95 ** self.t)).sqrt() + 1e-8)
+        if self.update == "orthogonal":
+            for m, out in self.matrices(self.m, step):
+                # a matrix whose singular values are 1, with the root mean square of an Adam step's elements that agree in a fifth of the signs
+                sdl.sdl_orthogonalize(m, out, sdl.alloc_orthogonalize(m, out), scale=0.2 * max(m.shape[1:]) ** 0.5)
         with torch.no_grad():
             self.flat.copy_(self.flat.float() - self.lr * step)
-        return loss.detach()
+        return loss
+
+    def matrices(self, *arrays):
+        """The blocks' matrices of one kind as batches [blocks, rows, cols]: views of flat arrays, a block's parameters apart."""
+        each = sum(n for (_, _, unit), n in zip(self.shape.groups, self.shape.numel) if unit == 0)
+        at = 0
+        for (name, shape, unit), n in zip(self.shape.groups, self.shape.numel):
+            if unit == 0 and len(shape) == 2:
+                yield [x.as_strided((self.shape.blocks, *shape), (each, shape[1], 1), at) for x in arrays]
+            at += n
 
 
 def text(shape, batch, length, seed):
@@ -169,7 +221,7 @@ def answer(shape, params, prompt, frequencies, new):
     return torch.cat(tokens, 1), torch.stack(logits, 1)
 
 
-def train(steps=60, replicas=2, batch=16, length=65, H=20, tau=2, lr=3e-3, seed=0, say=print):
+def train(steps=60, replicas=2, batch=16, length=65, H=20, tau=2, lr=3e-3, seed=0, say=print, update="adam"):
     """Returns the losses [steps][replicas], the shape, the mean of the replicas as bf16 and the frequencies."""
     shape = Shape()
     plan = sdl.sdl_fragment_plan(shape.numel, [u for _, _, u in shape.groups], shape.blocks, 2, sdl.PATTERN_STRIDED, H, tau)
@@ -187,7 +239,7 @@ def train(steps=60, replicas=2, batch=16, length=65, H=20, tau=2, lr=3e-3, seed=
     buffers = [[torch.empty(max(m[i], 16), dtype=torch.uint8, device="cuda") for m in messages for _ in range(replicas)] for i in range(2)]
     engine = sdl.sdl_engine_create(plan, H, [tau] * replicas, sdl.FMT_E3M0, 0.7, 0.9, 0.5)
     sdl.sdl_engine_bind(engine, g, mom, w, *buffers)
-    workers = [Replica(shape, x, lr) for x in w]
+    workers = [Replica(shape, x, lr, update) for x in w]
     frequencies = sdl.sdl_rotary_frequencies(shape.head).cuda()
     positions = torch.arange(length - 1, dtype=torch.int32, device="cuda").expand(batch, length - 1).contiguous()
     losses = []
@@ -206,8 +258,9 @@ def main():
     parser = argparse.ArgumentParser()
     parser.add_argument("--steps", type=int, default=60)
     parser.add_argument("--replicas", type=int, default=2)
+    parser.add_argument("--update", choices=("adam", "orthogonal"), default="adam")
     a = parser.parse_args()
-    _, shape, flat, frequencies = train(a.steps, a.replicas)
+    _, shape, flat, frequencies = train(a.steps, a.replicas, update=a.update)
     prompt = text(shape, 4, 12, seed=99)
     with torch.no_grad():
         tokens, _ = answer(shape, shape.views(flat), prompt, frequencies, 8)

@@ -575,8 +575,8 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
     };
     // tiles on and under the diagonal: the t-th of them
     const auto place = [](uint32_t t, uint32_t* i, uint32_t* j) {
-        uint32_t row = 0;
-        while ((row + 1) * (row + 2) / 2 <= t) ++row;
+        // (the root of a square is exact, and t is small)
+        const uint32_t row = __builtin_amdgcn_readfirstlane((uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f));
         *i = row * 16;
         *j = (t - row * (row + 1) / 2) * 16;
     };

@@ -141,7 +141,7 @@ static PyObject* py_sdl_cross_entropy_backward(PyObject* self, PyObject* const* 
 /* A list or tuple of (a, b, c). */
 static int coefficients_of(PyObject* v, float* out, uint32_t* steps)
 {
-    PyObject *all = PySequence_Fast(v, "coefficients are a list of (a, b, c)"), *each;
+    PyObject *all = PySequence_Fast(v, "coefficients are a list of (a, b, c)"), *each, *item;
     Py_ssize_t i, k, n;
     if (!all) return -1;
     n = PySequence_Fast_GET_SIZE(all);
@@ -155,7 +155,10 @@ static int coefficients_of(PyObject* v, float* out, uint32_t* steps)
             PyErr_SetString(PyExc_ValueError, "the coefficients changed while they were read");
             goto bad;
         }
-        each = PySequence_Tuple(PySequence_Fast_GET_ITEM(all, i));
+        item = PySequence_Fast_GET_ITEM(all, i);
+        Py_INCREF(item);
+        each = PySequence_Tuple(item);
+        Py_DECREF(item);
         if (!each) goto bad;
         if (PyTuple_GET_SIZE(each) != 3) {
             PyErr_SetString(PyExc_ValueError, "three coefficients a step are needed");
