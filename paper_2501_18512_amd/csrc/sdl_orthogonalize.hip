@@ -7,11 +7,13 @@
 //
 // The products run on fp16 matrix instructions with fp32 sums.  X lies within the unit ball (the coefficients are checked on the host), so a power of
 // two keeps its elements in the middle of fp16's range: X 2^14, A 2^12, and b A + c A^2 by what its bound allows.
-//   - X itself is kept in fp32 beside its fp16 image, and a X is taken from there.  What the images lose is then a factor near 1 on what a
-//     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.  A matrix whose norm is far under eps
-//     keeps its digits too, where its products are nothing beside a X.
-//   - results in bf16: one image, 11 bits.  An error of 2^-12 an element, 0.0003 to 0.0005 of the result after five steps, under the 0.0017 of its own rounding.
-//   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.
+//   - X itself is kept with more digits than its image has, and a X is taken from there.  What the images lose is then a factor near 1 on what a
+//     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.
+//   - results in bf16: one image, 11 bits.  An error of 2^-12 an element, 0.0003 to 0.0005 of the result after five steps, under the 0.0017 of its own rounding.  X is its image and what that
+//     leaves, rounded to bf16: 19 bits, and 8 of an element too small for the image (2^-38 of a norm, which takes an eps far above the norm).  The write of X is what an update
+//     waits for, and in fp32 it was half as much again.
+//   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.  X in fp32, which has its digits
+//     wherever the norm is.
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
 #include <algorithm>
 #include <cmath>
@@ -38,7 +40,7 @@ constexpr uint32_t kMostSmallSteps = 32;
 struct Work {
     char* base;
     size_t each;
-    size_t x32, x16, xt16, xt16_other, a16, b16;     // offsets
+    size_t rest, x16, x16_other, a16, b16;           // offsets; rest: X in fp32, or in bf16 what its one image leaves
     uint32_t n, m;                                    // n <= m, filled up
     uint32_t split;
     __host__ __device__ uint32_t pitch(uint32_t k) const { return k * (split ? 4u : 2u); }     // bytes of a row of k elements of an image
@@ -74,7 +76,25 @@ __device__ __forceinline__ void put(char* row, uint32_t k, const Parts& p)
     if constexpr (SPLIT) at[4] = p.lo;
 }
 
-// ------------------------------------------------------------------------------------------- norm, first images
+// Eight elements of X, as its image (at x16) and what is kept beside it.
+template <bool SPLIT>
+__device__ __forceinline__ void put_x(char* base, const Work& w, size_t x16, uint32_t i, uint32_t j, const float* v)
+{
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = v[e] * kScaleX;
+    const Parts image = parts_of(s);
+    put<SPLIT>(base + x16 + (size_t)i * w.pitch(w.m), j, image);
+    if constexpr (SPLIT) {
+        store8(reinterpret_cast<float*>(base + w.rest) + (size_t)i * w.m, j, j + 8, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] -= (float)image.hi[e];
+        store8(reinterpret_cast<__bf16*>(base + w.rest) + (size_t)i * w.m, j, j + 8, s);
+    }
+}
+
+// ------------------------------------------------------------------------------------------- norm, first image
 
 struct FirstArgs {
     View x;                     // rows along `token`
@@ -109,7 +129,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_norm_kernel(const First
     if (threadIdx.x == 0) a.squares[(size_t)matrix * a.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// x over its norm, as images of both orders, in tiles of 64 by 64 of what the workspace holds.
+// x over its norm, or its transpose, in tiles of 64 by 64 of what the workspace holds.
 template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(256) sdl_orthogonalize_first_kernel(const FirstArgs a)
 {
@@ -142,14 +162,10 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_first_kernel(const Firs
     char* base = a.w.base + matrix * a.w.each;
     for (uint32_t i = threadIdx.x; i < 512; i += 256) {
         const uint32_t r = i / 8, c = i % 8 * 8;
-        float v[8], s[8];
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = tile[r][c + j], s[j] = v[j] * kScaleX;
-        store8(reinterpret_cast<float*>(base + a.w.x32) + (size_t)(i0 + r) * a.w.m + j0, c, c + 8, v);
-        put<SPLIT>(base + a.w.x16 + (size_t)(i0 + r) * a.w.pitch(a.w.m), j0 + c, parts_of(s));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = tile[c + j][r] * kScaleX;
-        put<SPLIT>(base + a.w.xt16 + (size_t)(j0 + r) * a.w.pitch(a.w.n), i0 + c, parts_of(s));
+        for (int j = 0; j < 8; ++j) v[j] = tile[r][c + j];
+        put_x<SPLIT>(base, a.w, a.w.x16, i0 + r, j0 + c, v);
     }
 }
 
@@ -162,7 +178,7 @@ enum { WHOLE, PART, JOIN };
 
 struct ProductArgs {
     Work w;
-    size_t p, q, t;             // offsets of the two operands' images, and of what is written: images (UPDATE: of the transpose)
+    size_t p, q, t;             // offsets of the two operands' images, and of the one that is written
     uint32_t pitch_p, pitch_q, steps;
     Div slice_of;               // slices of a sum, and the partial sums of each:
     f32x4_t* partial;           // [workgroup][slice][4 registers][thread]
@@ -184,8 +200,9 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// TILE by TILE of C = P Q^T, both operands with k along their rows, by 2 by 2 wavefronts.  In shared memory a row's step is 128 bytes, its eight
-// pieces swapped around by an xor with bits 1 to 3 of the row's number: neither the copies nor the reads (16 rows, one piece) meet in a bank.
+// TILE by TILE of C = P Q^T (UPDATE: P Q), by 2 by 2 wavefronts.  An operand with k along its rows: in shared memory a row's step is 128 bytes, its eight
+// pieces swapped around by an xor with bits 1 to 3 of the row's number; neither the copies nor the reads (16 rows, one piece) meet in a bank.  Q of an update, X with k down its columns: a
+// step is 64 (of two images 32) rows of the tile's columns, read by transposing reads of four rows at a time, whose pieces are moved apart by an xor of bits 2 and 3 with the row's number.
 // Two steps' tiles in turn.  A step is G groups of products; a group's operands are read while the one before is multiplied, and the wait for the next step's tile
 // comes in front of the last group, whose operands are in registers by then: its products run while the next step's first operands are read and the copies of the one after
 // that are started.
@@ -194,7 +211,7 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p)
 // D column c, rows 8 (i / 4) + 4 half + i % 4.
 //
 // The columns of D are the rows of C, of which a lane so has four neighbours at a time.  Results go through shared memory in blocks of a wavefront's own, so that they are written (and
-// what they are added to is read) in pieces of 16 bytes, and their images once more: transposing reads give the other half of what is symmetric, and X's transpose.
+// what they are added to is read) in pieces of 16 bytes, and the images of what is symmetric once more: transposing reads give its other half.
 template <int TILE, bool SPLIT, int MODE, int HOW, typename O>
 __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const ProductArgs a)
 {
@@ -224,7 +241,10 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
     char* base = a.w.base + matrix * a.w.each;
     const uint32_t first = HOW == PART ? slice * a.steps / a.slice_of.d : 0, steps = (HOW == PART ? (slice + 1) * a.steps / a.slice_of.d : a.steps) - first;
     const char* from_p = base + a.p + (size_t)(ti * TILE + wave * kCopies * 8) * a.pitch_p + (size_t)first * 128;
-    const char* from_q = base + a.q + (size_t)(tj * TILE + wave * kCopies * 8) * a.pitch_q + (size_t)first * 128;
+    constexpr int kRow = MODE == UPDATE ? TILE * (SPLIT ? 4 : 2) : 128, kRowPieces = kRow / 16, kRowsOfCopy = 1024 / kRow, kStepRows = SPLIT ? 32 : 64;      // of Q in shared memory
+    const char* from_q = base + a.q + (MODE == UPDATE ? (size_t)tj * kRow : (size_t)(tj * TILE + wave * kCopies * 8) * a.pitch_q + (size_t)first * 128);
+    const size_t step_q = MODE == UPDATE ? (size_t)kStepRows * a.pitch_q : 128;
+    const auto apart = [](uint32_t row) { return kRowPieces >= 16 ? (row & 3) << 2 : (row & 2) << 1; };
     // the piece that comes to lie where the lane's 16 bytes land, in the even instructions; 4 further, by xor, in the odd ones
     const uint32_t piece_at = ((lane % 8) ^ (lane / 16)) * 16;
     const uint32_t off_p = lane / 8 * a.pitch_p + piece_at, off_q = lane / 8 * a.pitch_q + piece_at;
@@ -233,23 +253,47 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
         offs_p[i] = (off_p ^ (i % 2 * 64)) + i * 8 * a.pitch_p;
-        offs_q[i] = (off_q ^ (i % 2 * 64)) + i * 8 * a.pitch_q;
+        if constexpr (MODE == UPDATE) {
+            const uint32_t row = (wave * kCopies + i) * kRowsOfCopy + lane / kRowPieces;
+            offs_q[i] = row * a.pitch_q + ((lane % kRowPieces) ^ apart(row)) * 16;
+        } else {
+            offs_q[i] = (off_q ^ (i % 2 * 64)) + i * 8 * a.pitch_q;
+        }
     }
     // the i-th of a wavefront's copies of a step's tiles
     const auto copy = [&](uint32_t step, int i) {
         const uint32_t to = lds_offset(lds) + (step % 2) * (2 * kBytes) + wave * kCopies * 1024;
         if (i % 2 == 0) copy_pieces(from_p + step * 128, offs_p[i / 2], to + i / 2 * 1024);
-        else copy_pieces(from_q + step * 128, offs_q[i / 2], to + kBytes + i / 2 * 1024);
+        else copy_pieces(from_q + step * step_q, offs_q[i / 2], to + kBytes + i / 2 * 1024);
     };
     const uint32_t i0 = wave / 2 * kSide, j0 = wave % 2 * kSide, mix = (c >> 1) & 7;
     constexpr int kImages = SPLIT ? 2 : 1, kReads = 2 * kParts * kImages, kProducts = kParts * kParts * (SPLIT ? 3 : 1);     // of a group
     f16x8_t p[2][kImages][kParts], q[2][kImages][kParts];
+    // The transposing read of two times four rows: lane 4 r + q of 16 names the q-th quarter of row r of 4, and gets the four rows of its column of 16.
+    const auto across = [](const char* at, int four) {
+        typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+        const i16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + four));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // where this lane's reads of an update's Q start: row 8 half + its number of four, the piece of the columns of its half of 32
+    uint32_t read_q[kImages][kParts];
+    if constexpr (MODE == UPDATE) {
+        const uint32_t row = 8 * half + lane % 16 / 4;
+#pragma unroll
+        for (int image = 0; image < kImages; ++image)
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+                const uint32_t piece = (SPLIT ? (j0 / 32 + i) * 8 + image * 4 : (j0 / 32 + i) * 4) + lane % 32 / 16 * 2 + lane % 4 / 2;
+                read_q[image][i] = kBytes + row * kRow + (piece ^ apart(row)) * 16 + lane % 2 * 8;
+            }
+    }
     // the r-th of the reads of a group's operands
     const auto read = [&](uint32_t step, int g, int to, int r) {
         const char* rows = lds + (step % 2) * (2 * kBytes) + c * 128;
         const int image = r / (2 * kParts), i = r % (2 * kParts) / 2;
         const uint32_t at = ((4 * image + 2 * g + half) ^ mix) * 16;
         if (r % 2 == 0) p[to][image][i] = *reinterpret_cast<const f16x8_t*>(rows + (i0 + i * 32) * 128 + at);
+        else if constexpr (MODE == UPDATE) q[to][image][i] = across(lds + (step % 2) * (2 * kBytes) + read_q[image][i] + g * 16 * kRow, 4 * kRow);
         else q[to][image][i] = *reinterpret_cast<const f16x8_t*>(rows + kBytes + (j0 + i * 32) * 128 + at);
     };
     f32x16_t acc[kParts][kParts] = {};
@@ -339,12 +383,6 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
     __syncthreads();        // the tiles' memory becomes the blocks'
     const uint32_t n = a.w.n, m = a.w.m;
     char* block = lds + wave * kOwn;
-    // The transposing read: lane 4 r + q of 16 names the q-th quarter of row r of 4, and gets the four rows of its column of 16.
-    const auto across = [](const char* at) {
-        typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
-        const i16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 4 * kImagePitch));
-        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
     constexpr int kSpan = kBlock / 8, kRows = kWave / kSpan, kPasses = kBlock / kRows, kIn = kBlock / 32;     // lanes of a row; rows of a pass
     const uint32_t r0 = lane / kSpan, c0 = lane % kSpan * 8;
 #pragma unroll
@@ -352,8 +390,9 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
 #pragma unroll
         for (int bj = 0; bj < kParts / kIn; ++bj) {
             const uint32_t i = ti * TILE + i0 + bi * kBlock, j = tj * TILE + j0 + bj * kBlock;     // the block's first row and column
-            Parts old[MODE == POLY ? kPasses : 1];
-            Eight<float> x[MODE == UPDATE ? kPasses : 1];
+            Parts old[MODE == POLY || (MODE == UPDATE && !SPLIT) ? kPasses : 1];
+            Eight<float> x[MODE == UPDATE && SPLIT ? kPasses : 1];
+            Eight<__bf16> rest[MODE == UPDATE && !SPLIT ? kPasses : 1];
             if constexpr (MODE == POLY) {
 #pragma unroll
                 for (int k = 0; k < kPasses; ++k) {
@@ -364,8 +403,15 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
             }
             if constexpr (MODE == UPDATE) {
 #pragma unroll
-                for (int k = 0; k < kPasses; ++k)
-                    x[k] = load8(reinterpret_cast<const float*>(base + a.w.x32) + (size_t)(i + k * kRows + r0) * m + j, c0, c0 + 8);
+                for (int k = 0; k < kPasses; ++k) {
+                    const uint32_t row = i + k * kRows + r0;
+                    if constexpr (SPLIT) {
+                        x[k] = load8(reinterpret_cast<const float*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
+                    } else {
+                        old[k].hi = *piece<false>(base + a.q + (size_t)row * a.w.pitch(m), j + c0);
+                        rest[k] = load8(reinterpret_cast<const __bf16*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
+                    }
+                }
             }
 #pragma unroll
             for (int pi = 0; pi < kIn; ++pi)
@@ -388,7 +434,8 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                     const float s = e < 4 ? lo[e & 3] : hi[e & 3];
                     if constexpr (MODE == GRAM) v[k][e] = s * a.on_sum;
                     if constexpr (MODE == POLY) v[k][e] = fmaf(s, a.on_sum, a.on_old * (SPLIT ? (float)old[k].hi[e] + (float)old[k].lo[e] : (float)old[k].hi[e]));
-                    if constexpr (MODE == UPDATE) v[k][e] = fmaf(s, a.on_sum, a.on_old * x[k].get(e));
+                    if constexpr (MODE == UPDATE && SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old * x[k].get(e));
+                    if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old / kScaleX * ((float)old[k].hi[e] + rest[k].get(e)));
                 }
             }
             if constexpr (MODE == UPDATE) {
@@ -416,18 +463,15 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                     continue;
                 }
 #pragma unroll
-                for (int k = 0; k < kPasses; ++k) {
-                    store8(reinterpret_cast<float*>(base + a.w.x32) + (size_t)(i + k * kRows + r0) * m + j, c0, c0 + 8, v[k]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[k][e] *= kScaleX;
-                }
+                for (int k = 0; k < kPasses; ++k) put_x<SPLIT>(base, a.w, a.t, i + k * kRows + r0, j + c0, v[k]);
+                continue;
             }
-            const bool turned = MODE == UPDATE || ti != tj;
+            const bool turned = ti != tj;
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
                 const uint32_t row = k * kRows + r0;
                 const Parts image = parts_of(v[k]);
-                put<SPLIT>(base + (MODE == UPDATE ? a.w.x16 : a.t) + (size_t)(i + row) * a.w.pitch(MODE == UPDATE ? m : n), j + c0, image);
+                put<SPLIT>(base + a.t + (size_t)(i + row) * a.w.pitch(n), j + c0, image);
                 if (turned) {
                     *reinterpret_cast<f16x8_t*>(block + row * kImagePitch + c0 * 2) = image.hi;
                     if constexpr (SPLIT) *reinterpret_cast<f16x8_t*>(block + (kBlock + row) * kImagePitch + c0 * 2) = image.lo;
@@ -440,8 +484,8 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                 const uint32_t col = k % (kBlock / 16) * 16, row = k / (kBlock / 16) * 32 + lane / 16 * 8;
                 const char* at = block + (row + lane % 16 / 4) * kImagePitch + col * 2 + lane % 4 * 8;
                 Parts image;
-                image.hi = across(at);
-                if constexpr (SPLIT) image.lo = across(at + kBlock * kImagePitch);
+                image.hi = across(at, 4 * kImagePitch);
+                if constexpr (SPLIT) image.lo = across(at + kBlock * kImagePitch, 4 * kImagePitch);
                 put<SPLIT>(base + a.t + (size_t)(j + col + lane % 16) * a.w.pitch(n), i + row, image);
             }
         }
@@ -712,9 +756,8 @@ Layout layout_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
         return here;
     };
     w.x16 = place((size_t)w.n * w.pitch(w.m));
-    w.x32 = place((size_t)w.n * w.m * 4);
-    w.xt16 = place((size_t)w.m * w.pitch(w.n));
-    w.xt16_other = place((size_t)w.m * w.pitch(w.n));
+    w.x16_other = place((size_t)w.n * w.pitch(w.m));
+    w.rest = place((size_t)w.n * w.m * (split ? 4 : 2));
     w.a16 = place((size_t)w.n * w.pitch(w.n));
     w.b16 = place((size_t)w.n * w.pitch(w.n));
     w.each = at;
@@ -778,7 +821,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
 {
     const Work& w = l.w;
     const uint32_t per = SPLIT ? 32 : 64, n = w.n / TILE, m = w.m / TILE;
-    size_t xt = w.xt16, other = w.xt16_other;
+    size_t now = w.x16, other = w.x16_other;
     double h = 1.0;
     for (uint32_t s = 0; s < steps; ++s) {
         const double ca = coefficients[3 * s], cb = coefficients[3 * s + 1], cc = coefficients[3 * s + 2];
@@ -788,7 +831,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.w = w;
         a.partial = reinterpret_cast<f32x4_t*>(w.base + l.partial);
         a.slice_of = make_div(l.gram_slices);
-        a.p = a.q = w.x16;
+        a.p = a.q = now;
         a.t = w.a16;
         a.pitch_p = a.pitch_q = w.pitch(w.m);
         a.steps = w.m / per;
@@ -804,8 +847,9 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.on_sum = (float)(cc / ((double)kScaleA * kScaleA) * scale_b);
         if (product<TILE, SPLIT, POLY, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         a.p = w.b16;
-        a.q = xt;
+        a.q = now;
         a.t = other;
+        a.pitch_q = w.pitch(w.m);
         a.tiles = make_div(n * m);
         a.across = make_div(m);
         a.last = s + 1 == steps;
@@ -817,7 +861,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.rows = rows;
         a.cols = cols;
         if (product<TILE, SPLIT, UPDATE, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
-        std::swap(xt, other);
+        std::swap(now, other);
     }
     return SDL_OK;
 }
