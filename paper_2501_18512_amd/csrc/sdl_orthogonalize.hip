@@ -712,21 +712,30 @@ uint32_t slices_of(uint32_t batch, uint32_t tile, uint32_t n, uint32_t k, bool s
     return (uint32_t)std::min(want, most);
 }
 
-// Side of the products' tiles: the one whose rounds of workgroups take least. Larger tiles read less for every product, smaller ones leave fewer compute units without
-// one at the end.
-uint32_t tile_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
+// Sides of the tiles of the symmetric products and of the updates: those whose rounds of workgroups take least.  Larger tiles read less for every product, smaller ones leave fewer
+// compute units without one at the end.  us a step, the same sides for both: four of 2048 x 2048 in bf16 256 183, 128 193, 64 250; 48 of 768 x 768 217, 199, 228; one of 768 x 768
+// 78, 38, 27; 4096 x 4096 310, 357, 552.
+struct Tiles {
+    uint32_t symmetric, update;
+};
+
+Tiles tiles_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
 {
-    uint32_t best = 0;
+    Tiles best{};
     double least = 0.0;
-    for (const uint32_t tile : {256u, 128u, 64u}) {
-        const uint64_t rows = (n + tile - 1) / tile, cols = (m + tile - 1) / tile, symmetric = batch * (rows * (rows + 1) / 2);
-        const auto rounds = [&](uint64_t tiles, uint32_t slices) {
-            return (double)((tiles * slices + slots_of(tile) - 1) / slots_of(tile)) / slices;
-        };
-        const double k = rounds(symmetric, slices_of(batch, tile, n, m, split)) * m + rounds(symmetric, slices_of(batch, tile, n, n, split)) * n + rounds(batch * rows * cols, 1) * n;
-        const double cost = k * (tile == 256 ? 256.0 * 256.0 : tile == 128 ? 2.5 * 128.0 * 128.0 : 6.8 * 64.0 * 64.0);
-        if (best == 0 || cost < least) best = tile, least = cost;
-    }
+    const auto weight = [](uint32_t tile) { return tile == 256 ? 256.0 * 256.0 : tile == 128 ? 2.5 * 128.0 * 128.0 : 6.8 * 64.0 * 64.0; };
+    const auto rounds = [](uint64_t tiles, uint32_t tile, uint32_t slices) { return (double)((tiles * slices + slots_of(tile) - 1) / slots_of(tile)) / slices; };
+    for (const uint32_t s : {256u, 128u, 64u})
+        for (const uint32_t u : {256u, 128u, 64u}) {
+            const uint32_t whole = std::max(s, u), N = (n + whole - 1) / whole * whole, M = (m + whole - 1) / whole * whole;     // as they are filled up
+            const uint64_t side = N / s, symmetric = batch * (side * (side + 1) / 2), update = (uint64_t)batch * (N / u) * (M / u);
+            // a tile's start and end cost as much as so many values of k: with 256 no other workgroup of the compute unit multiplies meanwhile
+            const auto longer = [](uint32_t k, uint32_t tile) { return (double)k + (tile == 256 ? 384 : tile); };
+            const double cost = weight(s) * (rounds(symmetric, s, slices_of(batch, s, N, M, split)) * longer(M, s) +
+                                             rounds(symmetric, s, slices_of(batch, s, N, N, split)) * longer(N, s)) +
+                                weight(u) * rounds(update, u, 1) * longer(N, u);
+            if (best.update == 0 || cost < least) best = Tiles{s, u}, least = cost;
+        }
     return best;
 }
 
@@ -735,7 +744,7 @@ uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(256u, 2048u / b
 
 struct Layout {
     Work w;
-    uint32_t tile;
+    Tiles tiles;
     size_t squares, partial, bytes;
     uint32_t parts, gram_slices, poly_slices;
 };
@@ -744,11 +753,12 @@ Layout layout_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
 {
     Layout l{};
     const uint32_t n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    l.tile = tile_of(batch, n, m, split);
+    l.tiles = tiles_of(batch, n, m, split);
+    const uint32_t whole = std::max(l.tiles.symmetric, l.tiles.update);
     Work& w = l.w;
     w.split = split;
-    w.n = (n + l.tile - 1) / l.tile * l.tile;
-    w.m = (m + l.tile - 1) / l.tile * l.tile;
+    w.n = (n + whole - 1) / whole * whole;
+    w.m = (m + whole - 1) / whole * whole;
     size_t at = 0;
     const auto place = [&at](size_t bytes) {
         const size_t here = at;
@@ -764,10 +774,10 @@ Layout layout_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
     l.parts = parts_of(batch);
     l.squares = (size_t)batch * w.each;
     l.partial = l.squares + ((size_t)batch * l.parts * sizeof(double) + 127) / 128 * 128;
-    l.gram_slices = slices_of(batch, l.tile, w.n, w.m, split);
-    l.poly_slices = slices_of(batch, l.tile, w.n, w.n, split);
-    const uint32_t slices = std::max(l.gram_slices, l.poly_slices), side = w.n / l.tile;
-    l.bytes = l.partial + (slices > 1 ? (size_t)batch * (side * (side + 1) / 2) * slices * l.tile * l.tile * sizeof(float) : 0);
+    l.gram_slices = slices_of(batch, l.tiles.symmetric, w.n, w.m, split);
+    l.poly_slices = slices_of(batch, l.tiles.symmetric, w.n, w.n, split);
+    const uint32_t slices = std::max(l.gram_slices, l.poly_slices), side = w.n / l.tiles.symmetric;
+    l.bytes = l.partial + (slices > 1 ? (size_t)batch * (side * (side + 1) / 2) * slices * l.tiles.symmetric * l.tiles.symmetric * sizeof(float) : 0);
     return l;
 }
 
@@ -800,7 +810,7 @@ float image_scale(double b, double c, double h)
 }
 
 template <int TILE, bool SPLIT, int MODE, typename O>
-int product(const ProductArgs& a, uint32_t batch, hipStream_t st)
+int product_of(const ProductArgs& a, uint32_t batch, hipStream_t st)
 {
     const uint32_t groups = batch * a.tiles.d;
     if constexpr (MODE != UPDATE && TILE != 256) {
@@ -815,12 +825,18 @@ int product(const ProductArgs& a, uint32_t batch, hipStream_t st)
     return launched();
 }
 
-template <int TILE, bool SPLIT, typename O>
+template <bool SPLIT, int MODE, typename O>
+int product(const ProductArgs& a, uint32_t tile, uint32_t batch, hipStream_t st)
+{
+    return tile == 256 ? product_of<256, SPLIT, MODE, O>(a, batch, st) : tile == 128 ? product_of<128, SPLIT, MODE, O>(a, batch, st) : product_of<64, SPLIT, MODE, O>(a, batch, st);
+}
+
+template <bool SPLIT, typename O>
 int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, const float* coefficients, uint32_t steps, float scale, const sdl_view_t* out,
              hipStream_t st)
 {
     const Work& w = l.w;
-    const uint32_t per = SPLIT ? 32 : 64, n = w.n / TILE, m = w.m / TILE;
+    const uint32_t per = SPLIT ? 32 : 64, side = w.n / l.tiles.symmetric, down = w.n / l.tiles.update, across = w.m / l.tiles.update;
     size_t now = w.x16, other = w.x16_other;
     double h = 1.0;
     for (uint32_t s = 0; s < steps; ++s) {
@@ -835,9 +851,9 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.t = w.a16;
         a.pitch_p = a.pitch_q = w.pitch(w.m);
         a.steps = w.m / per;
-        a.tiles = make_div(n * (n + 1) / 2);
+        a.tiles = make_div(side * (side + 1) / 2);
         a.on_sum = kScaleA / (kScaleX * kScaleX);
-        if (product<TILE, SPLIT, GRAM, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<SPLIT, GRAM, O>(a, l.tiles.symmetric, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         a.slice_of = make_div(l.poly_slices);
         a.p = a.q = w.a16;
         a.t = w.b16;
@@ -845,13 +861,13 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.steps = w.n / per;
         a.on_old = (float)(cb / kScaleA * scale_b);
         a.on_sum = (float)(cc / ((double)kScaleA * kScaleA) * scale_b);
-        if (product<TILE, SPLIT, POLY, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<SPLIT, POLY, O>(a, l.tiles.symmetric, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         a.p = w.b16;
         a.q = now;
         a.t = other;
         a.pitch_q = w.pitch(w.m);
-        a.tiles = make_div(n * m);
-        a.across = make_div(m);
+        a.tiles = make_div(down * across);
+        a.across = make_div(across);
         a.last = s + 1 == steps;
         const double to = a.last ? scale : 1.0;
         a.on_old = (float)(ca * to);
@@ -860,7 +876,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.tall = rows > cols;
         a.rows = rows;
         a.cols = cols;
-        if (product<TILE, SPLIT, UPDATE, O>(a, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<SPLIT, UPDATE, O>(a, l.tiles.update, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         std::swap(now, other);
     }
     return SDL_OK;
@@ -967,11 +983,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (dtype == SDL_DTYPE_BF16) rc = split ? first<__bf16, true>(a, batch, st) : first<__bf16, false>(a, batch, st);
     else rc = split ? first<float, true>(a, batch, st) : first<float, false>(a, batch, st);
     if (rc != SDL_OK) return rc;
-#define SDL_STEPS(TILE)                                                                                                \
-    (split ? steps_of<TILE, true, float>(l, batch, rows, cols, coefficients, steps, scale, out, st)                 \
-           : steps_of<TILE, false, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st))
-    return l.tile == 256 ? SDL_STEPS(256) : l.tile == 128 ? SDL_STEPS(128) : SDL_STEPS(64);
-#undef SDL_STEPS
+    return split ? steps_of<true, float>(l, batch, rows, cols, coefficients, steps, scale, out, st) : steps_of<false, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st);
 }
 
 }  // extern "C"
