@@ -99,29 +99,36 @@ __device__ __forceinline__ void put_x(char* base, const Work& w, size_t x16, uin
 struct FirstArgs {
     View x;                     // rows along `token`
     uint32_t rows, cols, tall, parts;
+    Div groups;                 // of eight, of a row
     double* squares;            // [matrix][parts]
     double eps;
     Work w;
 };
 
-// Sum of squares of a matrix' rows part, part + parts, ...: in 64 bits, in which no square of a 32-bit number is out of range.
+// Sum of squares of a part of a matrix: in 64 bits, in which no square of a 32-bit number is out of range.
 template <typename T>
 __global__ void __launch_bounds__(256) sdl_orthogonalize_norm_kernel(const FirstArgs a)
 {
     __shared__ double sums[4];
     const uint32_t part = blockIdx.x, matrix = blockIdx.y;
     const T* x = reinterpret_cast<const T*>(a.x.data) + (int64_t)matrix * a.x.batch;
-    const uint32_t groups = (a.cols + 7) / 8;
-    // threads beyond a row's groups take further rows
-    const uint32_t across = min(groups, 256u), down = 256 / across, r0 = threadIdx.x / across, g0 = threadIdx.x % across;
+    const uint32_t n = a.rows * a.groups.d;         // groups of eight of all rows
     double s = 0.0;
-    if (r0 < down)
-        for (uint32_t r = part * down + r0; r < a.rows; r += a.parts * down)
-            for (uint32_t g = g0; g < groups; g += across) {
-                const Eight<T> e = load8(x + (int64_t)r * a.x.token, g * 8, a.cols);
+    for (uint32_t i0 = part * 256 + threadIdx.x; i0 < n; i0 += 4 * a.parts * 256) {
+        // four loads wait together; those behind the end are the last group, and not counted
+        Eight<T> e[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s += (double)e.get(j) * (double)e.get(j);
-            }
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t i = min(i0 + k * a.parts * 256, n - 1), r = div(i, a.groups);
+            e[k] = load8(x + (int64_t)r * a.x.token, (i - r * a.groups.d) * 8, a.cols);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i0 + k * a.parts * 256 >= n) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += (double)e[k].get(j) * (double)e[k].get(j);
+        }
+    }
 #pragma unroll
     for (int k = 32; k; k /= 2) s += __shfl_xor(s, k);
     if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = s;
@@ -740,7 +747,7 @@ Tiles tiles_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
 }
 
 // Sums of squares of a matrix: enough workgroups for all compute units.
-uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(256u, 2048u / batch)); }
+uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(1024u, 2048u / batch)); }
 
 struct Layout {
     Work w;
@@ -977,6 +984,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     a.cols = cols;
     a.tall = rows > cols;
     a.parts = l.parts;
+    a.groups = make_div((cols + 7) / 8);
     a.squares = reinterpret_cast<double*>(l.w.base + l.squares);
     a.eps = (double)eps;
     a.w = l.w;
