@@ -29,21 +29,26 @@ def cross_entropy(x, targets, smoothing, z):
     """(loss, lse) of rows; 0 without a target."""
     x, V = x.double(), x.shape[-1]
     there = targets.ge(0) & targets.lt(V)
-    lse = torch.logsumexp(x, -1)
-    hit = x.gather(-1, targets.long().clamp(0, V - 1)[..., None])[..., 0]
-    loss = lse - (1.0 - smoothing) * hit + z * lse ** 2
+    # around the row's maximum: log 5 is lost in 64 bits, too, beside logits of 10^38
+    top = x.amax(-1, keepdim=True)
+    top = torch.where(top.isfinite(), top, torch.zeros(()).double())
+    lse = top[..., 0] + torch.logsumexp(x - top, -1)
+    hit = (x - top).gather(-1, targets.long().clamp(0, V - 1)[..., None])[..., 0]
+    loss = torch.logsumexp(x - top, -1) - (1.0 - smoothing) * hit + z * lse ** 2
     if smoothing:
-        loss = loss - smoothing * x.mean(-1)
+        loss = loss - smoothing * (x - top).mean(-1)
     return loss.where(there, torch.zeros(())), lse.where(there, torch.zeros(()))
 
 
 def cross_entropy_backward(x, targets, lse, d_loss, smoothing, z):
-    """The gradient of the rows' losses, weighted by d_loss, from lse."""
-    x, V, lse = x.double(), x.shape[-1], lse.double()
+    """The gradient of the rows' losses, weighted by d_loss, from lse; lse None: from the probabilities themselves."""
+    x, V = x.double(), x.shape[-1]
+    p = torch.softmax(x, -1) if lse is None else torch.exp(x - lse.double()[..., None])
+    lse = torch.logsumexp(x, -1) if lse is None else lse.double()
     there = targets.ge(0) & targets.lt(V)
     want = torch.full(x.shape, smoothing / V, dtype=F64)
     want.scatter_add_(-1, targets.long().clamp(0, V - 1)[..., None], torch.full((*targets.shape, 1), 1.0 - smoothing, dtype=F64))
-    d = (1.0 + 2.0 * z * lse)[..., None] * torch.exp(x - lse[..., None]) - want
+    d = (1.0 + 2.0 * z * lse)[..., None] * p - want
     return (d * d_loss.double()[..., None]).where(there[..., None], torch.zeros(()))
 
 

@@ -11,7 +11,7 @@ namespace {
 
 using namespace sdl_device;
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct LossArgs {
     View x, d;
@@ -19,7 +19,8 @@ struct LossArgs {
     const float* d_loss;
     float *loss, *lse;
     Div tokens;
-    uint32_t rows, vocab, wide;     // targets of 64 bits
+    uint32_t rows, vocab, line;     // groups are counted from multiples of so many bytes
+    bool wide;                      // targets of 64 bits
     float smoothing, hit, share, z; // hit = 1 - smoothing, share = smoothing / vocab
 };
 
@@ -38,20 +39,32 @@ __device__ __forceinline__ T* row_of(const LossArgs& a, const View& v, uint32_t 
 }
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // exp(x - m) where m is at least x
 __device__ __forceinline__ float exp_under(float x, float m) { return exp2_of((x - m) * kLog2e); }
 
-// Maximum, sum of exp(x - maximum), and sum of x of some of a row's elements.
+// What logits are taken as powers of two around m with: exp(x - m) = 2^(x log2(e) - from), one fused multiply-add and one exponential an element, and from = m log2(e) as it is rounded.
+// That rounding has to be small, and m up to 2^21; around any other number nothing is lost but zeros (numbers so far down have none but those beside a number
+// of 2^20, and rows of larger ones go another way, below).
+struct Base {
+    float from;
+    bool near;
+    __device__ __forceinline__ explicit Base(float m) : from(fabsf(m) <= 0x1p21f ? m * kLog2e : 0.0f), near(fabsf(m) <= 0x1p21f) {}
+    __device__ __forceinline__ float exp(float x) const { return exp2_of(fmaf(x, kLog2e, -from)); }
+    // what a sum of exp() around this is to be multiplied with for one around another, larger one
+    __device__ __forceinline__ float into(const Base& to) const { return near && to.near ? exp2_of(from - to.from) : 1.0f; }
+};
+
+// Maximum, sum of exp() around it, and sum of x of some of a row's elements.  A part of nothing but -infinity has s = 0.
 struct Part {
     float m, s, sum;
 };
 
-// A part of nothing but -infinity has s = 0.
 __device__ __forceinline__ Part join(const Part& a, const Part& b)
 {
     const float m = fmaxf(a.m, b.m);
-    const float base = m == -__builtin_inff() ? 0.0f : m;
-    return Part{m, a.s * exp_under(a.m, base) + b.s * exp_under(b.m, base), a.sum + b.sum};
+    const Base to(m);
+    return Part{m, a.s * Base(a.m).into(to) + b.s * Base(b.m).into(to), a.sum + b.sum};
 }
 
 __device__ __forceinline__ float wave_max(float x)
@@ -69,115 +82,163 @@ __device__ __forceinline__ float wave_max(float x)
 // The lanes' parts as one, in all of them.
 __device__ __forceinline__ Part wave_join(const Part& p, bool smooth)
 {
-    const float m = wave_max(p.m), base = m == -__builtin_inff() ? 0.0f : m;
-    return Part{m, lane_sum<kWave>(p.s * exp_under(p.m, base)), smooth ? lane_sum<kWave>(p.sum) : 0.0f};
+    const float m = wave_max(p.m);
+    const Base to(m);
+    return Part{m, lane_sum<kWave>(p.s * Base(p.m).into(to)), smooth ? lane_sum<kWave>(p.sum) : 0.0f};
 }
 
-// The same bits, for the compiler others, that it has when `now` is worked out: else it would keep eight numbers instead of the four words that they come in, for all that
-// a thread holds (104 registers instead of 70 for eight groups, and memory for sixteen).
-__device__ __forceinline__ void forget(Eight<__bf16>& e, float& now) { asm volatile("" : "+v"(e.w), "+v"(now)); }
-__device__ __forceinline__ void forget(Eight<float>&, float&) {}
+constexpr int kLine = 128;      // bytes of a cache's line
 
-// A row of n elements in groups of eight that start on 16 bytes: group g stands for [8 g - lead, 8 g - lead + 8).  The first and the last, which may stick out, are the eight
-// elements at the row's end instead, so that others' are among them too: those are not counted, and what two threads write to one place is the same.  All of a thread's accesses are
-// whole ones that wait for nothing.  Rows of 32001 in bf16 instead of 32000: 219 us with groups that start with the row, 179 so.  (TINY rows, which may have less than eight
-// elements, go element by element.)
-template <bool TINY>
+// 16 bytes from any element on
+typedef uint32_t At __attribute__((ext_vector_type(4), aligned(2)));
+
+// As many elements of a row as are 16 bytes: what one access of a thread's moves.
+template <typename T>
+struct Group {
+    static constexpr int W = 16 / sizeof(T);
+    u32x4 w;
+    __device__ __forceinline__ float get(int j) const
+    {
+        if constexpr (sizeof(T) == 4) return u2f(w[j]);
+        else return u2f(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+    }
+    static __device__ __forceinline__ Group of(const float* v)
+    {
+        if constexpr (sizeof(T) == 4) return Group{u32x4{f2u(v[0]), f2u(v[1]), f2u(v[2]), f2u(v[3])}};
+        else return Group{u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}};
+    }
+};
+
+// The same bits, for the compiler others, that it has when `now` is worked out: else it would keep eight numbers instead of the four words that they come in, for all that
+// a thread holds (104 registers instead of 70 for eight groups, and memory for sixteen); fp32 too is worked on in fewer registers so.
+template <typename T>
+__device__ __forceinline__ void forget(Group<T>& e, float& now)
+{
+    asm volatile("" : "+v"(e.w), "+v"(now));
+}
+
+// A row of n elements in groups of W that are counted from the cache line that it starts in, `lead` elements before it: group g stands for [W g - lead, W g - lead + W).  Those that
+// stick out at either end are the W elements at that end instead, so that others' are among them too: those are not counted, and what two threads write to one place is the same.  All
+// of a thread's accesses are whole ones that wait for nothing, and all of a wavefront's are whole lines.  8192 rows of 32001 in bf16: 219 us with groups that start with the row,
+// 189 with groups on 16 bytes, 176 so, as long as rows of 32000.  (TINY rows, which may have less than W elements, go element by element.)
+template <typename T, bool TINY>
 struct Groups {
+    static constexpr int W = Group<T>::W;
     uint32_t n;
     int32_t lead;
 
-    template <typename T>
-    __device__ __forceinline__ Groups(uint32_t n_, const T* row) : n(n_), lead(TINY ? 0 : (int32_t)((uintptr_t)row % 16 / sizeof(T))) {}
-    __device__ __forceinline__ bool there(uint32_t first) const { return first < n + lead; }      // first = 8 g
+    __device__ __forceinline__ Groups(const LossArgs& a, const T* row) : n(a.vocab), lead(TINY ? 0 : (int32_t)(((uint32_t)(uintptr_t)row & (a.line - 1)) / sizeof(T))) {}
+    __device__ __forceinline__ bool below(uint32_t first) const { return first < n + lead; }      // first = W g
+    __device__ __forceinline__ bool there(uint32_t first) const { return below(first) && (TINY || first + W > (uint32_t)lead); }
     __device__ __forceinline__ uint32_t from(uint32_t first) const
     {
-        return TINY ? first : (uint32_t)min(max((int32_t)first - lead, 0), (int32_t)n - 8);
+        return TINY ? first : (uint32_t)min(max((int32_t)first - lead, 0), (int32_t)n - W);
     }
+    // whether a group is there as a whole and in its place
+    __device__ __forceinline__ bool whole(uint32_t first) const { return !TINY && first >= (uint32_t)lead && first + W <= n + lead; }
     // whether the j-th element from from(first) on is the group's
     __device__ __forceinline__ bool has(uint32_t first, int j) const
     {
-        return TINY ? first + j < n : from(first) + j + lead - first < 8;
+        return TINY ? first + j < n : from(first) + j + lead - first < W;
     }
-    // whether a group that this thread, whose first one is 8 g, has of every TPR touches the element
+    // whether a group that this thread, whose first one is W g, has of every TPR touches the element
     template <int TPR>
     __device__ __forceinline__ bool touches(uint32_t first, uint32_t element) const
     {
-        const uint32_t own = first / 8;
-        if (TINY) return element / 8 % TPR == own;
-        return (element + lead) / 8 % TPR == own || (element < 8 && own == 0) || (element >= n - 8 && (n - 1 + lead) / 8 % TPR == own);
+        const uint32_t own = first / W;
+        if (TINY) return element / W % TPR == own;
+        return (element + lead) / W % TPR == own || (element < W && own == (uint32_t)lead / W) || (element >= n - W && (n - 1 + lead) / W % TPR == own);
     }
-    template <typename T>
-    __device__ __forceinline__ Eight<T> load(const T* row, uint32_t first) const;
-    template <typename T>
-    __device__ __forceinline__ void store(T* row, uint32_t first, const float* v) const;
+    // Rows go past the caches: 8192 of 32000 in bf16 with their gradient 195 us with cached accesses, 179 so; 4096 in fp32 194 and 180.  (1551 of 5003 in fp32, which the
+    // last cache holds: 11.8 and 13.0.)
+    __device__ __forceinline__ Group<T> load(const T* row, uint32_t first) const
+    {
+        if constexpr (TINY) {
+            const T low = (T)-__builtin_inff();
+            T v[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = first + j < n ? row[first + j] : low;
+            return __builtin_bit_cast(Group<T>, v);
+        } else {
+            const At at = __builtin_nontemporal_load(reinterpret_cast<const At*>(row + from(first)));
+            return Group<T>{u32x4{at.x, at.y, at.z, at.w}};
+        }
+    }
+    __device__ __forceinline__ void store(T* row, uint32_t first, const float* v) const
+    {
+        if constexpr (TINY) {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (first + j < n) row[first + j] = (T)v[j];
+        } else {
+            const u32x4 w = Group<T>::of(v).w;
+            __builtin_nontemporal_store(At{w.x, w.y, w.z, w.w}, reinterpret_cast<At*>(row + from(first)));
+        }
+    }
+    // The same for no element but the group's, in their places.
+    __device__ __forceinline__ Group<T> load_own(const T* row, uint32_t first) const
+    {
+        if (whole(first)) return load(row, first);
+        T v[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[j] = first + j - lead < n ? row[first + j - lead] : (T)0.0f;
+        return __builtin_bit_cast(Group<T>, v);
+    }
+    __device__ __forceinline__ void store_own(T* row, uint32_t first, const float* v) const
+    {
+        if (whole(first)) return store(row, first, v);
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            if (first + j - lead < n) row[first + j - lead] = (T)v[j];
+    }
+
 };
 
-// In bf16, where an access of a wavefront's is whole cache lines, rows go past the caches: 8192 of 32000 with their gradient 195 us with cached accesses, 179 so; 256 of them 10.4
-// and 9.0.  In fp32 it is two halves of every 32 bytes: 4096 rows 203 us and 216, 1551 of 5003 13.0 and 16.1.
-typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
-
-template <bool TINY>
-template <typename T>
-__device__ __forceinline__ Eight<T> Groups<TINY>::load(const T* row, uint32_t first) const
+template <int W>
+__device__ __forceinline__ float sum_of(const float* v)
 {
-    if constexpr (TINY) {
-        const T low = (T)-__builtin_inff();
-        T v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = first + j < n ? row[first + j] : low;
-        return __builtin_bit_cast(Eight<T>, v);
-    } else if constexpr (sizeof(T) == 2) {
-        const u32x4_at2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_at2*>(row + from(first)));
-        return Eight<T>{u32x4{w.x, w.y, w.z, w.w}};
-    } else {
-        return load8(row, from(first), ~0u);
-    }
+    float s = (v[0] + v[1]) + (v[2] + v[3]);
+    if constexpr (W == 8) s += (v[4] + v[5]) + (v[6] + v[7]);
+    return s;
 }
 
-template <bool TINY>
-template <typename T>
-__device__ __forceinline__ void Groups<TINY>::store(T* row, uint32_t first, const float* v) const
+// What K groups of elements, TPR groups apart, are as a part of their row.  No branch goes by an element: a thread's groups stay in the words they came in.
+template <bool FIT, bool TINY, typename T, int K, int TPR>
+__device__ __forceinline__ Part part_of(Group<T> (&e)[K], uint32_t first, const Groups<T, TINY>& groups, bool smooth)
 {
-    if constexpr (TINY) {
-        store8(row, first, n, v);
-    } else if constexpr (sizeof(T) == 2) {
-        const u32x4_at2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-        __builtin_nontemporal_store(w, reinterpret_cast<u32x4_at2*>(row + from(first)));
-    } else {
-        store8(row, from(first), ~0u, v);
-    }
-}
-
-// What K groups of eight elements, TPR groups apart, are as a part of their row.  No branch goes by an element: a thread's groups stay in the words they came in.
-template <bool TINY, typename T, int K, int TPR>
-__device__ __forceinline__ Part part_of(Eight<T> (&e)[K], uint32_t first, const Groups<TINY>& groups, bool smooth)
-{
+    constexpr int W = Group<T>::W;
     Part p{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         float m = e[k].get(0);
 #pragma unroll
-        for (int j = 1; j < 8; ++j) m = fmaxf(m, e[k].get(j));
+        for (int j = 1; j < W; ++j) m = fmaxf(m, e[k].get(j));
         p.m = fmaxf(p.m, m);
         forget(e[k], p.m);
     }
-    const float base = p.m == -__builtin_inff() ? 0.0f : p.m;
+    const Base base(p.m);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        float v[8];
+        float v[W];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = groups.has(first + k * TPR * 8, j) ? exp_under(e[k].get(j), base) : 0.0f;
-        p.s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        for (int j = 0; j < W; ++j) v[j] = base.exp(e[k].get(j));
+        // (a row that stays in the registers has half of the groups that its kernel has room for, but for seven elements)
+        if ((!FIT || k == 0 || k + 1 >= K / 2) && !__all(groups.whole(first + k * TPR * W)))
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = groups.has(first + k * TPR * W, j) ? v[j] : 0.0f;
+        p.s += sum_of<W>(v);
         forget(e[k], p.s);
     }
     if (smooth) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float sum = 0.0f;
+            float v[W];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += groups.has(first + k * TPR * 8, j) ? e[k].get(j) : 0.0f;
-            p.sum += sum;
+            for (int j = 0; j < W; ++j) v[j] = e[k].get(j);
+            if ((!FIT || k == 0 || k + 1 >= K / 2) && !__all(groups.whole(first + k * TPR * W)))
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[j] = groups.has(first + k * TPR * W, j) ? v[j] : 0.0f;
+            p.sum += sum_of<W>(v);
             forget(e[k], p.sum);
         }
     }
@@ -189,40 +250,75 @@ struct Slope {
     float m, factor, even, hit;
 };
 
-template <bool TINY, typename T, int K, int TPR>
-__device__ __forceinline__ void write_gradient(T* row, uint32_t first, const Groups<TINY>& groups, Eight<T> (&e)[K], const Slope& g)
+// NEAR: the factor is one of exp() around the base.
+template <bool NEAR>
+__device__ __forceinline__ float slope_at(const Slope& g, const Base& base, float x)
 {
+    return fmaf(g.factor, NEAR ? base.exp(x) : exp_under(x, g.m), -g.even);
+}
+
+template <bool TINY, typename T, int K, int TPR>
+__device__ __forceinline__ void write_gradient(T* row, uint32_t first, const Groups<T, TINY>& groups, Group<T> (&e)[K], const Slope& g)
+{
+    constexpr int W = Group<T>::W;
+    const Base base(g.m);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        float v[8];
+        float v[W];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = g.factor * exp_under(e[k].get(j), g.m) - g.even;
-        if (groups.there(first + k * TPR * 8)) groups.store(row, first + k * TPR * 8, v);
+        for (int j = 0; j < W; ++j) v[j] = slope_at<true>(g, base, e[k].get(j));
+        if (groups.there(first + k * TPR * W)) groups.store(row, first + k * TPR * W, v);
+    }
+}
+
+// The gradient of a row that is read for it, and may be written in its place: a group that sticks out reads and writes no one else's elements.
+template <bool NEAR, bool TINY, typename T, int K, int TPR>
+__device__ __forceinline__ void read_and_write_gradient(const T* x, T* d, uint32_t first, const Groups<T, TINY>& groups, int32_t target, const Slope& g)
+{
+    constexpr int W = Group<T>::W;
+    const Base base(g.m);
+    for (uint32_t at = first; groups.below(at); at += TPR * W * K) {
+        Group<T> e[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) e[k] = groups.load_own(x, at + k * TPR * W);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const uint32_t one = at + k * TPR * W;
+            float v[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = slope_at<NEAR>(g, base, e[k].get(j));
+            if (((uint32_t)target + groups.lead) / W == one / W)
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[j] -= (uint32_t)target + groups.lead == one + j ? g.hit : 0.0f;
+            groups.store_own(d, one, v);
+        }
     }
 }
 
 // The target's element, once more by every thread that has written it: a wavefront's stores to one place keep their order.
 template <bool TINY, typename T, int TPR>
-__device__ __forceinline__ void write_target(T* row, uint32_t first, const Groups<TINY>& groups, int32_t target, float x, const Slope& g)
+__device__ __forceinline__ void write_target(T* row, uint32_t first, const Groups<T, TINY>& groups, int32_t target, float x, const Slope& g)
 {
-    if (groups.template touches<TPR>(first, (uint32_t)target)) row[target] = (T)(g.factor * exp_under(x, g.m) - g.even - g.hit);
+    if (groups.template touches<TPR>(first, (uint32_t)target)) row[target] = (T)(slope_at<true>(g, Base(g.m), x) - g.hit);
 }
 
 template <bool TINY, typename T, int TPR>
-__device__ __forceinline__ void write_zeros(T* row, uint32_t first, const Groups<TINY>& groups)
+__device__ __forceinline__ void write_zeros(T* row, uint32_t first, const Groups<T, TINY>& groups)
 {
-    const float zero[8] = {};
-    for (uint32_t at = first; groups.there(at); at += TPR * 8) groups.store(row, at, zero);
+    constexpr int W = Group<T>::W;
+    const float zero[W] = {};
+    for (uint32_t at = first; groups.below(at); at += TPR * W)
+        if (groups.there(at)) groups.store(row, at, zero);
 }
 
 // TPR threads a row, K groups of eight elements each; FIT: a row is that long at most and stays in the registers, else it is read again for its gradient.
 template <typename T, int BLOCK, int TPR, int K, bool FIT, bool TINY = false>
 __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs a)
 {
-    constexpr int kWaves = TPR / kWave;
+    constexpr int kWaves = TPR / kWave, W = Group<T>::W;
     static_assert(TPR == kWave || TPR == BLOCK, "a row is a wavefront's or a workgroup's");
     const uint32_t row = TPR == BLOCK ? workgroup() : workgroup() * (BLOCK / TPR) + threadIdx.x / TPR, n = a.vocab;
-    uint32_t first = threadIdx.x % TPR * 8;
+    uint32_t first = threadIdx.x % TPR * W;
     if (row >= a.rows) return;
     const int32_t target = target_of(a, row);
     T* d = a.d.data ? row_of<T>(a, a.d, row) : nullptr;
@@ -231,123 +327,146 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
             if (a.loss) a.loss[row] = 0.0f;
             if (a.lse) a.lse[row] = 0.0f;
         }
-        if (d) write_zeros<TINY, T, TPR>(d, first, Groups<TINY>(n, d));
+        if (d) write_zeros<TINY, T, TPR>(d, first, Groups<T, TINY>(a, d));
         return;
     }
     const T* x = row_of<const T>(a, a.x, row);
     const bool smooth = a.smoothing > 0.0f;
     const float at_target = (float)x[target], g = d && a.d_loss ? a.d_loss[row] : 1.0f;
-    const Groups<TINY> groups(n, d ? d : x);
-    Eight<T> e[K];
+    const Groups<T, TINY> groups(a, d ? d : x);
+    Group<T> e[K];
     Part p{-__builtin_inff(), 0.0f, 0.0f};
     if constexpr (FIT) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) e[k] = groups.load(x, first + k * TPR * 8);
-        p = part_of<TINY, T, K, TPR>(e, first, groups, smooth);
+        for (int k = 0; k < K; ++k) e[k] = groups.load(x, first + k * TPR * W);
+        p = part_of<FIT, TINY, T, K, TPR>(e, first, groups, smooth);
     } else {
-        for (uint32_t at = first; groups.there(at); at += TPR * 8 * K) {
+        for (uint32_t at = first; groups.below(at); at += TPR * W * K) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * 8);
-            p = join(p, part_of<TINY, T, K, TPR>(e, at, groups, smooth));
+            for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * W);
+            p = join(p, part_of<FIT, TINY, T, K, TPR>(e, at, groups, smooth));
         }
     }
     p = wave_join(p, smooth);
     // all of the row is read before any of it is written, which may be in its place
     asm volatile("" : : "v"(at_target) : "memory");
+    __shared__ Part parts[kWaves];
     if constexpr (kWaves > 1) {
-        __shared__ Part parts[kWaves];
         if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = p;
         __syncthreads();
-        p = parts[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) p = join(p, parts[w]);
+        const uint32_t lane = threadIdx.x % kWave;
+        p = wave_join(lane < kWaves ? parts[lane] : Part{-__builtin_inff(), 0.0f, 0.0f}, smooth);
     }
-    const float log_s = logf(p.s), lse = p.m + log_s;
+    // a row whose maximum is no number that the sums could be taken around: once more, by differences from it
+    const bool far = fabsf(p.m) > 0x1p20f && fabsf(p.m) < __builtin_inff();
+    if (far) {
+        float s = 0.0f;
+        for (uint32_t at = first; groups.below(at); at += TPR * W) {
+            const Group<T> x8 = groups.load(x, at);
+#pragma unroll
+            for (int j = 0; j < W; ++j) s += groups.has(at, j) ? exp_under(x8.get(j), p.m) : 0.0f;
+        }
+        p.s = lane_sum<kWave>(s);
+        if constexpr (kWaves > 1) {
+            __syncthreads();
+            if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave].s = p.s;
+            __syncthreads();
+            p.s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) p.s += parts[w].s;
+        }
+    }
+    const Base base(p.m);
+    // log of the sum of exp(x - m): that of the sum around the base, less what the base's rounding has made of it
+    const float log_s = logf(p.s) - (!far && base.near ? fmaf(p.m, kLog2e, -base.from) * kLn2 : 0.0f);
+    const float lse = p.m == __builtin_inff() ? __builtin_nanf("") : p.m + log_s;
     if (threadIdx.x % TPR == 0) {
         float loss = log_s + a.hit * (p.m - at_target);
         if (smooth) loss += a.smoothing * (p.m - p.sum / (float)n);
         if (a.z != 0.0f) loss += a.z * lse * lse;
-        if (a.loss) a.loss[row] = loss;
+        if (a.loss) a.loss[row] = p.m == __builtin_inff() ? lse : loss;
         if (a.lse) a.lse[row] = lse;
     }
     if (!d) return;
-    const Slope slope{p.m, g * (1.0f + 2.0f * a.z * lse) / p.s, g * a.share, g * a.hit};
+    const Slope slope{p.m, p.m == __builtin_inff() ? lse : g * (1.0f + 2.0f * a.z * lse) / p.s, g * a.share, g * a.hit};
     asm volatile("" : "+v"(first));         // places are worked out again, and not kept
-    if constexpr (FIT) {
+    if (far) {
+        read_and_write_gradient<false, TINY, T, 1, TPR>(x, d, first, groups, target, slope);
+    } else if constexpr (FIT) {
         write_gradient<TINY, T, K, TPR>(d, first, groups, e, slope);
+        write_target<TINY, T, TPR>(d, first, groups, target, at_target, slope);
     } else {
-        for (uint32_t at = first; groups.there(at); at += TPR * 8 * K) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * 8);
-            write_gradient<TINY, T, K, TPR>(d, at, groups, e, slope);
-        }
+        read_and_write_gradient<true, TINY, T, K, TPR>(x, d, first, groups, target, slope);
     }
-    write_target<TINY, T, TPR>(d, first, groups, target, at_target, slope);
 }
 
 // The gradient alone, from the forward pass' lse.
 template <typename T, int BLOCK, int TPR, int K, bool TINY>
 __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_backward_kernel(const LossArgs a)
 {
-    const uint32_t row = TPR == BLOCK ? workgroup() : workgroup() * (BLOCK / TPR) + threadIdx.x / TPR, n = a.vocab;
-    uint32_t first = threadIdx.x % TPR * 8;
+    constexpr int W = Group<T>::W;
+    const uint32_t row = TPR == BLOCK ? workgroup() : workgroup() * (BLOCK / TPR) + threadIdx.x / TPR;
+    uint32_t first = threadIdx.x % TPR * W;
     if (row >= a.rows) return;
     const int32_t target = target_of(a, row);
     T* d = row_of<T>(a, a.d, row);
     if (target < 0) {
-        write_zeros<TINY, T, TPR>(d, first, Groups<TINY>(n, d));
+        write_zeros<TINY, T, TPR>(d, first, Groups<T, TINY>(a, d));
         return;
     }
     const T* x = row_of<const T>(a, a.x, row);
-    const float at_target = (float)x[target], lse = a.lse[row], g = a.d_loss ? a.d_loss[row] : 1.0f;
-    const Groups<TINY> groups(n, d);
-    const Slope slope{lse, g * (1.0f + 2.0f * a.z * lse), g * a.share, g * a.hit};
-    for (uint32_t at = first; groups.there(at); at += TPR * 8 * K) {
-        Eight<T> e[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * 8);
-        write_gradient<TINY, T, K, TPR>(d, at, groups, e, slope);
+    const float lse = a.lse[row], g = a.d_loss ? a.d_loss[row] : 1.0f;
+    const Groups<T, TINY> groups(a, d);
+    // around lse, with what its rounding makes of the base taken back; an infinite or far lse by differences
+    if (fabsf(lse) <= 0x1p20f) {
+        const Slope slope{lse, g * (1.0f + 2.0f * a.z * lse) * exp2_of(-fmaf(lse, kLog2e, -Base(lse).from)), g * a.share, g * a.hit};
+        read_and_write_gradient<true, TINY, T, K, TPR>(x, d, first, groups, target, slope);
+    } else {
+        const Slope slope{lse, g * (1.0f + 2.0f * a.z * lse), g * a.share, g * a.hit};
+        read_and_write_gradient<false, TINY, T, 1, TPR>(x, d, first, groups, target, slope);
     }
-    write_target<TINY, T, TPR>(d, first, groups, target, at_target, slope);
 }
 
 template <typename T>
-int loss(const LossArgs& a, hipStream_t st)
+int loss(LossArgs a, hipStream_t st)
 {
-    const uint32_t V = a.vocab;
-#define SDL_LAUNCH(BLOCK, TPR, K, ...) \
-    hipLaunchKernelGGL((sdl_cross_entropy_kernel<T, BLOCK, TPR, K, __VA_ARGS__>), grid_of((a.rows - 1) / (BLOCK / TPR) + 1), dim3(BLOCK), 0, st, a)
     const View& rows = a.d.data ? a.d : a.x;
-    const bool even = aligned_to(rows.data, 16) && rows.batch * (int64_t)sizeof(T) % 16 == 0 && rows.token * (int64_t)sizeof(T) % 16 == 0;
-    const uint32_t room = even ? V : V + 7;         // a row's groups are one more where it does not start on 16 bytes
-    if (V <= 512) SDL_LAUNCH(256, 64, 1, true, true);
-    else if (room <= 1024) SDL_LAUNCH(256, 64, 2, true);
-    else if (room <= 2048) SDL_LAUNCH(256, 64, 4, true);
-    else if (room <= 4096) SDL_LAUNCH(256, 256, 2, true);
-    else if (room <= 8192) SDL_LAUNCH(256, 256, 4, true);
-    else if (room <= 16384) SDL_LAUNCH(512, 512, 4, true);
-    // without a gradient, fewer threads a row and more rows at a time: 8192 of 32000, half of them without a target, 51.7 us with 512 and 47.1 with 256; with one 179 and 185
-    else if (room <= 32768 && !a.d.data) SDL_LAUNCH(256, 256, 16, true);
-    else if (room <= 32768) SDL_LAUNCH(512, 512, 8, true);
-    else if (room <= 65536) SDL_LAUNCH(512, 512, 16, true);
-    else {
-        if constexpr (sizeof(T) == 2) {
-            if (room <= 131072) {
-                SDL_LAUNCH(1024, 1024, 16, true);
-                return launched();
-            }
-        }
-        SDL_LAUNCH(1024, 1024, 4, false);
-    }
+    const auto lie_on = [&](uint32_t line) {
+        return aligned_to(rows.data, line) && rows.batch * (int64_t)sizeof(T) % line == 0 && rows.token * (int64_t)sizeof(T) % line == 0;
+    };
+    // the elements that a row's groups have room for, from a line on, or where that would take a longer kernel from 16 bytes on
+    const uint32_t V = a.vocab, room = V + (lie_on(16) ? 0 : 16 / sizeof(T) - 1), room_line = V + (lie_on(kLine) ? 0 : kLine / sizeof(T) - 1);
+#define SDL_LAUNCH(LIMIT, BLOCK, TPR, K, ...) \
+    do { \
+        a.line = room_line <= (LIMIT) ? kLine : 16; \
+        hipLaunchKernelGGL((sdl_cross_entropy_kernel<T, BLOCK, TPR, (K) * (8 / Group<T>::W), __VA_ARGS__>), grid_of((a.rows - 1) / (BLOCK / TPR) + 1), dim3(BLOCK), 0, st, \
+                           a); \
+        return launched(); \
+    } while (0)
+#define SDL_FIT(LIMIT, BLOCK, TPR, K) \
+    if (room <= (LIMIT)) SDL_LAUNCH(LIMIT, BLOCK, TPR, K, true)
+    // 64 bytes of a row and less in a thread's registers up to 16384 elements, 256 in the end
+    constexpr uint32_t kLongest = sizeof(T) == 2 ? 512 : 1024;
+    if (V <= 512) SDL_LAUNCH(512, 256, 64, 1, true, true);
+    SDL_FIT(1024, 256, 64, 2);
+    SDL_FIT(2048, 256, 64, 4);
+    SDL_FIT(4096, 256, 256, 2);
+    SDL_FIT(8192, 256, 256, 4);
+    SDL_FIT(16384, 512, 512, 4);
+    SDL_FIT(32768, 512, 512, 8);
+    SDL_FIT(65536, kLongest, kLongest, 16 * 512 / kLongest);
+    if constexpr (sizeof(T) == 2) SDL_FIT(131072, 1024, 1024, 16);
+    SDL_LAUNCH(~0u, 1024, 1024, 4, false);
+#undef SDL_FIT
 #undef SDL_LAUNCH
-    return launched();
 }
 
 template <typename T>
-int gradient(const LossArgs& a, hipStream_t st)
+int gradient(LossArgs a, hipStream_t st)
 {
+    a.line = kLine;
 #define SDL_LAUNCH(TPR, K, TINY) \
-    hipLaunchKernelGGL((sdl_cross_entropy_backward_kernel<T, 256, TPR, K, TINY>), grid_of((a.rows - 1) / (256 / TPR) + 1), dim3(256), 0, st, a)
+    hipLaunchKernelGGL((sdl_cross_entropy_backward_kernel<T, 256, TPR, (K) * (8 / Group<T>::W), TINY>), grid_of((a.rows - 1) / (256 / TPR) + 1), dim3(256), 0, st, a)
     if (a.vocab <= 512) SDL_LAUNCH(64, 1, true);
     else if (a.vocab <= 2048) SDL_LAUNCH(64, 2, false);
     else SDL_LAUNCH(256, 4, false);
@@ -380,7 +499,7 @@ int check_gradient(const sdl_view_t* d, const sdl_view_t* x, sdl_dtype_t dtype, 
 LossArgs arguments(const sdl_view_t* logits, const sdl_view_t* d_logits, uint32_t batch, uint32_t tokens, uint32_t vocab, const void* targets, sdl_index_t index,
                    float smoothing, float z, const float* d_loss)
 {
-    return LossArgs{kernel_view(logits), d_logits ? kernel_view(d_logits) : View{}, targets, d_loss, nullptr, nullptr, make_div(tokens), batch * tokens, vocab,
+    return LossArgs{kernel_view(logits), d_logits ? kernel_view(d_logits) : View{}, targets, d_loss, nullptr, nullptr, make_div(tokens), batch * tokens, vocab, 16,
                     index == SDL_INDEX_INT64, smoothing, 1.0f - smoothing, smoothing / (float)vocab, z};
 }
 
