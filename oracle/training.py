@@ -61,19 +61,24 @@ def orthogonalize(x, coefficients, eps, scale):
     return scale * (u * s) @ vt
 
 
-def orthogonalize_rounded(x, coefficients, eps, scale, bits, held):
-    """The steps themselves with operands of `bits` bits and X and the products' results of `held` bits, everything else in 64: what these roundings cost is how
-    far this is from orthogonalize()."""
+def orthogonalize_rounded(x, coefficients, eps, scale, bits, held, apart):
+    """The steps themselves with operands of `bits` bits and X, the products' results and, where they are kept apart, the diagonals of the symmetric ones of `held` bits, everything
+    else in 64: what these roundings cost is how far this is from orthogonalize()."""
     def to(v, n):
         m, e = torch.frexp(v)
         return torch.ldexp((m * 2.0 ** n).round() * 2.0 ** -n, e)
+    def cut(v):
+        d = v.diagonal() if apart else torch.zeros_like(v[0])
+        return d, to(v - torch.diag(d), bits)
     x = x.double()
     tall = x.shape[0] > x.shape[1]
     x = x.T if tall else x
     x = to(x / (x.square().sum().sqrt() + eps), held)
     for a, b, c in coefficients:
         low = to(x, bits)
-        gram = to(to(low @ low.T, held), bits)
-        mix = to(to(b * gram + c * to(gram @ gram, held), held), bits)
-        x = to(a * x + to(mix @ low, held), held)
+        d, gram = cut(to(low @ low.T, held))
+        whole = gram + torch.diag(d)
+        square = to(gram @ gram, held) + (d[:, None] + d[None]) * gram + torch.diag(d * d)
+        d, mix = cut(to(b * whole + c * square, held))
+        x = to((a + d)[:, None] * x + to(mix @ low, held), held)
     return scale * (x.T if tall else x)

@@ -9,9 +9,10 @@
 // two keeps its elements in the middle of fp16's range: X 2^14, A 2^12, and b A + c A^2 by what its bound allows.
 //   - X itself is kept with more digits than its image has, and a X is taken from there.  What the images lose is then a factor near 1 on what a
 //     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.
-//   - results in bf16: one image, 11 bits.  An error of 2^-12 an element, 0.0003 to 0.0005 of the result after five steps, under the 0.0017 of its own rounding.  X is its image and what that
-//     leaves, rounded to bf16: 19 bits, and 8 of an element too small for the image (2^-38 of a norm, which takes an eps far above the norm).  The write of X is what an update
-//     waits for, and in fp32 it was half as much again.
+//   - results in bf16: one image, 11 bits.  Near its end A is nearly diagonal, and an image's error on the diagonal would go into a whole row of X: so the diagonals of A and of
+//     b A + c A^2 are kept apart in fp32, and are zero in the images.  Five steps are off by 0.0003 of the result, under the 0.0017 of its own rounding (0.0013 with the diagonals in
+//     the images of matrices of 64 rows).  X is its image and what that leaves, rounded to bf16: 19 bits, and 8 of an element too small for the image (2^-38 of a norm, which
+//     takes an eps far above the norm).  The write of X is what an update waits for, and in fp32 it was half as much again.
 //   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.  X in fp32, which has its digits
 //     wherever the norm is.
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
@@ -41,6 +42,7 @@ struct Work {
     char* base;
     size_t each;
     size_t rest, x16, x16_other, a16, b16;           // offsets; rest: X in fp32, or in bf16 what its one image leaves
+    size_t a_diagonal, b_diagonal;                    // of one image, in fp32, as large as the images
     uint32_t n, m;                                    // n <= m, filled up
     uint32_t split;
     __host__ __device__ uint32_t pitch(uint32_t k) const { return k * (split ? 4u : 2u); }     // bytes of a row of k elements of an image
@@ -400,13 +402,17 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
             Parts old[MODE == POLY || (MODE == UPDATE && !SPLIT) ? kPasses : 1];
             Eight<float> x[MODE == UPDATE && SPLIT ? kPasses : 1];
             Eight<__bf16> rest[MODE == UPDATE && !SPLIT ? kPasses : 1];
+            float own[MODE != GRAM && !SPLIT ? kPasses : 1];          // the rows' places of the diagonal
+            Eight<float> others;
             if constexpr (MODE == POLY) {
 #pragma unroll
                 for (int k = 0; k < kPasses; ++k) {
                     const f16x8_t* at = piece<SPLIT>(base + a.w.a16 + (size_t)(i + k * kRows + r0) * a.w.pitch(n), j + c0);
                     old[k].hi = at[0];
                     old[k].lo = SPLIT ? at[4] : f16x8_t{};
+                    if constexpr (!SPLIT) own[k] = reinterpret_cast<const float*>(base + a.w.a_diagonal)[i + k * kRows + r0];
                 }
+                if constexpr (!SPLIT) others = load8(reinterpret_cast<const float*>(base + a.w.a_diagonal) + j, c0, c0 + 8);
             }
             if constexpr (MODE == UPDATE) {
 #pragma unroll
@@ -416,6 +422,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                         x[k] = load8(reinterpret_cast<const float*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
                     } else {
                         old[k].hi = *piece<false>(base + a.q + (size_t)row * a.w.pitch(m), j + c0);
+                        own[k] = reinterpret_cast<const float*>(base + a.w.b_diagonal)[row];
                         rest[k] = load8(reinterpret_cast<const __bf16*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
                     }
                 }
@@ -440,9 +447,25 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                 for (int e = 0; e < 8; ++e) {
                     const float s = e < 4 ? lo[e & 3] : hi[e & 3];
                     if constexpr (MODE == GRAM) v[k][e] = s * a.on_sum;
-                    if constexpr (MODE == POLY) v[k][e] = fmaf(s, a.on_sum, a.on_old * (SPLIT ? (float)old[k].hi[e] + (float)old[k].lo[e] : (float)old[k].hi[e]));
+                    if constexpr (MODE == POLY && SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old * ((float)old[k].hi[e] + (float)old[k].lo[e]));
+                    if constexpr (MODE == POLY && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k] + others.get(e), a.on_old) * (float)old[k].hi[e]);
                     if constexpr (MODE == UPDATE && SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old * x[k].get(e));
-                    if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old / kScaleX * ((float)old[k].hi[e] + rest[k].get(e)));
+                    if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k], a.on_old / kScaleX) * ((float)old[k].hi[e] + rest[k].get(e)));
+                }
+            }
+            if constexpr (MODE != UPDATE && !SPLIT) {
+                if (i == j) {       // the diagonal goes apart, and is zero in the image
+#pragma unroll
+                    for (int k = 0; k < kPasses; ++k) {
+                        const uint32_t row = k * kRows + r0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (row != c0 + e) continue;
+                            if constexpr (MODE == GRAM) reinterpret_cast<float*>(base + a.w.a_diagonal)[i + row] = v[k][e];
+                            else reinterpret_cast<float*>(base + a.w.b_diagonal)[i + row] = fmaf(fmaf(a.on_sum, own[k], a.on_old), own[k], v[k][e]);
+                            v[k][e] = 0.0f;
+                        }
+                    }
                 }
             }
             if constexpr (MODE == UPDATE) {
@@ -509,6 +532,9 @@ struct SmallArgs {
     float a[kMostSmallSteps], b[kMostSmallSteps], c[kMostSmallSteps], image[kMostSmallSteps];     // image: the scale of b A + c A^2
 };
 
+// Tiles of a symmetric product of a wavefront's, at most: what two images leave room for has fewer.
+constexpr uint32_t halves_of(bool split) { return split ? 3 : 5; }
+
 // A matrix whose images fit the shared memory of a workgroup is worked on there from its norm to its last step: with a launch for every product it would be the launches, 80 us for
 // five steps of 100 x 131.  Tiles of 16 by 16 go round among the wavefronts; those of X stay in the registers of theirs, in fp32, and what a step makes of them is what the next one
 // starts from.
@@ -525,6 +551,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
     const uint32_t down = (a.n + 15) / 16, across = a.across.d, nk = (a.n + 31) / 32 * 32, mk = (a.m + 31) / 32 * 32;
     const uint32_t pitch_x = mk * 2 + 16, pitch_a = nk * 2 + 16, bytes_x = nk * pitch_x, bytes_a = nk * pitch_a;
     char *const image_x = lds, *const image_a = lds + kImages * bytes_x;
+    float *const a_diagonal = reinterpret_cast<float*>(image_a + bytes_a), *const b_diagonal = a_diagonal + nk;      // of one image
     // what no tile writes is zero
     for (uint32_t i = threadIdx.x * 16; i < kImages * (bytes_x + bytes_a); i += WAVES * kWave * 16) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
 
@@ -617,8 +644,16 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         }
         return d;
     };
-    // D of rows i and columns j, in its place and in the one across
-    const auto put_symmetric = [&](uint32_t i, uint32_t j, const f32x4_t& v) {
+    // D of rows i and columns j, in its place and in the one across; what one image leaves out, its diagonal, apart
+    const auto put_symmetric = [&](uint32_t i, uint32_t j, f32x4_t v, float* diagonal) {
+        if constexpr (!SPLIT)
+            if (i == j)
+#pragma unroll
+                for (uint32_t r = 0; r < 4; ++r) {
+                    if (4 * q + r != c) continue;
+                    diagonal[i + c] = v[r];
+                    v[r] = 0.0f;
+                }
         put4(image_a, bytes_a, pitch_a, j + c, i + 4 * q, v);
         if (i != j)
 #pragma unroll
@@ -632,7 +667,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         *j = (t - row * (row + 1) / 2) * 16;
     };
     const uint32_t halves = down * (down + 1) / 2;
-    constexpr int kHalves = 5;                  // of a wavefront
+    constexpr int kHalves = halves_of(SPLIT);
     for (uint32_t step = 0; step < a.steps; ++step) {
         // X's image, once everyone has read the one before
         __syncthreads();
@@ -645,7 +680,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         for (uint32_t t = wave; t < halves; t += WAVES) {
             uint32_t i, j;
             place(t, &i, &j);
-            put_symmetric(i, j, symmetric(image_x, bytes_x, pitch_x, i, j, mk) * (kScaleA / (kScaleX * kScaleX)));
+            put_symmetric(i, j, symmetric(image_x, bytes_x, pitch_x, i, j, mk) * (kScaleA / (kScaleX * kScaleX)), a_diagonal);
         }
         __syncthreads();
         f32x4_t mix[kHalves];
@@ -659,9 +694,17 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
             const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(image_a + (j + c) * pitch_a + (i + 4 * q) * 2);
             f16x4_t lo = {};
             if constexpr (SPLIT) lo = *reinterpret_cast<const f16x4_t*>(image_a + bytes_a + (j + c) * pitch_a + (i + 4 * q) * 2);
+            const float on_square = a.c[step] * a.image[step] / (kScaleA * kScaleA), on_a = a.b[step] * a.image[step] / kScaleA;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                mix[s][r] = fmaf(square[r], a.c[step] * a.image[step] / (kScaleA * kScaleA), a.b[step] * a.image[step] / kScaleA * ((float)hi[r] + (float)lo[r]));
+            for (uint32_t r = 0; r < 4; ++r) {
+                if constexpr (SPLIT) {
+                    mix[s][r] = fmaf(square[r], on_square, on_a * ((float)hi[r] + (float)lo[r]));
+                } else {
+                    const float own = a_diagonal[i + 4 * q + r];
+                    mix[s][r] = i == j && 4 * q + r == c ? fmaf(on_square, fmaf(own, own, square[r]), on_a * own)
+                                                         : fmaf(square[r], on_square, fmaf(on_square, own + a_diagonal[j + c], on_a) * (float)hi[r]);
+                }
+            }
         }
         __syncthreads();
 #pragma unroll
@@ -670,7 +713,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
             if (t >= halves) continue;
             uint32_t i, j;
             place(t, &i, &j);
-            put_symmetric(i, j, mix[s]);
+            put_symmetric(i, j, mix[s], b_diagonal);
         }
         __syncthreads();
         const float on_sum = 1.0f / (a.image[step] * kScaleX);
@@ -690,7 +733,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
                 }
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, a.a[step] * x[s][r]);
+            for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, (SPLIT ? a.a[step] : fmaf(b_diagonal[i + c], 1.0f / a.image[step], a.a[step])) * x[s][r]);
         }
     }
     O* out = reinterpret_cast<O*>(a.out.data) + (int64_t)matrix * a.out.batch;
@@ -749,6 +792,13 @@ Tiles tiles_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
 // Sums of squares of a matrix: enough workgroups for all compute units.
 uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(1024u, 2048u / batch)); }
 
+// Whether images are two: for results in fp32, and of matrices of few rows or few elements, where the errors of an image of one do not average out: of the results of rows alone 0.004, of
+// 4 x 4 0.005, of 17 x 17 0.0024, beside 0.0017 of bf16's own rounding, which is all that is left of 32 x 256.  8 x 24 x 192 takes 24 us instead of 21, 16 x 16 x 4000 162 instead of 101.
+bool is_split(uint32_t rows, uint32_t cols, sdl_dtype_t out)
+{
+    return out == SDL_DTYPE_FP32 || std::min(rows, cols) <= 16 || (uint64_t)rows * cols <= 2048;
+}
+
 struct Layout {
     Work w;
     Tiles tiles;
@@ -777,6 +827,8 @@ Layout layout_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
     w.rest = place((size_t)w.n * w.m * (split ? 4 : 2));
     w.a16 = place((size_t)w.n * w.pitch(w.n));
     w.b16 = place((size_t)w.n * w.pitch(w.n));
+    w.a_diagonal = place(w.n * sizeof(float));
+    w.b_diagonal = place(w.n * sizeof(float));
     w.each = at;
     l.parts = parts_of(batch);
     l.squares = (size_t)batch * w.each;
@@ -860,7 +912,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.steps = w.m / per;
         a.tiles = make_div(side * (side + 1) / 2);
         a.on_sum = kScaleA / (kScaleX * kScaleX);
-        if (product<SPLIT, GRAM, O>(a, l.tiles.symmetric, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<SPLIT, GRAM, float>(a, l.tiles.symmetric, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         a.slice_of = make_div(l.poly_slices);
         a.p = a.q = w.a16;
         a.t = w.b16;
@@ -868,7 +920,7 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
         a.steps = w.n / per;
         a.on_old = (float)(cb / kScaleA * scale_b);
         a.on_sum = (float)(cc / ((double)kScaleA * kScaleA) * scale_b);
-        if (product<SPLIT, POLY, O>(a, l.tiles.symmetric, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
+        if (product<SPLIT, POLY, float>(a, l.tiles.symmetric, batch, st) != SDL_OK) return SDL_ERR_DEVICE;
         a.p = w.b16;
         a.q = now;
         a.t = other;
@@ -892,13 +944,15 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
 // Wavefronts of a workgroup, tiles of X that each of them keeps, and shared memory of the kernels of small matrices: four workgroups of the first find room on a compute unit.
 struct Small {
     uint32_t waves, slots, bytes;
+    // (two images leave no room for more)
+    constexpr uint32_t slots_of(bool split) const { return split && slots > 10 ? 10 : slots; }
 };
 constexpr Small kSmall[] = {{4, 4, 39 * 1024}, {4, 12, 39 * 1024}, {16, 6, 159 * 1024}, {16, 12, 159 * 1024}};
 
 bool fits(const Small& k, uint32_t n, uint32_t m, bool split)
 {
     const uint64_t down = (n + 15) / 16, across = (m + 15) / 16, nk = (n + 31) / 32 * 32, mk = (m + 31) / 32 * 32;
-    return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) <= k.bytes && down * across <= k.waves * k.slots && down * (down + 1) / 2 <= k.waves * 5;
+    return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) + (split ? 0 : 2 * nk * 4) <= k.bytes && down * across <= k.waves * k.slots_of(split) && down * (down + 1) / 2 <= k.waves * halves_of(split);
 }
 
 bool is_small(uint32_t n, uint32_t m, uint32_t steps, bool split)
@@ -910,13 +964,20 @@ template <typename T, bool SPLIT, typename O>
 int small(const SmallArgs& a, uint32_t batch, hipStream_t st)
 {
 #define SDL_LAUNCH(N)                                                                                                                                  \
-    hipLaunchKernelGGL((sdl_orthogonalize_small_kernel<T, SPLIT, O, kSmall[N].waves, kSmall[N].slots, kSmall[N].bytes>), dim3(batch), dim3(kSmall[N].waves * kWave), 0, st, a)
+    hipLaunchKernelGGL((sdl_orthogonalize_small_kernel<T, SPLIT, O, kSmall[N].waves, kSmall[N].slots_of(SPLIT), kSmall[N].bytes>), dim3(batch), dim3(kSmall[N].waves * kWave), 0, st, a)
     if (fits(kSmall[0], a.n, a.m, SPLIT)) SDL_LAUNCH(0);
     else if (fits(kSmall[1], a.n, a.m, SPLIT)) SDL_LAUNCH(1);
     else if (fits(kSmall[2], a.n, a.m, SPLIT)) SDL_LAUNCH(2);
     else SDL_LAUNCH(3);
 #undef SDL_LAUNCH
     return launched();
+}
+
+template <typename T>
+int small_of(const SmallArgs& a, bool split, sdl_dtype_t out, uint32_t batch, hipStream_t st)
+{
+    if (out == SDL_DTYPE_FP32) return small<T, true, float>(a, batch, st);
+    return split ? small<T, true, __bf16>(a, batch, st) : small<T, false, __bf16>(a, batch, st);
 }
 
 template <typename T, bool SPLIT>
@@ -941,7 +1002,7 @@ extern "C" {
 size_t sdl_orthogonalize_workspace_bytes(uint32_t batch, uint32_t rows, uint32_t cols, sdl_dtype_t out_dtype)
 {
     if (batch == 0 || rows == 0 || cols == 0 || !known(out_dtype) || check_shape(batch, rows, cols) != SDL_OK) return 0;
-    return layout_of(batch, rows, cols, out_dtype == SDL_DTYPE_FP32).bytes;
+    return layout_of(batch, rows, cols, is_split(rows, cols, out_dtype)).bytes;
 }
 
 int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32_t cols, sdl_dtype_t dtype, const float* coefficients, uint32_t steps, float eps,
@@ -957,7 +1018,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     int rc = check_shape(batch, rows, cols);
     if (rc != SDL_OK || batch == 0 || rows == 0 || cols == 0) return rc;
     if ((rc = check_view(x, dtype)) != SDL_OK || (rc = check_output(out, out_dtype, batch, rows, 1)) != SDL_OK) return rc;
-    const bool split = out_dtype == SDL_DTYPE_FP32;
+    const bool split = is_split(rows, cols, out_dtype);
     const Layout l0 = layout_of(batch, rows, cols, split);
     if (!workspace || workspace_bytes < l0.bytes) return SDL_ERR_INVALID_ARG;
     if (!aligned_to(workspace, 16)) return SDL_ERR_ALIGNMENT;
@@ -973,8 +1034,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
             a.image[s] = image_scale(a.b[s], a.c[s], h);
             h = reach(a.a[s], a.b[s], a.c[s], h);
         }
-        if (dtype == SDL_DTYPE_BF16) return split ? small<__bf16, true, float>(a, batch, st) : small<__bf16, false, __bf16>(a, batch, st);
-        return split ? small<float, true, float>(a, batch, st) : small<float, false, __bf16>(a, batch, st);
+        return dtype == SDL_DTYPE_BF16 ? small_of<__bf16>(a, split, out_dtype, batch, st) : small_of<float>(a, split, out_dtype, batch, st);
     }
     Layout l = l0;
     l.w.base = static_cast<char*>(workspace);
@@ -991,7 +1051,8 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (dtype == SDL_DTYPE_BF16) rc = split ? first<__bf16, true>(a, batch, st) : first<__bf16, false>(a, batch, st);
     else rc = split ? first<float, true>(a, batch, st) : first<float, false>(a, batch, st);
     if (rc != SDL_OK) return rc;
-    return split ? steps_of<true, float>(l, batch, rows, cols, coefficients, steps, scale, out, st) : steps_of<false, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st);
+    if (out_dtype == SDL_DTYPE_FP32) return steps_of<true, float>(l, batch, rows, cols, coefficients, steps, scale, out, st);
+    return split ? steps_of<true, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st) : steps_of<false, __bf16>(l, batch, rows, cols, coefficients, steps, scale, out, st);
 }
 
 }  // extern "C"
