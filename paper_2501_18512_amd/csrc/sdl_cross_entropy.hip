@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
     const float log_s = logf(p.s) - (!far && base.near ? fmaf(p.m, kLog2e, -base.from) * kLn2 : 0.0f);
     const float lse = p.m == __builtin_inff() ? __builtin_nanf("") : p.m + log_s;
     if (threadIdx.x % TPR == 0) {
-        float loss = log_s + a.hit * (p.m - at_target);
+        float loss = log_s + (a.hit > 0.0f ? a.hit * (p.m - at_target) : 0.0f);       // (an infinite logit counts as the mean's, if it counts as nothing else)
         if (smooth) loss += a.smoothing * (p.m - p.sum / (float)n);
         if (a.z != 0.0f) loss += a.z * lse * lse;
         if (a.loss) a.loss[row] = p.m == __builtin_inff() ? lse : loss;

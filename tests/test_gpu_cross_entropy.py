@@ -180,6 +180,9 @@ def test_what_is_not_finite_stays_in_its_row(V):
         sdl.sdl_cross_entropy_backward(x.cuda(), t.cuda(), lse, got)
     assert torch.isnan(loss).tolist() == [False, True, False, True, True, False, False, False]
     assert loss[2] == 0 and loss[6] == 0 and lse[2] == 0 and lse[6] == 0 and loss[5] == math.inf and lse[4] == -math.inf
+    for smoothing in (0.1, 1.0):                             # a mean of logits with one that cannot come
+        sdl.sdl_cross_entropy(x.cuda(), t.cuda(), loss, lse, smoothing=smoothing)
+        assert loss[5] == math.inf and loss[2] == 0 and torch.isfinite(loss[[0, 7]]).all() and torch.isfinite(lse[5])
 
 
 @pytest.mark.parametrize("V", [3, 100, 1001, 3000, 3003, 32000, 32001, 50257, 100000, 150000, 150001])
