@@ -35,7 +35,7 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f;
 constexpr uint32_t kDies = 8;
-constexpr uint32_t kMostSmallSteps = 32;
+constexpr uint32_t kMostSmallSteps = 32, kMostParts = 1024;
 
 // One matrix in the workspace, of which the next lies `each` bytes further.  Both sides are filled up with zeros to whole tiles.
 struct Work {
@@ -143,38 +143,47 @@ template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(256) sdl_orthogonalize_first_kernel(const FirstArgs a)
 {
     __shared__ float tile[64][65];
-    __shared__ double inverse;
+    __shared__ double sums[4];
     const uint32_t matrix = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;      // of the n by m matrix
-    if (threadIdx.x < kWave) {
-        double s = 0.0;
-        for (uint32_t p = threadIdx.x; p < a.parts; p += kWave) s += a.squares[(size_t)matrix * a.parts + p];
-#pragma unroll
-        for (int k = 32; k; k /= 2) s += __shfl_xor(s, k);
-        const double norm = sqrt(s) + a.eps;
-        if (threadIdx.x == 0) inverse = norm == 0.0 ? 0.0 : 1.0 / norm;
-    }
-    __syncthreads();
     const T* x = reinterpret_cast<const T*>(a.x.data) + (int64_t)matrix * a.x.batch;
-    const uint32_t r0 = a.tall ? j0 : i0, c0 = a.tall ? i0 : j0;
-    for (uint32_t i = threadIdx.x; i < 512; i += 256) {
-        const uint32_t r = i / 8, c = i % 8 * 8;
-        Eight<T> e{};
-        if (r0 + r < a.rows && c0 + c < a.cols) e = load8(x + (int64_t)(r0 + r) * a.x.token, c0 + c, a.cols);
+    const uint32_t r0 = a.tall ? j0 : i0, c0 = a.tall ? i0 : j0, c = threadIdx.x % 8 * 8;
+    Eight<T> e[2];
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        const uint32_t row = r0 + threadIdx.x / 8 + 32 * k;
+        e[k] = Eight<T>{};
+        if (row < a.rows && c0 + c < a.cols) e[k] = load8(x + (int64_t)row * a.x.token, c0 + c, a.cols);
+    }
+    double s = 0.0;
+#pragma unroll
+    for (uint32_t k = 0; k < kMostParts / 256; ++k) {
+        const uint32_t p = k * 256 + threadIdx.x;
+        if (p < a.parts) s += a.squares[(size_t)matrix * a.parts + p];
+    }
+#pragma unroll
+    for (int k = 32; k; k /= 2) s += __shfl_xor(s, k);
+    if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = s;
+    __syncthreads();
+    const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + a.eps, inverse = norm == 0.0 ? 0.0 : 1.0 / norm;
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        const uint32_t row = threadIdx.x / 8 + 32 * k;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float v = (float)((double)e.get(j) * inverse);
-            if (a.tall) tile[c + j][r] = v;
-            else tile[r][c + j] = v;
+            const float v = (float)((double)e[k].get(j) * inverse);
+            if (a.tall) tile[c + j][row] = v;
+            else tile[row][c + j] = v;
         }
     }
     __syncthreads();
     char* base = a.w.base + matrix * a.w.each;
-    for (uint32_t i = threadIdx.x; i < 512; i += 256) {
-        const uint32_t r = i / 8, c = i % 8 * 8;
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        const uint32_t row = threadIdx.x / 8 + 32 * k;
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = tile[r][c + j];
-        put_x<SPLIT>(base, a.w, a.w.x16, i0 + r, j0 + c, v);
+        for (int j = 0; j < 8; ++j) v[j] = tile[row][c + j];
+        put_x<SPLIT>(base, a.w, a.w.x16, i0 + row, j0 + c, v);
     }
 }
 
@@ -790,7 +799,7 @@ Tiles tiles_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
 }
 
 // Sums of squares of a matrix: enough workgroups for all compute units.
-uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(1024u, 2048u / batch)); }
+uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(kMostParts, 2048u / batch)); }
 
 // Whether images are two: for results in fp32, and of matrices of few rows or few elements, where the errors of an image of one do not average out: of the results of rows alone 0.004, of
 // 4 x 4 0.005, of 17 x 17 0.0024, beside 0.0017 of bf16's own rounding, which is all that is left of 32 x 256.  8 x 24 x 192 takes 24 us instead of 21, 16 x 16 x 4000 162 instead of 101.
