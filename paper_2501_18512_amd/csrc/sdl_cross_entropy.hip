@@ -1,7 +1,8 @@
 // Cross entropy of logits with targets, and its gradient (gfx950).
 //
 // A row of logits is read once and stays in the registers of 64 to 1024 threads, its gradient is written once: both passes in one call move
-// what one pass has to, and that is what bounds them.  Every thread takes the maximum m of its elements and the sum s of exp(x - m) over them; two such pairs
+// what one pass has to, and that is what bounds them: 8192 rows of 32000 in bf16 177 us, 5.9 TB/s, the loss alone 6.2.  An element costs one fused multiply-add and one exponential
+// in each pass.  Every thread takes the maximum m of its elements and the sum s of exp(x - m) over them; two such pairs
 // are one with M = max(m1, m2), s = s1 exp(m1 - M) + s2 exp(m2 - M), so that a row costs one exchange between its threads.  With M and s of the row,
 //     lse = M + log s,   p = exp(x - M) / s
 // and the loss is formed from M - x[target] and log s, which loses nothing where the target is nearly certain and lse and x[target] are nearly equal.
@@ -445,7 +446,9 @@ int loss(LossArgs a, hipStream_t st)
     } while (0)
 #define SDL_FIT(LIMIT, BLOCK, TPR, K) \
     if (room <= (LIMIT)) SDL_LAUNCH(LIMIT, BLOCK, TPR, K, true)
-    // 64 bytes of a row and less in a thread's registers up to 16384 elements, 256 in the end
+    // Rows in as many threads as keep them in registers, and no more.  A wavefront: 65536 rows of 1000 in bf16 47 us, 256 threads 109; 32768 of 2000 45 and 60.  256 threads: 16384 of 4000
+    // 43, a wavefront 45, 512 threads 57; of 8000 84 and 85.  512 threads: 8192 of 16000 86, 256 91, 1024 88; of 32000 178, 184 and 169, but the loss alone, half the rows without a
+    // target, 42 and with 1024 threads 52; 6000 of 40000 166 and 163, 91 and 97.  1024 threads: 2048 of 131072 204, read a second time instead 272.
     constexpr uint32_t kLongest = sizeof(T) == 2 ? 512 : 1024;
     if (V <= 512) SDL_LAUNCH(512, 256, 64, 1, true, true);
     SDL_FIT(1024, 256, 64, 2);
