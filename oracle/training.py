@@ -61,9 +61,9 @@ def orthogonalize(x, coefficients, eps, scale):
     return scale * (u * s) @ vt
 
 
-def orthogonalize_rounded(x, coefficients, eps, scale, bits, held, apart):
-    """The steps themselves with operands of `bits` bits and X, the products' results and, where they are kept apart, the diagonals of the symmetric ones of `held` bits, everything
-    else in 64: what these roundings cost is how far this is from orthogonalize()."""
+def orthogonalize_rounded(x, coefficients, eps, scale, bits, held, apart, held_x):
+    """The steps themselves with operands of `bits` bits, X of `held_x`, the products' results and, where they are kept apart, the diagonals of the symmetric ones of `held` bits,
+    everything else in 64: what these roundings cost is how far this is from orthogonalize()."""
     def to(v, n):
         m, e = torch.frexp(v)
         return torch.ldexp((m * 2.0 ** n).round() * 2.0 ** -n, e)
@@ -73,12 +73,12 @@ def orthogonalize_rounded(x, coefficients, eps, scale, bits, held, apart):
     x = x.double()
     tall = x.shape[0] > x.shape[1]
     x = x.T if tall else x
-    x = to(x / (x.square().sum().sqrt() + eps), held)
+    x = to(x / (x.square().sum().sqrt() + eps), held_x)
     for a, b, c in coefficients:
         low = to(x, bits)
         d, gram = cut(to(low @ low.T, held))
         whole = gram + torch.diag(d)
         square = to(gram @ gram, held) + (d[:, None] + d[None]) * gram + torch.diag(d * d)
         d, mix = cut(to(b * whole + c * square, held))
-        x = to((a + d)[:, None] * x + to(mix @ low, held), held)
+        x = to((a + d)[:, None] * x + to(mix @ low, held), held_x)
     return scale * (x.T if tall else x)

@@ -1027,6 +1027,9 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     int rc = check_shape(batch, rows, cols);
     if (rc != SDL_OK || batch == 0 || rows == 0 || cols == 0) return rc;
     if ((rc = check_view(x, dtype)) != SDL_OK || (rc = check_output(out, out_dtype, batch, rows, 1)) != SDL_OK) return rc;
+    // in x's place only as x lies there: a small matrix may be written before another one is read
+    if (out->data == x->data && (out_dtype != dtype || (batch > 1 && out->stride_batch != x->stride_batch) || (rows > 1 && out->stride_token != x->stride_token)))
+        return SDL_ERR_INVALID_ARG;
     const bool split = is_split(rows, cols, out_dtype);
     const Layout l0 = layout_of(batch, rows, cols, split);
     if (!workspace || workspace_bytes < l0.bytes) return SDL_ERR_INVALID_ARG;

@@ -1,7 +1,7 @@
 """GPU parity of sdl_orthogonalize with singular values and vectors in 64 bits.
 
 Bounds are on the root of the sum of squares.  What the documented roundings cost (operands of 11 bits but for the diagonals of symmetric ones, or 22 for results in fp32 and of
-small matrices; X and sums held in 24) is found by doing them in 64 bits; the kernels' are others of the same kind, so twice that, and the rounding of the results.  A sum of K terms
+small matrices; sums held in 24, X in 19 or 24) is found by doing them in 64 bits; the kernels' are others of the same kind, so twice that, and the rounding of the results.  A sum of K terms
 in fp32 has K roundings instead of the one that is done there, which add up as their root: so many times as much for results in fp32, where they count."""
 import math
 
@@ -36,7 +36,7 @@ def check(x, out_dtype, coefficients=QUINTIC, eps=1e-7, scale=1.0, how="dense"):
     for b in range(x.shape[0]):
         want = ref.orthogonalize(x[b], coefficients, eps, scale)
         split = out_dtype == FP32 or min(x.shape[1:]) <= 16 or x[b].numel() <= 2048
-        rounded = ref.orthogonalize_rounded(x[b], coefficients, eps, scale, 22 if split else 11, 24, not split)
+        rounded = ref.orthogonalize_rounded(x[b], coefficients, eps, scale, 22 if split else 11, 24, not split, 24 if split else 19)
         cost = float((rounded - want).norm())
         times = 2.0 if out_dtype == BF16 else 2.0 + math.sqrt(max(x.shape[1:]))
         bound = times * cost + (U[out_dtype] + 16 * U32) * float(want.norm())
@@ -96,6 +96,7 @@ def test_low_rank_and_orthogonal():
     a = randn((1, 60, 2), FP32, 1) @ randn((1, 2, 90), FP32, 2)
     check(a, FP32)
     check(a, BF16)
+    check(randn((1, 300, 2), FP32, 1) @ randn((1, 2, 520), FP32, 2), BF16)
     q = torch.linalg.qr(randn((64, 64), torch.float64, 3))[0].float().contiguous()[None]
     check(q, FP32)
     got, space = torch.empty(1, 64, 64, device="cuda"), sdl.alloc_orthogonalize(q.cuda(), q.cuda())
@@ -104,14 +105,15 @@ def test_low_rank_and_orthogonal():
     assert float((got.cpu() - q).norm()) < 24 * 64 * U32 * 8
 
 
-def test_zeros_and_what_is_not_finite():
-    x = momentum((5, 40, 50), FP32, 5)
+@pytest.mark.parametrize("shape", [(5, 40, 50), (5, 300, 520), (5, 700, 260)])
+def test_zeros_and_what_is_not_finite(shape):
+    x = momentum(shape, FP32, 5)
     x[1] = 0.0
     x[2, 3, 4], x[3, 39, 49] = math.nan, math.inf
     clean = x.clone()
     clean[2:4] = 0.0
     for out in (BF16, FP32):
-        got, want = (torch.empty((5, 40, 50), dtype=out, device="cuda") for _ in range(2))
+        got, want = (torch.empty(shape, dtype=out, device="cuda") for _ in range(2))
         for eps in (1e-7, 0.0):
             sdl.sdl_orthogonalize(x.cuda(), got, sdl.alloc_orthogonalize(x.cuda(), got), eps=eps)
             sdl.sdl_orthogonalize(clean.cuda(), want, sdl.alloc_orthogonalize(x.cuda(), got), eps=eps)

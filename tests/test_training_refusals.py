@@ -85,6 +85,7 @@ def test_cross_entropy_backward(status, change):
     (INVALID, dict(eps=INF)), (INVALID, dict(scale=NAN)), (INVALID, dict(scale=-INF)), (INVALID, dict(workspace=None)), (INVALID, dict(workspace_bytes=1000)),
     (UNSUPPORTED, dict(rows=65537)), (UNSUPPORTED, dict(cols=1 << 31)), (UNSUPPORTED, dict(batch=65536)), (UNSUPPORTED, dict(batch=65535, rows=8192, cols=8192)),
     (ALIGNMENT, dict(x=view(0x10001))), (ALIGNMENT, dict(out=view(0x40001))), (ALIGNMENT, dict(workspace=0x80008)), (ALIGNMENT, dict(dtype=0, x=view(0x10002))),
+    (INVALID, dict(out=view(token=1 << 9))), (INVALID, dict(out=view(batch=1 << 19))), (INVALID, dict(out=view(), out_dtype=0)),
     (OK, dict(batch=0)), (OK, dict(rows=0, x=None, out=None)), (OK, dict(cols=0))])
 def test_orthogonalize(status, change):
     assert call("sdl_orthogonalize", **change) == status
