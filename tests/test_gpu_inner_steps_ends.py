@@ -42,7 +42,7 @@ def test_loss_and_gradients_with_the_z_term_against_torch():
     want = torch.autograd.grad(want_loss, mine)[0].float()
     # the same blocks in the same arithmetic: what differs is the order of sums in fp32, and roundings of d_logits and of the table's gradient that fall the other way, 2^-9 on average
     # each; a few of them on the way back
-    assert abs(float(loss) - float(want_loss)) < 1e-4 * float(want_loss)
+    assert abs(float(loss.detach()) - float(want_loss.detach())) < 1e-4 * float(want_loss.detach())
     for name, got in shape.views(grad).items():
         w = shape.views(want)[name]
         assert float((got - w).norm()) < 8 * 2.0 ** -9 * float(w.norm()), name
