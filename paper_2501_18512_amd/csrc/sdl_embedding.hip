@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(256) sdl_embedding_kernel(const LookupArgs a)
 
 // ------------------------------------------------------------------------------------------------------ backward
 
-constexpr uint32_t kChunk = 1024;           // places that a workgroup sorts, one a thread
+constexpr uint32_t kChunk = 1024;           // places that a workgroup sorts, one a thread (10 bits)
 constexpr uint32_t kFan = 32;               // sorted runs that become one
 constexpr uint32_t kFill = 1024 * 8;        // elements of a table without gaps that a workgroup clears at a time
 
@@ -168,17 +168,19 @@ __device__ __forceinline__ uint32_t of_lane(uint32_t x)
 constexpr uint32_t log2_of(uint32_t x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
 
 // One exchange of a bitonic sort: places J apart, in runs of S that go up and down in turn.
-template <uint32_t S, uint32_t J>
-__device__ __forceinline__ void exchange(uint64_t& key, uint64_t (*lds)[kChunk])
+template <uint32_t S, uint32_t J, typename K>
+__device__ __forceinline__ void exchange(K& key, K (*lds)[kChunk])
 {
-    uint64_t other;
+    K other;
     if constexpr (J >= (uint32_t)kWave) {
         // two arrays in turn, so that one barrier is enough: the exchanges of S = 128, 256, .. through shared memory are 1, 2, .., counted from the first
         constexpr uint32_t kStage = log2_of(S) - 7, kNumber = kStage * (kStage + 1) / 2 + log2_of(S / 2) - log2_of(J);
-        uint64_t* at = lds[kNumber % 2];
+        K* at = lds[kNumber % 2];
         at[threadIdx.x] = key;
         __syncthreads();
         other = at[threadIdx.x ^ J];
+    } else if constexpr (sizeof(K) == 4) {
+        other = of_lane<(int)J>(key);
     } else {
         other = (uint64_t)of_lane<(int)J>((uint32_t)(key >> 32)) << 32 | of_lane<(int)J>((uint32_t)key);
     }
@@ -188,26 +190,39 @@ __device__ __forceinline__ void exchange(uint64_t& key, uint64_t (*lds)[kChunk])
 }
 
 // Bitonic sort of one chunk (K. E. Batcher, Sorting networks and their applications, 1968): keys differ, so that equal tokens keep their order.
-template <uint32_t S>
-__device__ __forceinline__ void sort_runs(uint64_t& key, uint32_t n, uint64_t (*lds)[kChunk])
+template <uint32_t S, typename K>
+__device__ __forceinline__ void sort_runs(K& key, uint32_t n, K (*lds)[kChunk])
 {
     exchange<S, S / 2>(key, lds);
     if constexpr (S < kChunk)
         if (S < n) sort_runs<2 * S>(key, n, lds);
 }
 
-template <typename P>
+// K: what a key is while it is sorted, 32 bits where the token fits beside the place in the chunk (4551 places 26 us instead of 27, in all).
+constexpr uint32_t kMostShort = (1u << 22) - 1;        // rows of a table whose tokens do, and the token of no row then
+template <typename P, typename K>
 __global__ void __launch_bounds__(1024) sdl_embedding_sort_kernel(const SortArgs a)
 {
-    __shared__ uint64_t lds[2][kChunk];
+    __shared__ K lds[2][kChunk];
     if (blockIdx.x >= a.chunks) {
         fill<P>(a.fill, blockIdx.x - a.chunks, gridDim.x - a.chunks);
         return;
     }
     const uint32_t i = blockIdx.x * kChunk + threadIdx.x, n = min(kChunk, a.n - blockIdx.x * kChunk);
-    uint64_t key = threadIdx.x < n ? ((uint64_t)a.tokens.get(i) << 32) | i : ~0ull;
+    K key = (K)~(K)0;
+    if (threadIdx.x < n) {
+        const uint32_t v = a.tokens.get(i);
+        if constexpr (sizeof(K) == 4) key = min(v, kMostShort) << 10 | threadIdx.x;
+        else key = (uint64_t)v << 32 | i;
+    }
     sort_runs<2>(key, n, lds);
-    if (threadIdx.x < n) a.keys[i] = key;
+    if (threadIdx.x >= n) return;
+    if constexpr (sizeof(K) == 4) {
+        const uint32_t v = key >> 10;
+        a.keys[i] = (uint64_t)(v == kMostShort ? kNone : v) << 32 | (blockIdx.x * kChunk + key % kChunk);
+    } else {
+        a.keys[i] = key;
+    }
 }
 
 struct MergeArgs {
@@ -541,7 +556,9 @@ int gradient(const Places& places, const Tokens& tokens, const Table& table, flo
     const auto fillers = [](uint64_t share) { return (uint32_t)(share < kFillGroups ? share : kFillGroups); };
     if (chunks || half) {
         const SortArgs a{tokens, n, chunks, keys, Fill{table, 0, half, dense}};
-        hipLaunchKernelGGL((sdl_embedding_sort_kernel<P>), dim3(chunks + fillers(half)), dim3(1024), 0, st, a);
+        const dim3 groups(chunks + fillers(half));
+        if (table.vocab <= kMostShort) hipLaunchKernelGGL((sdl_embedding_sort_kernel<P, uint32_t>), groups, dim3(1024), 0, st, a);
+        else hipLaunchKernelGGL((sdl_embedding_sort_kernel<P, uint64_t>), groups, dim3(1024), 0, st, a);
         if (launched() != SDL_OK) return SDL_ERR_DEVICE;
     }
     if (n == 0) return SDL_OK;

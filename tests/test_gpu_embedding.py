@@ -78,6 +78,22 @@ def test_rows_where_they_lie(dtype):
         check(shape, dtype, dtype, "padded", place="odd", seed=200 + 10 * i)
 
 
+@pytest.mark.parametrize("vocab", [(1 << 22) - 2, (1 << 22) - 1, 1 << 22, 5000011])
+def test_tables_longer_than_short_keys_name(vocab):
+    """Tokens from both ends of the table; all of its rows are looked at."""
+    for n, how in ((1500, "padded"), (40, "one")):
+        print(f"embedding {n} places of {vocab}", flush=True)
+        t = tokens_of((n,), vocab, how, n).to(torch.int64)
+        t[::7], t[1::7] = vocab - 1, 0
+        t = t.cuda()
+        d = (torch.arange(n * 3, device="cuda") % 11).float().view(n, 3)
+        got = torch.full((vocab, 3), float("nan"), device="cuda")
+        sdl.sdl_embedding_backward(d, t, got, sdl.alloc_embedding(t, 3))
+        there = (t >= 0) & (t < vocab)
+        want = torch.zeros((vocab, 3), device="cuda").index_add_(0, t[there], d[there])          # whole numbers: exact in any order
+        assert torch.equal(got, want)
+
+
 def test_more_places_than_are_merged_at_once():
     """The sum of a column of ones counts the places of a token, exactly."""
     for n in (65536, 65537, 150000):
