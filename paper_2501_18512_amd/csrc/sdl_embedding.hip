@@ -397,12 +397,13 @@ __global__ void __launch_bounds__(256) sdl_embedding_reduce_kernel(const ReduceA
         write_row<TINY, P>(a.table, cur, at, a.scale, acc);
 }
 
-// The lines of the runs that leave their first segments: a wavefront a segment, which adds up a few lines in order; of many, all sixteen of the workgroup a share each, and
-// then the shares.  (A workgroup a segment and part of the columns: 17 us for 4000 that have nothing to do.)
-constexpr uint32_t kJoined = 16, kFew = 16;
+// The lines of the runs that leave their first segments: a wavefront a segment, which adds up a few lines in order; of many, all eight of the workgroup a share each, and
+// then the shares.  (A workgroup a segment and part of the columns: 17 us for 4000 that have nothing to do.)  With sixteen wavefronts a workgroup 4551 places, a third of
+// them of one token, take 26.0 us in all, with eight 24.8, with four 25.1; 16384 of one token 44.0, 44.7 and 52.0.
+constexpr uint32_t kJoined = 8, kFew = 8;
 
 template <typename P, bool TINY>
-__global__ void __launch_bounds__(1024) sdl_embedding_join_kernel(const ReduceArgs a)
+__global__ void __launch_bounds__(kJoined * kWave) sdl_embedding_join_kernel(const ReduceArgs a)
 {
     __shared__ f32x4_t sums[kJoined][kWave];
     __shared__ uint32_t many[kJoined], tokens[kJoined];          // lines, where they are many
@@ -593,9 +594,9 @@ int gradient(const Places& places, const Tokens& tokens, const Table& table, flo
         r.slices = make_div((W + kSlice - 1) / kSlice);
         const dim3 groups(r.slices.d * ((s.segments + kJoined - 1) / kJoined));
         if (W < 8)
-            hipLaunchKernelGGL((sdl_embedding_join_kernel<P, true>), groups, dim3(1024), 0, st, r);
+            hipLaunchKernelGGL((sdl_embedding_join_kernel<P, true>), groups, dim3(kJoined * kWave), 0, st, r);
         else
-            hipLaunchKernelGGL((sdl_embedding_join_kernel<P, false>), groups, dim3(1024), 0, st, r);
+            hipLaunchKernelGGL((sdl_embedding_join_kernel<P, false>), groups, dim3(kJoined * kWave), 0, st, r);
     }
     return launched();
 }
