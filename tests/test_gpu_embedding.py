@@ -10,7 +10,7 @@ from operator_util import BF16, FP32, U, U32, close, output, placed, randn
 from oracle import training as ref
 
 pytestmark = pytest.mark.gpu
-# batch, tokens, vocab, width: one place and many, widths on both sides of what a wavefront takes, chunks of 2048 places and one more, more chunks than are merged at once
+# batch, tokens, vocab, width: one place and many, widths on both sides of what a wavefront takes, two chunks of places and one more, more chunks than are merged at once
 SHAPES = [(1, 1, 5, 3), (2, 3, 7, 8), (1, 17, 100, 64), (3, 5, 33, 65), (2, 40, 300, 257), (1, 2048, 50, 33), (1, 2049, 1000, 16), (2, 1500, 777, 100), (3, 700, 64, 520),
           (1, 5000, 3, 1021), (8, 1, 50, 768), (1, 300, 1, 40), (5, 13, 2000, 2048)]
 

@@ -75,3 +75,46 @@ def test_replicas_run_with_orthogonal_updates():
     losses, shape, flat, _ = ex.train(steps=40, say=lambda *_: None, update="orthogonal")
     assert all(x == x and x < 100 for row in losses for x in row)
     assert bool(torch.isfinite(flat.float()).all()) and len(losses) == 40
+
+
+def test_two_captured_graphs_share_a_workspace():
+    """Lookup, loss, both gradients and an update in two graphs of other sizes over one workspace, replayed in turn."""
+    import paper_2501_18512_amd as sdl
+    gen = torch.Generator("cuda").manual_seed(5)
+
+    def part(places, vocab, width, rows):
+        t = dict(tokens=torch.randint(-1, vocab, (places,), device="cuda", generator=gen), table=torch.randn(vocab, width, device="cuda", generator=gen).bfloat16(),
+                 m=torch.randn(2, rows, width, device="cuda", generator=gen))
+        t.update(x=torch.empty(places, width, dtype=torch.bfloat16, device="cuda"), logits=torch.randn(places, vocab, device="cuda", generator=gen).bfloat16(),
+                 loss=torch.empty(places, device="cuda"), d_table=torch.empty_like(t["table"]), step=torch.empty_like(t["m"]))
+        t["d"] = torch.empty_like(t["logits"])
+        return t
+
+    def run(t, space):
+        sdl.sdl_embedding(t["table"], t["tokens"], t["x"])
+        sdl.sdl_cross_entropy(t["logits"], t["tokens"], t["loss"], None, t["d"], z=1e-4)
+        sdl.sdl_embedding_backward(t["x"], t["tokens"], t["d_table"], space)
+        sdl.sdl_orthogonalize(t["m"], t["step"], space)
+
+    parts = [part(2500, 300, 260, 200), part(70, 5000, 512, 700)]
+    space = torch.empty(max(max(sdl.alloc_embedding(t["tokens"], t["x"].shape[1]).numel(), sdl.alloc_orthogonalize(t["m"], t["step"]).numel()) for t in parts),
+                        dtype=torch.uint8, device="cuda")
+    graphs = []
+    for t in parts:
+        run(t, space)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(t, space)
+    for replay in range(3):
+        for t, graph in zip(parts, graphs):
+            t["tokens"].copy_(torch.randint(-1, t["table"].shape[0], t["tokens"].shape, device="cuda", generator=gen))
+            t["m"].normal_(generator=gen)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for t in parts:
+            want = {k: torch.empty_like(v) if k in ("x", "loss", "d", "d_table", "step") else v for k, v in t.items()}
+            run(want, torch.empty_like(space))
+            for name in ("x", "loss", "d", "d_table", "step"):
+                assert torch.equal(t[name], want[name]), (replay, name)
