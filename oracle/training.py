@@ -61,14 +61,14 @@ def orthogonalize(x, coefficients, eps, scale):
     return scale * (u * s) @ vt
 
 
-def orthogonalize_rounded(x, coefficients, eps, scale, bits, held, apart, held_x):
-    """The steps themselves with operands of `bits` bits, X of `held_x`, the products' results and, where they are kept apart, the diagonals of the symmetric ones of `held` bits,
+def orthogonalize_rounded(x, coefficients, eps, scale, bits, held, held_x):
+    """The steps themselves with operands of `bits` bits, X of `held_x`, the products' results and the diagonals of the symmetric ones, which are kept apart, of `held` bits,
     everything else in 64: what these roundings cost is how far this is from orthogonalize()."""
     def to(v, n):
         m, e = torch.frexp(v)
         return torch.ldexp((m * 2.0 ** n).round() * 2.0 ** -n, e)
     def cut(v):
-        d = v.diagonal() if apart else torch.zeros_like(v[0])
+        d = v.diagonal()
         return d, to(v - torch.diag(d), bits)
     x = x.double()
     tall = x.shape[0] > x.shape[1]

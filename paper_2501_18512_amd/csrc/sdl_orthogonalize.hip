@@ -9,12 +9,13 @@
 // two keeps its elements in the middle of fp16's range: X 2^14, A 2^12, and b A + c A^2 by what its bound allows.
 //   - X itself is kept with more digits than its image has, and a X is taken from there.  What the images lose is then a factor near 1 on what a
 //     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.
-//   - results in bf16: one image, 11 bits.  Near its end A is nearly diagonal, and an image's error on the diagonal would go into a whole row of X: so the diagonals of A and of
-//     b A + c A^2 are kept apart in fp32, and are zero in the images.  Five steps are off by 0.0003 of the result, under the 0.0017 of its own rounding (0.0013 with the diagonals in
-//     the images of matrices of 64 rows).  X is its image and what that leaves, rounded to bf16: 19 bits, and 8 of an element too small for the image (2^-38 of a norm, which
-//     takes an eps far above the norm).  The write of X is what an update waits for, and in fp32 it was half as much again.
+//   - Near its end A is nearly diagonal, and an image's error on the diagonal would go into a whole row of X: so the diagonals of A and of b A + c A^2 are kept apart in fp32, and are
+//     zero in the images.
+//   - results in bf16: one image, 11 bits.  Five steps are off by 0.0003 of the result, under the 0.0017 of its own rounding (0.0013 with the diagonals in the images of matrices of
+//     64 rows).  X is its image and what that leaves, rounded to bf16: 19 bits, and 8 of an element too small for the image (2^-38 of a norm, which takes an eps far above the
+//     norm).  The write of X is what an update waits for, and in fp32 it was half as much again.
 //   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.  X in fp32, which has its digits
-//     wherever the norm is.
+//     wherever the norm is.  16 x 128 are off by 1.1e-6 (1.7e-6 with the diagonals in the images), 400 x 801 by 1.1e-6.
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
 #include <algorithm>
 #include <cmath>
@@ -42,7 +43,7 @@ struct Work {
     char* base;
     size_t each;
     size_t rest, x16, x16_other, a16, b16;           // offsets; rest: X in fp32, or in bf16 what its one image leaves
-    size_t a_diagonal, b_diagonal;                    // of one image, in fp32, as large as the images
+    size_t a_diagonal, b_diagonal;                    // in fp32, as large as the images
     uint32_t n, m;                                    // n <= m, filled up
     uint32_t split;
     __host__ __device__ uint32_t pitch(uint32_t k) const { return k * (split ? 4u : 2u); }     // bytes of a row of k elements of an image
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
             Parts old[MODE == POLY || (MODE == UPDATE && !SPLIT) ? kPasses : 1];
             Eight<float> x[MODE == UPDATE && SPLIT ? kPasses : 1];
             Eight<__bf16> rest[MODE == UPDATE && !SPLIT ? kPasses : 1];
-            float own[MODE != GRAM && !SPLIT ? kPasses : 1];          // the rows' places of the diagonal
+            float own[MODE != GRAM ? kPasses : 1];                     // the rows' places of the diagonal
             Eight<float> others;
             if constexpr (MODE == POLY) {
 #pragma unroll
@@ -419,19 +420,19 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                     const f16x8_t* at = piece<SPLIT>(base + a.w.a16 + (size_t)(i + k * kRows + r0) * a.w.pitch(n), j + c0);
                     old[k].hi = at[0];
                     old[k].lo = SPLIT ? at[4] : f16x8_t{};
-                    if constexpr (!SPLIT) own[k] = reinterpret_cast<const float*>(base + a.w.a_diagonal)[i + k * kRows + r0];
+                    own[k] = reinterpret_cast<const float*>(base + a.w.a_diagonal)[i + k * kRows + r0];
                 }
-                if constexpr (!SPLIT) others = load8(reinterpret_cast<const float*>(base + a.w.a_diagonal) + j, c0, c0 + 8);
+                others = load8(reinterpret_cast<const float*>(base + a.w.a_diagonal) + j, c0, c0 + 8);
             }
             if constexpr (MODE == UPDATE) {
 #pragma unroll
                 for (int k = 0; k < kPasses; ++k) {
                     const uint32_t row = i + k * kRows + r0;
+                    own[k] = reinterpret_cast<const float*>(base + a.w.b_diagonal)[row];
                     if constexpr (SPLIT) {
                         x[k] = load8(reinterpret_cast<const float*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
                     } else {
                         old[k].hi = *piece<false>(base + a.q + (size_t)row * a.w.pitch(m), j + c0);
-                        own[k] = reinterpret_cast<const float*>(base + a.w.b_diagonal)[row];
                         rest[k] = load8(reinterpret_cast<const __bf16*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
                     }
                 }
@@ -456,13 +457,13 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                 for (int e = 0; e < 8; ++e) {
                     const float s = e < 4 ? lo[e & 3] : hi[e & 3];
                     if constexpr (MODE == GRAM) v[k][e] = s * a.on_sum;
-                    if constexpr (MODE == POLY && SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old * ((float)old[k].hi[e] + (float)old[k].lo[e]));
-                    if constexpr (MODE == POLY && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k] + others.get(e), a.on_old) * (float)old[k].hi[e]);
-                    if constexpr (MODE == UPDATE && SPLIT) v[k][e] = fmaf(s, a.on_sum, a.on_old * x[k].get(e));
+                    if constexpr (MODE == POLY)
+                        v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k] + others.get(e), a.on_old) * (SPLIT ? (float)old[k].hi[e] + (float)old[k].lo[e] : (float)old[k].hi[e]));
+                    if constexpr (MODE == UPDATE && SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum * kScaleX, own[k], a.on_old) * x[k].get(e));
                     if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k], a.on_old / kScaleX) * ((float)old[k].hi[e] + rest[k].get(e)));
                 }
             }
-            if constexpr (MODE != UPDATE && !SPLIT) {
+            if constexpr (MODE != UPDATE) {
                 if (i == j) {       // the diagonal goes apart, and is zero in the image
 #pragma unroll
                     for (int k = 0; k < kPasses; ++k) {
@@ -560,7 +561,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
     const uint32_t down = (a.n + 15) / 16, across = a.across.d, nk = (a.n + 31) / 32 * 32, mk = (a.m + 31) / 32 * 32;
     const uint32_t pitch_x = mk * 2 + 16, pitch_a = nk * 2 + 16, bytes_x = nk * pitch_x, bytes_a = nk * pitch_a;
     char *const image_x = lds, *const image_a = lds + kImages * bytes_x;
-    float *const a_diagonal = reinterpret_cast<float*>(image_a + bytes_a), *const b_diagonal = a_diagonal + nk;      // of one image
+    float *const a_diagonal = reinterpret_cast<float*>(image_a + kImages * bytes_a), *const b_diagonal = a_diagonal + nk;
     // what no tile writes is zero
     for (uint32_t i = threadIdx.x * 16; i < kImages * (bytes_x + bytes_a); i += WAVES * kWave * 16) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
 
@@ -653,16 +654,15 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         }
         return d;
     };
-    // D of rows i and columns j, in its place and in the one across; what one image leaves out, its diagonal, apart
+    // D of rows i and columns j, in its place and in the one across; its diagonal apart
     const auto put_symmetric = [&](uint32_t i, uint32_t j, f32x4_t v, float* diagonal) {
-        if constexpr (!SPLIT)
-            if (i == j)
+        if (i == j)
 #pragma unroll
-                for (uint32_t r = 0; r < 4; ++r) {
-                    if (4 * q + r != c) continue;
-                    diagonal[i + c] = v[r];
-                    v[r] = 0.0f;
-                }
+            for (uint32_t r = 0; r < 4; ++r) {
+                if (4 * q + r != c) continue;
+                diagonal[i + c] = v[r];
+                v[r] = 0.0f;
+            }
         put4(image_a, bytes_a, pitch_a, j + c, i + 4 * q, v);
         if (i != j)
 #pragma unroll
@@ -706,13 +706,9 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
             const float on_square = a.c[step] * a.image[step] / (kScaleA * kScaleA), on_a = a.b[step] * a.image[step] / kScaleA;
 #pragma unroll
             for (uint32_t r = 0; r < 4; ++r) {
-                if constexpr (SPLIT) {
-                    mix[s][r] = fmaf(square[r], on_square, on_a * ((float)hi[r] + (float)lo[r]));
-                } else {
-                    const float own = a_diagonal[i + 4 * q + r];
-                    mix[s][r] = i == j && 4 * q + r == c ? fmaf(on_square, fmaf(own, own, square[r]), on_a * own)
-                                                         : fmaf(square[r], on_square, fmaf(on_square, own + a_diagonal[j + c], on_a) * (float)hi[r]);
-                }
+                const float own = a_diagonal[i + 4 * q + r];
+                mix[s][r] = i == j && 4 * q + r == c ? fmaf(on_square, fmaf(own, own, square[r]), on_a * own)
+                                                     : fmaf(square[r], on_square, fmaf(on_square, own + a_diagonal[j + c], on_a) * ((float)hi[r] + (float)lo[r]));
             }
         }
         __syncthreads();
@@ -742,7 +738,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
                 }
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, (SPLIT ? a.a[step] : fmaf(b_diagonal[i + c], 1.0f / a.image[step], a.a[step])) * x[s][r]);
+            for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, fmaf(b_diagonal[i + c], 1.0f / a.image[step], a.a[step]) * x[s][r]);
         }
     }
     O* out = reinterpret_cast<O*>(a.out.data) + (int64_t)matrix * a.out.batch;
@@ -963,7 +959,7 @@ constexpr Small kSmall[] = {{4, 1, 15 * 1024}, {8, 2, 39 * 1024}, {8, 6, 39 * 10
 bool fits(const Small& k, uint32_t n, uint32_t m, bool split)
 {
     const uint64_t down = (n + 15) / 16, across = (m + 15) / 16, nk = (n + 31) / 32 * 32, mk = (m + 31) / 32 * 32;
-    return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) + (split ? 0 : 2 * nk * 4) <= k.bytes && down * across <= k.waves * k.slots_of(split) && down * (down + 1) / 2 <= k.waves * halves_of(split);
+    return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) + 2 * nk * 4 <= k.bytes && down * across <= k.waves * k.slots_of(split) && down * (down + 1) / 2 <= k.waves * halves_of(split);
 }
 
 bool is_small(uint32_t n, uint32_t m, uint32_t steps, bool split)
