@@ -853,15 +853,13 @@ double reach(double a, double b, double c, double h)
     const auto look = [&](double u) {
         if (u > 0.0 && u < h * h && p(u) > most) most = p(u);
     };
-    // zeros of the derivative a + 3 b u + 5 c u^2
-    if (c == 0.0) {
-        if (b != 0.0) look(-a / (3.0 * b));
-    } else {
-        const double d = 9.0 * b * b - 20.0 * a * c;
-        if (d >= 0.0) {
-            look((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-            look((-3.0 * b - std::sqrt(d)) / (10.0 * c));
-        }
+    // zeros of the derivative a + 3 b u + 5 c u^2: one from terms of the same sign, the other from the two's product, so that none is lost where c is next to nothing.
+    // One that is infinite or no number is none.
+    const double d = 9.0 * b * b - 20.0 * a * c;
+    if (d >= 0.0) {
+        const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(d), b));
+        look(q / (5.0 * c));
+        look(a / q);
     }
     return most;
 }
