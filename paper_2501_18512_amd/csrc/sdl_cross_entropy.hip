@@ -6,6 +6,8 @@
 // are one with M = max(m1, m2), s = s1 exp(m1 - M) + s2 exp(m2 - M), so that a row costs one exchange between its threads.  With M and s of the row,
 //     lse = M + log s,   p = exp(x - M) / s
 // and the loss is formed from M - x[target] and log s, which loses nothing where the target is nearly certain and lse and x[target] are nearly equal.
+#include <cmath>
+
 #include "sdl_operand.h"
 
 namespace {
@@ -23,6 +25,7 @@ struct LossArgs {
     uint32_t rows, vocab, line;     // groups are counted from multiples of so many bytes
     bool wide;                      // targets of 64 bits
     float smoothing, hit, share, z; // hit = 1 - smoothing, share = smoothing / vocab
+    float each;                     // a power of two, at most 1 / (2 vocab)
 };
 
 // The row's target, or a negative number where it has none.
@@ -56,7 +59,8 @@ struct Base {
     __device__ __forceinline__ float into(const Base& to) const { return near && to.near ? exp2_of(from - to.from) : 1.0f; }
 };
 
-// Maximum, sum of exp() around it, and sum of x of some of a row's elements.  A part of nothing but -infinity has s = 0.
+// Maximum, sum of exp() around it, and sum of x of some of a row's elements, of which each counts as x times a power of two: exact, and no sum of up to `vocab` of them
+// leaves fp32 (logits that are masked with the lowest number).  A part of nothing but -infinity has s = 0.
 struct Part {
     float m, s, sum;
 };
@@ -203,9 +207,18 @@ __device__ __forceinline__ float sum_of(const float* v)
     return s;
 }
 
+// The same of v times a power of two.
+template <int W>
+__device__ __forceinline__ float sum_of(const float* v, float each)
+{
+    float s = fmaf(v[0], each, v[1] * each) + fmaf(v[2], each, v[3] * each);
+    if constexpr (W == 8) s += fmaf(v[4], each, v[5] * each) + fmaf(v[6], each, v[7] * each);
+    return s;
+}
+
 // What K groups of elements, TPR groups apart, are as a part of their row.  No branch goes by an element: a thread's groups stay in the words they came in.
 template <bool FIT, bool TINY, typename T, int K, int TPR>
-__device__ __forceinline__ Part part_of(Group<T> (&e)[K], uint32_t first, const Groups<T, TINY>& groups, bool smooth)
+__device__ __forceinline__ Part part_of(Group<T> (&e)[K], uint32_t first, const Groups<T, TINY>& groups, bool smooth, float each)
 {
     constexpr int W = Group<T>::W;
     Part p{-__builtin_inff(), 0.0f, 0.0f};
@@ -239,7 +252,7 @@ __device__ __forceinline__ Part part_of(Group<T> (&e)[K], uint32_t first, const 
             if ((!FIT || k == 0 || k + 1 >= K / 2) && !__all(groups.whole(first + k * TPR * W)))
 #pragma unroll
                 for (int j = 0; j < W; ++j) v[j] = groups.has(first + k * TPR * W, j) ? v[j] : 0.0f;
-            p.sum += sum_of<W>(v);
+            p.sum += sum_of<W>(v, each);
             forget(e[k], p.sum);
         }
     }
@@ -340,12 +353,12 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
     if constexpr (FIT) {
 #pragma unroll
         for (int k = 0; k < K; ++k) e[k] = groups.load(x, first + k * TPR * W);
-        p = part_of<FIT, TINY, T, K, TPR>(e, first, groups, smooth);
+        p = part_of<FIT, TINY, T, K, TPR>(e, first, groups, smooth, a.each);
     } else {
         for (uint32_t at = first; groups.below(at); at += TPR * W * K) {
 #pragma unroll
             for (int k = 0; k < K; ++k) e[k] = groups.load(x, at + k * TPR * W);
-            p = join(p, part_of<FIT, TINY, T, K, TPR>(e, at, groups, smooth));
+            p = join(p, part_of<FIT, TINY, T, K, TPR>(e, at, groups, smooth, a.each));
         }
     }
     p = wave_join(p, smooth);
@@ -382,8 +395,9 @@ __global__ void __launch_bounds__(BLOCK) sdl_cross_entropy_kernel(const LossArgs
     const float log_s = logf(p.s) - (!far && base.near ? fmaf(p.m, kLog2e, -base.from) * kLn2 : 0.0f);
     const float lse = p.m == __builtin_inff() ? __builtin_nanf("") : p.m + log_s;
     if (threadIdx.x % TPR == 0) {
-        float loss = log_s + (a.hit > 0.0f ? a.hit * (p.m - at_target) : 0.0f);       // (an infinite logit counts as the mean's, if it counts as nothing else)
-        if (smooth) loss += a.smoothing * (p.m - p.sum / (float)n);
+        // (an infinite logit counts as the mean's, if it counts as nothing else; differences by half, which have room for any two numbers)
+        float loss = log_s + (a.hit > 0.0f ? 2.0f * (a.hit * (0.5f * p.m - 0.5f * at_target)) : 0.0f);
+        if (smooth) loss += 2.0f * (a.smoothing * (0.5f * p.m - 0.5f * (p.sum / ((float)n * a.each))));
         if (a.z != 0.0f) loss += a.z * lse * lse;
         if (a.loss) a.loss[row] = p.m == __builtin_inff() ? lse : loss;
         if (a.lse) a.lse[row] = lse;
@@ -503,7 +517,7 @@ LossArgs arguments(const sdl_view_t* logits, const sdl_view_t* d_logits, uint32_
                    float smoothing, float z, const float* d_loss)
 {
     return LossArgs{kernel_view(logits), d_logits ? kernel_view(d_logits) : View{}, targets, d_loss, nullptr, nullptr, make_div(tokens), batch * tokens, vocab, 16,
-                    index == SDL_INDEX_INT64, smoothing, 1.0f - smoothing, smoothing / (float)vocab, z};
+                    index == SDL_INDEX_INT64, smoothing, 1.0f - smoothing, smoothing / (float)vocab, z, std::ldexp(0.5f, -(int)make_div(vocab).l)};
 }
 
 }  // namespace
