@@ -651,7 +651,8 @@ int sdl_cross_entropy_backward(const sdl_view_t* logits, uint32_t batch, uint32_
  * strides and type.  Products have fp32 sums; of their operands they have 11 bits where out is bf16, and 22 where it is fp32 and of small matrices (a side up to 16, or
  * 2048 elements), but for the diagonals of A and of b A + c A^2, which are fp32.  What is added to a X is fp32, X itself has 19 bits, or with products of 22 bits is fp32, norms are
  * 64 bits.  A matrix of zeros gives zeros; one with NaN or infinity gives NaN, to itself only.  workspace: device memory, 16-byte aligned, of at least
- * sdl_orthogonalize_workspace_bytes(...) bytes, contents irrelevant.
+ * sdl_orthogonalize_workspace_bytes(...) bytes, contents irrelevant; that is for any number of steps, and for matrices that a workgroup works on by itself (100 x 131, say) what x
+ * takes in fp32.
  * Errors: SDL_ERR_INVALID_ARG (missing array, bad type, no steps, coefficients, eps negative or not finite, scale not finite, out at x with
  * other strides or type, workspace too small), SDL_ERR_UNSUPPORTED
  * (a side above SDL_ORTHOGONALIZE_MAX_SIDE, 2^16 matrices and more, more than 2^22 tiles of 64 by 64), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */

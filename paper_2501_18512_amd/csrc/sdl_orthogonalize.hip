@@ -539,6 +539,8 @@ struct SmallArgs {
     uint32_t tall, n, m, steps;                  // n <= m
     double eps;
     float scale;
+    float* between;                              // [matrix][n][m]: X where a launch's steps are not all of them
+    uint32_t resumes, pauses;                    // X comes from there, is left there
     float a[kMostSmallSteps], b[kMostSmallSteps], c[kMostSmallSteps], image[kMostSmallSteps];     // image: the scale of b A + c A^2
 };
 
@@ -577,20 +579,23 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         return t < tiles;
     };
     f32x4_t x[SLOTS];
+    float* const between = a.between + (size_t)matrix * a.n * a.m;
     const T* from = reinterpret_cast<const T*>(a.x.data) + (int64_t)matrix * a.x.batch;
     double squares = 0.0;
     // no load waits for another: what is not there is the last element, and not counted
+    const auto load = [&](const auto* at, int64_t down, int64_t over) {
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-        uint32_t i, j;
-        tile(s, &i, &j);
-        const uint32_t row = min(i + c, a.n - 1);
+        for (int s = 0; s < SLOTS; ++s) {
+            uint32_t i, j;
+            tile(s, &i, &j);
+            const uint32_t row = min(i + c, a.n - 1);
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) {
-            const uint32_t col = min(j + 4 * q + r, a.m - 1);
-            x[s][r] = (float)from[a.tall ? (int64_t)col * a.x.token + row : (int64_t)row * a.x.token + col];
+            for (uint32_t r = 0; r < 4; ++r) x[s][r] = (float)at[row * down + min(j + 4 * q + r, a.m - 1) * over];
         }
-    }
+    };
+    if (a.resumes) load(between, a.m, 1);
+    else if (a.tall) load(from, 1, a.x.token);
+    else load(from, a.x.token, 1);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
         uint32_t i, j;
@@ -608,7 +613,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
     squares = 0.0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) squares += sums[w];
-    const double norm = sqrt(squares) + a.eps, inverse = norm == 0.0 ? 0.0 : 1.0 / norm;
+    const double norm = a.resumes ? 1.0 : sqrt(squares) + a.eps, inverse = norm == 0.0 ? 0.0 : 1.0 / norm;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s)
 #pragma unroll
@@ -741,16 +746,21 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
             for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, fmaf(b_diagonal[i + c], 1.0f / a.image[step], a.a[step]) * x[s][r]);
         }
     }
+    const auto store = [&](auto* at, int64_t down, int64_t over, float scale) {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            uint32_t i, j;
+            if (!tile(s, &i, &j) || i + c >= a.n) continue;
+            const uint32_t row = i + c, col = j + 4 * q;
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r)
+                if (col + r < a.m) at[row * down + (col + r) * over] = (std::remove_pointer_t<decltype(at)>)(x[s][r] * scale);
+        }
+    };
     O* out = reinterpret_cast<O*>(a.out.data) + (int64_t)matrix * a.out.batch;
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-        uint32_t i, j;
-        if (!tile(s, &i, &j) || i + c >= a.n) continue;
-        const uint32_t row = i + c, col = j + 4 * q;
-#pragma unroll
-        for (uint32_t r = 0; r < 4; ++r)
-            if (col + r < a.m) out[a.tall ? (int64_t)(col + r) * a.out.token + row : (int64_t)row * a.out.token + col + r] = (O)(x[s][r] * a.scale);
-    }
+    if (a.pauses) store(between, a.m, 1, 1.0f);
+    else if (a.tall) store(out, 1, a.out.token, a.scale);
+    else store(out, a.out.token, 1, a.scale);
 }
 
 // -------------------------------------------------------------------------------------------------------- host
@@ -902,7 +912,8 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
     size_t now = w.x16, other = w.x16_other;
     double h = 1.0;
     for (uint32_t s = 0; s < steps; ++s) {
-        const double ca = coefficients[3 * s], cb = coefficients[3 * s + 1], cc = coefficients[3 * s + 2];
+        const float* each = coefficients + 3 * (size_t)s;
+        const double ca = each[0], cb = each[1], cc = each[2];
         const float scale_b = image_scale(cb, cc, h);
         h = reach(ca, cb, cc, h);
         ProductArgs a{};
@@ -960,9 +971,17 @@ bool fits(const Small& k, uint32_t n, uint32_t m, bool split)
     return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) + 2 * nk * 4 <= k.bytes && down * across <= k.waves * k.slots_of(split) && down * (down + 1) / 2 <= k.waves * halves_of(split);
 }
 
-bool is_small(uint32_t n, uint32_t m, uint32_t steps, bool split)
+bool is_small(uint32_t n, uint32_t m, bool split)
 {
-    return steps <= kMostSmallSteps && std::any_of(std::begin(kSmall), std::end(kSmall), [=](const Small& k) { return fits(k, n, m, split); });
+    return std::any_of(std::begin(kSmall), std::end(kSmall), [=](const Small& k) { return fits(k, n, m, split); });
+}
+
+// What a call is to be given, whatever its steps: X of small matrices in fp32, between launches of kMostSmallSteps steps each (with the layout of the others 65535 matrices of 16 x 16
+// had to come with 5.4 GB, and this is 67 MB).
+size_t workspace_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
+{
+    const uint32_t n = std::min(rows, cols), m = std::max(rows, cols);
+    return is_small(n, m, split) ? (size_t)batch * n * m * sizeof(float) : layout_of(batch, rows, cols, split).bytes;
 }
 
 template <typename T, bool SPLIT, typename O>
@@ -1017,7 +1036,7 @@ extern "C" {
 size_t sdl_orthogonalize_workspace_bytes(uint32_t batch, uint32_t rows, uint32_t cols, sdl_dtype_t out_dtype)
 {
     if (batch == 0 || rows == 0 || cols == 0 || !known(out_dtype) || check_shape(batch, rows, cols) != SDL_OK) return 0;
-    return layout_of(batch, rows, cols, is_split(rows, cols, out_dtype)).bytes;
+    return workspace_of(batch, rows, cols, is_split(rows, cols, out_dtype));
 }
 
 int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32_t cols, sdl_dtype_t dtype, const float* coefficients, uint32_t steps, float eps,
@@ -1027,7 +1046,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (!(eps >= 0.0f && eps - eps == 0.0f) || !(scale - scale == 0.0f)) return SDL_ERR_INVALID_ARG;
     double h = 1.0;
     for (uint32_t s = 0; s < steps; ++s) {
-        h = reach(coefficients[3 * s], coefficients[3 * s + 1], coefficients[3 * s + 2], h);
+        h = reach(coefficients[3 * (size_t)s], coefficients[3 * (size_t)s + 1], coefficients[3 * (size_t)s + 2], h);
         if (!(h <= 2.0)) return SDL_ERR_INVALID_ARG;
     }
     int rc = check_shape(batch, rows, cols);
@@ -1037,24 +1056,31 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (out->data == x->data && (out_dtype != dtype || (batch > 1 && out->stride_batch != x->stride_batch) || (rows > 1 && out->stride_token != x->stride_token)))
         return SDL_ERR_INVALID_ARG;
     const bool split = is_split(rows, cols, out_dtype);
-    const Layout l0 = layout_of(batch, rows, cols, split);
-    if (!workspace || workspace_bytes < l0.bytes) return SDL_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < workspace_of(batch, rows, cols, split)) return SDL_ERR_INVALID_ARG;
     if (!aligned_to(workspace, 16)) return SDL_ERR_ALIGNMENT;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    if (is_small(n, m, steps, split)) {
-        SmallArgs a{kernel_view(x), kernel_view(out), make_div((m + 15) / 16), rows > cols, n, m, steps, (double)eps, scale, {}, {}, {}, {}};
+    if (is_small(n, m, split)) {
+        SmallArgs a{kernel_view(x), kernel_view(out), make_div((m + 15) / 16), rows > cols, n, m, 0, (double)eps, scale, static_cast<float*>(workspace), 0, 0, {}, {}, {}, {}};
         h = 1.0;
-        for (uint32_t s = 0; s < steps; ++s) {
-            a.a[s] = coefficients[3 * s];
-            a.b[s] = coefficients[3 * s + 1];
-            a.c[s] = coefficients[3 * s + 2];
-            a.image[s] = image_scale(a.b[s], a.c[s], h);
-            h = reach(a.a[s], a.b[s], a.c[s], h);
+        for (uint32_t s0 = 0; s0 < steps; s0 += kMostSmallSteps) {
+            a.steps = std::min(kMostSmallSteps, steps - s0);
+            a.resumes = s0 > 0;
+            a.pauses = s0 + a.steps < steps;
+            for (uint32_t s = 0; s < a.steps; ++s) {
+                const float* each = coefficients + 3 * (size_t)(s0 + s);
+                a.a[s] = each[0];
+                a.b[s] = each[1];
+                a.c[s] = each[2];
+                a.image[s] = image_scale(a.b[s], a.c[s], h);
+                h = reach(a.a[s], a.b[s], a.c[s], h);
+            }
+            rc = dtype == SDL_DTYPE_BF16 ? small_of<__bf16>(a, split, out_dtype, batch, st) : small_of<float>(a, split, out_dtype, batch, st);
+            if (rc != SDL_OK) return rc;
         }
-        return dtype == SDL_DTYPE_BF16 ? small_of<__bf16>(a, split, out_dtype, batch, st) : small_of<float>(a, split, out_dtype, batch, st);
+        return SDL_OK;
     }
-    Layout l = l0;
+    Layout l = layout_of(batch, rows, cols, split);
     l.w.base = static_cast<char*>(workspace);
     FirstArgs a{};
     a.x = kernel_view(x);
