@@ -191,6 +191,15 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_first_kernel(const Firs
 // ----------------------------------------------------------------------------------------------------- products
 
 enum { GRAM, POLY, UPDATE };
+
+// Between what lanes of a wavefront write to shared memory and what others of it read there, either way.  A wavefront's accesses keep the order they are issued in; this keeps the
+// compiler from issuing them in another one, and is no instruction.
+__device__ __forceinline__ void lanes_meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A symmetric product has few tiles, and with one long matrix few compute units are at work: then every tile's sum is cut into slices, whose partial sums go
 // through memory (PART), and are added up in order by a launch that goes on as the other way does (JOIN).
 enum { WHOLE, PART, JOIN };
@@ -448,6 +457,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                         for (int r = 0; r < 4; ++r) v[r] = acc[bi * kIn + pi][bj * kIn + pj][4 * u + r];
                         *reinterpret_cast<f32x4_t*>(block + (pi * 32 + c) * kPitch + (pj * 32 + 8 * u + 4 * half) * 4) = v;
                     }
+            lanes_meet();
             float v[kPasses][8];
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
@@ -463,6 +473,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                     if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k], a.on_old / kScaleX) * ((float)old[k].hi[e] + rest[k].get(e)));
                 }
             }
+            lanes_meet();           // the block is written again: turned, as an image, or with the next one
             if constexpr (MODE != UPDATE) {
                 if (i == j) {       // the diagonal goes apart, and is zero in the image
 #pragma unroll
@@ -492,6 +503,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
 #pragma unroll
                     for (int k = 0; k < kPasses; ++k)
                         store8(reinterpret_cast<float*>(block + (k * kRows + r0) * kPitch), c0, c0 + 8, v[k]);
+                    lanes_meet();
 #pragma unroll
                     for (int k = 0; k < kPasses; ++k) {
                         const uint32_t row = lane % kBlock, col = (k * (kWave / kBlock) + lane / kBlock) * 8;
@@ -500,6 +512,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                         for (int e = 0; e < 8; ++e) t[e] = *reinterpret_cast<const float*>(block + (col + e) * kPitch + row * 4);
                         if (j + row < a.rows && i + col < a.cols) store8(out + (int64_t)(j + row) * a.out.token, i + col, a.cols, t);
                     }
+                    lanes_meet();
                     continue;
                 }
 #pragma unroll
@@ -518,6 +531,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                 }
             }
             if (!turned) continue;
+            lanes_meet();
             // lanes of a group of 16 have a column each, of 16; the groups have eight rows each, of 32
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
@@ -528,6 +542,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                 if constexpr (SPLIT) image.lo = across(at + kBlock * kImagePitch, 4 * kImagePitch);
                 put<SPLIT>(base + a.t + (size_t)(j + col + lane % 16) * a.w.pitch(n), i + row, image);
             }
+            lanes_meet();
         }
 }
 
