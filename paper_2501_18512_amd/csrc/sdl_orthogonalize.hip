@@ -12,8 +12,9 @@
 //   - Near its end A is nearly diagonal, and an image's error on the diagonal would go into a whole row of X: so the diagonals of A and of b A + c A^2 are kept apart in fp32, and are
 //     zero in the images.
 //   - results in bf16: one image, 11 bits.  Five steps are off by 0.0003 of the result, under the 0.0017 of its own rounding (0.0013 with the diagonals in the images of matrices of
-//     64 rows).  X is its image and what that leaves, rounded to bf16: 19 bits, and 8 of an element too small for the image (2^-38 of a norm, which takes an eps far above the
-//     norm).  The write of X is what an update waits for, and in fp32 it was half as much again.
+//     64 rows).  X is its image and what that leaves, as fp16 too: together the digits of fp32, down to 2^-50 of the norm, in the same four bytes.  (With what is left in bf16, 19 bits,
+//     the results of low rank were off by up to 2.5 times as much: what X's rounding puts into the directions that are not there is lifted with them.  The write of X is what an update
+//     waits for: in fp32 beside its image it was half as much again.)
 //   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.  X in fp32, which has its digits
 //     wherever the norm is.  16 x 128 are off by 1.1e-6 (1.7e-6 with the diagonals in the images), 400 x 801 by 1.1e-6.
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
@@ -35,6 +36,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kScaleX = 16384.0f, kScaleA = 4096.0f;
+constexpr float kScaleRest = 2048.0f;       // of what one image leaves of X: a part of 2^12 at most, so that it lies where the image did
 constexpr uint32_t kDies = 8;
 constexpr uint32_t kMostSmallSteps = 32, kMostParts = 1024;
 
@@ -42,7 +44,7 @@ constexpr uint32_t kMostSmallSteps = 32, kMostParts = 1024;
 struct Work {
     char* base;
     size_t each;
-    size_t rest, x16, x16_other, a16, b16;           // offsets; rest: X in fp32, or in bf16 what its one image leaves
+    size_t rest, x16, x16_other, a16, b16;           // offsets; rest: X in fp32, or in fp16 what its one image leaves
     size_t a_diagonal, b_diagonal;                    // in fp32, as large as the images
     uint32_t n, m;                                    // n <= m, filled up
     uint32_t split;
@@ -92,8 +94,8 @@ __device__ __forceinline__ void put_x(char* base, const Work& w, size_t x16, uin
         store8(reinterpret_cast<float*>(base + w.rest) + (size_t)i * w.m, j, j + 8, v);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] -= (float)image.hi[e];
-        store8(reinterpret_cast<__bf16*>(base + w.rest) + (size_t)i * w.m, j, j + 8, s);
+        for (int e = 0; e < 8; ++e) s[e] = (s[e] - (float)image.hi[e]) * kScaleRest;
+        *reinterpret_cast<f16x8_t*>(base + w.rest + ((size_t)i * w.m + j) * 2) = parts_of(s).hi;
     }
 }
 
@@ -420,7 +422,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
             const uint32_t i = ti * TILE + i0 + bi * kBlock, j = tj * TILE + j0 + bj * kBlock;     // the block's first row and column
             Parts old[MODE == POLY || (MODE == UPDATE && !SPLIT) ? kPasses : 1];
             Eight<float> x[MODE == UPDATE && SPLIT ? kPasses : 1];
-            Eight<__bf16> rest[MODE == UPDATE && !SPLIT ? kPasses : 1];
+            f16x8_t rest[MODE == UPDATE && !SPLIT ? kPasses : 1];
             float own[MODE != GRAM ? kPasses : 1];                     // the rows' places of the diagonal
             Eight<float> others;
             if constexpr (MODE == POLY) {
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                         x[k] = load8(reinterpret_cast<const float*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
                     } else {
                         old[k].hi = *piece<false>(base + a.q + (size_t)row * a.w.pitch(m), j + c0);
-                        rest[k] = load8(reinterpret_cast<const __bf16*>(base + a.w.rest) + (size_t)row * m + j, c0, c0 + 8);
+                        rest[k] = *reinterpret_cast<const f16x8_t*>(base + a.w.rest + ((size_t)row * m + j + c0) * 2);
                     }
                 }
             }
@@ -470,7 +472,7 @@ __global__ void __launch_bounds__(256) sdl_orthogonalize_product_kernel(const Pr
                     if constexpr (MODE == POLY)
                         v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k] + others.get(e), a.on_old) * (SPLIT ? (float)old[k].hi[e] + (float)old[k].lo[e] : (float)old[k].hi[e]));
                     if constexpr (MODE == UPDATE && SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum * kScaleX, own[k], a.on_old) * x[k].get(e));
-                    if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k], a.on_old / kScaleX) * ((float)old[k].hi[e] + rest[k].get(e)));
+                    if constexpr (MODE == UPDATE && !SPLIT) v[k][e] = fmaf(s, a.on_sum, fmaf(a.on_sum, own[k], a.on_old / kScaleX) * fmaf((float)rest[k][e], 1.0f / kScaleRest, (float)old[k].hi[e]));
                 }
             }
             lanes_meet();           // the block is written again: turned, as an image, or with the next one
