@@ -648,8 +648,9 @@ int sdl_cross_entropy_backward(const sdl_view_t* logits, uint32_t batch, uint32_
  *     for every (a, b, c):  A = X X^T,  X = a X + (b A + c A^2) X          out = scale X
  * which takes every singular value s of X to a s + b s^3 + c s^5 and leaves the singular vectors.  x, out: views [batch][rows][cols] (stride_token between rows).
  * coefficients: HOST array [steps][3], read during the call; the polynomials, one after the other, may take no s in [0, 1] beyond 2.  out may be x itself, with the same
- * strides and type.  Products have fp32 sums; of their operands they have 11 bits where out is bf16, and 22 where it is fp32 and of small matrices (a side up to 16, or
- * 2048 elements), but for the diagonals of A and of b A + c A^2, which are fp32.  What is added to a X is fp32, and so is X itself (or two fp16 with its digits); norms are
+ * strides and type.  Products have fp32 sums; of their operands they have 22 bits where out is fp32 and of matrices of up to 256 rows or columns, and 11 where out is bf16 and the matrix larger,
+ * but for the diagonals of A and of b A + c A^2, which are fp32 (elements of X under 2^-17 and of A under 2^-15 have fewer: they are good to 2^-39 and 2^-37).  11 bits cost the results
+ * 0.0003 to 0.0005 (root mean square) beside the 0.0017 of their own rounding, and 0.42 / rows of rank one.  What is added to a X is fp32, and so is X itself (or two fp16 with its digits); norms are
  * 64 bits.  A matrix of zeros gives zeros; one with NaN or infinity gives NaN, to itself only.  workspace: device memory, 16-byte aligned, of at least
  * sdl_orthogonalize_workspace_bytes(...) bytes, contents irrelevant; that is for any number of steps, and for matrices that a workgroup works on by itself (100 x 131, say) what x
  * takes in fp32.

@@ -11,12 +11,12 @@
 //     direction already is: an error of X itself would be lifted with the small singular values, 3.4 times a step.
 //   - Near its end A is nearly diagonal, and an image's error on the diagonal would go into a whole row of X: so the diagonals of A and of b A + c A^2 are kept apart in fp32, and are
 //     zero in the images.
-//   - results in bf16: one image, 11 bits.  Five steps are off by 0.0003 of the result, under the 0.0017 of its own rounding (0.0013 with the diagonals in the images of matrices of
-//     64 rows).  X is its image and what that leaves, as fp16 too: together the digits of fp32, down to 2^-50 of the norm, in the same four bytes.  (With what is left in bf16, 19 bits,
-//     the results of low rank were off by up to 2.5 times as much: what X's rounding puts into the directions that are not there is lifted with them.  The write of X is what an update
-//     waits for: in fp32 beside its image it was half as much again.)
-//   - results in fp32: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.  X in fp32, which has its digits
-//     wherever the norm is.  16 x 128 are off by 1.1e-6 (1.7e-6 with the diagonals in the images), 400 x 801 by 1.1e-6.
+//   - results in bf16, more than 256 rows: one image, 11 bits.  Five steps are off by 0.0003 to 0.0005 of the result beside the 0.0017 of its own rounding, of rank one by 0.42 / rows.  X is its
+//     image and what that leaves, as fp16 too: together the digits of fp32, down to 2^-50 of the norm, in the same four bytes.  (With what is left in bf16, 20 bits, results of rank one
+//     were off by up to 1.4 times as much: what X's rounding puts into the directions that are not there is lifted with them.  The write of X is what an update waits for: in fp32 beside
+//     its image it was half as much again.)
+//   - results in fp32, and matrices of fewer rows: two images, x 2^14 = hi + lo, 22 bits, and three products hi hi + hi lo + lo hi.  What is left out is 2^-24.  X in fp32.  All sizes are off
+//     by 0.4 to 1.7e-6, of rank one by up to 9e-5.
 // An operand's rows are cut into pieces of 128 bytes, one step of a product's loop each: 64 elements, or 32 of hi and the same 32 of lo.
 #include <algorithm>
 #include <cmath>
@@ -561,19 +561,19 @@ struct SmallArgs {
     float a[kMostSmallSteps], b[kMostSmallSteps], c[kMostSmallSteps], image[kMostSmallSteps];     // image: the scale of b A + c A^2
 };
 
-// Tiles of a symmetric product of a wavefront's, at most: what two images leave room for has fewer.
-constexpr uint32_t halves_of(bool split) { return split ? 3 : 5; }
+// Tiles of a symmetric product of a wavefront's, at most.
+constexpr uint32_t kHalves = 3;
 
-// A matrix whose images fit the shared memory of a workgroup is worked on there from its norm to its last step: with a launch for every product it would be the launches, 80 us for
+// A matrix whose two images fit the shared memory of a workgroup is worked on there from its norm to its last step: with a launch for every product it would be the launches, 80 us for
 // five steps of 100 x 131, which take 60 so.  Tiles of 16 by 16 go round among the wavefronts; those of X stay in the registers of theirs, in fp32, and what a step makes of them is what the next one
 // starts from.
 //
 // Layouts of the 16x16x32 instruction, lane l, q = l / 16, c = l % 16:  A row c, k = 8 q + j;  B column c, k = 8 q + j;  D column c, rows 4 q + i.  X's tile
 // has its rows along c, so that a lane has four neighbours of a row: A = the columns of X, by transposing reads, B = the rows of b A + c A^2.
-template <typename T, bool SPLIT, typename O, int WAVES, int SLOTS, int BYTES>
+template <typename T, typename O, int WAVES, int SLOTS, int BYTES>
 __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(const SmallArgs a)
 {
-    constexpr int kImages = SPLIT ? 2 : 1;
+    constexpr int kImages = 2;
     __shared__ __attribute__((aligned(16))) char lds[BYTES];
     __shared__ double sums[WAVES];
     const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), q = lane / 16, c = lane % 16, matrix = blockIdx.x;
@@ -640,17 +640,15 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
     const auto put4 = [&](char* image, uint32_t bytes, uint32_t pitch, uint32_t row, uint32_t k, const f32x4_t& v) {
         const f16x4_t hi = __builtin_convertvector(v, f16x4_t);
         *reinterpret_cast<f16x4_t*>(image + row * pitch + k * 2) = hi;
-        if constexpr (SPLIT) {
-            f32x4_t rest;
+        f32x4_t rest;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) rest[r] = v[r] - (float)hi[r];
-            *reinterpret_cast<f16x4_t*>(image + bytes + row * pitch + k * 2) = __builtin_convertvector(rest, f16x4_t);
-        }
+        for (int r = 0; r < 4; ++r) rest[r] = v[r] - (float)hi[r];
+        *reinterpret_cast<f16x4_t*>(image + bytes + row * pitch + k * 2) = __builtin_convertvector(rest, f16x4_t);
     };
     const auto put1 = [&](char* image, uint32_t bytes, uint32_t pitch, uint32_t row, uint32_t k, float v) {
         const _Float16 hi = (_Float16)v;
         *reinterpret_cast<_Float16*>(image + row * pitch + k * 2) = hi;
-        if constexpr (SPLIT) *reinterpret_cast<_Float16*>(image + bytes + row * pitch + k * 2) = (_Float16)(v - (float)hi);
+        *reinterpret_cast<_Float16*>(image + bytes + row * pitch + k * 2) = (_Float16)(v - (float)hi);
     };
     const auto along = [&](const char* image, uint32_t pitch, uint32_t row, uint32_t k) {
         return *reinterpret_cast<const f16x8_t*>(image + (row + c) * pitch + (k + 8 * q) * 2);
@@ -667,12 +665,10 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
 #pragma unroll 2
         for (uint32_t k = 0; k < kk; k += 32) {
             const f16x8_t p = along(image, pitch, i, k), r = along(image, pitch, j, k);
+            const f16x8_t pl = along(image + bytes, pitch, i, k), rl = along(image + bytes, pitch, j, k);
             d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, r, d, 0, 0, 0);
-            if constexpr (SPLIT) {
-                const f16x8_t pl = along(image + bytes, pitch, i, k), rl = along(image + bytes, pitch, j, k);
-                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, rl, d, 0, 0, 0);
-                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, r, d, 0, 0, 0);
-            }
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, rl, d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, r, d, 0, 0, 0);
         }
         return d;
     };
@@ -698,7 +694,6 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         *j = (t - row * (row + 1) / 2) * 16;
     };
     const uint32_t halves = down * (down + 1) / 2;
-    constexpr int kHalves = halves_of(SPLIT);
     for (uint32_t step = 0; step < a.steps; ++step) {
         // X's image, once everyone has read the one before
         __syncthreads();
@@ -716,15 +711,14 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         __syncthreads();
         f32x4_t mix[kHalves];
 #pragma unroll
-        for (int s = 0; s < kHalves; ++s) {
+        for (uint32_t s = 0; s < kHalves; ++s) {
             const uint32_t t = s * WAVES + wave;
             if (t >= halves) continue;
             uint32_t i, j;
             place(t, &i, &j);
             const f32x4_t square = symmetric(image_a, bytes_a, pitch_a, i, j, nk);
             const f16x4_t hi = *reinterpret_cast<const f16x4_t*>(image_a + (j + c) * pitch_a + (i + 4 * q) * 2);
-            f16x4_t lo = {};
-            if constexpr (SPLIT) lo = *reinterpret_cast<const f16x4_t*>(image_a + bytes_a + (j + c) * pitch_a + (i + 4 * q) * 2);
+            const f16x4_t lo = *reinterpret_cast<const f16x4_t*>(image_a + bytes_a + (j + c) * pitch_a + (i + 4 * q) * 2);
             const float on_square = a.c[step] * a.image[step] / (kScaleA * kScaleA), on_a = a.b[step] * a.image[step] / kScaleA;
 #pragma unroll
             for (uint32_t r = 0; r < 4; ++r) {
@@ -735,7 +729,7 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
         }
         __syncthreads();
 #pragma unroll
-        for (int s = 0; s < kHalves; ++s) {
+        for (uint32_t s = 0; s < kHalves; ++s) {
             const uint32_t t = s * WAVES + wave;
             if (t >= halves) continue;
             uint32_t i, j;
@@ -752,12 +746,10 @@ __global__ void __launch_bounds__(WAVES * kWave) sdl_orthogonalize_small_kernel(
 #pragma unroll 2
             for (uint32_t k = 0; k < nk; k += 32) {
                 const f16x8_t p = across_rows(image_x, pitch_x, k, j), r = along(image_a, pitch_a, i, k);
+                const f16x8_t pl = across_rows(image_x + bytes_x, pitch_x, k, j), rl = along(image_a + bytes_a, pitch_a, i, k);
                 d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, r, d, 0, 0, 0);
-                if constexpr (SPLIT) {
-                    const f16x8_t pl = across_rows(image_x + bytes_x, pitch_x, k, j), rl = along(image_a + bytes_a, pitch_a, i, k);
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, rl, d, 0, 0, 0);
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, r, d, 0, 0, 0);
-                }
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, rl, d, 0, 0, 0);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, r, d, 0, 0, 0);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[s][r] = fmaf(d[r], on_sum, fmaf(b_diagonal[i + c], 1.0f / a.image[step], a.a[step]) * x[s][r]);
@@ -824,12 +816,13 @@ Tiles tiles_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
 // Sums of squares of a matrix: enough workgroups for all compute units.
 uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(kMostParts, 2048u / batch)); }
 
-// Whether images are two: for results in fp32, and of matrices of few rows or few elements, where the errors of an image of one do not average out: of the results of rows alone 0.004, of
-// 4 x 4 0.005, of 17 x 17 0.0024, beside 0.0017 of bf16's own rounding, which is all that is left of 32 x 256.  8 x 24 x 192 takes 24 us instead of 21, 16 x 16 x 4000 162 instead of 101.
-bool is_split(uint32_t rows, uint32_t cols, sdl_dtype_t out)
-{
-    return out == SDL_DTYPE_FP32 || std::min(rows, cols) <= 16 || (uint64_t)rows * cols <= 2048;
-}
+// Whether images are two: for results in fp32, and of matrices of up to 256 rows (the fewer of rows and columns).  What one image costs most is a matrix of rank one, of which the diagonal of
+// b A + c A^2 meets X and the rest of it X's image: 0.42 / rows of the results (root mean square), and up to 256 rows that is more than the 0.00166 of bf16's own rounding.  With one image and with
+// two, with that rounding: 16 x 4000 0.021 and 0.0017, 64 x 64 0.0068 and 0.0017, 128 x 512 0.0037, 200 x 300 0.0028, 256 x 1024 0.0025; then 384 x 384 0.0020, 768 x 768 0.00175, 2048 x 2048 0.0017.  Of
+// a momentum with noise 0.0017 to 0.0018 whatever the size.  us: 300 of 64 x 64 27 with one and 35 with two, 8 of 100 x 131 42, 62, 48 of 128 x 512 94, 161, 4 of 200 x 300 86, 109,
+// 8 of 256 x 1024 101, 157, 8 of 768 x 768 203, 538.
+constexpr uint32_t kMostSplit = 256;
+bool is_split(uint32_t rows, uint32_t cols, sdl_dtype_t out) { return out == SDL_DTYPE_FP32 || std::min(rows, cols) <= kMostSplit; }
 
 struct Layout {
     Work w;
@@ -973,62 +966,55 @@ int steps_of(const Layout& l, uint32_t batch, uint32_t rows, uint32_t cols, cons
 }
 
 // Wavefronts of a workgroup, tiles of X that each of them keeps, and shared memory of the kernels of small matrices.  A step is five stretches between barriers, of which a wavefront's
-// tiles come one after the other: the more wavefronts the shorter, down to a tile each, and for many matrices as few as fill the compute units.  us, with 4, 8 and 16 wavefronts:
-// 30 of 64 x 64 in bf16 27.7, 21.0, 18.4; 300 30.6, 25.1, 34.7; 4000 132, 134, 261.  2000 of 24 x 24 with room for four tiles of a wavefront 30, for one 23.
+// tiles come one after the other: the more wavefronts the shorter, down to a tile each, and for many matrices as few as fill the compute units.  us, with 8 and 16 wavefronts:
+// 30 of 64 x 64 26.3, 23.1; 300 34.7, 43.6; 4000 187, 330.  2000 of 24 x 24 with 4 wavefronts 28, with 16 100; with room for four tiles of a wavefront 30 instead of 23 for one.
 struct Small {
     uint32_t waves, slots, bytes;
-    // (two images leave no room for more)
-    constexpr uint32_t slots_of(bool split) const { return split && slots > 10 ? 10 : slots; }
 };
-constexpr Small kSmall[] = {{4, 1, 15 * 1024}, {8, 2, 39 * 1024}, {8, 6, 39 * 1024}, {16, 2, 39 * 1024}, {16, 4, 159 * 1024}, {16, 6, 159 * 1024}, {16, 12, 159 * 1024}};
+constexpr Small kSmall[] = {{4, 1, 15 * 1024}, {8, 2, 39 * 1024}, {8, 6, 39 * 1024}, {16, 2, 39 * 1024}, {16, 4, 159 * 1024}, {16, 6, 159 * 1024}, {16, 10, 159 * 1024}};
 
-bool fits(const Small& k, uint32_t n, uint32_t m, bool split)
+bool fits(const Small& k, uint32_t n, uint32_t m)
 {
     const uint64_t down = (n + 15) / 16, across = (m + 15) / 16, nk = (n + 31) / 32 * 32, mk = (m + 31) / 32 * 32;
-    return (split ? 2 : 1) * nk * (mk * 2 + 16 + nk * 2 + 16) + 2 * nk * 4 <= k.bytes && down * across <= k.waves * k.slots_of(split) && down * (down + 1) / 2 <= k.waves * halves_of(split);
+    return 2 * nk * (mk * 2 + 16 + nk * 2 + 16) + 2 * nk * 4 <= k.bytes && down * across <= k.waves * k.slots && down * (down + 1) / 2 <= k.waves * kHalves;
 }
 
-bool is_small(uint32_t n, uint32_t m, bool split)
+bool is_small(uint32_t n, uint32_t m)
 {
-    return std::any_of(std::begin(kSmall), std::end(kSmall), [=](const Small& k) { return fits(k, n, m, split); });
+    return std::any_of(std::begin(kSmall), std::end(kSmall), [=](const Small& k) { return fits(k, n, m); });
 }
+static_assert(2 * (kMostSplit + 1) * (kMostSplit + 1) * 2 > 160 * 1024, "matrices that have one image are not small");
 
 // What a call is to be given, whatever its steps: X of small matrices in fp32, between launches of kMostSmallSteps steps each (with the layout of the others 65535 matrices of 16 x 16
 // had to come with 5.4 GB, and this is 67 MB).
 size_t workspace_of(uint32_t batch, uint32_t rows, uint32_t cols, bool split)
 {
     const uint32_t n = std::min(rows, cols), m = std::max(rows, cols);
-    return is_small(n, m, split) ? (size_t)batch * n * m * sizeof(float) : layout_of(batch, rows, cols, split).bytes;
+    return is_small(n, m) ? (size_t)batch * n * m * sizeof(float) : layout_of(batch, rows, cols, split).bytes;
 }
 
-template <typename T, bool SPLIT, typename O>
+template <typename T, typename O>
 int small(const SmallArgs& a, uint32_t batch, hipStream_t st)
 {
-#define SDL_LAUNCH(N)                                                                                                                                  \
-    hipLaunchKernelGGL((sdl_orthogonalize_small_kernel<T, SPLIT, O, kSmall[N].waves, kSmall[N].slots_of(SPLIT), kSmall[N].bytes>), dim3(batch), dim3(kSmall[N].waves * kWave), 0, st, a)
+#define SDL_LAUNCH(N) \
+    hipLaunchKernelGGL((sdl_orthogonalize_small_kernel<T, O, kSmall[N].waves, kSmall[N].slots, kSmall[N].bytes>), dim3(batch), dim3(kSmall[N].waves * kWave), 0, st, a)
     // more than one for a compute unit, or too few tiles for sixteen wavefronts
     const bool many = batch > 256 || ((a.n + 15) / 16) * ((a.m + 15) / 16) < 16;
-    if constexpr (SPLIT) {      // (matrices of so few tiles have two images)
-        if (many && fits(kSmall[0], a.n, a.m, SPLIT)) {
-            SDL_LAUNCH(0);
-            return launched();
-        }
-    }
-    if (many && fits(kSmall[1], a.n, a.m, SPLIT)) SDL_LAUNCH(1);
-    else if (many && fits(kSmall[2], a.n, a.m, SPLIT)) SDL_LAUNCH(2);
-    else if (fits(kSmall[3], a.n, a.m, SPLIT)) SDL_LAUNCH(3);
-    else if (fits(kSmall[4], a.n, a.m, SPLIT)) SDL_LAUNCH(4);
-    else if (fits(kSmall[5], a.n, a.m, SPLIT)) SDL_LAUNCH(5);
+    if (many && fits(kSmall[0], a.n, a.m)) SDL_LAUNCH(0);
+    else if (many && fits(kSmall[1], a.n, a.m)) SDL_LAUNCH(1);
+    else if (many && fits(kSmall[2], a.n, a.m)) SDL_LAUNCH(2);
+    else if (fits(kSmall[3], a.n, a.m)) SDL_LAUNCH(3);
+    else if (fits(kSmall[4], a.n, a.m)) SDL_LAUNCH(4);
+    else if (fits(kSmall[5], a.n, a.m)) SDL_LAUNCH(5);
     else SDL_LAUNCH(6);
 #undef SDL_LAUNCH
     return launched();
 }
 
 template <typename T>
-int small_of(const SmallArgs& a, bool split, sdl_dtype_t out, uint32_t batch, hipStream_t st)
+int small_of(const SmallArgs& a, sdl_dtype_t out, uint32_t batch, hipStream_t st)
 {
-    if (out == SDL_DTYPE_FP32) return small<T, true, float>(a, batch, st);
-    return split ? small<T, true, __bf16>(a, batch, st) : small<T, false, __bf16>(a, batch, st);
+    return out == SDL_DTYPE_FP32 ? small<T, float>(a, batch, st) : small<T, __bf16>(a, batch, st);
 }
 
 template <typename T, bool SPLIT>
@@ -1077,7 +1063,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (!aligned_to(workspace, 16)) return SDL_ERR_ALIGNMENT;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-    if (is_small(n, m, split)) {
+    if (is_small(n, m)) {
         SmallArgs a{kernel_view(x), kernel_view(out), make_div((m + 15) / 16), rows > cols, n, m, 0, (double)eps, scale, static_cast<float*>(workspace), 0, 0, {}, {}, {}, {}};
         h = 1.0;
         for (uint32_t s0 = 0; s0 < steps; s0 += kMostSmallSteps) {
@@ -1092,7 +1078,7 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
                 a.image[s] = image_scale(a.b[s], a.c[s], h);
                 h = reach(a.a[s], a.b[s], a.c[s], h);
             }
-            rc = dtype == SDL_DTYPE_BF16 ? small_of<__bf16>(a, split, out_dtype, batch, st) : small_of<float>(a, split, out_dtype, batch, st);
+            rc = dtype == SDL_DTYPE_BF16 ? small_of<__bf16>(a, out_dtype, batch, st) : small_of<float>(a, out_dtype, batch, st);
             if (rc != SDL_OK) return rc;
         }
         return SDL_OK;

@@ -17,7 +17,7 @@ from oracle import training as ref
 QUINTIC = ((3.4445, -4.7750, 2.0315),) * 5
 # matrices enough that a mean tells; a workgroup a matrix of every kind, and tiles
 SHAPES = [(300, 2, 2), (200, 5, 5), (60, 3, 20), (60, 20, 9), (30, 8, 256), (30, 256, 8), (16, 5, 300), (16, 300, 6), (30, 16, 16), (30, 17, 17), (16, 17, 100), (270, 24, 24), (16, 31, 40),
-          (8, 45, 45), (8, 64, 64), (8, 50, 45), (4, 100, 131), (4, 131, 100), (8, 16, 500), (2, 200, 300), (2, 129, 70), (1, 400, 801), (1, 385, 129)]
+          (8, 45, 45), (8, 64, 64), (8, 50, 45), (4, 100, 131), (4, 131, 100), (8, 16, 500), (2, 200, 300), (2, 129, 70), (1, 256, 700), (1, 257, 300), (1, 400, 801), (1, 385, 129)]
 ROWS = [(200, 1, 9), (60, 12, 1), (60, 1, 100), (16, 1, 2048), (16, 1, 2049)]
 
 
@@ -31,7 +31,7 @@ def momentum(shape, dtype, seed):
 
 def is_split(shape, out):
     """Whether products have 22 bits, as the header says."""
-    return out == FP32 or min(shape[1:]) <= 16 or shape[1] * shape[2] <= 2048
+    return out == FP32 or min(shape[1:]) <= 256
 
 
 def exact(x, coefficients=QUINTIC):
