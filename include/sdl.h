@@ -632,7 +632,8 @@ int sdl_embedding_backward(const sdl_view_t* d_out, sdl_dtype_t dtype, const voi
  *     lse = log sum exp(x),  loss = lse - (1 - smoothing) x[target] - smoothing * mean(x) + z lse^2
  *     d_x = d_loss ((1 + 2 z lse) exp(x - lse) - smoothing / vocab - (1 - smoothing) [target])
  * loss, lse, d_loss: fp32 [batch][tokens].  A row whose target is not in [0, vocab) has loss 0, lse 0 and a gradient of zeros, whatever its logits are (they are not
- * read).  A logit of -infinity is a token that cannot come (its loss as a target is infinite); a row with NaN or +infinity, or with nothing but -infinity, gives NaN, to itself only.
+ * read).  A logit of -infinity is a token that cannot come (its loss as a target is infinite); a row with NaN or +infinity, or with nothing but -infinity, gives NaN, to itself
+ * only; its lse is -infinity where all of it is.
  * d_logits: NULL, or the gradient in the same pass, in the logits' type; it may be logits itself, with the same strides.  d_loss: NULL for 1.  loss, lse: NULL where
  * not wanted.  Errors: SDL_ERR_INVALID_ARG (missing array, bad type, vocab 0, smoothing outside [0, 1], z negative or not finite, nothing to write),
  * SDL_ERR_UNSUPPORTED (vocab above SDL_CROSS_ENTROPY_MAX_VOCAB, 2^31 rows and more), SDL_ERR_ALIGNMENT, SDL_ERR_DEVICE. */

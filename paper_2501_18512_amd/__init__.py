@@ -794,5 +794,5 @@ def alloc_orthogonalize(x, out):
 
 
 def sdl_orthogonalize(x, out, workspace, coefficients=ORTHOGONALIZE_QUINTIC, eps: float = 1e-7, scale: float = 1.0, stream=None):
-    """x, out: [rows, cols] or [batch, rows, cols], of one shape; coefficients: (a, b, c) of every step."""
+    """x, out: [rows, cols] or [batch, rows, cols], of one shape; coefficients: (a, b, c) of every step, up to 64 of them (the C call takes any number)."""
     _check(_training.sdl_orthogonalize(x, out, workspace, coefficients, eps, scale, stream), "sdl_orthogonalize")
