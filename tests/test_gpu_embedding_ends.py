@@ -62,3 +62,23 @@ def test_places_of_more_than_two_merges(n, width, how):
     want = torch.zeros((V, width), dtype=torch.float64).index_add_(0, t.cpu(), d.double().cpu())       # (one row's atomics on the device take minutes)
     assert float(want.max()) < 2 ** 24
     assert torch.equal(got.cpu().double(), want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("n,width", [(9, 5), (700, 64), (2500, 300), (40000, 40)])
+def test_what_is_not_finite_in_padded_places_goes_nowhere(n, width, dtype):
+    """d_out of padding is not looked at; elsewhere it stays in its token's row and column."""
+    V = 70
+    t, d = tokens_of((n,), V, "padded", 6), randn((n, width), dtype, 7)
+    clean = d.clone()
+    there = (t >= 0) & (t < V)
+    d[~there] = float("nan")
+    d[~there, :2] = float("inf")
+    at = int(there.nonzero()[0])
+    d[at, 3] = float("nan")
+    got, want = (torch.full((V, width), -1.0, dtype=dtype, device="cuda") for _ in range(2))
+    sdl.sdl_embedding_backward(d.cuda(), t.cuda(), got, sdl.alloc_embedding(t.cuda(), width))
+    sdl.sdl_embedding_backward(clean.cuda(), t.cuda(), want, sdl.alloc_embedding(t.cuda(), width))
+    assert torch.isnan(got[t[at], 3])
+    got[t[at], 3] = want[t[at], 3]
+    assert torch.equal(got, want)
