@@ -817,7 +817,7 @@ Tiles tiles_of(uint32_t batch, uint32_t n, uint32_t m, bool split)
 uint32_t parts_of(uint32_t batch) { return std::max(8u, std::min(kMostParts, 2048u / batch)); }
 
 // Whether images are two: for results in fp32, and of matrices of up to 256 rows (the fewer of rows and columns).  What one image costs most is a matrix of rank one, of which the diagonal of
-// b A + c A^2 meets X and the rest of it X's image: 0.42 / rows of the results (root mean square), and up to 256 rows that is more than the 0.00166 of bf16's own rounding.  With one image and with
+// b A + c A^2 meets X and the rest of it X's image: 0.42 / rows of the results (root mean square), and up to 250 rows that is more than the 0.00166 of bf16's own rounding.  With one image and with
 // two, with that rounding: 16 x 4000 0.021 and 0.0017, 64 x 64 0.0068 and 0.0017, 128 x 512 0.0037, 200 x 300 0.0028, 256 x 1024 0.0025; then 384 x 384 0.0020, 768 x 768 0.00175, 2048 x 2048 0.0017.  Of
 // a momentum with noise 0.0017 to 0.0018 whatever the size.  us: 300 of 64 x 64 27 with one and 35 with two, 8 of 100 x 131 42, 62, 48 of 128 x 512 94, 161, 4 of 200 x 300 86, 109,
 // 8 of 256 x 1024 101, 157, 8 of 768 x 768 203, 538.
@@ -1066,12 +1066,12 @@ int sdl_orthogonalize(const sdl_view_t* x, uint32_t batch, uint32_t rows, uint32
     if (is_small(n, m)) {
         SmallArgs a{kernel_view(x), kernel_view(out), make_div((m + 15) / 16), rows > cols, n, m, 0, (double)eps, scale, static_cast<float*>(workspace), 0, 0, {}, {}, {}, {}};
         h = 1.0;
-        for (uint32_t s0 = 0; s0 < steps; s0 += kMostSmallSteps) {
-            a.steps = std::min(kMostSmallSteps, steps - s0);
-            a.resumes = s0 > 0;
-            a.pauses = s0 + a.steps < steps;
-            for (uint32_t s = 0; s < a.steps; ++s) {
-                const float* each = coefficients + 3 * (size_t)(s0 + s);
+        const float* each = coefficients;
+        for (uint32_t left = steps; left; left -= a.steps) {
+            a.steps = std::min(kMostSmallSteps, left);
+            a.resumes = left < steps;
+            a.pauses = left > a.steps;
+            for (uint32_t s = 0; s < a.steps; ++s, each += 3) {
                 a.a[s] = each[0];
                 a.b[s] = each[1];
                 a.c[s] = each[2];
